@@ -3,10 +3,13 @@
  * sharding for Delayed Tensor Parallelism ("Affinity-Aware Sharding for
  * Delayed Tensor Parallelism", arXiv 2609.13846).
  *
- * Two parts, both defined in Sec. 3 of the paper:
+ * Two parts defined in Sec. 3 of the paper, and what runs the layers they act on:
  *   1. the first-order head->neuron affinity of one layer ("Affinity scores"),
  *   2. the coordinate-ascent layout optimiser over balanced head partitions
- *      and neuron assignments ("Objective", "Optimiser").
+ *      and neuron assignments ("Objective", "Optimiser"),
+ *   3. the linear layer and the gated feed-forward block, forward and
+ *      backward, and gradient clipping: calibration, serving and distillation
+ *      (Sec. 4) of the permuted layers.
  *
  * Conventions for every entry point:
  *   - Tensor arguments are DEVICE pointers owned by the caller; the library
@@ -592,6 +595,118 @@ int dtp_apply_layout(const int32_t* head_part, const int32_t* neuron_dev, int la
                      int q_per_group, int head_dim, int d, int elem_bytes, const void* const* src,
                      void* const* dst, int32_t* head_order, int32_t* neuron_order, void* workspace,
                      size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* 3. Running and distilling the permuted layers (Sec. 4)                    */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * The layers whose weights a layout permutes, run forward (calibration,
+ * serving) and backward (the distillation of Sec. 4).  dtype is that of every
+ * tensor without a stated type: DTP_BF16 (tensor cores, fp32 accumulation,
+ * each output rounded once) or DTP_F32 (CUDA cores, fp32 throughout).
+ * Sizes: 0 <= T <= 2^31 - 256, every width 1 <= . <= 2^24.  Widths need not be
+ * multiples of anything; rows of bf16 matrices that are no multiple of 16
+ * bytes cost a copy to an aligned pitch in the workspace.  Outputs must not
+ * overlap inputs (Y may be `residual` itself).  Results are deterministic: no
+ * floating-point atomics, and sums whose order depends on the sizes alone.  A
+ * bounded device-side wait that gave up is reported through the workspace
+ * status word.
+ */
+typedef enum {
+    DTP_ACT_NONE = 0, /* z                                                */
+    DTP_ACT_SILU = 1, /* z / (1 + e^-z)                                   */
+    DTP_ACT_GELU = 2, /* z Phi(z), Phi the normal distribution function   */
+    DTP_ACT_RELU = 3  /* max(z, 0); a NaN stays a NaN                     */
+} dtp_activation;
+
+/*
+ * Linear layer with its epilogue:
+ *     Z = X W^T + bias,  Y = act(Z) + residual
+ *   X        [T, K]   inputs
+ *   W        [N, K]   weights (nn.Linear [out, in])
+ *   bias     [N] or NULL;  residual [T, N] or NULL
+ *   act      a dtp_activation
+ *   Y        [T, N]   out
+ *   Z        [T, N] fp32 out or NULL: the pre-activations that
+ *            dtp_linear_backward needs when act is not DTP_ACT_NONE
+ * T == 0 returns DTP_OK.  Workspace from dtp_linear_workspace_size (backward:
+ * nonzero for the size that both directions need).  Asynchronous.
+ */
+int dtp_linear_workspace_size(int64_t T, int K, int N, int dtype, int backward, size_t* bytes);
+int dtp_linear(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
+               int act, int dtype, void* Y, float* Z, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of dtp_linear for dY [T, N], the gradient of Y (the residual's
+ * gradient is dY itself):
+ *     dZ = dY act'(Z),  dX = dZ W,  dW = dZ^T X,  dbias = sum_t dZ
+ *   Z      as dtp_linear wrote it; NULL when act is DTP_ACT_NONE
+ *   dX     [T, K], dW [N, K], dbias [N]: each out or NULL (not computed)
+ * dZ is rounded once to dtype before the products; dbias sums the unrounded
+ * values.  T == 0 writes zeros to dW and dbias.  Asynchronous.
+ */
+int dtp_linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N,
+                        int act, int dtype, void* dX, void* dW, void* dbias, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * The gated feed-forward block (SwiGLU with DTP_ACT_SILU; the FFN of Sec. 2):
+ *     G = X W_gate^T,  U = X W_up^T,  H = act(G) . U,  Y = H W_down^T + residual
+ *   X        [T, d];  W_gate, W_up [N, d];  W_down [d, N]
+ *   residual [T, d] or NULL;  Y [T, d] out
+ *   H        NULL, or out for dtp_gated_ffn_backward: T rows of N entries at a
+ *            pitch of N rounded up to a multiple of 8 (entries beyond N are
+ *            not written)
+ *   pre      NULL, or out for dtp_gated_ffn_backward: G and U in fp32 in the
+ *            library's own order, dtp_gated_ffn_saved_size bytes
+ * H is rounded once to dtype before the down projection.  T == 0 returns
+ * DTP_OK.  Workspace from dtp_gated_ffn_workspace_size (backward: nonzero for
+ * the size that both directions need).  Asynchronous.
+ */
+int dtp_gated_ffn_workspace_size(int64_t T, int d, int N, int dtype, int backward, size_t* bytes);
+int dtp_gated_ffn_saved_size(int64_t T, int N, size_t* bytes);
+int dtp_gated_ffn(const void* X, const void* W_gate, const void* W_up, const void* W_down, const void* residual,
+                  int64_t T, int d, int N, int act, int dtype, void* Y, void* H, float* pre, void* workspace,
+                  size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of dtp_gated_ffn for dY [T, d], the gradient of Y (the residual's
+ * gradient is dY itself):
+ *     dH = dY W_down,  dU = dH act(G),  dG = dH U act'(G)
+ *     dX = dG W_gate + dU W_up,  dW_gate = dG^T X,  dW_up = dU^T X,  dW_down = dY^T H
+ *   H, pre   as dtp_gated_ffn wrote them for the same X, weights and act
+ *   dX [T, d], dW_gate, dW_up [N, d], dW_down [d, N]: each out or NULL
+ * dG and dU are rounded once to dtype before the products.  T == 0 writes
+ * zeros to the weights' gradients.  Asynchronous.
+ */
+int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, const void* W_up, const void* W_down,
+                           const void* H, const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX,
+                           void* dW_gate, void* dW_up, void* dW_down, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * The global norm of many gradients, and their clipping:
+ *     n = sqrt(sum over all tensors of sum g^2),  out = g max_norm / n where n > max_norm, else g
+ *   grads   host array of `count` device pointers, each aligned to its element
+ *           (not to 16 bytes: views into a packed buffer are fine)
+ *   out     host array of device pointers like grads (each equal to its
+ *           gradient, or not overlapping any), or NULL: in place, and then
+ *           nothing is written unless n > max_norm
+ *   numel   host array: elements of each (0 allowed, the pointer may be NULL)
+ *   dtypes  host array: DTP_BF16 or DTP_F32 of each (out has the same)
+ *   max_norm  >= 0, may be infinite (the norm alone)
+ *   norm    device fp32 out: n
+ * A norm that is not finite leaves the gradients as they are (out receives
+ * copies); the caller reads it and skips the step.  Squares are summed in fp32
+ * within a chunk of 16384 elements, with a power of two taken out where they
+ * would leave fp32's range, and in fp64 beyond.  Deterministic.  The host
+ * arrays are read before the call returns.  At most 2^31 - 1 chunks.
+ * Workspace from dtp_clip_grad_norm_workspace_size.  Asynchronous.
+ */
+int dtp_clip_grad_norm_workspace_size(int count, const int64_t* numel, size_t* bytes);
+int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int count,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -71,6 +71,27 @@ int launch_chain_score(const float* S_up, const float* S_down, int Lyr, int G, i
                        const int32_t* nu, int64_t* edge_q, int64_t* J_q, double* J, void* workspace,
                        cudaStream_t stream);
 }  // namespace search
+namespace layer {
+size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward);
+int linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
+                   int act, int dtype, void* Y, float* Z, void* workspace, cudaStream_t stream);
+int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
+                    int dtype, void* dX, void* dW, void* dbias, void* workspace, cudaStream_t stream);
+size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward);
+size_t gated_saved_bytes(int64_t T, int N);
+int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd, const void* residual, int64_t T,
+                  int d, int N, int act, int dtype, void* Y, void* H, float* pre, void* workspace,
+                  cudaStream_t stream);
+int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* H,
+                   const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX, void* dWg, void* dWu,
+                   void* dWd, void* workspace, cudaStream_t stream);
+}  // namespace layer
+namespace clip {
+int64_t chunk_count(int count, const int64_t* numel);
+size_t workspace_bytes(int64_t chunks);
+int launch(const void* const* grads, void* const* out, const int64_t* numel, const int* dtype, int count,
+           float max_norm, float* norm, void* workspace, cudaStream_t stream);
+}  // namespace clip
 }  // namespace dtp
 
 using namespace dtp;
@@ -111,6 +132,20 @@ bool search_sizes_ok(int layers, int H, int N, int D, int iters) {
     if (N > (1 << 18) || static_cast<int64_t>(H) * N > (int64_t(1) << 22)) return false;
     if (search::partition_count(H, D) > (int64_t(1) << 26)) return false;
     return true;
+}
+
+bool layer_sizes_ok(int64_t T, int K, int N, int dtype) {
+    if (dtype != DTP_BF16 && dtype != DTP_F32) return false;
+    return T >= 0 && T <= (int64_t(1) << 31) - 256 && K >= 1 && K <= (1 << 24) && N >= 1 && N <= (1 << 24);
+}
+
+bool act_ok(int act) { return act >= DTP_ACT_NONE && act <= DTP_ACT_RELU; }
+
+// A tensor argument: set unless it may be left out, and on a 16-byte boundary.
+bool arg_ok(const void* p, bool needed = true) { return p ? aligned16(p) : !needed; }
+
+bool workspace_ok(const void* workspace, size_t bytes, size_t needed) {
+    return workspace && bytes >= needed && aligned16(workspace);
 }
 
 }  // namespace
@@ -510,6 +545,106 @@ int dtp_search_layout(const float* A, int H_kv, int N, int D, int iters, int32_t
                       void* stream) {
     return dtp_search_layout_batched(A, 1, H_kv, N, D, iters, head_part, neuron_dev, score_q, score, iters_done,
                                      workspace, workspace_bytes, stream);
+}
+
+int dtp_linear_workspace_size(int64_t T, int K, int N, int dtype, int backward, size_t* bytes) {
+    if (!bytes || !layer_sizes_ok(T, K, N, dtype)) return DTP_ERR_ARG;
+    *bytes = layer::linear_workspace_bytes(T, K, N, dtype, backward);
+    return DTP_OK;
+}
+
+int dtp_linear(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
+               int act, int dtype, void* Y, float* Z, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!layer_sizes_ok(T, K, N, dtype) || !act_ok(act)) return DTP_ERR_ARG;
+    if (T == 0) return DTP_OK;
+    if (!arg_ok(X) || !arg_ok(W) || !arg_ok(bias, false) || !arg_ok(residual, false) || !arg_ok(Y) ||
+        !arg_ok(Z, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::linear_workspace_bytes(T, K, N, dtype, 0)))
+        return DTP_ERR_WORKSPACE;
+    return layer::linear_forward(X, W, bias, residual, T, K, N, act, dtype, Y, Z, workspace,
+                                 static_cast<cudaStream_t>(stream));
+}
+
+int dtp_linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N,
+                        int act, int dtype, void* dX, void* dW, void* dbias, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    if (!layer_sizes_ok(T, K, N, dtype) || !act_ok(act)) return DTP_ERR_ARG;
+    const bool some = T > 0;
+    if (!arg_ok(dY, some) || !arg_ok(X, some && dW) || !arg_ok(W, some && dX) ||
+        !arg_ok(Z, some && act != DTP_ACT_NONE) || !arg_ok(dX, false) || !arg_ok(dW, false) || !arg_ok(dbias, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::linear_workspace_bytes(T, K, N, dtype, 1)))
+        return DTP_ERR_WORKSPACE;
+    return layer::linear_backward(dY, X, W, Z, T, K, N, act, dtype, dX, dW, dbias, workspace,
+                                  static_cast<cudaStream_t>(stream));
+}
+
+int dtp_gated_ffn_workspace_size(int64_t T, int d, int N, int dtype, int backward, size_t* bytes) {
+    if (!bytes || !layer_sizes_ok(T, d, N, dtype)) return DTP_ERR_ARG;
+    *bytes = layer::gated_workspace_bytes(T, d, N, dtype, backward);
+    return DTP_OK;
+}
+
+int dtp_gated_ffn_saved_size(int64_t T, int N, size_t* bytes) {
+    if (!bytes || !layer_sizes_ok(T, 1, N, DTP_F32)) return DTP_ERR_ARG;
+    *bytes = layer::gated_saved_bytes(T, N);
+    return DTP_OK;
+}
+
+int dtp_gated_ffn(const void* X, const void* W_gate, const void* W_up, const void* W_down, const void* residual,
+                  int64_t T, int d, int N, int act, int dtype, void* Y, void* H, float* pre, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+    if (!layer_sizes_ok(T, d, N, dtype) || !act_ok(act)) return DTP_ERR_ARG;
+    if (T == 0) return DTP_OK;
+    if (!arg_ok(X) || !arg_ok(W_gate) || !arg_ok(W_up) || !arg_ok(W_down) || !arg_ok(residual, false) ||
+        !arg_ok(Y) || !arg_ok(H, false) || !arg_ok(pre, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::gated_workspace_bytes(T, d, N, dtype, 0)))
+        return DTP_ERR_WORKSPACE;
+    return layer::gated_forward(X, W_gate, W_up, W_down, residual, T, d, N, act, dtype, Y, H, pre, workspace,
+                                static_cast<cudaStream_t>(stream));
+}
+
+int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, const void* W_up, const void* W_down,
+                           const void* H, const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX,
+                           void* dW_gate, void* dW_up, void* dW_down, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+    if (!layer_sizes_ok(T, d, N, dtype) || !act_ok(act)) return DTP_ERR_ARG;
+    const bool some = T > 0;
+    if (!arg_ok(dY, some) || !arg_ok(X, some) || !arg_ok(W_gate, some) || !arg_ok(W_up, some) ||
+        !arg_ok(W_down, some) || !arg_ok(H, some) || !arg_ok(pre, some) || !arg_ok(dX, false) ||
+        !arg_ok(dW_gate, false) || !arg_ok(dW_up, false) || !arg_ok(dW_down, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::gated_workspace_bytes(T, d, N, dtype, 1)))
+        return DTP_ERR_WORKSPACE;
+    return layer::gated_backward(dY, X, W_gate, W_up, W_down, H, pre, T, d, N, act, dtype, dX, dW_gate, dW_up,
+                                 dW_down, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int dtp_clip_grad_norm_workspace_size(int count, const int64_t* numel, size_t* bytes) {
+    if (!bytes || count < 0 || (count > 0 && !numel)) return DTP_ERR_ARG;
+    const int64_t chunks = clip::chunk_count(count, numel);
+    if (chunks < 0) return DTP_ERR_ARG;
+    *bytes = clip::workspace_bytes(chunks);
+    return DTP_OK;
+}
+
+int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int count,
+                       float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+    if (count < 0 || (count > 0 && (!grads || !numel || !dtypes)) || !(max_norm >= 0.0f)) return DTP_ERR_ARG;
+    const int64_t chunks = clip::chunk_count(count, numel);
+    if (chunks < 0 || !norm || (reinterpret_cast<uintptr_t>(norm) & 3)) return DTP_ERR_ARG;
+    for (int i = 0; i < count; ++i) {
+        if (dtypes[i] != DTP_BF16 && dtypes[i] != DTP_F32) return DTP_ERR_ARG;
+        const uintptr_t mask = dtypes[i] == DTP_BF16 ? 1 : 3;
+        if (numel[i] == 0) continue;
+        if (!grads[i] || (reinterpret_cast<uintptr_t>(grads[i]) & mask)) return DTP_ERR_ARG;
+        if (out && (!out[i] || (reinterpret_cast<uintptr_t>(out[i]) & mask))) return DTP_ERR_ARG;
+    }
+    if (!workspace_ok(workspace, workspace_bytes, clip::workspace_bytes(chunks))) return DTP_ERR_WORKSPACE;
+    return clip::launch(grads, out, numel, dtypes, count, max_norm, norm, workspace,
+                        static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,242 @@
+// layer_ops.cu -- the linear layer and the gated feed-forward block, forward and backward, as sequences of
+// matrix products with fused epilogues, and the elementwise kernels between them.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dtp_common.cuh"
+#include "layer_common.cuh"
+
+namespace dtp {
+namespace simt {
+int launch(const layer::Product& p, int dtype, cudaStream_t stream);
+}  // namespace simt
+
+namespace layer {
+
+constexpr int kRowChunk = 256;    // tokens per partial sum of the bias gradient
+
+// dZ = dY act'(Z), rounded once, and the partial sums over kRowChunk tokens of the unrounded values (the bias
+// gradient).  A block takes 32 columns x kRowChunk tokens; each of its 8 warps sums its tokens in order.
+template <typename E>
+__global__ void __launch_bounds__(256)
+act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T, int N, int64_t ldz, int act,
+                E* __restrict__ dZ, float* __restrict__ partial) {
+    __shared__ float red[8][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = blockIdx.x * 32 + lane;
+    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kRowChunk;
+    float sum = 0.0f;
+    if (n < N) {
+        for (int r = warp; r < kRowChunk; r += 8) {
+            const int64_t t = t0 + r;
+            if (t >= T) break;
+            float g = to_f32(dY[t * N + n]);
+            if (act != DTP_ACT_NONE) {
+                float v, s;
+                act_both<IsFast<E>::value>(act, Z[t * N + n], v, s);
+                g *= s;
+            }
+            sum += g;
+            if (dZ) dZ[t * ldz + n] = from_f32<E>(g);
+        }
+    }
+    if (!partial) return;
+    red[warp][lane] = sum;
+    __syncthreads();
+    if (warp == 0 && n < N) {
+        float s = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) s += red[w][lane];
+        partial[static_cast<int64_t>(blockIdx.y) * N + n] = s;
+    }
+}
+
+// out[n] = sum over the chunks, in order.
+template <typename E>
+__global__ void bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* __restrict__ out) {
+    const int n = blockIdx.x * blockDim.x + threadIdx.x;
+    if (n >= N) return;
+    float s = 0.0f;
+    for (int64_t c = 0; c < chunks; ++c) s += partial[c * N + n];
+    out[n] = from_f32<E>(s);
+}
+
+// Pieces of a workspace, in the order in which they are asked for.
+struct Carver {
+    uint8_t* base;
+    size_t used = kWorkspaceHeader;
+    explicit Carver(void* p) : base(static_cast<uint8_t*>(p)) {}
+    void* take(size_t bytes) {
+        void* r = base ? base + used : nullptr;
+        used += align_up(bytes, 256);
+        return r;
+    }
+};
+
+static size_t elem(int dtype) { return dtype == DTP_BF16 ? 2 : 4; }
+static int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+static int64_t chunks_of(int64_t T) { return (T + kRowChunk - 1) / kRowChunk; }
+
+static Mat by_row(const void* p, int64_t ld) { return Mat{p, ld, 1}; }      // [rows, K]
+static Mat by_col(const void* p, int64_t ld) { return Mat{p, 1, ld}; }      // [K, rows]
+
+static int product(const Product& p, int dtype, cudaStream_t stream) { return simt::launch(p, dtype, stream); }
+
+// ------------------------------------------------------------------------------- linear layer
+
+static size_t linear_bytes(int64_t T, int K, int N, int dtype, int backward) {
+    (void)K;
+    Carver c(nullptr);
+    if (backward) {
+        c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+        c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float));
+    }
+    return c.used;
+}
+
+size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) {
+    return linear_bytes(T, K, N, dtype, backward);
+}
+
+int linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
+                   int act, int dtype, void* Y, float* Z, void* workspace, cudaStream_t stream) {
+    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Product p;
+    p.A[0] = by_row(X, K);
+    p.B[0] = by_row(W, K);
+    p.M = T, p.N = N, p.K = K;
+    p.epi.act = act, p.epi.bias = bias, p.epi.residual = residual, p.epi.out = Y, p.epi.ldo = N, p.epi.Z = Z;
+    p.epi.M = T, p.epi.N = N;
+    return product(p, dtype, stream);
+}
+
+template <typename E>
+static int launch_act_grad(const void* dY, const float* Z, int64_t T, int N, int act, void* dZ, int64_t ldz,
+                           float* partial, void* dbias, cudaStream_t stream) {
+    const dim3 grid((N + 31) / 32, static_cast<unsigned>(chunks_of(T)));
+    if (T > 0) {
+        act_grad_kernel<E><<<grid, 256, 0, stream>>>(static_cast<const E*>(dY), Z, T, N, ldz, act,
+                                                     static_cast<E*>(dZ), dbias ? partial : nullptr);
+        DTP_CUDA_TRY(cudaGetLastError());
+    }
+    if (dbias) {
+        bias_reduce_kernel<E><<<(N + 255) / 256, 256, 0, stream>>>(partial, chunks_of(T), N, static_cast<E*>(dbias));
+        DTP_CUDA_TRY(cudaGetLastError());
+    }
+    return DTP_OK;
+}
+
+int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
+                    int dtype, void* dX, void* dW, void* dbias, void* workspace, cudaStream_t stream) {
+    if (chunks_of(T) > 65535) return DTP_ERR_UNSUPPORTED;
+    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Carver c(workspace);
+    void* dz = c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    float* partial = static_cast<float*>(c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float)));
+    const bool own_dz = act != DTP_ACT_NONE;
+    const int64_t ldz = own_dz ? padded(N) : N;
+    if (own_dz || dbias) {
+        auto go = dtype == DTP_BF16 ? launch_act_grad<__nv_bfloat16> : launch_act_grad<float>;
+        const int st = go(dY, Z, T, N, act, own_dz ? dz : nullptr, ldz, partial, dbias, stream);
+        if (st != DTP_OK) return st;
+    }
+    const void* g = own_dz ? dz : dY;
+    if (dX && T > 0) {
+        Product p;
+        p.A[0] = by_row(g, ldz);
+        p.B[0] = by_col(W, K);
+        p.M = T, p.N = K, p.K = N;
+        p.epi.out = dX, p.epi.ldo = K, p.epi.M = T, p.epi.N = K;
+        const int st = product(p, dtype, stream);
+        if (st != DTP_OK) return st;
+    }
+    if (dW) {
+        Product p;
+        p.A[0] = by_col(g, ldz);
+        p.B[0] = by_col(X, K);
+        p.M = N, p.N = K, p.K = T;
+        p.epi.out = dW, p.epi.ldo = K, p.epi.M = N, p.epi.N = K;
+        const int st = product(p, dtype, stream);
+        if (st != DTP_OK) return st;
+    }
+    return DTP_OK;
+}
+
+// ------------------------------------------------------------------------- gated feed-forward
+
+size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward) {
+    (void)d;
+    Carver c(nullptr);
+    c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    if (backward) c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    return c.used;
+}
+
+size_t gated_saved_bytes(int64_t T, int N) { return static_cast<size_t>(pre_floats(T, N)) * sizeof(float); }
+
+int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd, const void* residual, int64_t T,
+                  int d, int N, int act, int dtype, void* Y, void* H, float* pre, void* workspace,
+                  cudaStream_t stream) {
+    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Carver c(workspace);
+    void* h = H ? H : c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    Product p;
+    p.A[0] = by_row(X, d);
+    p.B[0] = by_row(Wg, d), p.B[1] = by_row(Wu, d);
+    p.M = T, p.N = N, p.K = d;
+    p.epi.kind = kEpiGated, p.epi.act = act, p.epi.out = h, p.epi.ldo = padded(N), p.epi.pre = pre;
+    p.epi.M = T, p.epi.N = N;
+    int st = product(p, dtype, stream);
+    if (st != DTP_OK) return st;
+    Product q;
+    q.A[0] = by_row(h, padded(N));
+    q.B[0] = by_row(Wd, N);
+    q.M = T, q.N = d, q.K = N;
+    q.epi.residual = residual, q.epi.out = Y, q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
+    return product(q, dtype, stream);
+}
+
+int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* H,
+                   const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX, void* dWg, void* dWu,
+                   void* dWd, void* workspace, cudaStream_t stream) {
+    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Carver c(workspace);
+    const int64_t ld = padded(N);
+    void* dg = c.take(static_cast<size_t>(T) * ld * elem(dtype));
+    void* du = c.take(static_cast<size_t>(T) * ld * elem(dtype));
+    int st = DTP_OK;
+    if (T > 0) {
+        Product p;
+        p.A[0] = by_row(dY, d);
+        p.B[0] = by_col(Wd, N);
+        p.M = T, p.N = N, p.K = d;
+        p.epi.kind = kEpiGatedGrad, p.epi.act = act, p.epi.out = dg, p.epi.out2 = du, p.epi.ldo = ld;
+        p.epi.pre = const_cast<float*>(pre), p.epi.M = T, p.epi.N = N;
+        if ((st = product(p, dtype, stream)) != DTP_OK) return st;
+    }
+    if (dX && T > 0) {
+        Product p;
+        p.segments = 2;
+        p.A[0] = by_row(dg, ld), p.A[1] = by_row(du, ld);
+        p.B[0] = by_col(Wg, d), p.B[1] = by_col(Wu, d);
+        p.M = T, p.N = d, p.K = N;
+        p.epi.out = dX, p.epi.ldo = d, p.epi.M = T, p.epi.N = d;
+        if ((st = product(p, dtype, stream)) != DTP_OK) return st;
+    }
+    auto weight = [&](const void* a, int64_t lda, int64_t rows, const void* b, int64_t ldb, int cols, void* out) {
+        if (!out) return static_cast<int>(DTP_OK);
+        Product p;
+        p.A[0] = by_col(a, lda);
+        p.B[0] = by_col(b, ldb);
+        p.M = rows, p.N = cols, p.K = T;
+        p.epi.out = out, p.epi.ldo = cols, p.epi.M = rows, p.epi.N = cols;
+        return product(p, dtype, stream);
+    };
+    if ((st = weight(dg, ld, N, X, d, d, dWg)) != DTP_OK) return st;
+    if ((st = weight(du, ld, N, X, d, d, dWu)) != DTP_OK) return st;
+    return weight(dY, d, d, H, ld, N, dWd);
+}
+
+}  // namespace layer
+}  // namespace dtp

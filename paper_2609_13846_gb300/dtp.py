@@ -101,7 +101,20 @@ def lib():
     L.dtp_search_layout.argtypes = [_vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
     L.dtp_search_layout_batched.argtypes = [_vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
                                             _vp]
-    for fn in ("dtp_search_chain_workspace_size", "dtp_search_chain", "dtp_search_chain_ex", "dtp_chain_score",
+    L.dtp_linear_workspace_size.argtypes = [_i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]
+    L.dtp_linear.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.dtp_linear_backward.argtypes = [_vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+    L.dtp_gated_ffn_workspace_size.argtypes = [_i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]
+    L.dtp_gated_ffn_saved_size.argtypes = [_i64, _i32, ctypes.POINTER(_sz)]
+    L.dtp_gated_ffn.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+    L.dtp_gated_ffn_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i32, _i32, _vp, _vp,
+                                         _vp, _vp, _vp, _sz, _vp]
+    L.dtp_clip_grad_norm_workspace_size.argtypes = [_i32, _vp, ctypes.POINTER(_sz)]
+    L.dtp_clip_grad_norm.argtypes = [_vp, _vp, _vp, _vp, _i32, ctypes.c_float, _vp, _vp, _sz, _vp]
+    for fn in ("dtp_linear_workspace_size", "dtp_linear", "dtp_linear_backward", "dtp_gated_ffn_workspace_size",
+               "dtp_gated_ffn_saved_size", "dtp_gated_ffn", "dtp_gated_ffn_backward",
+               "dtp_clip_grad_norm_workspace_size", "dtp_clip_grad_norm",
+               "dtp_search_chain_workspace_size", "dtp_search_chain", "dtp_search_chain_ex", "dtp_chain_score",
                "dtp_affinity_grouped_workspace_size", "dtp_affinity_accumulate_grouped",
                "dtp_head_writes_workspace_size", "dtp_head_writes", "dtp_layout_order", "dtp_permute_rows",
                "dtp_affinity_accumulate_opts", "dtp_search_global_workspace_size", "dtp_search_global",
@@ -796,3 +809,235 @@ def apply_layout(W: dict, h: torch.Tensor, nu: torch.Tensor, D: int, head_dim: i
     out["up"] = permute_rows(W["up"], no, 1, stream=stream, check=check)
     out["down"] = permute_cols(W["down"], no, 1, stream=stream, check=check)
     return out, ho, no
+
+
+# ------------------------------------------------------ layers of the permuted model (Sec. 4) --
+
+ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}
+
+
+def _act_code(name: str) -> int:
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {name!r}")
+    return code
+
+
+def _torch_code(dtype: torch.dtype) -> int:
+    if dtype is torch.bfloat16:
+        return DTP_BF16
+    if dtype is torch.float32:
+        return DTP_F32
+    raise TypeError(f"unsupported dtype {dtype}; use bfloat16 or float32")
+
+
+def _layer_check(ref: torch.Tensor, name: str, t: torch.Tensor, shape, dtype=None):
+    """``t`` is a contiguous CUDA tensor of this shape on ref's device, of ref's dtype (or ``dtype``)."""
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    if not t.is_cuda or not t.is_contiguous() or t.get_device() != ref.get_device():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the inputs' device")
+    if t.dtype is not (ref.dtype if dtype is None else dtype):
+        raise TypeError(f"{name} must be {ref.dtype if dtype is None else dtype}, got {t.dtype}")
+
+
+def _size_query(fn: str, *args) -> int:
+    n = _sz(0)
+    _check(fn, getattr(lib(), fn)(*args, ctypes.byref(n)))
+    return n.value
+
+
+def linear_workspace(T: int, K: int, N: int, dtype: torch.dtype, device, backward: bool = False) -> torch.Tensor:
+    """A device workspace for linear (and, with ``backward``, linear_backward) of these sizes."""
+    n = _size_query("dtp_linear_workspace_size", T, K, N, _torch_code(dtype), int(backward))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
+           activation: str = "none", save: bool = False, Y: torch.Tensor | None = None,
+           workspace: torch.Tensor | None = None, stream=None):
+    """Y = act(X W^T + bias) + residual; X [T,K], W [N,K], bias [N], residual [T,N], one dtype (bf16 or fp32).
+
+    activation: "none", "silu", "gelu" (erf) or "relu".  ``Y`` receives the result if given (it may be
+    ``residual``).  With ``save`` returns (Y, Z): Z [T,N] fp32 holds the pre-activations X W^T + bias that
+    linear_backward needs.
+    """
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("shapes must be X [T,K], W [N,K]")
+    T, K = X.shape
+    N = W.shape[0]
+    code, act = _torch_code(X.dtype), _act_code(activation)
+    _layer_check(X, "X", X, (T, K))
+    _layer_check(X, "W", W, (N, K))
+    if bias is not None:
+        _layer_check(X, "bias", bias, (N,))
+    if residual is not None:
+        _layer_check(X, "residual", residual, (T, N))
+    if Y is None:
+        Y = _keep(torch.empty((T, N), dtype=X.dtype, device=X.device), stream)
+    else:
+        _layer_check(X, "Y", Y, (T, N))
+    Z = _keep(torch.empty((T, N), dtype=torch.float32, device=X.device), stream) if save else None
+    if workspace is None:
+        workspace = _keep(linear_workspace(T, K, N, X.dtype, X.device), stream)
+    _check("dtp_linear", lib().dtp_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), T, K, N, act, code, _ptr(Y),
+                                          _ptr(Z), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return (Y, Z) if save else Y
+
+
+def linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: torch.Tensor | None = None,
+                    activation: str = "none", bias: bool = False, workspace: torch.Tensor | None = None, stream=None):
+    """Gradients (dX [T,K], dW [N,K], dbias [N] or None) of linear for dY [T,N]; the residual's gradient is dY.
+
+    ``Z`` as linear(save=True) returned it (not needed without an activation); ``bias``: whether dbias is wanted.
+    """
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("shapes must be X [T,K], W [N,K]")
+    T, K = X.shape
+    N = W.shape[0]
+    code, act = _torch_code(X.dtype), _act_code(activation)
+    _layer_check(X, "X", X, (T, K))
+    _layer_check(X, "W", W, (N, K))
+    _layer_check(X, "dY", dY, (T, N))
+    if act:
+        if Z is None:
+            raise ValueError("Z (of linear with save=True) is needed with an activation")
+        _layer_check(X, "Z", Z, (T, N), torch.float32)
+    else:
+        Z = None
+    dX = _keep(torch.empty_like(X), stream)
+    dW = _keep(torch.empty_like(W), stream)
+    db = _keep(torch.empty(N, dtype=X.dtype, device=X.device), stream) if bias else None
+    if workspace is None:
+        workspace = _keep(linear_workspace(T, K, N, X.dtype, X.device, backward=True), stream)
+    _check("dtp_linear_backward",
+           lib().dtp_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), T, K, N, act, code, _ptr(dX), _ptr(dW),
+                                     _ptr(db), _ptr(workspace), workspace.numel(), _stream(stream)))
+    return dX, dW, db
+
+
+def gated_ffn_workspace(T: int, d: int, N: int, dtype: torch.dtype, device, backward: bool = False) -> torch.Tensor:
+    """A device workspace for gated_ffn (and, with ``backward``, gated_ffn_backward) of these sizes."""
+    n = _size_query("dtp_gated_ffn_workspace_size", T, d, N, _torch_code(dtype), int(backward))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _gated_shapes(X, W_gate, W_up, W_down):
+    if X.dim() != 2 or W_gate.dim() != 2:
+        raise ValueError("shapes must be X [T,d], W_gate/W_up [N,d], W_down [d,N]")
+    T, d = X.shape
+    N = W_gate.shape[0]
+    _layer_check(X, "X", X, (T, d))
+    _layer_check(X, "W_gate", W_gate, (N, d))
+    _layer_check(X, "W_up", W_up, (N, d))
+    _layer_check(X, "W_down", W_down, (d, N))
+    return T, d, N
+
+
+def _gated_saved_shapes(T: int, N: int):
+    """(pitch of H, fp32 values of pre)."""
+    return (N + 7) // 8 * 8, _size_query("dtp_gated_ffn_saved_size", T, N) // 4
+
+
+def gated_ffn(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down: torch.Tensor,
+              residual: torch.Tensor | None = None, activation: str = "silu", save: bool = False,
+              Y: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Y = (act(X W_gate^T) * (X W_up^T)) W_down^T + residual, one dtype (bf16 or fp32).
+
+    X [T,d], W_gate/W_up [N,d], W_down [d,N], residual [T,d].  ``Y`` receives the result if given (it may be
+    ``residual``).  With ``save`` returns (Y, saved): what gated_ffn_backward needs (H in the inputs' dtype and
+    the gate and up pre-activations in fp32, in the library's own order: 8 bytes a token and neuron).
+    """
+    T, d, N = _gated_shapes(X, W_gate, W_up, W_down)
+    code, act = _torch_code(X.dtype), _act_code(activation)
+    if residual is not None:
+        _layer_check(X, "residual", residual, (T, d))
+    if Y is None:
+        Y = _keep(torch.empty((T, d), dtype=X.dtype, device=X.device), stream)
+    else:
+        _layer_check(X, "Y", Y, (T, d))
+    H = pre = None
+    if save:
+        ld, n = _gated_saved_shapes(T, N)
+        H = _keep(torch.empty((T, ld), dtype=X.dtype, device=X.device), stream)
+        pre = _keep(torch.empty(n, dtype=torch.float32, device=X.device), stream)
+    if workspace is None:
+        workspace = _keep(gated_ffn_workspace(T, d, N, X.dtype, X.device), stream)
+    _check("dtp_gated_ffn", lib().dtp_gated_ffn(_ptr(X), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(residual), T, d,
+                                                N, act, code, _ptr(Y), _ptr(H), _ptr(pre), _ptr(workspace),
+                                                workspace.numel(), _stream(stream)))
+    return (Y, (H, pre)) if save else Y
+
+
+def gated_ffn_backward(dY: torch.Tensor, X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor,
+                       W_down: torch.Tensor, saved, activation: str = "silu", workspace: torch.Tensor | None = None,
+                       stream=None):
+    """Gradients (dX, dW_gate, dW_up, dW_down) of gated_ffn for dY [T,d]; the residual's gradient is dY.
+
+    ``saved`` as gated_ffn(save=True) returned it for the same inputs and activation.
+    """
+    T, d, N = _gated_shapes(X, W_gate, W_up, W_down)
+    code, act = _torch_code(X.dtype), _act_code(activation)
+    _layer_check(X, "dY", dY, (T, d))
+    H, pre = saved
+    ld, n = _gated_saved_shapes(T, N)
+    _layer_check(X, "saved H", H, (T, ld))
+    _layer_check(X, "saved pre-activations", pre, (n,), torch.float32)
+    dX, dWg, dWu, dWd = (_keep(torch.empty_like(t), stream) for t in (X, W_gate, W_up, W_down))
+    if workspace is None:
+        workspace = _keep(gated_ffn_workspace(T, d, N, X.dtype, X.device, backward=True), stream)
+    _check("dtp_gated_ffn_backward",
+           lib().dtp_gated_ffn_backward(_ptr(dY), _ptr(X), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(H), _ptr(pre),
+                                        T, d, N, act, code, _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd),
+                                        _ptr(workspace), workspace.numel(), _stream(stream)))
+    return dX, dWg, dWu, dWd
+
+
+def clip_grad_norm_workspace(grads) -> torch.Tensor:
+    """A device workspace for clip_grad_norm of tensors of these sizes."""
+    n = len(grads)
+    if n == 0:
+        raise ValueError("grads must hold at least one tensor")
+    size = _size_query("dtp_clip_grad_norm_workspace_size", n, (_i64 * n)(*[g.numel() for g in grads]))
+    return torch.empty(size, dtype=torch.uint8, device=grads[0].device)
+
+
+def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None = None,
+                   workspace: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Scale all tensors by max_norm / n where n, their global 2-norm, is above max_norm; returns n (0-d fp32).
+
+    grads: contiguous CUDA tensors, each bf16 or fp32, scaled in place, or into ``out`` (a list of the same
+    shapes and dtypes, which receives the tensors unchanged when n <= max_norm).  max_norm may be infinite: the
+    norm alone.  A norm that is not finite leaves the gradients as they are.
+    """
+    grads = list(grads)
+    count = len(grads)
+    if count == 0:
+        raise ValueError("grads must hold at least one tensor")
+    index = grads[0].get_device()
+    out = None if out is None else list(out)
+    if out is not None and len(out) != count:
+        raise ValueError(f"out must hold {count} tensors, got {len(out)}")
+    codes = []
+    for name, ts in (("grads", grads), ("out", out)):
+        for t in ts or ():
+            if not t.is_cuda or t.get_device() != index or not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous CUDA tensors on one device")
+    for g in grads:
+        codes.append(_torch_code(g.dtype))
+    if out is not None:
+        for g, o in zip(grads, out):
+            if o.dtype is not g.dtype or o.shape != g.shape:
+                raise ValueError("out must have the shapes and dtypes of grads")
+    if norm is None:
+        norm = _keep(torch.empty((), dtype=torch.float32, device=grads[0].device), stream)
+    elif norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != index:
+        raise ValueError("norm must be one fp32 value on the gradients' device")
+    if workspace is None:
+        workspace = _keep(clip_grad_norm_workspace(grads), stream)
+    src = (_vp * count)(*[g.data_ptr() for g in grads])
+    dst = None if out is None else (_vp * count)(*[o.data_ptr() for o in out])
+    st = lib().dtp_clip_grad_norm(src, dst, (_i64 * count)(*[g.numel() for g in grads]), (_i32 * count)(*codes), count,
+                                  float(max_norm), _ptr(norm), _ptr(workspace), workspace.numel(), _stream(stream))
+    _check("dtp_clip_grad_norm", st)
+    return norm
