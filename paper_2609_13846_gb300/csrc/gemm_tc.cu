@@ -1,0 +1,590 @@
+// gemm_tc.cu -- the bf16 matrix products of the layer operators on the tcgen05 tensor cores, with their
+// epilogues fused:
+//
+//     acc[m, n] = sum over segments s, k of A_s[m, k] B_s[n, k]     (fp32 in TMEM)
+//
+// then, by kind, act(acc + bias) + residual (and the pre-activation), act(gate) up (and both), or the gradients
+// of gate and up from dH.  Each operand may be stored with k contiguous (weights and tokens in the forward
+// products) or with its rows contiguous (the transposed operands of the gradients): both are loaded by TMA into
+// 128-byte-swizzled tiles and described to the tensor core in their own order, so nothing is transposed in
+// memory.
+//
+// Structure: persistent grid, one CTA per SM, twelve warps: warp 0 loads tiles by TMA, warp 1 issues the MMAs,
+// eight warps drain the accumulator, which is double-buffered in TMEM so that a tile's epilogue overlaps the
+// next one's products.  Two forms: CTA pairs share 256 x BN x 16 tcgen05.mma of cta_group::2 (each CTA stages 128
+// rows of A and half of B), single CTAs issue 128 x BN x 16 ones.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dtp_common.cuh"
+#include "layer_common.cuh"
+
+namespace dtp {
+namespace gtc {
+
+using namespace layer;
+
+constexpr int BM = 128;       // rows of A per CTA (TMEM lanes)
+constexpr int BK = 64;
+constexpr int UK = 16;
+constexpr int kThreads = 384;
+constexpr int kEpiWarps = 8;
+constexpr int kEpiWarp0 = 4;
+constexpr uint32_t kTileA = BM * BK * 2;          // 16 KB
+constexpr uint32_t kStageOut = 32 * 64;           // a 32-row x 32-column bf16 box, 2 KB (64-byte swizzle)
+constexpr int kOutBufs = 2;                       // per epilogue warp
+
+template <bool kPair, int BN>
+struct Form {
+    static constexpr int kRowsB = kPair ? BN / 2 : BN;            // staged by this CTA
+    static constexpr uint32_t kTileB = kRowsB * BK * 2;
+    static constexpr uint32_t kStageBytes = kTileA + kTileB;
+    static constexpr int STAGES = static_cast<int>(192 * 1024 / kStageBytes) > 8 ? 8 : 192 * 1024 / kStageBytes;
+    static constexpr uint32_t kTmemCols = 2 * BN;                 // two accumulators: a power of two
+    static constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kEpiWarps * kOutBufs * kStageOut + 512;
+};
+
+struct Args {
+    CUtensorMap a[2], b[2], out, out2;
+    int segments;
+    int KB;               // k blocks of 64 per segment
+    int a_mn, b_mn;       // operand stored with its rows contiguous
+    int tiles_m, tiles_n; // per CTA or pair
+    int64_t units;
+    uint32_t idesc;
+    int direct;           // out rows are not on 16-byte boundaries: plain stores
+    int reset;            // this launch clears the status word
+    int* status;
+    Epilogue epi;
+};
+
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Descriptor of a tile stored with its rows contiguous: 64-row blocks of [k][64 rows], 128 bytes per k,
+// 128-byte swizzle.  Leading byte offset: from one 64-row block to the next (64 k x 128 bytes); stride byte
+// offset: from one group of 8 k to the next (1024 bytes).
+__device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr) {
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+    d |= static_cast<uint64_t>((64u * 128u) >> 4) << 16;
+    d |= static_cast<uint64_t>(1024u >> 4) << 32;
+    d |= static_cast<uint64_t>(1u) << 46;
+    d |= static_cast<uint64_t>(2u) << 61;
+    return d;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
+    a = __uint_as_float(v << 16);
+    b = __uint_as_float(v & 0xFFFF0000u);
+}
+
+// Eight consecutive bf16 of a row, n beyond the end as zero; `wide`: 16-byte loads are aligned.
+__device__ __forceinline__ void load8(const __nv_bfloat16* row, int n, int N, bool wide, float* v) {
+    if (wide && n + 8 <= N) {
+        const uint4 q = *reinterpret_cast<const uint4*>(row + n);
+        unpack_bf16(q.x, v[0], v[1]);
+        unpack_bf16(q.y, v[2], v[3]);
+        unpack_bf16(q.z, v[4], v[5]);
+        unpack_bf16(q.w, v[6], v[7]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = n + i < N ? to_f32(row[n + i]) : 0.0f;
+    }
+}
+
+// Units of a persistent worker: row tiles in groups of 8, column tile by column tile within a group, so that the
+// tiles in flight share their rows and columns in L2.
+constexpr int kGroupM = 8;
+__device__ __forceinline__ void decode(const Args& p, int64_t u, int& tm, int& tn) {
+    const int64_t per = static_cast<int64_t>(kGroupM) * p.tiles_n;
+    const int64_t g = u / per;
+    const int rest = static_cast<int>(u - g * per);
+    const int m0 = static_cast<int>(g) * kGroupM;
+    const int gm = p.tiles_m - m0 < kGroupM ? p.tiles_m - m0 : kGroupM;
+    tn = rest / gm;
+    tm = m0 + rest % gm;
+}
+
+template <bool kPair, int BN, int KIND>
+__global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_constant__ Args p) {
+    using F = Form<kPair, BN>;
+    constexpr int STAGES = F::STAGES;
+    constexpr uint32_t kStageBytes = F::kStageBytes;
+    // output columns per tile: the two accumulators of the gated kind share it
+    constexpr int kCols = KIND == kEpiGated ? BN / 2 : BN;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* tiles = smem;
+    uint8_t* staging = smem + STAGES * kStageBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + kEpiWarps * kOutBufs * kStageOut);
+    // In the pair form full and acc_empty are used in the even CTA only; empty, acc_full and drain receive its
+    // commits in both.
+    uint64_t* full_bar = bars;
+    uint64_t* empty_bar = bars + STAGES;
+    uint64_t* acc_full = bars + 2 * STAGES;
+    uint64_t* acc_empty = acc_full + 2;
+    uint64_t* drain_bar = acc_full + 4;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 5);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    const uint32_t rank = kPair ? cluster_ctarank() : 0u;   // 0: issues the MMAs; 1: its peer
+    const bool leader = rank == 0;
+    const int64_t worker = kPair ? blockIdx.x >> 1 : blockIdx.x;
+    const int64_t workers = kPair ? gridDim.x >> 1 : gridDim.x;
+    const int kblocks = p.segments * p.KB;
+
+    // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
+    // block 0, which starts first, has passed here.
+    if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(smem_u32(&full_bar[s]), 1);
+            mbar_init(smem_u32(&empty_bar[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&acc_full[b]), 1);
+            mbar_init(smem_u32(&acc_empty[b]), (kPair ? 2 : 1) * kEpiWarps);
+        }
+        mbar_init(smem_u32(drain_bar), 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&p.a[0]);
+        tma_prefetch_desc(&p.b[0]);
+        if (!p.direct) tma_prefetch_desc(&p.out);
+    }
+    if (warp == 1) {
+        if constexpr (kPair) {
+            tmem_alloc_pair(smem_u32(tmem_slot), F::kTmemCols);
+            tmem_relinquish_pair();
+        } else {
+            tmem_alloc(smem_u32(tmem_slot), F::kTmemCols);
+            tmem_relinquish();
+        }
+    }
+    tc_fence_before();
+    if constexpr (kPair)
+        cluster_sync();   // both CTAs' barriers initialised and TMEM allocated before any remote access
+    else
+        __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0 && lane == 0) {
+        // -------------------------------------------------------------------- producer
+        const uint32_t full_lead = kPair ? mapa_shared(smem_u32(full_bar), 0) : 0u;
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int64_t u = worker; ok && u < p.units; u += workers) {
+            int tm, tn;
+            decode(p, u, tm, tn);
+            const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
+            const int n0 = tn * kCols;
+            for (int kb = 0; kb < kblocks; ++kb) {
+                if (!mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abort_flag)) { ok = false; break; }
+                const uint32_t sa = smem_u32(tiles + stage * kStageBytes), sb = sa + kTileA;
+                const uint32_t fb = kPair ? full_lead + static_cast<uint32_t>(stage) * 8u : smem_u32(&full_bar[stage]);
+                if (leader) mbar_arrive_expect_tx(smem_u32(&full_bar[stage]), (kPair ? 2u : 1u) * kStageBytes);
+                const int seg = kb >= p.KB;
+                const int k0 = (kb - seg * p.KB) * BK;
+                auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y) {
+                    if constexpr (kPair) tma_load_2d_pair(dst, map, fb, x, y);
+                    else tma_load_2d(dst, map, fb, x, y);
+                };
+                if (p.a_mn) {
+                    load(sa, &p.a[seg], m0, k0);
+                    load(sa + kTileA / 2, &p.a[seg], m0 + 64, k0);
+                } else {
+                    load(sa, &p.a[seg], k0, m0);
+                }
+                // rows of B: halves of BN / 2, which are gate and up in the gated kind
+#pragma unroll
+                for (int h = 0; h < F::kRowsB / (BN / 2); ++h) {
+                    const int half = kPair ? static_cast<int>(rank) : h;
+                    const CUtensorMap* map = KIND == kEpiGated ? &p.b[half] : &p.b[seg];
+                    const int r0 = KIND == kEpiGated ? n0 : n0 + half * (BN / 2);
+                    const uint32_t dst = sb + h * (BN / 2) * BK * 2;
+                    if (p.b_mn) {
+#pragma unroll
+                        for (int q = 0; q < BN / 128; ++q) load(dst + q * 64 * BK * 2, map, r0 + 64 * q, k0);
+                    } else {
+                        load(dst, map, k0, r0);
+                    }
+                }
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1 && lane == 0 && leader) {
+        // ------------------------------------------------------------------ MMA issuer (the even CTA of a pair)
+        int stage = 0;
+        uint32_t phase = 0, unit_count = 0;
+        bool ok = true;
+        // one step of 16 k: 32 bytes along a row of k, 16 rows of 128 bytes where the rows are contiguous
+        const uint64_t step_a = p.a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
+        const uint64_t step_b = p.b_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
+        for (int64_t u = worker; ok && u < p.units; u += workers, ++unit_count) {
+            const uint32_t buf = unit_count & 1u;
+            const uint32_t use = (unit_count >> 1) & 1u;
+            const bool freed = kPair ? mbar_wait_cluster(smem_u32(&acc_empty[buf]), use ^ 1u, abort_flag)
+                                     : mbar_wait(smem_u32(&acc_empty[buf]), use ^ 1u, abort_flag);
+            if (!freed) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t d_acc = tmem + buf * BN;
+            for (int kb = 0; kb < kblocks; ++kb) {
+                const bool landed = kPair ? mbar_wait_cluster(smem_u32(&full_bar[stage]), phase, abort_flag)
+                                          : mbar_wait(smem_u32(&full_bar[stage]), phase, abort_flag);
+                if (!landed) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t sa = smem_u32(tiles + stage * kStageBytes), sb = sa + kTileA;
+                const uint64_t da = p.a_mn ? smem_desc_mn128(sa) : smem_desc_k128(sa);
+                const uint64_t db = p.b_mn ? smem_desc_mn128(sb) : smem_desc_k128(sb);
+#pragma unroll
+                for (int kk = 0; kk < BK / UK; ++kk) {
+                    const uint32_t accumulate = (kb == 0 && kk == 0) ? 0u : 1u;
+                    if constexpr (kPair)
+                        umma_bf16_pair(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
+                    else
+                        umma_bf16(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
+                }
+                if constexpr (kPair)
+                    umma_commit_pair(smem_u32(&empty_bar[stage]), 3);
+                else
+                    umma_commit(smem_u32(&empty_bar[stage]));
+                if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+            }
+            if (!ok) break;
+            if constexpr (kPair)
+                umma_commit_pair(smem_u32(&acc_full[buf]), 3);
+            else
+                umma_commit(smem_u32(&acc_full[buf]));
+        }
+        // Every MMA must have completed before TMEM or shared memory is released.
+        if constexpr (kPair)
+            umma_commit_pair(smem_u32(drain_bar), 3);
+        else
+            umma_commit(smem_u32(drain_bar));
+    } else if (warp >= kEpiWarp0) {
+        // -------------------------------------------------------------------- epilogue
+        const Epilogue& e = p.epi;
+        const int quad = warp & 3;                       // TMEM lanes 32*quad ..: a row per thread
+        const int half = (warp - kEpiWarp0) >> 2;        // columns kCols / 2 * half ..
+        const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        uint8_t* stg = staging + (warp - kEpiWarp0) * kOutBufs * kStageOut;
+        uint32_t sbuf = 0;
+        const bool wide = (e.ldo & 7) == 0;
+        // 32 columns of the thread's row, from column n, through the staging buffer (a bulk store of a 32 x 32 box)
+        // or, where rows are not on 16-byte boundaries, one by one
+        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int64_t m, int row0) {
+            if (p.direct) {
+                if (m < e.M) {
+                    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + m * e.ldo + n;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        float lo, hi;
+                        unpack_bf16(w[c], lo, hi);
+                        if (n + 2 * c < e.N) o[2 * c] = __float2bfloat16_rn(lo);
+                        if (n + 2 * c + 1 < e.N) o[2 * c + 1] = __float2bfloat16_rn(hi);
+                    }
+                }
+                return;
+            }
+            // the staging buffer is free once the store issued from it two boxes ago has read it
+            if (lane == 0) bulk_wait_read1();
+            __syncwarp();
+            uint8_t* sb = stg + sbuf * kStageOut + lane * 64;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                *reinterpret_cast<uint4*>(sb + ((c ^ ((lane >> 1) & 3)) << 4)) =
+                    make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store_2d(map, smem_u32(stg + sbuf * kStageOut), n, row0);
+                bulk_commit();
+            }
+            sbuf ^= 1u;
+        };
+        uint32_t unit_count = 0;
+        for (int64_t u = worker; u < p.units; u += workers, ++unit_count) {
+            int tm, tn;
+            decode(p, u, tm, tn);
+            const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
+            const int64_t m = static_cast<int64_t>(row0) + lane;
+            const int col0 = half * (kCols / 2);
+            const uint32_t buf = unit_count & 1u;
+            const uint32_t use = (unit_count >> 1) & 1u;
+            if (!mbar_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t acc = lane_base + buf * BN;
+#pragma unroll 1
+            for (int c = 0; c < kCols / 64; ++c) {
+                const int n = tn * kCols + col0 + 32 * c;
+                if (n >= e.N || row0 >= e.M) continue;     // box entirely outside (warp-uniform)
+                const uint32_t at = acc + static_cast<uint32_t>(col0 + 32 * c);
+                uint32_t w[16];
+                if constexpr (KIND == kEpiLinear) {
+                    float v[32];
+                    tmem_ld16(at, v);
+                    tmem_ld16(at + 16u, v + 16);
+                    tmem_wait_ld();
+                    if (e.bias) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float b[8];
+                            load8(reinterpret_cast<const __nv_bfloat16*>(e.bias), n + 8 * q, e.N, true, b);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
+                        }
+                    }
+                    if (e.Z && m < e.M) {
+                        float* z = e.Z + m * e.N + n;
+                        if ((e.N & 3) == 0) {
+#pragma unroll
+                            for (int q = 0; q < 8; ++q)
+                                if (n + 4 * q < e.N)
+                                    *reinterpret_cast<float4*>(z + 4 * q) =
+                                        make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (n + i < e.N) z[i] = v[i];
+                        }
+                    }
+                    if (e.act != DTP_ACT_NONE) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = act_value<true>(e.act, v[i]);
+                    }
+                    if (e.residual && m < e.M) {
+                        const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + m * e.ldo;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float b[8];
+                            load8(r, n + 8 * q, e.N, wide, b);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                    store32(&p.out, e.out, w, n, m, row0);
+                } else if constexpr (KIND == kEpiGated) {
+                    float* pre = e.pre ? e.pre + pre_index(m, n, e.N) : nullptr;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        float g[16], v[16];
+                        tmem_ld16(at + 16u * q, g);
+                        tmem_ld16(at + static_cast<uint32_t>(BN / 2) + 16u * q, v);
+                        tmem_wait_ld();
+                        if (pre) {       // whole tiles: rows and columns beyond the edges have their place
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                float* to = pre + (4 * q + i) * kPreTile * 4;
+                                *reinterpret_cast<float4*>(to) =
+                                    make_float4(g[4 * i], g[4 * i + 1], g[4 * i + 2], g[4 * i + 3]);
+                                *reinterpret_cast<float4*>(to + kPreTile * kPreTile) =
+                                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            w[8 * q + i] = pack_bf16(act_value<true>(e.act, g[2 * i]) * v[2 * i],
+                                                     act_value<true>(e.act, g[2 * i + 1]) * v[2 * i + 1]);
+                    }
+                    store32(&p.out, e.out, w, n, m, row0);
+                } else {
+                    const float* pre = e.pre + pre_index(m, n, e.N);
+                    uint32_t w2[16];
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        float dh[16];
+                        tmem_ld16(at + 16u * q, dh);
+                        float4 g[4], v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float* from = pre + (4 * q + i) * kPreTile * 4;
+                            g[i] = __ldcs(reinterpret_cast<const float4*>(from));
+                            v[i] = __ldcs(reinterpret_cast<const float4*>(from + kPreTile * kPreTile));
+                        }
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float gi[4] = {g[i].x, g[i].y, g[i].z, g[i].w};
+                            const float ui[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                            float dg[4], du[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float val, slope;
+                                act_both<true>(e.act, gi[j], val, slope);
+                                dg[j] = dh[4 * i + j] * ui[j] * slope;
+                                du[j] = dh[4 * i + j] * val;
+                            }
+                            w[8 * q + 2 * i] = pack_bf16(dg[0], dg[1]);
+                            w[8 * q + 2 * i + 1] = pack_bf16(dg[2], dg[3]);
+                            w2[8 * q + 2 * i] = pack_bf16(du[0], du[1]);
+                            w2[8 * q + 2 * i + 1] = pack_bf16(du[2], du[3]);
+                        }
+                    }
+                    store32(&p.out, e.out, w, n, m, row0);
+                    store32(&p.out2, e.out2, w2, n, m, row0);
+                }
+            }
+            // its TMEM loads have completed (tcgen05.wait::ld): hand the buffer back without release ordering,
+            // which would also wait for the warp's stores
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (kPair)
+                    mbar_arrive_cluster_relaxed(mapa_shared(smem_u32(&acc_empty[buf]), 0));
+                else
+                    mbar_arrive_relaxed(smem_u32(&acc_empty[buf]));
+            }
+        }
+        if (lane == 0) bulk_wait_all();
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1 && lane == 0) {
+        // the last MMA commit: every MMA (in the pair form reading both CTAs' tiles and writing
+        // both CTAs' TMEM) has completed
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait(smem_u32(drain_bar), 0) && globaltimer_ns() - t0 < kWaitLimitNs) {
+        }
+    }
+    // After a wait gave up, loads already issued (in the pair form also the peer's) may still be
+    // landing in this CTA's shared memory or on its barriers: let them finish before exiting.
+    if constexpr (kPair) {
+        cluster_sync();
+        if (threadIdx.x == 0) {
+            const int peer_abort = static_cast<int>(ld_shared_cluster_u32(
+                mapa_shared(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u)));
+            if (*abort_flag || peer_abort) {
+                const uint64_t t0 = globaltimer_ns();
+                while (globaltimer_ns() - t0 < 200ull * 1000ull) {
+                }
+            }
+        }
+        cluster_sync();
+    } else {
+        if (threadIdx.x == 0 && *abort_flag) {
+            const uint64_t t0 = globaltimer_ns();
+            while (globaltimer_ns() - t0 < 200ull * 1000ull) {
+            }
+        }
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        if constexpr (kPair)
+            tmem_dealloc_pair(tmem, F::kTmemCols);
+        else
+            tmem_dealloc(tmem, F::kTmemCols);
+    }
+    if (threadIdx.x == 0 && *abort_flag) atomicExch(p.status, static_cast<int>(DTP_ERR_NOT_CONVERGED));
+}
+
+// ------------------------------------------------------------------------------------ host
+
+static bool map_2d(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_x, int box_y,
+                   CUtensorMapSwizzle swz) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return false;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
+    cuuint32_t box[2] = {static_cast<cuuint32_t>(box_x), static_cast<cuuint32_t>(box_y)};
+    cuuint32_t estr[2] = {1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// rows x K operand: tiles of `box_rows` rows x 64 k, or where the rows are contiguous 64 rows x 64 k.
+static bool map_operand(CUtensorMap* m, const Mat& a, int64_t rows, int64_t K, int box_rows) {
+    if (a.ks == 1) return map_2d(m, a.p, K, rows, a.rs, BK, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
+    return map_2d(m, a.p, rows, K, a.ks, 64, BK, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+template <bool kPair, int BN>
+static int launch_form(const Product& p, int* status, int reset, int sms, cudaStream_t stream) {
+    using F = Form<kPair, BN>;
+    const bool gated = p.epi.kind == kEpiGated;
+    Args a;
+    for (int s = 0; s < 2; ++s) {
+        const int sa = s < p.segments ? s : 0, sb = s < p.segments || gated ? s : 0;
+        if (!map_operand(&a.a[s], p.A[sa], p.M, p.K, BM) || !map_operand(&a.b[s], p.B[sb], p.N, p.K, BN / 2))
+            return DTP_ERR_CUDA;
+    }
+    a.direct = (p.epi.ldo & 7) != 0;
+    if (!a.direct) {
+        if (!map_2d(&a.out, p.epi.out, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
+        const void* second = p.epi.out2 ? p.epi.out2 : p.epi.out;
+        if (!map_2d(&a.out2, second, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
+    }
+    const int rows = kPair ? 2 * BM : BM, cols = gated ? BN / 2 : BN;
+    a.segments = p.segments;
+    a.KB = static_cast<int>((p.K + BK - 1) / BK);
+    a.a_mn = p.A[0].ks != 1;
+    a.b_mn = p.B[0].ks != 1;
+    a.tiles_m = static_cast<int>((p.M + rows - 1) / rows);
+    a.tiles_n = (p.N + cols - 1) / cols;
+    a.units = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
+    // bits 15 and 16: A and B stored with their rows contiguous
+    a.idesc = idesc_bf16_f32(kPair ? 2 * BM : BM, BN) | (a.a_mn ? 1u << 15 : 0u) | (a.b_mn ? 1u << 16 : 0u);
+    a.reset = reset;
+    a.status = status;
+    a.epi = p.epi;
+    auto kernel = gated                              ? gemm_tc_kernel<kPair, BN, kEpiGated>
+                  : p.epi.kind == kEpiGatedGrad ? gemm_tc_kernel<kPair, BN, kEpiGatedGrad>
+                                                     : gemm_tc_kernel<kPair, BN, kEpiLinear>;
+    DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      static_cast<int>(F::kSmemBytes)));
+    const int64_t per = kPair ? 2 : 1;
+    const int64_t most = sms / per;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(per * (a.units < most ? a.units : most)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = F::kSmemBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(per);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = kPair ? 1 : 0;
+    DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+    return DTP_OK;
+}
+
+// bf16 operands whose rows are on 16-byte boundaries; M, N >= 1, K >= 1.
+int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
+    int dev = 0, sms = 0;
+    DTP_CUDA_TRY(cudaGetDevice(&dev));
+    DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const int64_t cols = p.epi.kind == kEpiGated ? 128 : 256;
+    const int64_t tiles = (p.M + 255) / 256 * ((p.N + cols - 1) / cols);
+    if (2 * tiles >= sms) return launch_form<true, 256>(p, status, reset, sms, stream);
+    return launch_form<false, 128>(p, status, reset, sms, stream);
+}
+
+}  // namespace gtc
+}  // namespace dtp

@@ -11,6 +11,13 @@ namespace dtp {
 namespace simt {
 int launch(const layer::Product& p, int dtype, cudaStream_t stream);
 }  // namespace simt
+namespace gtc {
+int launch(const layer::Product& p, int* status, int reset, cudaStream_t stream);
+}  // namespace gtc
+namespace few {
+bool takes(const layer::Product& p);
+int launch(const layer::Product& p, int* status, int reset, int second, cudaStream_t stream);
+}  // namespace few
 
 namespace layer {
 
@@ -62,6 +69,15 @@ __global__ void bias_reduce_kernel(const float* __restrict__ partial, int64_t ch
     out[n] = from_f32<E>(s);
 }
 
+// Rows copied to a pitch of whole 16 bytes, for the tensor cores' loads; the pitch's spare entries stay unwritten
+// (the loads' extents end before them).
+__global__ void __launch_bounds__(256)
+repitch_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t pitch, uint16_t* __restrict__ dst) {
+    const int64_t total = rows * cols;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll)
+        dst[i / cols * pitch + i % cols] = src[i];
+}
+
 // Pieces of a workspace, in the order in which they are asked for.
 struct Carver {
     uint8_t* base;
@@ -78,16 +94,69 @@ static size_t elem(int dtype) { return dtype == DTP_BF16 ? 2 : 4; }
 static int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 static int64_t chunks_of(int64_t T) { return (T + kRowChunk - 1) / kRowChunk; }
 
+// bf16 [rows, cols] as the tensor cores can load it: itself, or a copy at an aligned pitch from the workspace.
+struct Rows {
+    const void* p;
+    int64_t ld;
+};
+static size_t repitch_bytes(int64_t rows, int cols, int dtype) {
+    return dtype == DTP_BF16 && cols % 8 ? static_cast<size_t>(rows) * padded(cols) * 2 : 0;
+}
+static int aligned_rows(const void* p, int64_t rows, int cols, int dtype, Carver& c, cudaStream_t stream, Rows* out) {
+    const size_t bytes = repitch_bytes(rows, cols, dtype);
+    if (bytes == 0) {
+        *out = Rows{p, cols};
+        return DTP_OK;
+    }
+    void* to = c.take(bytes);
+    *out = Rows{to, padded(cols)};
+    const int64_t blocks = (rows * cols + 1023) / 1024;
+    repitch_kernel<<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(
+        static_cast<const uint16_t*>(p), rows, cols, padded(cols), static_cast<uint16_t*>(to));
+    DTP_CUDA_TRY(cudaGetLastError());
+    return DTP_OK;
+}
+
 static Mat by_row(const void* p, int64_t ld) { return Mat{p, ld, 1}; }      // [rows, K]
 static Mat by_col(const void* p, int64_t ld) { return Mat{p, 1, ld}; }      // [K, rows]
 
-static int product(const Product& p, int dtype, cudaStream_t stream) { return simt::launch(p, dtype, stream); }
+// One call's products, in order on its stream.  The first launch that may give up on a wait clears the status word.
+struct Call {
+    int dtype;
+    void* workspace;
+    cudaStream_t stream;
+    bool fresh = true;          // the status word is still an earlier call's
+    bool after_few = false;     // the last launch was the few-token kernel
+
+    int run(const Product& p) {
+        int* status = static_cast<int*>(workspace);
+        const int reset = fresh;
+        const bool second = after_few;
+        after_few = false;
+        if (dtype == DTP_BF16 && p.K > 0) {
+            fresh = false;
+            if (few::takes(p)) {
+                after_few = true;
+                return few::launch(p, status, reset, second, stream);
+            }
+            return gtc::launch(p, status, reset, stream);
+        }
+        return simt::launch(p, dtype, stream);
+    }
+    // calls without such a launch
+    int done() {
+        if (!fresh) return DTP_OK;
+        DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, sizeof(int), stream));
+        return DTP_OK;
+    }
+};
 
 // ------------------------------------------------------------------------------- linear layer
 
-static size_t linear_bytes(int64_t T, int K, int N, int dtype, int backward) {
-    (void)K;
+size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) {
     Carver c(nullptr);
+    c.take(repitch_bytes(T, K, dtype));
+    c.take(repitch_bytes(N, K, dtype));
     if (backward) {
         c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
         c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float));
@@ -95,20 +164,22 @@ static size_t linear_bytes(int64_t T, int K, int N, int dtype, int backward) {
     return c.used;
 }
 
-size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) {
-    return linear_bytes(T, K, N, dtype, backward);
-}
-
 int linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
                    int act, int dtype, void* Y, float* Z, void* workspace, cudaStream_t stream) {
-    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Call call{dtype, workspace, stream};
+    Carver c(workspace);
+    Rows x, w;
+    int st = aligned_rows(X, T, K, dtype, c, stream, &x);
+    if (st == DTP_OK) st = aligned_rows(W, N, K, dtype, c, stream, &w);
+    if (st != DTP_OK) return st;
     Product p;
-    p.A[0] = by_row(X, K);
-    p.B[0] = by_row(W, K);
+    p.A[0] = by_row(x.p, x.ld);
+    p.B[0] = by_row(w.p, w.ld);
     p.M = T, p.N = N, p.K = K;
     p.epi.act = act, p.epi.bias = bias, p.epi.residual = residual, p.epi.out = Y, p.epi.ldo = N, p.epi.Z = Z;
     p.epi.M = T, p.epi.N = N;
-    return product(p, dtype, stream);
+    if ((st = call.run(p)) != DTP_OK) return st;
+    return call.done();
 }
 
 template <typename E>
@@ -130,46 +201,54 @@ static int launch_act_grad(const void* dY, const float* Z, int64_t T, int N, int
 int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
                     int dtype, void* dX, void* dW, void* dbias, void* workspace, cudaStream_t stream) {
     if (chunks_of(T) > 65535) return DTP_ERR_UNSUPPORTED;
-    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Call call{dtype, workspace, stream};
     Carver c(workspace);
     void* dz = c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
     float* partial = static_cast<float*>(c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float)));
-    const bool own_dz = act != DTP_ACT_NONE;
+    // dY itself serves as dZ where nothing changes it and the tensor cores can load its rows
+    const bool own_dz = act != DTP_ACT_NONE || repitch_bytes(T, N, dtype) > 0;
     const int64_t ldz = own_dz ? padded(N) : N;
+    int st = DTP_OK;
     if (own_dz || dbias) {
         auto go = dtype == DTP_BF16 ? launch_act_grad<__nv_bfloat16> : launch_act_grad<float>;
-        const int st = go(dY, Z, T, N, act, own_dz ? dz : nullptr, ldz, partial, dbias, stream);
+        st = go(dY, Z, T, N, act, own_dz ? dz : nullptr, ldz, partial, dbias, stream);
         if (st != DTP_OK) return st;
     }
     const void* g = own_dz ? dz : dY;
     if (dX && T > 0) {
+        Rows w;
+        if ((st = aligned_rows(W, N, K, dtype, c, stream, &w)) != DTP_OK) return st;
         Product p;
         p.A[0] = by_row(g, ldz);
-        p.B[0] = by_col(W, K);
+        p.B[0] = by_col(w.p, w.ld);
         p.M = T, p.N = K, p.K = N;
         p.epi.out = dX, p.epi.ldo = K, p.epi.M = T, p.epi.N = K;
-        const int st = product(p, dtype, stream);
-        if (st != DTP_OK) return st;
+        if ((st = call.run(p)) != DTP_OK) return st;
     }
     if (dW) {
+        Rows x;
+        if ((st = aligned_rows(X, T, K, dtype, c, stream, &x)) != DTP_OK) return st;
         Product p;
         p.A[0] = by_col(g, ldz);
-        p.B[0] = by_col(X, K);
+        p.B[0] = by_col(x.p, x.ld);
         p.M = N, p.N = K, p.K = T;
         p.epi.out = dW, p.epi.ldo = K, p.epi.M = N, p.epi.N = K;
-        const int st = product(p, dtype, stream);
-        if (st != DTP_OK) return st;
+        if ((st = call.run(p)) != DTP_OK) return st;
     }
-    return DTP_OK;
+    return call.done();
 }
 
 // ------------------------------------------------------------------------- gated feed-forward
 
 size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward) {
-    (void)d;
     Carver c(nullptr);
     c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
-    if (backward) c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    for (int64_t rows : {T, static_cast<int64_t>(N), static_cast<int64_t>(N)}) c.take(repitch_bytes(rows, d, dtype));
+    c.take(repitch_bytes(d, N, dtype));
+    if (backward) {
+        c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+        c.take(repitch_bytes(T, d, dtype));
+    }
     return c.used;
 }
 
@@ -178,51 +257,63 @@ size_t gated_saved_bytes(int64_t T, int N) { return static_cast<size_t>(pre_floa
 int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd, const void* residual, int64_t T,
                   int d, int N, int act, int dtype, void* Y, void* H, float* pre, void* workspace,
                   cudaStream_t stream) {
-    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Call call{dtype, workspace, stream};
     Carver c(workspace);
     void* h = H ? H : c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
+    Rows x, wg, wu, wd;
+    int st = aligned_rows(X, T, d, dtype, c, stream, &x);
+    if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
+    if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
+    if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
+    if (st != DTP_OK) return st;
     Product p;
-    p.A[0] = by_row(X, d);
-    p.B[0] = by_row(Wg, d), p.B[1] = by_row(Wu, d);
+    p.A[0] = by_row(x.p, x.ld);
+    p.B[0] = by_row(wg.p, wg.ld), p.B[1] = by_row(wu.p, wu.ld);
     p.M = T, p.N = N, p.K = d;
     p.epi.kind = kEpiGated, p.epi.act = act, p.epi.out = h, p.epi.ldo = padded(N), p.epi.pre = pre;
     p.epi.M = T, p.epi.N = N;
-    int st = product(p, dtype, stream);
-    if (st != DTP_OK) return st;
+    if ((st = call.run(p)) != DTP_OK) return st;
     Product q;
     q.A[0] = by_row(h, padded(N));
-    q.B[0] = by_row(Wd, N);
+    q.B[0] = by_row(wd.p, wd.ld);
     q.M = T, q.N = d, q.K = N;
     q.epi.residual = residual, q.epi.out = Y, q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
-    return product(q, dtype, stream);
+    if ((st = call.run(q)) != DTP_OK) return st;
+    return call.done();
 }
 
 int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu, const void* Wd, const void* H,
                    const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX, void* dWg, void* dWu,
                    void* dWd, void* workspace, cudaStream_t stream) {
-    DTP_CUDA_TRY(cudaMemsetAsync(workspace, 0, kWorkspaceHeader, stream));
+    Call call{dtype, workspace, stream};
     Carver c(workspace);
     const int64_t ld = padded(N);
     void* dg = c.take(static_cast<size_t>(T) * ld * elem(dtype));
     void* du = c.take(static_cast<size_t>(T) * ld * elem(dtype));
-    int st = DTP_OK;
+    Rows x, wg, wu, wd, dy;
+    int st = aligned_rows(X, T, d, dtype, c, stream, &x);
+    if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
+    if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
+    if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
+    if (st == DTP_OK) st = aligned_rows(dY, T, d, dtype, c, stream, &dy);
+    if (st != DTP_OK) return st;
     if (T > 0) {
         Product p;
-        p.A[0] = by_row(dY, d);
-        p.B[0] = by_col(Wd, N);
+        p.A[0] = by_row(dy.p, dy.ld);
+        p.B[0] = by_col(wd.p, wd.ld);
         p.M = T, p.N = N, p.K = d;
         p.epi.kind = kEpiGatedGrad, p.epi.act = act, p.epi.out = dg, p.epi.out2 = du, p.epi.ldo = ld;
         p.epi.pre = const_cast<float*>(pre), p.epi.M = T, p.epi.N = N;
-        if ((st = product(p, dtype, stream)) != DTP_OK) return st;
+        if ((st = call.run(p)) != DTP_OK) return st;
     }
     if (dX && T > 0) {
         Product p;
         p.segments = 2;
         p.A[0] = by_row(dg, ld), p.A[1] = by_row(du, ld);
-        p.B[0] = by_col(Wg, d), p.B[1] = by_col(Wu, d);
+        p.B[0] = by_col(wg.p, wg.ld), p.B[1] = by_col(wu.p, wu.ld);
         p.M = T, p.N = d, p.K = N;
         p.epi.out = dX, p.epi.ldo = d, p.epi.M = T, p.epi.N = d;
-        if ((st = product(p, dtype, stream)) != DTP_OK) return st;
+        if ((st = call.run(p)) != DTP_OK) return st;
     }
     auto weight = [&](const void* a, int64_t lda, int64_t rows, const void* b, int64_t ldb, int cols, void* out) {
         if (!out) return static_cast<int>(DTP_OK);
@@ -231,11 +322,12 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
         p.B[0] = by_col(b, ldb);
         p.M = rows, p.N = cols, p.K = T;
         p.epi.out = out, p.epi.ldo = cols, p.epi.M = rows, p.epi.N = cols;
-        return product(p, dtype, stream);
+        return call.run(p);
     };
-    if ((st = weight(dg, ld, N, X, d, d, dWg)) != DTP_OK) return st;
-    if ((st = weight(du, ld, N, X, d, d, dWu)) != DTP_OK) return st;
-    return weight(dY, d, d, H, ld, N, dWd);
+    if ((st = weight(dg, ld, N, x.p, x.ld, d, dWg)) != DTP_OK) return st;
+    if ((st = weight(du, ld, N, x.p, x.ld, d, dWu)) != DTP_OK) return st;
+    if ((st = weight(dy.p, dy.ld, d, H, ld, N, dWd)) != DTP_OK) return st;
+    return call.done();
 }
 
 }  // namespace layer
