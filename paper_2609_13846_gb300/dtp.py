@@ -7,7 +7,9 @@ stream.  It raises if the library was not built: there is no CPU fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes
+import operator
 import os
 
 import torch
@@ -813,6 +815,9 @@ def apply_layout(W: dict, h: torch.Tensor, nu: torch.Tensor, D: int, head_dim: i
 
 # ------------------------------------------------------ layers of the permuted model (Sec. 4) --
 
+_dtype_of = operator.attrgetter("dtype")
+_CLIP_CODES = {torch.bfloat16: DTP_BF16, torch.float32: DTP_F32}
+
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}
 
 
@@ -998,8 +1003,21 @@ def clip_grad_norm_workspace(grads) -> torch.Tensor:
     n = len(grads)
     if n == 0:
         raise ValueError("grads must hold at least one tensor")
-    size = _size_query("dtp_clip_grad_norm_workspace_size", n, (_i64 * n)(*[g.numel() for g in grads]))
-    return torch.empty(size, dtype=torch.uint8, device=grads[0].device)
+    return _clip_workspace(array.array("q", map(torch.Tensor.numel, grads)), grads[0].device)
+
+
+def _clip_workspace(numel, device) -> torch.Tensor:
+    size = _size_query("dtp_clip_grad_norm_workspace_size", len(numel), numel.buffer_info()[0])
+    return torch.empty(size, dtype=torch.uint8, device=device)
+
+
+def _flat_tensors(name, ts, index):
+    """(addresses, sizes, dtypes) of contiguous CUDA tensors of device ``index``.  One pass per property with map, and
+    not one Python loop over the tensors: a model has hundreds of them, and the call is as long as its kernel."""
+    if index < 0 or set(map(torch.Tensor.get_device, ts)) != {index} or not all(map(torch.Tensor.is_contiguous, ts)):
+        raise ValueError(f"{name} must be contiguous CUDA tensors on one device")
+    return (array.array("Q", map(torch.Tensor.data_ptr, ts)), array.array("q", map(torch.Tensor.numel, ts)),
+            list(map(_dtype_of, ts)))
 
 
 def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None = None,
@@ -1007,7 +1025,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
     """Scale all tensors by max_norm / n where n, their global 2-norm, is above max_norm; returns n (0-d fp32).
 
     grads: contiguous CUDA tensors, each bf16 or fp32, scaled in place, or into ``out`` (a list of the same
-    shapes and dtypes, which receives the tensors unchanged when n <= max_norm).  max_norm may be infinite: the
+    sizes and dtypes, which receives the tensors unchanged when n <= max_norm).  max_norm may be infinite: the
     norm alone.  A norm that is not finite leaves the gradients as they are.
     """
     grads = list(grads)
@@ -1015,29 +1033,26 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
     if count == 0:
         raise ValueError("grads must hold at least one tensor")
     index = grads[0].get_device()
-    out = None if out is None else list(out)
-    if out is not None and len(out) != count:
-        raise ValueError(f"out must hold {count} tensors, got {len(out)}")
-    codes = []
-    for name, ts in (("grads", grads), ("out", out)):
-        for t in ts or ():
-            if not t.is_cuda or t.get_device() != index or not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous CUDA tensors on one device")
-    for g in grads:
-        codes.append(_torch_code(g.dtype))
+    src, numel, dtypes = _flat_tensors("grads", grads, index)
+    if not _CLIP_CODES.keys() >= set(dtypes):
+        raise TypeError("grads must be bfloat16 or float32")
+    dst = None
     if out is not None:
-        for g, o in zip(grads, out):
-            if o.dtype is not g.dtype or o.shape != g.shape:
-                raise ValueError("out must have the shapes and dtypes of grads")
+        out = list(out)
+        if len(out) != count:
+            raise ValueError(f"out must hold {count} tensors, got {len(out)}")
+        dst, out_numel, out_dtypes = _flat_tensors("out", out, index)
+        if out_numel != numel or out_dtypes != dtypes:
+            raise ValueError("out must have the sizes and dtypes of grads")
+    codes = array.array("i", map(_CLIP_CODES.__getitem__, dtypes))
     if norm is None:
         norm = _keep(torch.empty((), dtype=torch.float32, device=grads[0].device), stream)
     elif norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != index:
         raise ValueError("norm must be one fp32 value on the gradients' device")
     if workspace is None:
-        workspace = _keep(clip_grad_norm_workspace(grads), stream)
-    src = (_vp * count)(*[g.data_ptr() for g in grads])
-    dst = None if out is None else (_vp * count)(*[o.data_ptr() for o in out])
-    st = lib().dtp_clip_grad_norm(src, dst, (_i64 * count)(*[g.numel() for g in grads]), (_i32 * count)(*codes), count,
-                                  float(max_norm), _ptr(norm), _ptr(workspace), workspace.numel(), _stream(stream))
+        workspace = _keep(_clip_workspace(numel, grads[0].device), stream)
+    st = lib().dtp_clip_grad_norm(src.buffer_info()[0], None if dst is None else dst.buffer_info()[0],
+                                  numel.buffer_info()[0], codes.buffer_info()[0], count, float(max_norm), _ptr(norm),
+                                  _ptr(workspace), workspace.numel(), _stream(stream))
     _check("dtp_clip_grad_norm", st)
     return norm
