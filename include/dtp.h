@@ -699,8 +699,8 @@ int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, co
  *   norm    device fp32 out: n
  * A norm that is not finite leaves the gradients as they are (out receives
  * copies); the caller reads it and skips the step.  Squares are summed in fp32
- * within a chunk (16384 elements, more for large models), with a power of two
- * taken out where they would leave fp32's range, and in fp64 beyond.
+ * by each thread (with compensation) and block, with a power of two taken out
+ * where they would leave fp32's range, and in fp64 over the blocks.
  * Deterministic.  The host arrays are read before the call returns.  At most
  * 2^46 elements in all.
  * Workspace from dtp_clip_grad_norm_workspace_size.  Asynchronous.

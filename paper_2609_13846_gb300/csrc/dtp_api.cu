@@ -87,8 +87,8 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
                    void* dWd, void* workspace, cudaStream_t stream);
 }  // namespace layer
 namespace clip {
-int64_t chunk_count(int count, const int64_t* numel);
-size_t workspace_bytes(int64_t chunks);
+bool sizes_ok(int count, const int64_t* numel);
+size_t workspace_bytes(int count);
 int launch(const void* const* grads, void* const* out, const int64_t* numel, const int* dtype, int count,
            float max_norm, float* norm, void* workspace, cudaStream_t stream);
 }  // namespace clip
@@ -624,17 +624,15 @@ int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, co
 
 int dtp_clip_grad_norm_workspace_size(int count, const int64_t* numel, size_t* bytes) {
     if (!bytes || count < 0 || (count > 0 && !numel)) return DTP_ERR_ARG;
-    const int64_t chunks = clip::chunk_count(count, numel);
-    if (chunks < 0) return DTP_ERR_ARG;
-    *bytes = clip::workspace_bytes(chunks);
+    if (!clip::sizes_ok(count, numel)) return DTP_ERR_ARG;
+    *bytes = clip::workspace_bytes(count);
     return DTP_OK;
 }
 
 int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int count,
                        float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream) {
     if (count < 0 || (count > 0 && (!grads || !numel || !dtypes)) || !(max_norm >= 0.0f)) return DTP_ERR_ARG;
-    const int64_t chunks = clip::chunk_count(count, numel);
-    if (chunks < 0 || !norm || (reinterpret_cast<uintptr_t>(norm) & 3)) return DTP_ERR_ARG;
+    if (!clip::sizes_ok(count, numel) || !norm || (reinterpret_cast<uintptr_t>(norm) & 3)) return DTP_ERR_ARG;
     for (int i = 0; i < count; ++i) {
         if (dtypes[i] != DTP_BF16 && dtypes[i] != DTP_F32) return DTP_ERR_ARG;
         const uintptr_t mask = dtypes[i] == DTP_BF16 ? 1 : 3;
@@ -642,7 +640,7 @@ int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t
         if (!grads[i] || (reinterpret_cast<uintptr_t>(grads[i]) & mask)) return DTP_ERR_ARG;
         if (out && (!out[i] || (reinterpret_cast<uintptr_t>(out[i]) & mask))) return DTP_ERR_ARG;
     }
-    if (!workspace_ok(workspace, workspace_bytes, clip::workspace_bytes(chunks))) return DTP_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, workspace_bytes, clip::workspace_bytes(count))) return DTP_ERR_WORKSPACE;
     return clip::launch(grads, out, numel, dtypes, count, max_norm, norm, workspace,
                         static_cast<cudaStream_t>(stream));
 }

@@ -3,14 +3,15 @@
 //     n = sqrt(sum over tensors and elements of g^2),  c = n > max_norm ? max_norm / n : 1,  out = c g
 //
 // Bound by memory: one read for the norm, then one read and one write, of which the second read finds in L2 what fits
-// there.  The tensors are cut into chunks (16384 elements, or a larger power of two that keeps their number near 4096).
-// One cooperative launch: each block sums the squares of its chunks in fp32 and writes one fp64 partial per chunk; after a
-// barrier over the grid every block adds all partials in the same fixed order, so the norm does not depend on the grid, and
-// scales its chunks, the last read first.  The table of the tensors is a kernel argument; more of them than it holds take a
-// launch per table for the norm and one per table for the scaling.
-// A chunk whose fp32 sum left the range in which it is exact to fp32's precision (overflow, or so small that
-// squares were lost below 2^-126) is summed again with its elements scaled by a power of two.
-#include <cooperative_groups.h>
+// there.  The tensors are cut into chunks of 8 KB (more where that would be too many to count), and each block takes a
+// run of them, so that all blocks have the same bytes to read whatever the tensors' sizes.  The first launch sums the squares
+// of each block's run in fp32, each thread in rounds of four 16-byte words whose sums enter a compensated total, and writes
+// one fp64 partial per block; the second, which is under way before the first ends and waits for it, adds all partials in the
+// same order in every block and scales the runs, last words first.  (Both in one cooperative launch with a barrier over the
+// grid: 9 us for the smallest call, most of it the launch.)  The table of the tensors is a kernel argument; more of them than
+// it holds take a launch per table for the norm and one per table for the scaling.
+// A block whose fp32 sum left the range in which it is exact to fp32's precision (overflow, or so small that
+// squares were lost below 2^-126) sums again with its elements scaled by a power of two.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -26,8 +27,9 @@ using layer::to_f32;
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int64_t kMinChunk = 16384;   // elements
-constexpr int64_t kManyChunks = 4096;
+constexpr int64_t kMinChunk = 8192;    // bytes
+constexpr int64_t kManyChunks = 1 << 24;
+constexpr int R = 4;                   // 16-byte words in flight per thread
 constexpr int kBlocksPerSm = 2;
 
 template <int CAP>
@@ -39,9 +41,9 @@ struct Table {
     uint8_t f32[CAP];
     int count;
     int chunks;                        // of this table
-    int chunk0;                        // the table's first partial
-    int all_chunks;                    // of all tables
-    int64_t chunk;                     // elements
+    int partial0;                      // the table's first partial
+    int partials;                      // of all tables
+    int64_t chunk;                     // bytes
     float max_norm;
     double* partial;
     float* norm;
@@ -62,15 +64,14 @@ __device__ __forceinline__ int tensor_of(const Table<CAP>& t, int c) {
     return lo;
 }
 
-template <typename V>
-__device__ __forceinline__ V block_sum(V v, V* red) {
+__device__ __forceinline__ float block_sum(float v, float* red) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     __syncthreads();
     if (lane == 0) red[warp] = v;
     __syncthreads();
-    V s = 0;
+    float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) s += red[w];
     return s;
@@ -118,9 +119,19 @@ __device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(E)]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// This thread's share of sum (scale p[i])^2: a round of four words at a time, each round's sum added to the total.
+// A sum of many fp32 terms with the rounding errors of the additions carried along.
+struct Total {
+    float sum = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float y = x - lost, t = sum + y;
+        lost = (t - sum) - y;
+        sum = t;
+    }
+};
+
+// This thread's share of sum (scale p[i])^2.
 template <typename E>
-__device__ __forceinline__ float sum_squares(const E* p, int64_t n, float scale) {
+__device__ __forceinline__ void sum_squares(const E* p, int64_t n, float scale, Total& total) {
     const Span<E> s(p, n);
     const uint4* words = reinterpret_cast<const uint4*>(p + s.head);
     auto square = [&](float x, float& to) { x *= scale; to = fmaf(x, x, to); };
@@ -130,44 +141,31 @@ __device__ __forceinline__ float sum_squares(const E* p, int64_t n, float scale)
 #pragma unroll
         for (int i = 0; i < Span<E>::kPer; ++i) square(v[i], to);
     };
-    float total = 0.0f;
     int64_t i = threadIdx.x;
-    for (; i + 3 * kThreads < s.words; i += 4 * kThreads) {
-        uint4 q[4];
-        float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (; i + (R - 1) * kThreads < s.words; i += R * kThreads) {
+        uint4 q[R];
+        float r[R];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = words[i + j * kThreads];
+        for (int j = 0; j < R; ++j) q[j] = words[i + j * kThreads];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) word(q[j], r[j]);
-        total += (r[0] + r[1]) + (r[2] + r[3]);
+        for (int j = 0; j < R; ++j) r[j] = 0.0f, word(q[j], r[j]);
+        total.add((r[0] + r[1]) + (r[2] + r[3]));
     }
-    for (; i < s.words; i += kThreads) {
-        float r = 0.0f;
-        word(words[i], r);
-        total += r;
-    }
-    if (static_cast<int>(threadIdx.x) < s.head) square(to_f32(p[threadIdx.x]), total);
+    float rest = 0.0f;
+    for (; i < s.words; i += kThreads) word(words[i], rest);
+    if (static_cast<int>(threadIdx.x) < s.head) square(to_f32(p[threadIdx.x]), rest);
     const int64_t tail = s.head + s.words * Span<E>::kPer + threadIdx.x;
-    if (tail < n) square(to_f32(p[tail]), total);
-    return total;
+    if (tail < n) square(to_f32(p[tail]), rest);
+    total.add(rest);
 }
 
 constexpr float kTiny = 8.271806e-25f;         // 2^-80
 constexpr float kUp = 1.2676506e30f;           // 2^100
 constexpr float kDown = 7.888609e-31f;         // 2^-100
 
+// dst = c src, last words first.  Words where both are equally aligned; c == 1 copies bit for bit, NaNs too.
 template <typename E>
-__device__ __forceinline__ double chunk_squares(const E* p, int64_t n, float* red) {
-    float s = block_sum(sum_squares(p, n, 1.0f), red);
-    if (s >= kTiny && s <= 3.0e38f) return static_cast<double>(s);      // the same value in every thread
-    const float scale = s < kTiny ? kUp : kDown;                        // (a NaN stays one either way)
-    s = block_sum(sum_squares(p, n, scale), red);
-    return static_cast<double>(s) / (static_cast<double>(scale) * static_cast<double>(scale));
-}
-
-// dst = c src.  Words where both are equally aligned; c == 1 copies bit for bit, NaNs too.
-template <typename E>
-__device__ __forceinline__ void scale_chunk(const E* src, E* dst, int64_t n, float c) {
+__device__ __forceinline__ void scale_run(const E* src, E* dst, int64_t n, float c) {
     const bool copy = c == 1.0f;
     if (copy && src == dst) return;
     auto one = [&](int64_t i) { dst[i] = copy ? src[i] : from_f32<E>(to_f32(src[i]) * c); };
@@ -186,105 +184,132 @@ __device__ __forceinline__ void scale_chunk(const E* src, E* dst, int64_t n, flo
         for (int i = 0; i < Span<E>::kPer; ++i) v[i] *= c;
         return pack<E>(v);
     };
-    int64_t i = threadIdx.x;
-    for (; i + 3 * kThreads < s.words; i += 4 * kThreads) {
-        uint4 q[4];
+    const int64_t rounds = s.words / (R * kThreads) * (R * kThreads);
+    for (int64_t i = rounds + threadIdx.x; i < s.words; i += kThreads) __stcs(to + i, word(from[i]));
+    for (int64_t i = rounds - R * kThreads + threadIdx.x; i >= 0; i -= R * kThreads) {
+        uint4 q[R];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = from[i + j * kThreads];
+        for (int j = 0; j < R; ++j) q[j] = from[i + j * kThreads];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) __stcs(to + i + j * kThreads, word(q[j]));
+        for (int j = 0; j < R; ++j) __stcs(to + i + j * kThreads, word(q[j]));
     }
-    for (; i < s.words; i += kThreads) __stcs(to + i, word(from[i]));
     if (static_cast<int>(threadIdx.x) < s.head) one(threadIdx.x);
     const int64_t tail = s.head + s.words * Span<E>::kPer + threadIdx.x;
     if (tail < n) one(tail);
 }
 
-enum Mode { kBoth = 0, kNorm = 1, kScale = 2 };
+enum Mode { kNorm = 0, kScale = 1 };
 
 template <int CAP, int MODE>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clip_kernel(const __grid_constant__ Table<CAP> t) {
     __shared__ float red[kWarps];
-    __shared__ double red64[kWarps];
-    auto chunk_of = [&](int c, int& i, int64_t& at, int64_t& n) {
-        i = tensor_of(t, c);
-        at = (c - t.first[i]) * t.chunk;
-        n = t.numel[i] - at < t.chunk ? t.numel[i] - at : t.chunk;
+    __shared__ float coef;
+    // this block's chunks, and elements [a, b) of tensor i among them
+    const int c0 = static_cast<int>(static_cast<int64_t>(t.chunks) * blockIdx.x / gridDim.x);
+    const int c1 = static_cast<int>(static_cast<int64_t>(t.chunks) * (blockIdx.x + 1) / gridDim.x);
+    auto part = [&](int i, int64_t& a, int64_t& b) {
+        const int64_t per = t.chunk / (t.f32[i] ? 4 : 2);
+        a = c0 > t.first[i] ? (c0 - t.first[i]) * per : 0;
+        b = c1 < t.first[i + 1] ? (c1 - t.first[i]) * per : t.numel[i];
     };
-    if (blockIdx.x == 0 && threadIdx.x == 0) *t.status = DTP_OK;     // nothing here can give up
-    if constexpr (MODE != kScale) {
-        for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-            int i;
-            int64_t at, n;
-            chunk_of(c, i, at, n);
-            const double s = t.f32[i] ? chunk_squares(static_cast<const float*>(t.src[i]) + at, n, red)
-                                      : chunk_squares(static_cast<const __nv_bfloat16*>(t.src[i]) + at, n, red);
-            if (threadIdx.x == 0) t.partial[t.chunk0 + c] = s;
+    if (MODE == kNorm && blockIdx.x == 0 && threadIdx.x == 0) *t.status = DTP_OK;     // nothing here can give up
+    if constexpr (MODE == kNorm) {
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        auto squares = [&](float scale) {
+            Total total;
+            if (c0 < c1) {
+                for (int i = tensor_of(t, c0); i < t.count && t.first[i] < c1; ++i) {
+                    int64_t a, b;
+                    part(i, a, b);
+                    if (t.f32[i]) sum_squares(static_cast<const float*>(t.src[i]) + a, b - a, scale, total);
+                    else sum_squares(static_cast<const __nv_bfloat16*>(t.src[i]) + a, b - a, scale, total);
+                }
+            }
+            return block_sum(total.sum, red);          // the same value in every thread
+        };
+        float s = squares(1.0f), scale = 1.0f;
+        if (!(s >= kTiny && s <= 3.0e38f)) {
+            scale = s < kTiny ? kUp : kDown;           // (a NaN stays one either way)
+            s = squares(scale);
         }
-    }
-    if constexpr (MODE == kBoth) cooperative_groups::this_grid().sync();
-    if constexpr (MODE != kNorm) {
-        double s = 0.0;
-        for (int c = threadIdx.x; c < t.all_chunks; c += kThreads) s += __ldcg(t.partial + c);
-        const double r = sqrt(block_sum(s, red64));
-        // a norm that is not finite leaves the gradients as they are
-        const float f = isfinite(r) && r > static_cast<double>(t.max_norm) ? static_cast<float>(t.max_norm / r) : 1.0f;
-        if (blockIdx.x == 0 && threadIdx.x == 0) *t.norm = static_cast<float>(r);
-        const int last = t.chunks - 1 - static_cast<int>(blockIdx.x);
-        for (int c = static_cast<int>(blockIdx.x) + (last < 0 ? 0 : last / static_cast<int>(gridDim.x) * static_cast<int>(gridDim.x));
-             c >= 0 && c < t.chunks; c -= gridDim.x) {
-            int i;
-            int64_t at, n;
-            chunk_of(c, i, at, n);
-            if (t.f32[i])
-                scale_chunk(static_cast<const float*>(t.src[i]) + at, static_cast<float*>(t.dst[i]) + at, n, f);
-            else
-                scale_chunk(static_cast<const __nv_bfloat16*>(t.src[i]) + at,
-                            static_cast<__nv_bfloat16*>(t.dst[i]) + at, n, f);
+        if (threadIdx.x == 0)
+            t.partial[t.partial0 + blockIdx.x] = static_cast<double>(s) / (static_cast<double>(scale) * scale);
+    } else {
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        // one warp adds the partials: an SM has two fp64 additions a clock (all 512 threads taking part: 5 us)
+        if (threadIdx.x < 32) {
+            double s = 0.0;
+            for (int c = threadIdx.x; c < t.partials; c += 32) s += __ldcg(t.partial + c);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            if (threadIdx.x == 0) {
+                const double r = sqrt(s);
+                // a norm that is not finite leaves the gradients as they are
+                coef = isfinite(r) && r > static_cast<double>(t.max_norm) ? static_cast<float>(t.max_norm / r) : 1.0f;
+                if (blockIdx.x == 0) *t.norm = static_cast<float>(r);
+            }
+        }
+        __syncthreads();
+        const float f = coef;
+        if (c0 < c1) {
+            for (int i = tensor_of(t, c1 - 1); i >= 0 && t.first[i + 1] > c0; --i) {
+                int64_t a, b;
+                part(i, a, b);
+                if (t.f32[i])
+                    scale_run(static_cast<const float*>(t.src[i]) + a, static_cast<float*>(t.dst[i]) + a, b - a, f);
+                else
+                    scale_run(static_cast<const __nv_bfloat16*>(t.src[i]) + a,
+                              static_cast<__nv_bfloat16*>(t.dst[i]) + a, b - a, f);
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------------------------ host
 
-static int64_t chunk_elements(int count, const int64_t* numel) {
+static int64_t bytes_of(int64_t numel, int dtype) { return numel * (dtype == DTP_F32 ? 4 : 2); }
+
+static int64_t chunk_bytes(int count, const int64_t* numel, const int* dtype) {
     int64_t total = 0, chunk = kMinChunk;
-    for (int i = 0; i < count; ++i) total += numel[i];
+    for (int i = 0; i < count; ++i) total += bytes_of(numel[i], dtype[i]);
     while (total / chunk > kManyChunks) chunk *= 2;
     return chunk;
 }
 
-// Chunks of all tensors; -1 for a negative size or too many of them.
-int64_t chunk_count(int count, const int64_t* numel) {
+// Whether the sizes can be counted.
+bool sizes_ok(int count, const int64_t* numel) {
     int64_t total = 0;
     for (int i = 0; i < count; ++i) {
-        if (numel[i] < 0 || numel[i] > (int64_t(1) << 46)) return -1;
+        if (numel[i] < 0 || numel[i] > (int64_t(1) << 46)) return false;
         total += numel[i];
-        if (total > (int64_t(1) << 46)) return -1;
+        if (total > (int64_t(1) << 46)) return false;
     }
-    const int64_t chunk = chunk_elements(count, numel);
-    int64_t chunks = 0;
-    for (int i = 0; i < count; ++i) chunks += (numel[i] + chunk - 1) / chunk;
-    return chunks;
+    return count < (1 << 24);
 }
 
-size_t workspace_bytes(int64_t chunks) {
-    return kWorkspaceHeader + align_up(static_cast<size_t>(chunks) * sizeof(double), 256);
+// Blocks of a table's launch; a partial for each of them.
+constexpr int kMostBlocks = 512;
+size_t workspace_bytes(int count) {
+    return kWorkspaceHeader + static_cast<size_t>(count / kLargeTable + 1) * kMostBlocks * sizeof(double);
+}
+
+static int blocks_of(int chunks, int sms) {
+    const int most = kBlocksPerSm * sms < kMostBlocks ? kBlocksPerSm * sms : kMostBlocks;
+    return chunks < 1 ? 1 : chunks < most ? chunks : most;
 }
 
 template <int CAP, int MODE>
-static int launch_table(const Table<CAP>& t, int sms, cudaStream_t stream) {
+static int launch_table(const Table<CAP>& t, bool early, int sms, cudaStream_t stream) {
     auto kernel = clip_kernel<CAP, MODE>;
     cudaLaunchConfig_t cfg = {};
-    const int most = kBlocksPerSm * sms;
-    cfg.gridDim = dim3(static_cast<unsigned>(t.chunks < 1 ? 1 : t.chunks < most ? t.chunks : most));
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks_of(t.chunks, sms)));
     cfg.blockDim = dim3(kThreads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeCooperative;
-    attr[0].val.cooperative = 1;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = MODE == kBoth ? 1 : 0;
+    cfg.numAttrs = early ? 1 : 0;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, t));
     return DTP_OK;
 }
@@ -292,14 +317,14 @@ static int launch_table(const Table<CAP>& t, int sms, cudaStream_t stream) {
 // Tables of at most CAP non-empty tensors (one, perhaps empty, if there are none), each passed to fn.
 template <int CAP, typename F>
 static int each_table(const void* const* grads, void* const* out, const int64_t* numel, const int* dtype, int count,
-                      Table<CAP>& t, F fn) {
-    t.count = 0, t.chunk0 = 0;
+                      int sms, Table<CAP>& t, F fn) {
+    t.count = 0, t.partial0 = 0;
     int chunks = 0, launched = 0;
     auto flush = [&]() {
         t.chunks = chunks;
         t.first[t.count] = chunks;
         const int st = fn();
-        t.chunk0 += chunks;
+        t.partial0 += blocks_of(chunks, sms);
         t.count = 0, chunks = 0;
         ++launched;
         return st;
@@ -316,29 +341,30 @@ static int each_table(const void* const* grads, void* const* out, const int64_t*
         t.first[t.count] = chunks;
         t.f32[t.count] = dtype[i] == DTP_F32;
         ++t.count;
-        chunks += static_cast<int>((numel[i] + t.chunk - 1) / t.chunk);
+        chunks += static_cast<int>((bytes_of(numel[i], dtype[i]) + t.chunk - 1) / t.chunk);
     }
     return t.count || !launched ? flush() : static_cast<int>(DTP_OK);
 }
 
 template <int CAP>
 static int launch_capacity(const void* const* grads, void* const* out, const int64_t* numel, const int* dtype,
-                           int count, bool one, float max_norm, float* norm, void* workspace, int sms,
-                           cudaStream_t stream) {
+                           int count, float max_norm, float* norm, void* workspace, int sms, cudaStream_t stream) {
     Table<CAP> t;
-    t.chunk = chunk_elements(count, numel);
-    t.all_chunks = static_cast<int>(chunk_count(count, numel));
+    t.chunk = chunk_bytes(count, numel, dtype);
     t.max_norm = max_norm;
     t.norm = norm;
     t.status = static_cast<int*>(workspace);
     t.partial = reinterpret_cast<double*>(static_cast<uint8_t*>(workspace) + kWorkspaceHeader);
-    if (one)
-        return each_table(grads, out, numel, dtype, count, t,
-                          [&] { return launch_table<CAP, kBoth>(t, sms, stream); });
-    const int st = each_table(grads, out, numel, dtype, count, t,
-                              [&] { return launch_table<CAP, kNorm>(t, sms, stream); });
+    const int st = each_table(grads, out, numel, dtype, count, sms, t,
+                              [&] { return launch_table<CAP, kNorm>(t, false, sms, stream); });
     if (st != DTP_OK) return st;
-    return each_table(grads, out, numel, dtype, count, t, [&] { return launch_table<CAP, kScale>(t, sms, stream); });
+    t.partials = t.partial0;             // of all the tables
+    bool early = true;                   // the launch before is the norm's
+    return each_table(grads, out, numel, dtype, count, sms, t, [&] {
+        const int r = launch_table<CAP, kScale>(t, early, sms, stream);
+        early = false;
+        return r;
+    });
 }
 
 int launch(const void* const* grads, void* const* out, const int64_t* numel, const int* dtype, int count,
@@ -349,9 +375,8 @@ int launch(const void* const* grads, void* const* out, const int64_t* numel, con
     int filled = 0;
     for (int i = 0; i < count; ++i) filled += numel[i] != 0;
     if (filled <= kSmallTable)
-        return launch_capacity<kSmallTable>(grads, out, numel, dtype, count, true, max_norm, norm, workspace, sms, stream);
-    return launch_capacity<kLargeTable>(grads, out, numel, dtype, count, filled <= kLargeTable, max_norm, norm, workspace,
-                                        sms, stream);
+        return launch_capacity<kSmallTable>(grads, out, numel, dtype, count, max_norm, norm, workspace, sms, stream);
+    return launch_capacity<kLargeTable>(grads, out, numel, dtype, count, max_norm, norm, workspace, sms, stream);
 }
 
 }  // namespace clip
