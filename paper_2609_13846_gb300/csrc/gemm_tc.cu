@@ -12,12 +12,19 @@
 // Structure: persistent grid, one CTA per SM, twelve warps: warp 0 loads tiles by TMA, warp 1 issues the MMAs,
 // eight warps drain the accumulator, which is double-buffered in TMEM so that a tile's epilogue overlaps the
 // next one's products.  Two forms: CTA pairs share 256 x BN x 16 tcgen05.mma of cta_group::2 (each CTA stages 128
-// rows of A and half of B), single CTAs issue 128 x BN x 16 ones.
+// rows of A and half of B), single CTAs issue 128 x BN x 16 ones (up to 128 rows).  Shared memory bounds both: a 64-wide k
+// block is written once and read once by the tensor core, 64 KB per CTA at 128 bytes a clock for 256 x 256 pairs, as long as
+// its MMAs take (512 clocks), 384 clocks against 256 for 256 x 128 ones, 512 against 256 for single 128 x 128 tiles.
+// Where tiles are fewer than the pairs that the chip holds, a cluster of two or four pairs shares a tile, each pair with its
+// own range of k (kSplit): the partial sums meet in the shared memory that the stages leave free, are added in the order of
+// the ranges, and each CTA finishes a slice of the columns.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <atomic>
 
 #include "dtp_common.cuh"
 #include "layer_common.cuh"
@@ -48,14 +55,17 @@ struct Form {
 };
 
 struct Args {
-    CUtensorMap a[2], b[2], out, out2;
+    CUtensorMap a[2], b[2], out, out2, z;
     int segments;
     int KB;               // k blocks of 64 per segment
     int a_mn, b_mn;       // operand stored with its rows contiguous
     int tiles_m, tiles_n; // per CTA or pair
-    int64_t units;
+    int64_t unit0, units; // this launch's tiles: unit0 .. units - 1
+    int split;            // pairs per tile (kSplit)
+    int early;            // kSplit: begun while the launch before it, of the same product's other tiles, still runs
     uint32_t idesc;
     int direct;           // out rows are not on 16-byte boundaries: plain stores
+    int direct_z;         // the same of Z
     int reset;            // this launch clears the status word
     int* status;
     Epilogue epi;
@@ -121,7 +131,12 @@ __device__ __forceinline__ void decode(const Args& p, int64_t u, int& tm, int& t
     tm = m0 + rest % gm;
 }
 
-template <bool kPair, int BN, int KIND>
+__device__ __forceinline__ void st_shared_cluster_f32x4(uint32_t cluster_addr, float a, float b, float c, float d) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(cluster_addr), "f"(a), "f"(b), "f"(c), "f"(d)
+                 : "memory");
+}
+
+template <bool kPair, int BN, int KIND, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_constant__ Args p) {
     using F = Form<kPair, BN>;
     constexpr int STAGES = F::STAGES;
@@ -145,15 +160,23 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 
     const int warp = threadIdx.x >> 5;
     const int lane = threadIdx.x & 31;
-    const uint32_t rank = kPair ? cluster_ctarank() : 0u;   // 0: issues the MMAs; 1: its peer
+    const uint32_t cluster_rank = kPair ? cluster_ctarank() : 0u;
+    const uint32_t rank = cluster_rank & 1u;                // 0: issues the MMAs; 1: its peer
+    const uint32_t lead_rank = cluster_rank & ~1u;
+    const uint16_t pair_mask = static_cast<uint16_t>(3u << lead_rank);
     const bool leader = rank == 0;
-    const int64_t worker = kPair ? blockIdx.x >> 1 : blockIdx.x;
-    const int64_t workers = kPair ? gridDim.x >> 1 : gridDim.x;
-    const int kblocks = p.segments * p.KB;
+    // a worker (a CTA, a pair, or a cluster of pairs) takes tiles first, first + workers, ..
+    const int ctas = kSplit ? 2 * p.split : kPair ? 2 : 1;
+    const int64_t first = p.unit0 + blockIdx.x / ctas, workers = gridDim.x / ctas;
+    const int part = kSplit ? static_cast<int>(cluster_rank >> 1) : 0;
+    const int all_blocks = p.segments * p.KB;
+    const int kb0 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
+    const int kb1 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * (part + 1) / p.split) : all_blocks;
 
     // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
     // block 0, which starts first, has passed here.
     if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
+    if (!kSplit && kPair) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
@@ -189,16 +212,16 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 
     if (warp == 0 && lane == 0) {
         // -------------------------------------------------------------------- producer
-        const uint32_t full_lead = kPair ? mapa_shared(smem_u32(full_bar), 0) : 0u;
+        const uint32_t full_lead = kPair ? mapa_shared(smem_u32(full_bar), lead_rank) : 0u;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int64_t u = worker; ok && u < p.units; u += workers) {
+        for (int64_t u = first; ok && u < p.units; u += workers) {
             int tm, tn;
             decode(p, u, tm, tn);
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
-            for (int kb = 0; kb < kblocks; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abort_flag)) { ok = false; break; }
                 const uint32_t sa = smem_u32(tiles + stage * kStageBytes), sb = sa + kTileA;
                 const uint32_t fb = kPair ? full_lead + static_cast<uint32_t>(stage) * 8u : smem_u32(&full_bar[stage]);
@@ -224,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     const uint32_t dst = sb + h * (BN / 2) * BK * 2;
                     if (p.b_mn) {
 #pragma unroll
-                        for (int q = 0; q < BN / 128; ++q) load(dst + q * 64 * BK * 2, map, r0 + 64 * q, k0);
+                        for (int q = 0; q < BN / 128; ++q) load(dst + q * 64 * BK * 2, map, r0 + 64 * q, k0);   // BN >= 128 then
                     } else {
                         load(dst, map, k0, r0);
                     }
@@ -240,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         // one step of 16 k: 32 bytes along a row of k, 16 rows of 128 bytes where the rows are contiguous
         const uint64_t step_a = p.a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
         const uint64_t step_b = p.b_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
-        for (int64_t u = worker; ok && u < p.units; u += workers, ++unit_count) {
+        for (int64_t u = first; ok && u < p.units; u += workers, ++unit_count) {
             const uint32_t buf = unit_count & 1u;
             const uint32_t use = (unit_count >> 1) & 1u;
             const bool freed = kPair ? mbar_wait_cluster(smem_u32(&acc_empty[buf]), use ^ 1u, abort_flag)
@@ -248,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             if (!freed) { ok = false; break; }
             tc_fence_after();
             const uint32_t d_acc = tmem + buf * BN;
-            for (int kb = 0; kb < kblocks; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 const bool landed = kPair ? mbar_wait_cluster(smem_u32(&full_bar[stage]), phase, abort_flag)
                                           : mbar_wait(smem_u32(&full_bar[stage]), phase, abort_flag);
                 if (!landed) { ok = false; break; }
@@ -258,54 +281,73 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 const uint64_t db = p.b_mn ? smem_desc_mn128(sb) : smem_desc_k128(sb);
 #pragma unroll
                 for (int kk = 0; kk < BK / UK; ++kk) {
-                    const uint32_t accumulate = (kb == 0 && kk == 0) ? 0u : 1u;
+                    const uint32_t accumulate = (kb == kb0 && kk == 0) ? 0u : 1u;
                     if constexpr (kPair)
                         umma_bf16_pair(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
                     else
                         umma_bf16(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
                 }
                 if constexpr (kPair)
-                    umma_commit_pair(smem_u32(&empty_bar[stage]), 3);
+                    umma_commit_pair(smem_u32(&empty_bar[stage]), pair_mask);
                 else
                     umma_commit(smem_u32(&empty_bar[stage]));
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
             if (!ok) break;
             if constexpr (kPair)
-                umma_commit_pair(smem_u32(&acc_full[buf]), 3);
+                umma_commit_pair(smem_u32(&acc_full[buf]), pair_mask);
             else
                 umma_commit(smem_u32(&acc_full[buf]));
         }
         // Every MMA must have completed before TMEM or shared memory is released.
         if constexpr (kPair)
-            umma_commit_pair(smem_u32(drain_bar), 3);
+            umma_commit_pair(smem_u32(drain_bar), pair_mask);
         else
             umma_commit(smem_u32(drain_bar));
-    } else if (warp >= kEpiWarp0) {
+    }
+    if constexpr (kSplit) {
+        // ------------------------------------------------- partial sums to the CTAs that finish them
+        __syncwarp();
+        const bool epi_warp = warp >= kEpiWarp0;
+        bool ok = true;
+        if (epi_warp) {
+            ok = mbar_wait(smem_u32(&acc_full[0]), 0, abort_flag);
+            tc_fence_after();
+        }
+        cluster_sync();                  // every pair's MMAs are done: the stages may be written over
+        constexpr int kAcc = BN / kCols;
+        const int width = kCols / p.split;       // columns that a CTA finishes
+        if (epi_warp && ok) {
+            const int quad = warp & 3, half = (warp - kEpiWarp0) >> 2;
+            const uint32_t lane_acc = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+#pragma unroll 1
+            for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 16) {
+                const int q = c / kCols, col = c % kCols, dst = col / width;
+                float v[16];
+                tmem_ld16(lane_acc + static_cast<uint32_t>(c), v);
+                tmem_wait_ld();
+                // at the destination: [pair][accumulator][group of 4 columns][row][4 columns]
+                const int at = (((part * kAcc + q) * (width / 4) + col % width / 4) * BM + quad * 32 + lane) * 16;
+                const uint32_t to = mapa_shared(smem_u32(tiles) + at, 2u * dst + rank);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    st_shared_cluster_f32x4(to + i * BM * 16, v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            tc_fence_before();
+        }
+        cluster_sync();
+    }
+    if (warp >= kEpiWarp0) {
         // -------------------------------------------------------------------- epilogue
         const Epilogue& e = p.epi;
         const int quad = warp & 3;                       // TMEM lanes 32*quad ..: a row per thread
-        const int half = (warp - kEpiWarp0) >> 2;        // columns kCols / 2 * half ..
+        const int half = (warp - kEpiWarp0) >> 2;
         const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         uint8_t* stg = staging + (warp - kEpiWarp0) * kOutBufs * kStageOut;
         uint32_t sbuf = 0;
         const bool wide = (e.ldo & 7) == 0;
-        // 32 columns of the thread's row, from column n, through the staging buffer (a bulk store of a 32 x 32 box)
-        // or, where rows are not on 16-byte boundaries, one by one
-        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int64_t m, int row0) {
-            if (p.direct) {
-                if (m < e.M) {
-                    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + m * e.ldo + n;
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        float lo, hi;
-                        unpack_bf16(w[c], lo, hi);
-                        if (n + 2 * c < e.N) o[2 * c] = __float2bfloat16_rn(lo);
-                        if (n + 2 * c + 1 < e.N) o[2 * c + 1] = __float2bfloat16_rn(hi);
-                    }
-                }
-                return;
-            }
+        // 64 bytes of the thread's row through the staging buffer: a bulk store of a box of 32 rows, from column x
+        auto store_box = [&](const CUtensorMap* map, const uint32_t* w, int x, int row0) {
             // the staging buffer is free once the store issued from it two boxes ago has read it
             if (lane == 0) bulk_wait_read1();
             __syncwarp();
@@ -317,34 +359,73 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
-                tma_store_2d(map, smem_u32(stg + sbuf * kStageOut), n, row0);
+                tma_store_2d(map, smem_u32(stg + sbuf * kStageOut), x, row0);
                 bulk_commit();
             }
             sbuf ^= 1u;
         };
+        // 32 columns of the thread's row, from column n: a box or, where rows are not on 16-byte boundaries, one by one
+        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int64_t m, int row0) {
+            if (!p.direct) return store_box(map, w, n, row0);
+            if (m < e.M) {
+                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + m * e.ldo + n;
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    float lo, hi;
+                    unpack_bf16(w[c], lo, hi);
+                    if (n + 2 * c < e.N) o[2 * c] = __float2bfloat16_rn(lo);
+                    if (n + 2 * c + 1 < e.N) o[2 * c + 1] = __float2bfloat16_rn(hi);
+                }
+            }
+        };
         uint32_t unit_count = 0;
-        for (int64_t u = worker; u < p.units; u += workers, ++unit_count) {
+        for (int64_t u = first; u < p.units; u += workers, ++unit_count) {
             int tm, tn;
             decode(p, u, tm, tn);
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
-            const int col0 = half * (kCols / 2);
             const uint32_t buf = unit_count & 1u;
-            const uint32_t use = (unit_count >> 1) & 1u;
-            if (!mbar_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
-            tc_fence_after();
+            if constexpr (!kSplit) {
+                const uint32_t use = (unit_count >> 1) & 1u;
+                if (!mbar_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
+                tc_fence_after();
+            }
             const uint32_t acc = lane_base + buf * BN;
+            // this CTA's columns of the tile, 32 at a time, shared by the two halves of the warps
+            const int width = kSplit ? kCols / p.split : kCols;
+            const int base = tn * kCols + (kSplit ? part * width : 0);
+            // 16 columns from column col of accumulator q
+            auto get16 = [&](int q, int col, float* v) {
+                if constexpr (kSplit) {
+                    constexpr int kAcc = BN / kCols;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                    for (int s = 0; s < p.split; ++s) {
+                        const uint8_t* from =
+                            tiles + (((s * kAcc + q) * (width / 4) + col / 4) * BM + quad * 32 + lane) * 16;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float4 w = *reinterpret_cast<const float4*>(from + i * BM * 16);
+                            v[4 * i] += w.x, v[4 * i + 1] += w.y, v[4 * i + 2] += w.z, v[4 * i + 3] += w.w;
+                        }
+                    }
+                } else {
+                    tmem_ld16(acc + static_cast<uint32_t>(q * (BN / 2) + col), v);
+                }
+            };
+            auto got = [&] {
+                if constexpr (!kSplit) tmem_wait_ld();
+            };
 #pragma unroll 1
-            for (int c = 0; c < kCols / 64; ++c) {
-                const int n = tn * kCols + col0 + 32 * c;
+            for (int c = 32 * half; c < width; c += 64) {
+                const int n = base + c;
                 if (n >= e.N || row0 >= e.M) continue;     // box entirely outside (warp-uniform)
-                const uint32_t at = acc + static_cast<uint32_t>(col0 + 32 * c);
                 uint32_t w[16];
                 if constexpr (KIND == kEpiLinear) {
                     float v[32];
-                    tmem_ld16(at, v);
-                    tmem_ld16(at + 16u, v + 16);
-                    tmem_wait_ld();
+                    get16(0, c, v);
+                    get16(0, c + 16, v + 16);
+                    got();
                     if (e.bias) {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
@@ -354,15 +435,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
                         }
                     }
-                    if (e.Z && m < e.M) {
-                        float* z = e.Z + m * e.N + n;
-                        if ((e.N & 3) == 0) {
+                    if (e.Z) {
+                        if (!p.direct_z) {
 #pragma unroll
-                            for (int q = 0; q < 8; ++q)
-                                if (n + 4 * q < e.N)
-                                    *reinterpret_cast<float4*>(z + 4 * q) =
-                                        make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-                        } else {
+                            for (int q = 0; q < 2; ++q) {
+                                if (n + 16 * q < e.N) {
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
+                                    store_box(&p.z, w, n + 16 * q, row0);
+                                }
+                            }
+                        } else if (m < e.M) {
+                            float* z = e.Z + m * e.N + n;
 #pragma unroll
                             for (int i = 0; i < 32; ++i)
                                 if (n + i < e.N) z[i] = v[i];
@@ -390,9 +474,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         float g[16], v[16];
-                        tmem_ld16(at + 16u * q, g);
-                        tmem_ld16(at + static_cast<uint32_t>(BN / 2) + 16u * q, v);
-                        tmem_wait_ld();
+                        get16(0, c + 16 * q, g);
+                        get16(1, c + 16 * q, v);
+                        got();
                         if (pre) {       // whole tiles: rows and columns beyond the edges have their place
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
@@ -415,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         float dh[16];
-                        tmem_ld16(at + 16u * q, dh);
+                        get16(0, c + 16 * q, dh);
                         float4 g[4], v[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -423,7 +507,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             g[i] = __ldcs(reinterpret_cast<const float4*>(from));
                             v[i] = __ldcs(reinterpret_cast<const float4*>(from + kPreTile * kPreTile));
                         }
-                        tmem_wait_ld();
+                        got();
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float gi[4] = {g[i].x, g[i].y, g[i].z, g[i].w};
@@ -446,20 +530,24 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     store32(&p.out2, e.out2, w2, n, m, row0);
                 }
             }
-            // its TMEM loads have completed (tcgen05.wait::ld): hand the buffer back without release ordering,
-            // which would also wait for the warp's stores
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (kPair)
-                    mbar_arrive_cluster_relaxed(mapa_shared(smem_u32(&acc_empty[buf]), 0));
-                else
-                    mbar_arrive_relaxed(smem_u32(&acc_empty[buf]));
+            if constexpr (!kSplit) {
+                // its TMEM loads have completed (tcgen05.wait::ld): hand the buffer back without release ordering,
+                // which would also wait for the warp's stores
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (kPair)
+                        mbar_arrive_cluster_relaxed(mapa_shared(smem_u32(&acc_empty[buf]), lead_rank));
+                    else
+                        mbar_arrive_relaxed(smem_u32(&acc_empty[buf]));
+                }
             }
         }
         if (lane == 0) bulk_wait_all();
         __syncwarp();
     }
+    // a launch that began before the one ahead of it on the stream had ended does not end before it
+    if (kSplit && p.early && threadIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 
     tc_fence_before();
     __syncthreads();
@@ -476,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         cluster_sync();
         if (threadIdx.x == 0) {
             const int peer_abort = static_cast<int>(ld_shared_cluster_u32(
-                mapa_shared(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u)));
+                mapa_shared(smem_u32(const_cast<int*>(abort_flag)), cluster_rank ^ 1u)));
             if (*abort_flag || peer_abort) {
                 const uint64_t t0 = globaltimer_ns();
                 while (globaltimer_ns() - t0 < 200ull * 1000ull) {
@@ -505,15 +593,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 // ------------------------------------------------------------------------------------ host
 
 static bool map_2d(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t pitch, int box_x, int box_y,
-                   CUtensorMapSwizzle swz) {
+                   CUtensorMapSwizzle swz, bool f32 = false) {
     auto enc = tensor_map_encoder();
     if (!enc) return false;
     cuuint64_t dims[2] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer)};
-    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(pitch) * (f32 ? 4 : 2)};
     cuuint32_t box[2] = {static_cast<cuuint32_t>(box_x), static_cast<cuuint32_t>(box_y)};
     cuuint32_t estr[2] = {1, 1};
-    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base),
+               dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -523,8 +611,11 @@ static bool map_operand(CUtensorMap* m, const Mat& a, int64_t rows, int64_t K, i
     return map_2d(m, a.p, rows, K, a.ks, 64, BK, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <bool kPair, int BN>
-static int launch_form(const Product& p, int* status, int reset, int sms, cudaStream_t stream) {
+// Tiles unit0 .. unit0 + count - 1 of the product (count < 0: all the others), on at most `most` workers; `split`: pairs per
+// tile; `early`: see Args.
+template <bool kPair, int BN, bool kSplit>
+static int launch_form(const Product& p, int* status, int reset, int split, int early, int64_t unit0, int64_t count,
+                       int64_t most, cudaStream_t stream) {
     using F = Form<kPair, BN>;
     const bool gated = p.epi.kind == kEpiGated;
     Args a;
@@ -539,6 +630,9 @@ static int launch_form(const Product& p, int* status, int reset, int sms, cudaSt
         const void* second = p.epi.out2 ? p.epi.out2 : p.epi.out;
         if (!map_2d(&a.out2, second, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
     }
+    a.direct_z = (p.N & 3) != 0;
+    if (p.epi.Z && !a.direct_z && !map_2d(&a.z, p.epi.Z, p.N, p.M, p.N, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B, true))
+        return DTP_ERR_CUDA;
     const int rows = kPair ? 2 * BM : BM, cols = gated ? BN / 2 : BN;
     a.segments = p.segments;
     a.KB = static_cast<int>((p.K + BK - 1) / BK);
@@ -546,44 +640,123 @@ static int launch_form(const Product& p, int* status, int reset, int sms, cudaSt
     a.b_mn = p.B[0].ks != 1;
     a.tiles_m = static_cast<int>((p.M + rows - 1) / rows);
     a.tiles_n = (p.N + cols - 1) / cols;
-    a.units = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
+    a.unit0 = unit0;
+    a.units = count < 0 ? static_cast<int64_t>(a.tiles_m) * a.tiles_n : unit0 + count;
+    a.split = split;
+    a.early = early;
     // bits 15 and 16: A and B stored with their rows contiguous
     a.idesc = idesc_bf16_f32(kPair ? 2 * BM : BM, BN) | (a.a_mn ? 1u << 15 : 0u) | (a.b_mn ? 1u << 16 : 0u);
     a.reset = reset;
     a.status = status;
     a.epi = p.epi;
-    auto kernel = gated                              ? gemm_tc_kernel<kPair, BN, kEpiGated>
-                  : p.epi.kind == kEpiGatedGrad ? gemm_tc_kernel<kPair, BN, kEpiGatedGrad>
-                                                     : gemm_tc_kernel<kPair, BN, kEpiLinear>;
+    auto kernel = gated ? gemm_tc_kernel<kPair, BN, kEpiGated, kSplit> : gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit>;
+    if constexpr (BN >= 128)
+        if (p.epi.kind == kEpiGatedGrad) kernel = gemm_tc_kernel<kPair, BN, kEpiGatedGrad, kSplit>;
     DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       static_cast<int>(F::kSmemBytes)));
-    const int64_t per = kPair ? 2 : 1;
-    const int64_t most = sms / per;
+    const int64_t per = kSplit ? 2 * split : kPair ? 2 : 1;
+    const int64_t units = a.units - unit0;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(per * (a.units < most ? a.units : most)));
+    // a split tile's cluster takes that tile alone
+    cfg.gridDim = dim3(static_cast<unsigned>(per * (kSplit || units < most ? units : most)));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = F::kSmemBytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = static_cast<unsigned>(per);
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = kPair ? 1 : 0;
+    cfg.numAttrs = early ? 2 : kPair ? 1 : 0;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return DTP_OK;
 }
 
+// Clusters of `split` pairs that the current device holds at once (they stay within a part of the chip).
+static int cluster_room(int split, int sms) {
+    static std::atomic<int> cached[2][16];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+    std::atomic<int>* slot = dev < 16 ? &cached[split == 4][dev] : nullptr;
+    int n = slot ? slot->load(std::memory_order_relaxed) : 0;
+    if (n) return n - 1;
+    using F = Form<true, 256>;
+    auto kernel = gemm_tc_kernel<true, 256, kEpiLinear, true>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(F::kSmemBytes)) !=
+        cudaSuccess)
+        return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(sms / (2 * split) * 2 * split));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = F::kSmemBytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(2 * split);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) n = 0;
+    if (slot) slot->store(n + 1, std::memory_order_relaxed);
+    return n;
+}
+
 // bf16 operands whose rows are on 16-byte boundaries; M, N >= 1, K >= 1.
+//
+// The form is the one with the smallest estimate, in clocks, from what the forms measured on a GB300: per launch 6000 (start,
+// pipeline fill, last epilogue), per round of tiles and k block what the form's shared-memory traffic takes (580 for 256 x
+// 256 pairs, 420 for 256 x 128, 330 for 256 x 64 where B has k contiguous; 560 for single 128 x 128 tiles, up to 128 rows
+// only), and for splitting a tile 9000 (256 columns) or 6000 (128) for the exchange.  Tiles left over after the full rounds
+// of 256 x 256 pairs may be split in a launch of their own, which begins as the first one's SMs fall free (3000).
 int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
     int dev = 0, sms = 0;
     DTP_CUDA_TRY(cudaGetDevice(&dev));
     DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const int64_t cols = p.epi.kind == kEpiGated ? 128 : 256;
-    const int64_t tiles = (p.M + 255) / 256 * ((p.N + cols - 1) / cols);
-    if (2 * tiles >= sms) return launch_form<true, 256>(p, status, reset, sms, stream);
-    return launch_form<false, 128>(p, status, reset, sms, stream);
+    const int64_t pairs = sms / 2;
+    const int64_t kb = (p.K + BK - 1) / BK * p.segments;
+    const bool gated = p.epi.kind == kEpiGated;
+    auto tiles = [&](int rows, int bn) {
+        const int cols = gated ? bn / 2 : bn;
+        return (p.M + rows - 1) / rows * ((p.N + cols - 1) / cols);
+    };
+    auto whole = [&](int64_t n, int64_t workers, int clocks) { return (n + workers - 1) / workers * kb * clocks + 6000; };
+    auto split_ok = [&](int64_t n, int bn, int split) {
+        return kb >= 4 * split && (gated ? bn / 2 : bn) / split >= 32 && n <= cluster_room(split, sms);
+    };
+    auto split_clocks = [&](int bn, int split) {
+        return (kb + split - 1) / split * (bn == 256 ? 580 : 420) + 6000 + (bn == 256 ? 9000 : 6000);
+    };
+    const int64_t n256 = tiles(2 * BM, 256);
+    int64_t best = whole(n256, pairs, 580), tail = 0;
+    int best_bn = 256, best_split = 1;
+    auto take = [&](int64_t estimate, int bn, int split, int64_t left) {
+        if (estimate < best) best = estimate, best_bn = bn, best_split = split, tail = left;
+    };
+    take(whole(tiles(2 * BM, 128), pairs, 420), 128, 1, 0);
+    if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad) take(whole(tiles(2 * BM, 64), pairs, 330), 64, 1, 0);
+    if (p.M <= BM) take(whole(tiles(BM, 128), sms, 560), 0, 1, 0);
+    const int64_t left = n256 % pairs;
+    for (int split : {2, 4}) {
+        for (int bn : {256, 128})
+            if (split_ok(tiles(2 * BM, bn), bn, split)) take(split_clocks(bn, split), bn, split, 0);
+        if (n256 > pairs && left > 0 && split_ok(left, 256, split))
+            take(whole(n256 - left, pairs, 580) + split_clocks(256, split) - 3000, 256, split, left);
+    }
+    if (tail) {
+        const int st = launch_form<true, 256, false>(p, status, reset, 1, 0, 0, n256 - tail, pairs, stream);
+        if (st != DTP_OK) return st;
+        return launch_form<true, 256, true>(p, status, 0, best_split, 1, n256 - tail, -1, pairs, stream);
+    }
+    if (best_bn == 0) return launch_form<false, 128, false>(p, status, reset, 1, 0, 0, -1, sms, stream);
+    if (best_bn == 64) return launch_form<true, 64, false>(p, status, reset, 1, 0, 0, -1, pairs, stream);
+    if (best_bn == 128)
+        return best_split == 1 ? launch_form<true, 128, false>(p, status, reset, 1, 0, 0, -1, pairs, stream)
+                               : launch_form<true, 128, true>(p, status, reset, best_split, 0, 0, -1, pairs, stream);
+    return best_split == 1 ? launch_form<true, 256, false>(p, status, reset, 1, 0, 0, -1, pairs, stream)
+                           : launch_form<true, 256, true>(p, status, reset, best_split, 0, 0, -1, pairs, stream);
 }
 
 }  // namespace gtc

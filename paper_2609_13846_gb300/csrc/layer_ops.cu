@@ -21,52 +21,121 @@ int launch(const layer::Product& p, int* status, int reset, int second, cudaStre
 
 namespace layer {
 
-constexpr int kRowChunk = 256;    // tokens per partial sum of the bias gradient
+constexpr int kRowChunk = 128;    // tokens per partial sum of the bias gradient
+constexpr int kPer = 8;           // columns per thread
 
 // dZ = dY act'(Z), rounded once, and the partial sums over kRowChunk tokens of the unrounded values (the bias
-// gradient).  A block takes 32 columns x kRowChunk tokens; each of its 8 warps sums its tokens in order.
-template <typename E>
+// gradient).  Bound by memory.  A block takes 256 columns x kRowChunk tokens, a thread 8 columns of every eighth token, two
+// tokens in flight; each of the 8 warps sums its tokens in order.  kWide: rows on 16-byte boundaries.
+template <typename E, bool kWide>
 __global__ void __launch_bounds__(256)
 act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T, int N, int64_t ldz, int act,
                 E* __restrict__ dZ, float* __restrict__ partial) {
-    __shared__ float red[8][33];
+    __shared__ float red[8][32 * kPer + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int n = blockIdx.x * 32 + lane;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kRowChunk;
-    float sum = 0.0f;
-    if (n < N) {
-        for (int r = warp; r < kRowChunk; r += 8) {
-            const int64_t t = t0 + r;
-            if (t >= T) break;
-            float g = to_f32(dY[t * N + n]);
+    const int wide_blocks = (N + 32 * kPer - 1) / (32 * kPer);
+    const int block = static_cast<int>(blockIdx.x) % wide_blocks;
+    const int64_t chunk = blockIdx.x / wide_blocks;
+    const int n0 = (block * 32 + lane) * kPer;
+    const int64_t t0 = chunk * kRowChunk;
+    const int64_t t1 = t0 + kRowChunk < T ? t0 + kRowChunk : T;
+    const bool full = kWide && n0 + kPer <= N;
+    constexpr int kWords = kPer * sizeof(E) / 16;
+    union Row { uint4 q[kWords]; E e[kPer]; };
+    float sum[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) sum[j] = 0.0f;
+    auto load = [&](int64_t t, Row& g, float (&z)[kPer]) {
+        if (full) {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) g.q[j] = reinterpret_cast<const uint4*>(dY + t * N + n0)[j];
+            if (act != DTP_ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < kPer / 4; ++j) {
+                    const float4 v = reinterpret_cast<const float4*>(Z + t * N + n0)[j];
+                    z[4 * j] = v.x, z[4 * j + 1] = v.y, z[4 * j + 2] = v.z, z[4 * j + 3] = v.w;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                const bool in = n0 + j < N;
+                g.e[j] = in ? dY[t * N + n0 + j] : from_f32<E>(0.0f);
+                z[j] = in && act != DTP_ACT_NONE ? Z[t * N + n0 + j] : 0.0f;
+            }
+        }
+    };
+    auto store = [&](int64_t t, const Row& g, const float (&z)[kPer]) {
+        Row o;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            float x = to_f32(g.e[j]);
             if (act != DTP_ACT_NONE) {
                 float v, s;
-                act_both<IsFast<E>::value>(act, Z[t * N + n], v, s);
-                g *= s;
+                act_both<IsFast<E>::value>(act, z[j], v, s);
+                x *= s;
             }
-            sum += g;
-            if (dZ) dZ[t * ldz + n] = from_f32<E>(g);
+            sum[j] += x;
+            o.e[j] = from_f32<E>(x);
+        }
+        if (!dZ) return;
+        if (full) {
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) reinterpret_cast<uint4*>(dZ + t * ldz + n0)[j] = o.q[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (n0 + j < N) dZ[t * ldz + n0 + j] = o.e[j];
+        }
+    };
+    if (n0 < N) {
+        int64_t t = t0 + warp;
+        for (; t + 8 < t1; t += 16) {
+            Row a, b;
+            float za[kPer], zb[kPer];
+            load(t, a, za);
+            load(t + 8, b, zb);
+            store(t, a, za);
+            store(t + 8, b, zb);
+        }
+        if (t < t1) {
+            Row a;
+            float za[kPer];
+            load(t, a, za);
+            store(t, a, za);
         }
     }
     if (!partial) return;
-    red[warp][lane] = sum;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) red[warp][lane * kPer + j] = sum[j];
     __syncthreads();
-    if (warp == 0 && n < N) {
+    const int n = block * 32 * kPer + threadIdx.x;
+    if (n < N) {
         float s = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += red[w][lane];
-        partial[static_cast<int64_t>(blockIdx.y) * N + n] = s;
+        for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
+        partial[chunk * N + n] = s;
     }
 }
 
-// out[n] = sum over the chunks, in order.
+// out[n] = sum over the chunks: each of 8 warps sums every eighth in order, then the warps' sums in order.
 template <typename E>
-__global__ void bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* __restrict__ out) {
-    const int n = blockIdx.x * blockDim.x + threadIdx.x;
-    if (n >= N) return;
+__global__ void __launch_bounds__(256)
+bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* __restrict__ out) {
+    __shared__ float red[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = blockIdx.x * 32 + lane;
     float s = 0.0f;
-    for (int64_t c = 0; c < chunks; ++c) s += partial[c * N + n];
-    out[n] = from_f32<E>(s);
+    if (n < N)
+        for (int64_t c = warp; c < chunks; c += 8) s += partial[c * N + n];
+    red[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && n < N) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += red[w][lane];
+        out[n] = from_f32<E>(v);
+    }
 }
 
 // Rows copied to a pitch of whole 16 bytes, for the tensor cores' loads; the pitch's spare entries stay unwritten
@@ -185,14 +254,16 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
 template <typename E>
 static int launch_act_grad(const void* dY, const float* Z, int64_t T, int N, int act, void* dZ, int64_t ldz,
                            float* partial, void* dbias, cudaStream_t stream) {
-    const dim3 grid((N + 31) / 32, static_cast<unsigned>(chunks_of(T)));
+    const int64_t blocks = chunks_of(T) * ((N + 32 * kPer - 1) / (32 * kPer));
+    if (blocks > 0x7FFFFFFF) return DTP_ERR_UNSUPPORTED;
     if (T > 0) {
-        act_grad_kernel<E><<<grid, 256, 0, stream>>>(static_cast<const E*>(dY), Z, T, N, ldz, act,
-                                                     static_cast<E*>(dZ), dbias ? partial : nullptr);
+        auto kernel = N % kPer == 0 ? act_grad_kernel<E, true> : act_grad_kernel<E, false>;
+        kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(static_cast<const E*>(dY), Z, T, N, ldz, act, static_cast<E*>(dZ),
+                                         dbias ? partial : nullptr);
         DTP_CUDA_TRY(cudaGetLastError());
     }
     if (dbias) {
-        bias_reduce_kernel<E><<<(N + 255) / 256, 256, 0, stream>>>(partial, chunks_of(T), N, static_cast<E*>(dbias));
+        bias_reduce_kernel<E><<<(N + 31) / 32, 256, 0, stream>>>(partial, chunks_of(T), N, static_cast<E*>(dbias));
         DTP_CUDA_TRY(cudaGetLastError());
     }
     return DTP_OK;
@@ -200,7 +271,6 @@ static int launch_act_grad(const void* dY, const float* Z, int64_t T, int N, int
 
 int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
                     int dtype, void* dX, void* dW, void* dbias, void* workspace, cudaStream_t stream) {
-    if (chunks_of(T) > 65535) return DTP_ERR_UNSUPPORTED;
     Call call{dtype, workspace, stream};
     Carver c(workspace);
     void* dz = c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
