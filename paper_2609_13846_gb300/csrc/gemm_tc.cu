@@ -44,12 +44,16 @@ constexpr uint32_t kTileA = BM * BK * 2;          // 16 KB
 constexpr uint32_t kStageOut = 32 * 64;           // a 32-row x 32-column bf16 box, 2 KB (64-byte swizzle)
 constexpr int kOutBufs = 2;                       // per epilogue warp
 
+// A stage holds two 64-wide k blocks of A and of B: the thread that issues the MMAs passes a barrier once for eight of them
+// (one block per stage: 600 to 650 clocks a block, whatever the tile).
+constexpr int kBoxes = 2;
 template <bool kPair, int BN>
 struct Form {
     static constexpr int kRowsB = kPair ? BN / 2 : BN;            // staged by this CTA
     static constexpr uint32_t kTileB = kRowsB * BK * 2;
-    static constexpr uint32_t kStageBytes = kTileA + kTileB;
-    static constexpr int STAGES = static_cast<int>(192 * 1024 / kStageBytes) > 8 ? 8 : 192 * 1024 / kStageBytes;
+    static constexpr uint32_t kBoxBytes = kTileA + kTileB;
+    static constexpr uint32_t kStageBytes = kBoxes * kBoxBytes;
+    static constexpr int STAGES = 192 * 1024 / kStageBytes;
     static constexpr uint32_t kTmemCols = 2 * BN;                 // two accumulators: a power of two
     static constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kEpiWarps * kOutBufs * kStageOut + 512;
 };
@@ -60,7 +64,7 @@ struct Args {
     int KB;               // k blocks of 64 per segment
     int a_mn, b_mn;       // operand stored with its rows contiguous
     int tiles_m, tiles_n; // per CTA or pair
-    int64_t unit0, units; // this launch's tiles: unit0 .. units - 1
+    int unit0, units;     // this launch's tiles: unit0 .. units - 1
     int split;            // pairs per tile (kSplit)
     int early;            // kSplit: begun while the launch before it, of the same product's other tiles, still runs
     uint32_t idesc;
@@ -79,20 +83,32 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Descriptor of a tile stored with its rows contiguous: 64-row blocks of [k][64 rows], 128 bytes per k,
-// 128-byte swizzle.  Leading byte offset: from one 64-row block to the next (64 k x 128 bytes); stride byte
-// offset: from one group of 8 k to the next (1024 bytes).
-__device__ __forceinline__ uint64_t smem_desc_mn128(uint32_t saddr) {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-    d |= static_cast<uint64_t>((64u * 128u) >> 4) << 16;
-    d |= static_cast<uint64_t>(1024u >> 4) << 32;
-    d |= static_cast<uint64_t>(1u) << 46;
-    d |= static_cast<uint64_t>(2u) << 61;
+// Shared-memory matrix descriptors (128-byte swizzle, version 1) as two words: the high word is the stride byte offset (1024
+// >> 4) and the layout, the same for both orders.  With k contiguous a tile is rows of 64 k, 8-row groups 1024 bytes apart.
+// With the rows contiguous it is 64-row blocks of [k][64 rows], 128 bytes per k: the stride byte offset leads from one group of
+// 8 k to the next, the leading byte offset (64 k x 128 bytes) from one 64-row block to the next.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, bool rows_contiguous) {
+    return ((saddr & 0x3FFFFu) >> 4) | ((rows_contiguous ? (64u * 128u) >> 4 : 1u) << 16);
+}
+__device__ __forceinline__ uint64_t desc(uint32_t low) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
     return d;
+}
+
+// One lane of the warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(p));
+    return p != 0;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
@@ -121,14 +137,13 @@ __device__ __forceinline__ void load8(const __nv_bfloat16* row, int n, int N, bo
 // Units of a persistent worker: row tiles in groups of 8, column tile by column tile within a group, so that the
 // tiles in flight share their rows and columns in L2.
 constexpr int kGroupM = 8;
-__device__ __forceinline__ void decode(const Args& p, int64_t u, int& tm, int& tn) {
-    const int64_t per = static_cast<int64_t>(kGroupM) * p.tiles_n;
-    const int64_t g = u / per;
-    const int rest = static_cast<int>(u - g * per);
+__device__ __forceinline__ void decode(const Args& p, int u, int& tm, int& tn) {
+    const unsigned per = static_cast<unsigned>(kGroupM) * p.tiles_n;
+    const unsigned g = static_cast<unsigned>(u) / per, rest = static_cast<unsigned>(u) - g * per;
     const int m0 = static_cast<int>(g) * kGroupM;
-    const int gm = p.tiles_m - m0 < kGroupM ? p.tiles_m - m0 : kGroupM;
-    tn = rest / gm;
-    tm = m0 + rest % gm;
+    const unsigned gm = p.tiles_m - m0 < kGroupM ? p.tiles_m - m0 : kGroupM;
+    tn = static_cast<int>(rest / gm);
+    tm = m0 + static_cast<int>(rest % gm);
 }
 
 __device__ __forceinline__ void st_shared_cluster_f32x4(uint32_t cluster_addr, float a, float b, float c, float d) {
@@ -148,17 +163,15 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     uint8_t* tiles = smem;
     uint8_t* staging = smem + STAGES * kStageBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(staging + kEpiWarps * kOutBufs * kStageOut);
-    // In the pair form full and acc_empty are used in the even CTA only; empty, acc_full and drain receive its
-    // commits in both.
+    // In the pair form full and acc_empty are used in the even CTA only; empty and acc_full receive its commits in both.
     uint64_t* full_bar = bars;
     uint64_t* empty_bar = bars + STAGES;
     uint64_t* acc_full = bars + 2 * STAGES;
     uint64_t* acc_empty = acc_full + 2;
-    uint64_t* drain_bar = acc_full + 4;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 5);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-    const int warp = threadIdx.x >> 5;
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0);     // the same register in every lane
     const int lane = threadIdx.x & 31;
     const uint32_t cluster_rank = kPair ? cluster_ctarank() : 0u;
     const uint32_t rank = cluster_rank & 1u;                // 0: issues the MMAs; 1: its peer
@@ -167,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     const bool leader = rank == 0;
     // a worker (a CTA, a pair, or a cluster of pairs) takes tiles first, first + workers, ..
     const int ctas = kSplit ? 2 * p.split : kPair ? 2 : 1;
-    const int64_t first = p.unit0 + blockIdx.x / ctas, workers = gridDim.x / ctas;
+    const int first = p.unit0 + static_cast<int>(blockIdx.x) / ctas, workers = static_cast<int>(gridDim.x) / ctas;
     const int part = kSplit ? static_cast<int>(cluster_rank >> 1) : 0;
     const int all_blocks = p.segments * p.KB;
     const int kb0 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
@@ -186,7 +199,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             mbar_init(smem_u32(&acc_full[b]), 1);
             mbar_init(smem_u32(&acc_empty[b]), (kPair ? 2 : 1) * kEpiWarps);
         }
-        mbar_init(smem_u32(drain_bar), 1);
         *abort_flag = 0;
         fence_mbar_init();
         tma_prefetch_desc(&p.a[0]);
@@ -210,100 +222,112 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    if (warp == 0 && lane == 0) {
-        // -------------------------------------------------------------------- producer
-        const uint32_t full_lead = kPair ? mapa_shared(smem_u32(full_bar), lead_rank) : 0u;
+    if (warp == 0) {
+        // -------------------------------------------------------------------- producer: one lane issues
+        const bool issuer = elect_one();
+        const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), tiles0 = smem_u32(tiles);
+        const uint32_t full_lead = kPair ? mapa_shared(full0, lead_rank) : full0;
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int64_t u = first; ok && u < p.units; u += workers) {
+        for (int u = first; ok && u < p.units; u += workers) {
             int tm, tn;
             decode(p, u, tm, tn);
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                if (!mbar_wait(smem_u32(&empty_bar[stage]), phase ^ 1u, abort_flag)) { ok = false; break; }
-                const uint32_t sa = smem_u32(tiles + stage * kStageBytes), sb = sa + kTileA;
-                const uint32_t fb = kPair ? full_lead + static_cast<uint32_t>(stage) * 8u : smem_u32(&full_bar[stage]);
-                if (leader) mbar_arrive_expect_tx(smem_u32(&full_bar[stage]), (kPair ? 2u : 1u) * kStageBytes);
-                const int seg = kb >= p.KB;
-                const int k0 = (kb - seg * p.KB) * BK;
-                auto load = [&](uint32_t dst, const CUtensorMap* map, int x, int y) {
-                    if constexpr (kPair) tma_load_2d_pair(dst, map, fb, x, y);
-                    else tma_load_2d(dst, map, fb, x, y);
-                };
-                if (p.a_mn) {
-                    load(sa, &p.a[seg], m0, k0);
-                    load(sa + kTileA / 2, &p.a[seg], m0 + 64, k0);
-                } else {
-                    load(sa, &p.a[seg], k0, m0);
-                }
-                // rows of B: halves of BN / 2, which are gate and up in the gated kind
+            for (int kb = kb0; kb < kb1; kb += kBoxes) {
+                if (!mbar_wait(empty0 + stage * 8u, phase ^ 1u, abort_flag)) { ok = false; break; }
+                const int boxes = kb1 - kb < kBoxes ? kb1 - kb : kBoxes;      // the last stage may hold one block
+                const uint32_t fb = full_lead + stage * 8u;
+                if (issuer) {
+                    if (leader) mbar_arrive_expect_tx(full0 + stage * 8u, (kPair ? 2u : 1u) * boxes * F::kBoxBytes);
 #pragma unroll
-                for (int h = 0; h < F::kRowsB / (BN / 2); ++h) {
-                    const int half = kPair ? static_cast<int>(rank) : h;
-                    const CUtensorMap* map = KIND == kEpiGated ? &p.b[half] : &p.b[seg];
-                    const int r0 = KIND == kEpiGated ? n0 : n0 + half * (BN / 2);
-                    const uint32_t dst = sb + h * (BN / 2) * BK * 2;
-                    if (p.b_mn) {
+                    for (int x = 0; x < kBoxes; ++x) {
+                        if (x >= boxes) break;
+                        const uint32_t sa = tiles0 + stage * kStageBytes + x * F::kBoxBytes, sb = sa + kTileA;
+                        const int seg = kb + x >= p.KB;
+                        const int k0 = (kb + x - seg * p.KB) * BK;
+                        auto load = [&](uint32_t dst, const CUtensorMap* map, int cx, int cy) {
+                            if constexpr (kPair) tma_load_2d_pair(dst, map, fb, cx, cy);
+                            else tma_load_2d(dst, map, fb, cx, cy);
+                        };
+                        if (p.a_mn) {
+                            load(sa, &p.a[seg], m0, k0);
+                            load(sa + kTileA / 2, &p.a[seg], m0 + 64, k0);
+                        } else {
+                            load(sa, &p.a[seg], k0, m0);
+                        }
+                        // rows of B: halves of BN / 2, which are gate and up in the gated kind
 #pragma unroll
-                        for (int q = 0; q < BN / 128; ++q) load(dst + q * 64 * BK * 2, map, r0 + 64 * q, k0);   // BN >= 128 then
-                    } else {
-                        load(dst, map, k0, r0);
+                        for (int h = 0; h < F::kRowsB / (BN / 2); ++h) {
+                            const int half = kPair ? static_cast<int>(rank) : h;
+                            const CUtensorMap* map = KIND == kEpiGated ? &p.b[half] : &p.b[seg];
+                            const int r0 = KIND == kEpiGated ? n0 : n0 + half * (BN / 2);
+                            const uint32_t dst = sb + h * (BN / 2) * BK * 2;
+                            if (p.b_mn) {
+#pragma unroll
+                                for (int q = 0; q < BN / 128; ++q)       // BN >= 128 then
+                                    load(dst + q * 64 * BK * 2, map, r0 + 64 * q, k0);
+                            } else {
+                                load(dst, map, k0, r0);
+                            }
+                        }
                     }
                 }
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
         }
-    } else if (warp == 1 && lane == 0 && leader) {
-        // ------------------------------------------------------------------ MMA issuer (the even CTA of a pair)
+    } else if (warp == 1 && leader) {
+        // ------------------------------------- MMA issuer (one lane of the even CTA's warp of a pair)
+        const bool issuer = elect_one();
+        const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar);
         int stage = 0;
         uint32_t phase = 0, unit_count = 0;
         bool ok = true;
         // one step of 16 k: 32 bytes along a row of k, 16 rows of 128 bytes where the rows are contiguous
-        const uint64_t step_a = p.a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
-        const uint64_t step_b = p.b_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
-        for (int64_t u = first; ok && u < p.units; u += workers, ++unit_count) {
+        const uint32_t step_a = p.a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
+        const uint32_t step_b = p.b_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
+        const uint32_t low_a = desc_low(smem_u32(tiles), p.a_mn), low_b = desc_low(smem_u32(tiles) + kTileA, p.b_mn);
+        const uint32_t idesc = p.idesc;
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            return kPair ? mbar_wait_cluster(bar, parity, abort_flag) : mbar_wait(bar, parity, abort_flag);
+        };
+        for (int u = first; ok && u < p.units; u += workers, ++unit_count) {
             const uint32_t buf = unit_count & 1u;
             const uint32_t use = (unit_count >> 1) & 1u;
-            const bool freed = kPair ? mbar_wait_cluster(smem_u32(&acc_empty[buf]), use ^ 1u, abort_flag)
-                                     : mbar_wait(smem_u32(&acc_empty[buf]), use ^ 1u, abort_flag);
-            if (!freed) { ok = false; break; }
+            if (!wait(smem_u32(&acc_empty[buf]), use ^ 1u)) { ok = false; break; }
             tc_fence_after();
             const uint32_t d_acc = tmem + buf * BN;
-            for (int kb = kb0; kb < kb1; ++kb) {
-                const bool landed = kPair ? mbar_wait_cluster(smem_u32(&full_bar[stage]), phase, abort_flag)
-                                          : mbar_wait(smem_u32(&full_bar[stage]), phase, abort_flag);
-                if (!landed) { ok = false; break; }
+            for (int kb = kb0; kb < kb1; kb += kBoxes) {
+                if (!wait(full0 + stage * 8u, phase)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t sa = smem_u32(tiles + stage * kStageBytes), sb = sa + kTileA;
-                const uint64_t da = p.a_mn ? smem_desc_mn128(sa) : smem_desc_k128(sa);
-                const uint64_t db = p.b_mn ? smem_desc_mn128(sb) : smem_desc_k128(sb);
+                const int boxes = kb1 - kb < kBoxes ? kb1 - kb : kBoxes;
+                if (issuer) {
 #pragma unroll
-                for (int kk = 0; kk < BK / UK; ++kk) {
-                    const uint32_t accumulate = (kb == kb0 && kk == 0) ? 0u : 1u;
-                    if constexpr (kPair)
-                        umma_bf16_pair(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
-                    else
-                        umma_bf16(d_acc, da + kk * step_a, db + kk * step_b, p.idesc, accumulate);
+                    for (int x = 0; x < kBoxes; ++x) {
+                        if (x >= boxes) break;
+                        const uint32_t off = (stage * kStageBytes + x * F::kBoxBytes) >> 4;
+#pragma unroll
+                        for (int kk = 0; kk < BK / UK; ++kk) {
+                            const uint32_t accumulate = (kb == kb0 && x == 0 && kk == 0) ? 0u : 1u;
+                            const uint64_t da = desc(low_a + off + kk * step_a), db = desc(low_b + off + kk * step_b);
+                            if constexpr (kPair) umma_bf16_pair(d_acc, da, db, idesc, accumulate);
+                            else umma_bf16(d_acc, da, db, idesc, accumulate);
+                        }
+                    }
+                    if constexpr (kPair) umma_commit_pair(empty0 + stage * 8u, pair_mask);
+                    else umma_commit(empty0 + stage * 8u);
                 }
-                if constexpr (kPair)
-                    umma_commit_pair(smem_u32(&empty_bar[stage]), pair_mask);
-                else
-                    umma_commit(smem_u32(&empty_bar[stage]));
+                __syncwarp();
                 if (++stage == STAGES) { stage = 0; phase ^= 1u; }
             }
             if (!ok) break;
-            if constexpr (kPair)
-                umma_commit_pair(smem_u32(&acc_full[buf]), pair_mask);
-            else
-                umma_commit(smem_u32(&acc_full[buf]));
+            if (issuer) {
+                if constexpr (kPair) umma_commit_pair(smem_u32(&acc_full[buf]), pair_mask);
+                else umma_commit(smem_u32(&acc_full[buf]));
+            }
+            __syncwarp();
         }
-        // Every MMA must have completed before TMEM or shared memory is released.
-        if constexpr (kPair)
-            umma_commit_pair(smem_u32(drain_bar), pair_mask);
-        else
-            umma_commit(smem_u32(drain_bar));
     }
     if constexpr (kSplit) {
         // ------------------------------------------------- partial sums to the CTAs that finish them
@@ -379,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             }
         };
         uint32_t unit_count = 0;
-        for (int64_t u = first; u < p.units; u += workers, ++unit_count) {
+        for (int u = first; u < p.units; u += workers, ++unit_count) {
             int tm, tn;
             decode(p, u, tm, tn);
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
@@ -543,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 }
             }
         }
-        if (lane == 0) bulk_wait_all();
+        if (lane == 0) bulk_wait_read0();      // the staging buffers may go; the writes end with the launch
         __syncwarp();
     }
     // a launch that began before the one ahead of it on the stream had ended does not end before it
@@ -551,35 +575,16 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 
     tc_fence_before();
     __syncthreads();
-    if (warp == 1 && lane == 0) {
-        // the last MMA commit: every MMA (in the pair form reading both CTAs' tiles and writing
-        // both CTAs' TMEM) has completed
+    // Every accumulator has been waited for, so every MMA and every load has completed.  After a wait gave up they may not
+    // have: loads already issued may still be landing in this CTA's or the peer's shared memory; let them finish.
+    if (threadIdx.x == 0 && *abort_flag) {
         const uint64_t t0 = globaltimer_ns();
-        while (!mbar_try_wait(smem_u32(drain_bar), 0) && globaltimer_ns() - t0 < kWaitLimitNs) {
+        while (globaltimer_ns() - t0 < 200ull * 1000ull) {
         }
     }
-    // After a wait gave up, loads already issued (in the pair form also the peer's) may still be
-    // landing in this CTA's shared memory or on its barriers: let them finish before exiting.
-    if constexpr (kPair) {
-        cluster_sync();
-        if (threadIdx.x == 0) {
-            const int peer_abort = static_cast<int>(ld_shared_cluster_u32(
-                mapa_shared(smem_u32(const_cast<int*>(abort_flag)), cluster_rank ^ 1u)));
-            if (*abort_flag || peer_abort) {
-                const uint64_t t0 = globaltimer_ns();
-                while (globaltimer_ns() - t0 < 200ull * 1000ull) {
-                }
-            }
-        }
-        cluster_sync();
-    } else {
-        if (threadIdx.x == 0 && *abort_flag) {
-            const uint64_t t0 = globaltimer_ns();
-            while (globaltimer_ns() - t0 < 200ull * 1000ull) {
-            }
-        }
-        __syncthreads();
-    }
+    // the peer's arrivals on this CTA's barriers have landed before either leaves
+    if constexpr (kPair) cluster_sync();
+    else __syncthreads();
     if (warp == 1) {
         tc_fence_after();
         if constexpr (kPair)
@@ -640,8 +645,10 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     a.b_mn = p.B[0].ks != 1;
     a.tiles_m = static_cast<int>((p.M + rows - 1) / rows);
     a.tiles_n = (p.N + cols - 1) / cols;
-    a.unit0 = unit0;
-    a.units = count < 0 ? static_cast<int64_t>(a.tiles_m) * a.tiles_n : unit0 + count;
+    const int64_t all = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
+    if (all > 0x3FFFFFFF) return DTP_ERR_UNSUPPORTED;
+    a.unit0 = static_cast<int>(unit0);
+    a.units = static_cast<int>(count < 0 ? all : unit0 + count);
     a.split = split;
     a.early = early;
     // bits 15 and 16: A and B stored with their rows contiguous
