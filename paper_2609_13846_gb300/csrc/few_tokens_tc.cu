@@ -84,11 +84,6 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     const int kb0 = static_cast<int>(static_cast<int64_t>(p.KB) * rank / S);
     const int kb1 = static_cast<int>(static_cast<int64_t>(p.KB) * (rank + 1) / S);
 
-    // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
-    // block 0, which starts first, has passed here.
-    if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
@@ -123,11 +118,15 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
             tma_load_2d(smem_u32(tiles + s * F::kStageBytes) + BM * BK * 2, &p.x, smem_u32(&full_bar[s]), kb * BK, 0);
         };
         const int first = kb1 - kb0 < STAGES ? kb1 - kb0 : STAGES;
+        // the second product's weights do not come from the first
+        if (!p.second) grid_wait();
         for (int i = 0; i < first; ++i) load_w(kb0 + i, i);
-        if (p.second) {
-            asm volatile("griddepcontrol.wait;" ::: "memory");
-            asm volatile("fence.proxy.async;" ::: "memory");
-        }
+        if (p.second) grid_wait();
+        grid_release();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
+        // block 0, which starts first, has passed here.
+        if (p.reset && blockIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
         for (int i = 0; i < first; ++i) load_x(kb0 + i, i);
         int stage = 0;
         uint32_t phase = 0;                      // of the stage's reuse
@@ -188,6 +187,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
         tc_fence_before();
     }
     cluster_sync();
+    grid_wait();            // of this thread's own accesses, long fulfilled
     if (warp == 5) {
         if (*abort_flag) {      // loads and MMAs already issued may still be under way: let them finish
             const uint64_t t0 = globaltimer_ns();
@@ -263,7 +263,7 @@ static int launch_form(const Product& p, int* status, int reset, int second, int
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = second ? 2 : 1;
+    cfg.numAttrs = 2;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return DTP_OK;
 }

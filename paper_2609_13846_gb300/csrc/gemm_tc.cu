@@ -186,10 +186,6 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     const int kb0 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
     const int kb1 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * (part + 1) / p.split) : all_blocks;
 
-    // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
-    // block 0, which starts first, has passed here.
-    if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
-    if (!kSplit && kPair) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(smem_u32(&full_bar[s]), 1);
@@ -221,6 +217,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    // An early launch works on other tiles than the one before it, which had itself waited: it waits at its end.
+    if (!(kSplit && p.early)) grid_wait();
+    grid_release();
+    // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
+    // block 0, which starts first, has passed here.
+    if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
 
     if (warp == 0) {
         // -------------------------------------------------------------------- producer: one lane issues
@@ -571,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         __syncwarp();
     }
     // a launch that began before the one ahead of it on the stream had ended does not end before it
-    if (kSplit && p.early && threadIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (kSplit && p.early && threadIdx.x == 0) grid_wait();
 
     tc_fence_before();
     __syncthreads();
@@ -677,7 +679,7 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = early ? 2 : kPair ? 1 : 0;
+    cfg.numAttrs = 2;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return DTP_OK;
 }
@@ -713,11 +715,12 @@ static int cluster_room(int split, int sms) {
 
 // bf16 operands whose rows are on 16-byte boundaries; M, N >= 1, K >= 1.
 //
-// The form is the one with the smallest estimate, in clocks, from what the forms measured on a GB300: per launch 6000 (start,
-// pipeline fill, last epilogue), per round of tiles and k block what the form's shared-memory traffic takes (580 for 256 x
-// 256 pairs, 420 for 256 x 128, 330 for 256 x 64 where B has k contiguous; 560 for single 128 x 128 tiles, up to 128 rows
-// only), and for splitting a tile 9000 (256 columns) or 6000 (128) for the exchange.  Tiles left over after the full rounds
-// of 256 x 256 pairs may be split in a launch of their own, which begins as the first one's SMs fall free (3000).
+// The form is the one with the smallest estimate, in clocks, from what the forms measured on a GB300: a launch's start, pipeline
+// fill and last epilogue (9000 for 256 x 256 pairs, 7000 for 256 x 128 and for single 128 x 128 tiles, which up to 128 rows may
+// take, 5500 for 256 x 64, where B has k contiguous); per round of tiles and k block what the form's shared-memory traffic
+// takes (515, 400, 500, 280), but no less than an epilogue; and for splitting a tile the exchange (8000 with 256 columns, 5000
+// with 128).  Tiles left over after the full rounds of 256 x 256 pairs may be split in a launch of their own, which begins as
+// the first one's SMs fall free (saving 4000).
 int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
     int dev = 0, sms = 0;
     DTP_CUDA_TRY(cudaGetDevice(&dev));
@@ -729,28 +732,31 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
         const int cols = gated ? bn / 2 : bn;
         return (p.M + rows - 1) / rows * ((p.N + cols - 1) / cols);
     };
-    auto whole = [&](int64_t n, int64_t workers, int clocks) { return (n + workers - 1) / workers * kb * clocks + 6000; };
+    auto whole = [&](int64_t n, int64_t workers, int clocks, int fixed) {
+        const int64_t round = kb * clocks > fixed / 3 ? kb * clocks : fixed / 3;
+        return (n + workers - 1) / workers * round + fixed;
+    };
     auto split_ok = [&](int64_t n, int bn, int split) {
         return kb >= 4 * split && (gated ? bn / 2 : bn) / split >= 32 && n <= cluster_room(split, sms);
     };
     auto split_clocks = [&](int bn, int split) {
-        return (kb + split - 1) / split * (bn == 256 ? 580 : 420) + 6000 + (bn == 256 ? 9000 : 6000);
+        return (kb + split - 1) / split * (bn == 256 ? 515 : 400) + (bn == 256 ? 9000 + 8000 : 7000 + 5000);
     };
     const int64_t n256 = tiles(2 * BM, 256);
-    int64_t best = whole(n256, pairs, 580), tail = 0;
+    int64_t best = whole(n256, pairs, 515, 9000), tail = 0;
     int best_bn = 256, best_split = 1;
     auto take = [&](int64_t estimate, int bn, int split, int64_t left) {
         if (estimate < best) best = estimate, best_bn = bn, best_split = split, tail = left;
     };
-    take(whole(tiles(2 * BM, 128), pairs, 420), 128, 1, 0);
-    if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad) take(whole(tiles(2 * BM, 64), pairs, 330), 64, 1, 0);
-    if (p.M <= BM) take(whole(tiles(BM, 128), sms, 560), 0, 1, 0);
+    take(whole(tiles(2 * BM, 128), pairs, 400, 7000), 128, 1, 0);
+    if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad) take(whole(tiles(2 * BM, 64), pairs, 280, 5500), 64, 1, 0);
+    if (p.M <= BM) take(whole(tiles(BM, 128), sms, 500, 7000), 0, 1, 0);
     const int64_t left = n256 % pairs;
     for (int split : {2, 4}) {
         for (int bn : {256, 128})
             if (split_ok(tiles(2 * BM, bn), bn, split)) take(split_clocks(bn, split), bn, split, 0);
         if (n256 > pairs && left > 0 && split_ok(left, 256, split))
-            take(whole(n256 - left, pairs, 580) + split_clocks(256, split) - 3000, 256, split, left);
+            take(whole(n256 - left, pairs, 515, 9000) + split_clocks(256, split) - 4000, 256, split, left);
     }
     if (tail) {
         const int st = launch_form<true, 256, false>(p, status, reset, 1, 0, 0, n256 - tail, pairs, stream);

@@ -57,6 +57,12 @@ __device__ __forceinline__ void act_both(int act, float z, float& value, float& 
     }
 }
 
+// The layer kernels are launched so that a kernel's set-up overlaps the end of the one before it on the stream.  Each waits
+// for that one (grid_wait) before it touches global memory, and only then lets the next one begin (grid_release): what
+// begins early may rely on everything before its predecessor.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Element types of the operands.
 template <typename E>
 __device__ __forceinline__ float to_f32(E v) { return static_cast<float>(v); }

@@ -32,6 +32,8 @@ __global__ void __launch_bounds__(256)
 act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T, int N, int64_t ldz, int act,
                 E* __restrict__ dZ, float* __restrict__ partial) {
     __shared__ float red[8][32 * kPer + 1];
+    grid_wait();
+    grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int wide_blocks = (N + 32 * kPer - 1) / (32 * kPer);
     const int block = static_cast<int>(blockIdx.x) % wide_blocks;
@@ -123,6 +125,8 @@ template <typename E>
 __global__ void __launch_bounds__(256)
 bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* __restrict__ out) {
     __shared__ float red[8][32];
+    grid_wait();
+    grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = blockIdx.x * 32 + lane;
     float s = 0.0f;
@@ -138,10 +142,29 @@ bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* 
     }
 }
 
+// A launch whose start may overlap the end of the one before it.
+template <typename... P, typename... A>
+static int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t stream, A... args) {
+    if (blocks > 0x7FFFFFFF) return DTP_ERR_UNSUPPORTED;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
+    return DTP_OK;
+}
+
 // Rows copied to a pitch of whole 16 bytes, for the tensor cores' loads; the pitch's spare entries stay unwritten
 // (the loads' extents end before them).
 __global__ void __launch_bounds__(256)
 repitch_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t pitch, uint16_t* __restrict__ dst) {
+    grid_wait();
+    grid_release();
     const int64_t total = rows * cols;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll)
         dst[i / cols * pitch + i % cols] = src[i];
@@ -180,10 +203,8 @@ static int aligned_rows(const void* p, int64_t rows, int cols, int dtype, Carver
     void* to = c.take(bytes);
     *out = Rows{to, padded(cols)};
     const int64_t blocks = (rows * cols + 1023) / 1024;
-    repitch_kernel<<<static_cast<unsigned>(blocks < 4096 ? blocks : 4096), 256, 0, stream>>>(
-        static_cast<const uint16_t*>(p), rows, cols, padded(cols), static_cast<uint16_t*>(to));
-    DTP_CUDA_TRY(cudaGetLastError());
-    return DTP_OK;
+    return launch_after(repitch_kernel, blocks < 4096 ? blocks : 4096, stream, static_cast<const uint16_t*>(p), rows, cols,
+                        padded(cols), static_cast<uint16_t*>(to));
 }
 
 static Mat by_row(const void* p, int64_t ld) { return Mat{p, ld, 1}; }      // [rows, K]
@@ -254,19 +275,16 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
 template <typename E>
 static int launch_act_grad(const void* dY, const float* Z, int64_t T, int N, int act, void* dZ, int64_t ldz,
                            float* partial, void* dbias, cudaStream_t stream) {
-    const int64_t blocks = chunks_of(T) * ((N + 32 * kPer - 1) / (32 * kPer));
-    if (blocks > 0x7FFFFFFF) return DTP_ERR_UNSUPPORTED;
     if (T > 0) {
+        const int64_t blocks = chunks_of(T) * ((N + 32 * kPer - 1) / (32 * kPer));
         auto kernel = N % kPer == 0 ? act_grad_kernel<E, true> : act_grad_kernel<E, false>;
-        kernel<<<static_cast<unsigned>(blocks), 256, 0, stream>>>(static_cast<const E*>(dY), Z, T, N, ldz, act, static_cast<E*>(dZ),
-                                         dbias ? partial : nullptr);
-        DTP_CUDA_TRY(cudaGetLastError());
+        const int st = launch_after(kernel, blocks, stream, static_cast<const E*>(dY), Z, T, N, ldz, act,
+                                    static_cast<E*>(dZ), dbias ? partial : nullptr);
+        if (st != DTP_OK) return st;
     }
-    if (dbias) {
-        bias_reduce_kernel<E><<<(N + 31) / 32, 256, 0, stream>>>(partial, chunks_of(T), N, static_cast<E*>(dbias));
-        DTP_CUDA_TRY(cudaGetLastError());
-    }
-    return DTP_OK;
+    if (!dbias) return DTP_OK;
+    return launch_after(bias_reduce_kernel<E>, (N + 31) / 32, stream, static_cast<const float*>(partial), chunks_of(T), N,
+                        static_cast<E*>(dbias));
 }
 
 int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
