@@ -36,8 +36,8 @@ __device__ __forceinline__ void act_both(int act, float z, float& value, float& 
     switch (act) {
         case DTP_ACT_SILU: {
             const float s = sigmoid<kFast>(z);
-            value = z * s;
             slope = s * fmaf(z, 1.0f - s, 1.0f);
+            value = z * s;
             return;
         }
         case DTP_ACT_GELU: {
@@ -54,6 +54,29 @@ __device__ __forceinline__ void act_both(int act, float z, float& value, float& 
         default:
             value = z;
             slope = 1.0f;
+    }
+}
+
+// act over an array in place: one switch for all of it.
+template <bool kFast, int N>
+__device__ __forceinline__ void act_values(int act, float (&v)[N]) {
+    if (act == DTP_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] *= sigmoid<kFast>(v[i]);
+    } else if (act != DTP_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = act_value<kFast>(act, v[i]);
+    }
+}
+// act and act' of four values, the values in place.
+template <bool kFast>
+__device__ __forceinline__ void act_both4(int act, float (&v)[4], float (&slope)[4]) {
+    if (act == DTP_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) act_both<kFast>(DTP_ACT_SILU, v[i], v[i], slope[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) act_both<kFast>(act, v[i], v[i], slope[i]);
     }
 }
 
