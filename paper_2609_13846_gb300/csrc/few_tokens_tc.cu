@@ -234,7 +234,7 @@ static int launch_form(const Product& p, int* status, int reset, int second, int
     using F = Form<TN>;
     const bool gated = p.epi.kind == kEpiGated;
     Args a;
-    if (!map_rows(&a.w[0], p.B[0], p.N, p.K, BM / 2) || !map_rows(&a.w[1], p.B[gated ? 1 : 0], p.N, p.K, BM / 2) ||
+    if (!map_rows(&a.w[0], p.B[0], p.N, p.K, BM / 2) || (gated && !map_rows(&a.w[1], p.B[1], p.N, p.K, BM / 2)) ||
         !map_rows(&a.x, p.A[0], p.M, p.K, TN))
         return DTP_ERR_CUDA;
     const int cols = gated ? BM / 2 : BM;

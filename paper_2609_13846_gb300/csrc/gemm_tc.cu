@@ -608,16 +608,15 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     using F = Form<kPair, BN>;
     const bool gated = p.epi.kind == kEpiGated;
     Args a;
-    for (int s = 0; s < 2; ++s) {
-        const int sa = s < p.segments ? s : 0, sb = s < p.segments || gated ? s : 0;
-        if (!map_operand(&a.a[s], p.A[sa], p.M, p.K, BM) || !map_operand(&a.b[s], p.B[sb], p.N, p.K, BN / 2))
-            return DTP_ERR_CUDA;
+    for (int s = 0; s < 2; ++s) {            // only the maps that the kernel reads: an encoding is host time
+        if (s < p.segments && !map_operand(&a.a[s], p.A[s], p.M, p.K, BM)) return DTP_ERR_CUDA;
+        if ((s < p.segments || gated) && !map_operand(&a.b[s], p.B[s], p.N, p.K, BN / 2)) return DTP_ERR_CUDA;
     }
     a.direct = (p.epi.ldo & 7) != 0;
     if (!a.direct) {
         if (!map_2d(&a.out, p.epi.out, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
-        const void* second = p.epi.out2 ? p.epi.out2 : p.epi.out;
-        if (!map_2d(&a.out2, second, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
+        if (p.epi.out2 && !map_2d(&a.out2, p.epi.out2, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+            return DTP_ERR_CUDA;
     }
     a.direct_z = (p.N & 3) != 0;
     if (p.epi.Z && !a.direct_z && !map_2d(&a.z, p.epi.Z, p.N, p.M, p.N, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B, true))

@@ -21,7 +21,7 @@ int launch(const layer::Product& p, int* status, int reset, int second, cudaStre
 
 namespace layer {
 
-constexpr int kRowChunk = 128;    // tokens per partial sum of the bias gradient
+constexpr int kRowChunk = 32;     // tokens per partial sum of the bias gradient
 constexpr int kPer = 8;           // columns per thread
 
 // dZ = dY act'(Z), rounded once, and the partial sums over kRowChunk tokens of the unrounded values (the bias

@@ -816,7 +816,9 @@ def apply_layout(W: dict, h: torch.Tensor, nu: torch.Tensor, D: int, head_dim: i
 # ------------------------------------------------------ layers of the permuted model (Sec. 4) --
 
 _dtype_of = operator.attrgetter("dtype")
-_CLIP_CODES = {torch.bfloat16: DTP_BF16, torch.float32: DTP_F32}
+_device_of, _contiguous = torch.Tensor.get_device, torch.Tensor.is_contiguous
+_address_of, _numel_of = torch.Tensor.data_ptr, torch.Tensor.numel
+_LAYER_CODES = {torch.bfloat16: DTP_BF16, torch.float32: DTP_F32}
 
 ACTIVATIONS = {"none": 0, "silu": 1, "gelu": 2, "relu": 3}
 
@@ -836,14 +838,28 @@ def _torch_code(dtype: torch.dtype) -> int:
     raise TypeError(f"unsupported dtype {dtype}; use bfloat16 or float32")
 
 
-def _layer_check(ref: torch.Tensor, name: str, t: torch.Tensor, shape, dtype=None):
-    """``t`` is a contiguous CUDA tensor of this shape on ref's device, of ref's dtype (or ``dtype``)."""
+def _layer_check(name: str, t: torch.Tensor, shape, dtype, index: int):
+    """``t`` is a contiguous CUDA tensor of this shape and dtype on device ``index``.  The checks of a call are a good part
+    of a small one's time: one condition, and what failed is found out only then."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == index >= 0 and t.is_contiguous():
+        return
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
-    if not t.is_cuda or not t.is_contiguous() or t.get_device() != ref.get_device():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor on the inputs' device")
-    if t.dtype is not (ref.dtype if dtype is None else dtype):
-        raise TypeError(f"{name} must be {ref.dtype if dtype is None else dtype}, got {t.dtype}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    raise ValueError(f"{name} must be a contiguous CUDA tensor on the inputs' device")
+
+
+def _layer_stream(stream, index: int) -> int:
+    """The raw handle of ``stream``, or of device ``index``'s current one."""
+    if stream is None and _current_raw_stream is not None:
+        return _current_raw_stream(index)
+    return _stream(stream)
+
+
+def _code_of(dtype: torch.dtype) -> int:
+    code = _LAYER_CODES.get(dtype)
+    return _torch_code(dtype) if code is None else code
 
 
 def _size_query(fn: str, *args) -> int:
@@ -858,6 +874,17 @@ def linear_workspace(T: int, K: int, N: int, dtype: torch.dtype, device, backwar
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
+def _linear_shapes(X, W):
+    """(T, K, N, dtype, device index) of X [T,K] and W [N,K]."""
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("shapes must be X [T,K], W [N,K]")
+    T, K = shape = X.shape
+    N, dtype, index = W.shape[0], X.dtype, X.get_device()
+    _layer_check("X", X, shape, dtype, index)
+    _layer_check("W", W, (N, K), dtype, index)
+    return T, K, N, dtype, index
+
+
 def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, residual: torch.Tensor | None = None,
            activation: str = "none", save: bool = False, Y: torch.Tensor | None = None,
            workspace: torch.Tensor | None = None, stream=None):
@@ -867,26 +894,23 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, r
     ``residual``).  With ``save`` returns (Y, Z): Z [T,N] fp32 holds the pre-activations X W^T + bias that
     linear_backward needs.
     """
-    if X.dim() != 2 or W.dim() != 2:
-        raise ValueError("shapes must be X [T,K], W [N,K]")
-    T, K = X.shape
-    N = W.shape[0]
-    code, act = _torch_code(X.dtype), _act_code(activation)
-    _layer_check(X, "X", X, (T, K))
-    _layer_check(X, "W", W, (N, K))
+    T, K, N, dtype, index = _linear_shapes(X, W)
+    code, act = _code_of(dtype), _act_code(activation)
     if bias is not None:
-        _layer_check(X, "bias", bias, (N,))
+        _layer_check("bias", bias, (N,), dtype, index)
     if residual is not None:
-        _layer_check(X, "residual", residual, (T, N))
+        _layer_check("residual", residual, (T, N), dtype, index)
     if Y is None:
-        Y = _keep(torch.empty((T, N), dtype=X.dtype, device=X.device), stream)
+        Y = _keep(torch.empty((T, N), dtype=dtype, device=X.device), stream)
     else:
-        _layer_check(X, "Y", Y, (T, N))
+        _layer_check("Y", Y, (T, N), dtype, index)
     Z = _keep(torch.empty((T, N), dtype=torch.float32, device=X.device), stream) if save else None
     if workspace is None:
-        workspace = _keep(linear_workspace(T, K, N, X.dtype, X.device), stream)
-    _check("dtp_linear", lib().dtp_linear(_ptr(X), _ptr(W), _ptr(bias), _ptr(residual), T, K, N, act, code, _ptr(Y),
-                                          _ptr(Z), _ptr(workspace), workspace.numel(), _stream(stream)))
+        workspace = _keep(linear_workspace(T, K, N, dtype, X.device), stream)
+    st = lib().dtp_linear(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), T, K, N, act, code, Y.data_ptr(),
+                          _ptr(Z), workspace.data_ptr(), workspace.numel(), _layer_stream(stream, index))
+    if st:
+        _check("dtp_linear", st)
     return (Y, Z) if save else Y
 
 
@@ -896,28 +920,23 @@ def linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: torch
 
     ``Z`` as linear(save=True) returned it (not needed without an activation); ``bias``: whether dbias is wanted.
     """
-    if X.dim() != 2 or W.dim() != 2:
-        raise ValueError("shapes must be X [T,K], W [N,K]")
-    T, K = X.shape
-    N = W.shape[0]
-    code, act = _torch_code(X.dtype), _act_code(activation)
-    _layer_check(X, "X", X, (T, K))
-    _layer_check(X, "W", W, (N, K))
-    _layer_check(X, "dY", dY, (T, N))
+    T, K, N, dtype, index = _linear_shapes(X, W)
+    code, act = _code_of(dtype), _act_code(activation)
+    _layer_check("dY", dY, (T, N), dtype, index)
     if act:
         if Z is None:
             raise ValueError("Z (of linear with save=True) is needed with an activation")
-        _layer_check(X, "Z", Z, (T, N), torch.float32)
+        _layer_check("Z", Z, (T, N), torch.float32, index)
     else:
         Z = None
     dX = _keep(torch.empty_like(X), stream)
     dW = _keep(torch.empty_like(W), stream)
     db = _keep(torch.empty(N, dtype=X.dtype, device=X.device), stream) if bias else None
     if workspace is None:
-        workspace = _keep(linear_workspace(T, K, N, X.dtype, X.device, backward=True), stream)
+        workspace = _keep(linear_workspace(T, K, N, dtype, X.device, backward=True), stream)
     _check("dtp_linear_backward",
            lib().dtp_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), T, K, N, act, code, _ptr(dX), _ptr(dW),
-                                     _ptr(db), _ptr(workspace), workspace.numel(), _stream(stream)))
+                                     _ptr(db), _ptr(workspace), workspace.numel(), _layer_stream(stream, index)))
     return dX, dW, db
 
 
@@ -928,15 +947,16 @@ def gated_ffn_workspace(T: int, d: int, N: int, dtype: torch.dtype, device, back
 
 
 def _gated_shapes(X, W_gate, W_up, W_down):
+    """(T, d, N, dtype, device index) of X [T,d], W_gate and W_up [N,d], W_down [d,N]."""
     if X.dim() != 2 or W_gate.dim() != 2:
         raise ValueError("shapes must be X [T,d], W_gate/W_up [N,d], W_down [d,N]")
-    T, d = X.shape
-    N = W_gate.shape[0]
-    _layer_check(X, "X", X, (T, d))
-    _layer_check(X, "W_gate", W_gate, (N, d))
-    _layer_check(X, "W_up", W_up, (N, d))
-    _layer_check(X, "W_down", W_down, (d, N))
-    return T, d, N
+    T, d = shape = X.shape
+    N, dtype, index = W_gate.shape[0], X.dtype, X.get_device()
+    _layer_check("X", X, shape, dtype, index)
+    _layer_check("W_gate", W_gate, (N, d), dtype, index)
+    _layer_check("W_up", W_up, (N, d), dtype, index)
+    _layer_check("W_down", W_down, (d, N), dtype, index)
+    return T, d, N, dtype, index
 
 
 def _gated_saved_shapes(T: int, N: int):
@@ -953,24 +973,26 @@ def gated_ffn(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down:
     ``residual``).  With ``save`` returns (Y, saved): what gated_ffn_backward needs (H in the inputs' dtype and
     the gate and up pre-activations in fp32, in the library's own order: 8 bytes a token and neuron).
     """
-    T, d, N = _gated_shapes(X, W_gate, W_up, W_down)
-    code, act = _torch_code(X.dtype), _act_code(activation)
+    T, d, N, dtype, index = _gated_shapes(X, W_gate, W_up, W_down)
+    code, act = _code_of(dtype), _act_code(activation)
     if residual is not None:
-        _layer_check(X, "residual", residual, (T, d))
+        _layer_check("residual", residual, (T, d), dtype, index)
     if Y is None:
-        Y = _keep(torch.empty((T, d), dtype=X.dtype, device=X.device), stream)
+        Y = _keep(torch.empty((T, d), dtype=dtype, device=X.device), stream)
     else:
-        _layer_check(X, "Y", Y, (T, d))
+        _layer_check("Y", Y, (T, d), dtype, index)
     H = pre = None
     if save:
         ld, n = _gated_saved_shapes(T, N)
-        H = _keep(torch.empty((T, ld), dtype=X.dtype, device=X.device), stream)
+        H = _keep(torch.empty((T, ld), dtype=dtype, device=X.device), stream)
         pre = _keep(torch.empty(n, dtype=torch.float32, device=X.device), stream)
     if workspace is None:
-        workspace = _keep(gated_ffn_workspace(T, d, N, X.dtype, X.device), stream)
-    _check("dtp_gated_ffn", lib().dtp_gated_ffn(_ptr(X), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(residual), T, d,
-                                                N, act, code, _ptr(Y), _ptr(H), _ptr(pre), _ptr(workspace),
-                                                workspace.numel(), _stream(stream)))
+        workspace = _keep(gated_ffn_workspace(T, d, N, dtype, X.device), stream)
+    st = lib().dtp_gated_ffn(X.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), _ptr(residual), T, d, N,
+                             act, code, Y.data_ptr(), _ptr(H), _ptr(pre), workspace.data_ptr(), workspace.numel(),
+                             _layer_stream(stream, index))
+    if st:
+        _check("dtp_gated_ffn", st)
     return (Y, (H, pre)) if save else Y
 
 
@@ -981,20 +1003,20 @@ def gated_ffn_backward(dY: torch.Tensor, X: torch.Tensor, W_gate: torch.Tensor, 
 
     ``saved`` as gated_ffn(save=True) returned it for the same inputs and activation.
     """
-    T, d, N = _gated_shapes(X, W_gate, W_up, W_down)
-    code, act = _torch_code(X.dtype), _act_code(activation)
-    _layer_check(X, "dY", dY, (T, d))
+    T, d, N, dtype, index = _gated_shapes(X, W_gate, W_up, W_down)
+    code, act = _code_of(dtype), _act_code(activation)
+    _layer_check("dY", dY, (T, d), dtype, index)
     H, pre = saved
     ld, n = _gated_saved_shapes(T, N)
-    _layer_check(X, "saved H", H, (T, ld))
-    _layer_check(X, "saved pre-activations", pre, (n,), torch.float32)
+    _layer_check("saved H", H, (T, ld), dtype, index)
+    _layer_check("saved pre-activations", pre, (n,), torch.float32, index)
     dX, dWg, dWu, dWd = (_keep(torch.empty_like(t), stream) for t in (X, W_gate, W_up, W_down))
     if workspace is None:
-        workspace = _keep(gated_ffn_workspace(T, d, N, X.dtype, X.device, backward=True), stream)
+        workspace = _keep(gated_ffn_workspace(T, d, N, dtype, X.device, backward=True), stream)
     _check("dtp_gated_ffn_backward",
            lib().dtp_gated_ffn_backward(_ptr(dY), _ptr(X), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(H), _ptr(pre),
                                         T, d, N, act, code, _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd),
-                                        _ptr(workspace), workspace.numel(), _stream(stream)))
+                                        _ptr(workspace), workspace.numel(), _layer_stream(stream, index)))
     return dX, dWg, dWu, dWd
 
 
@@ -1003,7 +1025,7 @@ def clip_grad_norm_workspace(grads) -> torch.Tensor:
     n = len(grads)
     if n == 0:
         raise ValueError("grads must hold at least one tensor")
-    return _clip_workspace(array.array("q", map(torch.Tensor.numel, grads)), grads[0].device)
+    return _clip_workspace(array.array("q", list(map(_numel_of, grads))), grads[0].device)
 
 
 def _clip_workspace(numel, device) -> torch.Tensor:
@@ -1014,9 +1036,9 @@ def _clip_workspace(numel, device) -> torch.Tensor:
 def _flat_tensors(name, ts, index):
     """(addresses, sizes, dtypes) of contiguous CUDA tensors of device ``index``.  One pass per property with map, and
     not one Python loop over the tensors: a model has hundreds of them, and the call is as long as its kernel."""
-    if index < 0 or set(map(torch.Tensor.get_device, ts)) != {index} or not all(map(torch.Tensor.is_contiguous, ts)):
+    if index < 0 or list(map(_device_of, ts)).count(index) != len(ts) or not all(map(_contiguous, ts)):
         raise ValueError(f"{name} must be contiguous CUDA tensors on one device")
-    return (array.array("Q", map(torch.Tensor.data_ptr, ts)), array.array("q", map(torch.Tensor.numel, ts)),
+    return (array.array("Q", list(map(_address_of, ts))), array.array("q", list(map(_numel_of, ts))),
             list(map(_dtype_of, ts)))
 
 
@@ -1034,8 +1056,10 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
         raise ValueError("grads must hold at least one tensor")
     index = grads[0].get_device()
     src, numel, dtypes = _flat_tensors("grads", grads, index)
-    if not _CLIP_CODES.keys() >= set(dtypes):
-        raise TypeError("grads must be bfloat16 or float32")
+    try:
+        codes = array.array("i", [_LAYER_CODES[d] for d in dtypes])
+    except KeyError:
+        raise TypeError("grads must be bfloat16 or float32") from None
     dst = None
     if out is not None:
         out = list(out)
@@ -1044,7 +1068,6 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
         dst, out_numel, out_dtypes = _flat_tensors("out", out, index)
         if out_numel != numel or out_dtypes != dtypes:
             raise ValueError("out must have the sizes and dtypes of grads")
-    codes = array.array("i", map(_CLIP_CODES.__getitem__, dtypes))
     if norm is None:
         norm = _keep(torch.empty((), dtype=torch.float32, device=grads[0].device), stream)
     elif norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != index:
@@ -1053,6 +1076,6 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
         workspace = _keep(_clip_workspace(numel, grads[0].device), stream)
     st = lib().dtp_clip_grad_norm(src.buffer_info()[0], None if dst is None else dst.buffer_info()[0],
                                   numel.buffer_info()[0], codes.buffer_info()[0], count, float(max_norm), _ptr(norm),
-                                  _ptr(workspace), workspace.numel(), _stream(stream))
+                                  _ptr(workspace), workspace.numel(), _layer_stream(stream, index))
     _check("dtp_clip_grad_norm", st)
     return norm
