@@ -1,17 +1,17 @@
 // few_tokens_tc.cu -- the forward products of the layer operators for few tokens (single-token serving, small
-// batches), bf16, on the tcgen05 tensor cores:
+// batches up to 64), bf16, on the tcgen05 tensor cores:
 //
 //     acc[n, t] = sum_k W[n, k] X[t, k]     (fp32 in TMEM), then the epilogue at (t, n)
 //
 // Bound by streaming the weights once.  The operands change places: 128 weight rows are the MMA's rows and up to
-// TN = 16 .. 128 tokens its columns, so no tensor work is spent on absent tokens beyond TN.  A tile is 128 outputs,
+// TN = 16, 32 or 64 tokens its columns, so no tensor work is spent on absent tokens beyond TN.  A tile is 128 outputs,
 // or 64 neurons with their gate rows above their up rows.  To have enough loads in flight on the whole chip, a
 // cluster of up to 8 CTAs shares a tile, each with its own range of k; the partial sums meet in shared memory
 // (each CTA sends every peer the rows that the peer finishes) and are added in the order of the ranges, so the
 // result does not depend on timing.
 //
-// Six warps: warp 4 loads 64-wide k blocks by TMA, warp 5 issues the MMAs, warps 0 to 3 send the partial sums, and
-// all of them run the epilogue.  In a sequence of two products the second one starts early and loads its weights
+// Six warps: warp 4 loads 64-wide k blocks by TMA, two a stage up to 32 tokens (256 bytes of a row at a time, and half the
+// barriers), warp 5 issues the MMAs, warps 0 to 3 send the partial sums, and all of them run the epilogue.  In a sequence of two products the second one starts early and loads its weights
 // while the first finishes; it waits for the first before it touches the tokens.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -35,16 +35,17 @@ constexpr int kMaxSplit = 8;  // CTAs of a portable cluster
 
 template <int TN>
 struct Form {
-    static constexpr uint32_t kTileX = TN * BK * 2;
-    static constexpr uint32_t kStageBytes = BM * BK * 2 + kTileX;
+    static constexpr int kBoxes = TN <= 32 ? 2 : 1;                       // k blocks per stage
+    static constexpr uint32_t kBoxBytes = (BM + TN) * BK * 2;
+    static constexpr uint32_t kStageBytes = kBoxes * kBoxBytes;
     static constexpr size_t kSums = static_cast<size_t>(BM) * TN * 4;     // partial sums from all CTAs of the cluster
-    // two CTAs per SM up to 64 tokens (113 KB each), one beyond
-    static constexpr size_t kBudget = TN <= 64 ? 112 * 1024 : 200 * 1024;
-    static constexpr int STAGES = static_cast<int>((kBudget - kSums - 2048) / kStageBytes);
+    static constexpr int STAGES = static_cast<int>((112 * 1024 - kSums - 1536) / kStageBytes);     // two CTAs per SM
     static constexpr uint32_t kTmemCols = TN < 32 ? 32 : TN;
     static constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kSums + 256;
 };
-static_assert(Form<16>::STAGES >= 3 && Form<32>::STAGES >= 3 && Form<64>::STAGES >= 3 && Form<128>::STAGES >= 3, "");
+static_assert(Form<16>::STAGES >= 2 && Form<32>::STAGES >= 2 && Form<64>::STAGES >= 3, "");
+static_assert(Form<16>::kSmemBytes <= 113 * 1024 && Form<32>::kSmemBytes <= 113 * 1024 &&
+                  Form<64>::kSmemBytes <= 113 * 1024, "two CTAs per SM");
 
 struct Args {
     CUtensorMap w[2], x;
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_full + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int S = p.split;
     const int rank = static_cast<int>(blockIdx.x) % S, tile = static_cast<int>(blockIdx.x) / S;
     constexpr int kCols = KIND == kEpiGated ? BM / 2 : BM;      // outputs per tile
@@ -103,64 +104,93 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     const uint32_t tmem = *tmem_slot;
     asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");    // this CTA runs
 
-    if (warp == 4 && lane == 0) {
-        // -------------------------------------------------------------------- producer
-        tma_prefetch_desc(&p.w[0]);
-        tma_prefetch_desc(&p.x);
+    constexpr int kBoxes = F::kBoxes;
+    if (warp == 4) {
+        // -------------------------------------------------------------------- producer: one lane issues
+        const bool issuer = elect_one();
+        const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar), tiles0 = smem_u32(tiles);
+        const CUtensorMap* lower = KIND == kEpiGated ? &p.w[1] : &p.w[0];
+        const int lower_row = KIND == kEpiGated ? n0 : n0 + BM / 2;
+        if (issuer) {
+            tma_prefetch_desc(&p.w[0]);
+            tma_prefetch_desc(&p.x);
+        }
+        auto boxes_at = [&](int kb) { return kb1 - kb < kBoxes ? kb1 - kb : kBoxes; };
         auto load_w = [&](int kb, int s) {
-            const uint32_t fb = smem_u32(&full_bar[s]), st = smem_u32(tiles + s * F::kStageBytes);
-            mbar_arrive_expect_tx(fb, F::kStageBytes);
-            tma_load_2d(st, &p.w[0], fb, kb * BK, n0);
-            tma_load_2d(st + BM / 2 * BK * 2, KIND == kEpiGated ? &p.w[1] : &p.w[0], fb, kb * BK,
-                        KIND == kEpiGated ? n0 : n0 + BM / 2);
+            const uint32_t fb = full0 + s * 8u;
+            const int boxes = boxes_at(kb);
+            if (!issuer) return;
+            mbar_arrive_expect_tx(fb, boxes * F::kBoxBytes);
+            for (int x = 0; x < boxes; ++x) {
+                const uint32_t st = tiles0 + s * F::kStageBytes + x * F::kBoxBytes;
+                tma_load_2d(st, &p.w[0], fb, (kb + x) * BK, n0);
+                tma_load_2d(st + BM / 2 * BK * 2, lower, fb, (kb + x) * BK, lower_row);
+            }
         };
         auto load_x = [&](int kb, int s) {
-            tma_load_2d(smem_u32(tiles + s * F::kStageBytes) + BM * BK * 2, &p.x, smem_u32(&full_bar[s]), kb * BK, 0);
+            const int boxes = boxes_at(kb);
+            if (!issuer) return;
+            for (int x = 0; x < boxes; ++x)
+                tma_load_2d(tiles0 + s * F::kStageBytes + x * F::kBoxBytes + BM * BK * 2, &p.x, full0 + s * 8u,
+                            (kb + x) * BK, 0);
         };
-        const int first = kb1 - kb0 < STAGES ? kb1 - kb0 : STAGES;
+        const int filled = (kb1 - kb0 + kBoxes - 1) / kBoxes;
+        const int first = filled < STAGES ? filled : STAGES;
         // the second product's weights do not come from the first
         if (!p.second) grid_wait();
-        for (int i = 0; i < first; ++i) load_w(kb0 + i, i);
+        for (int i = 0; i < first; ++i) load_w(kb0 + i * kBoxes, i);
         if (p.second) grid_wait();
         grid_release();
         asm volatile("fence.proxy.async;" ::: "memory");
         // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
         // block 0, which starts first, has passed here.
-        if (p.reset && blockIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
-        for (int i = 0; i < first; ++i) load_x(kb0 + i, i);
+        if (p.reset && blockIdx.x == 0 && issuer) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
+        for (int i = 0; i < first; ++i) load_x(kb0 + i * kBoxes, i);
         int stage = 0;
         uint32_t phase = 0;                      // of the stage's reuse
-        for (int kb = kb0 + first; kb < kb1; ++kb) {
-            if (!mbar_wait(smem_u32(&empty_bar[stage]), phase, abort_flag)) break;
+        for (int kb = kb0 + first * kBoxes; kb < kb1; kb += kBoxes) {
+            if (!mbar_wait(empty0 + stage * 8u, phase, abort_flag)) break;
             load_w(kb, stage);
             load_x(kb, stage);
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
-    } else if (warp == 5 && lane == 0) {
+    } else if (warp == 5) {
         // ------------------------------------------------------------------ MMA issuer
+        const bool issuer = elect_one();
         constexpr uint32_t kIdesc = idesc_bf16_f32(BM, TN);
+        const uint32_t full0 = smem_u32(full_bar), empty0 = smem_u32(empty_bar);
+        const uint32_t low_w = desc_low(smem_u32(tiles), false);
         int stage = 0;
         uint32_t phase = 0;
-        for (int kb = kb0; kb < kb1; ++kb) {
-            if (!mbar_wait(smem_u32(&full_bar[stage]), phase, abort_flag)) break;
+        for (int kb = kb0; kb < kb1; kb += kBoxes) {
+            if (!mbar_wait(full0 + stage * 8u, phase, abort_flag)) break;
             tc_fence_after();
-            const uint32_t st = smem_u32(tiles + stage * F::kStageBytes);
-            const uint64_t da = smem_desc_k128(st), db = smem_desc_k128(st + BM * BK * 2);
+            const int boxes = kb1 - kb < kBoxes ? kb1 - kb : kBoxes;
+            if (issuer) {
 #pragma unroll
-            for (int kk = 0; kk < BK / UK; ++kk) {
-                const uint64_t off = static_cast<uint64_t>((kk * UK * 2) >> 4);
-                umma_bf16(tmem, da + off, db + off, kIdesc, (kb > kb0 || kk > 0) ? 1u : 0u);
+                for (int x = 0; x < kBoxes; ++x) {
+                    if (x >= boxes) break;
+                    const uint32_t w = low_w + ((stage * F::kStageBytes + x * F::kBoxBytes) >> 4);
+#pragma unroll
+                    for (int kk = 0; kk < BK / UK; ++kk) {
+                        const uint32_t at = w + ((kk * UK * 2) >> 4);
+                        umma_bf16(tmem, desc(at), desc(at + ((BM * BK * 2) >> 4)), kIdesc,
+                                  (kb > kb0 || x > 0 || kk > 0) ? 1u : 0u);
+                    }
+                }
+                umma_commit(empty0 + stage * 8u);
             }
-            umma_commit(smem_u32(&empty_bar[stage]));
+            __syncwarp();
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
-        umma_commit(smem_u32(acc_full));
+        if (issuer) umma_commit(smem_u32(acc_full));
     }
     __syncwarp();
     asm volatile("barrier.cluster.wait;" ::: "memory");              // every peer runs: its memory may be written
 
     const int T = static_cast<int>(p.epi.M);
-    const int own = kCols / S;                   // outputs that this CTA finishes: n0 + rank * own ..
+    // outputs that this CTA finishes: n0 + rank * own .., own a power of two
+    const int own_log = (KIND == kEpiGated ? 6 : 7) - (31 - __clz(S)), own = 1 << own_log;
     if (warp < 4) {
         // ------------------------------------------------- partial sums to the CTAs that finish them
         const bool ok = mbar_wait(smem_u32(acc_full), 0, abort_flag);
@@ -168,10 +198,10 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
         if (ok) {
             const int row = warp * 32 + lane;            // of the tile
             const int j = KIND == kEpiGated ? row & (BM / 2 - 1) : row;
-            const int dst = j / own;
+            const int dst = j >> own_log;
             // [rank][token][gate rows, then up rows, of the destination's outputs]
             const int pitch = KIND == kEpiGated ? 2 * own : own;
-            const int at = rank * TN * pitch + j % own + (KIND == kEpiGated && row >= BM / 2 ? own : 0);
+            const int at = rank * TN * pitch + (j & (own - 1)) + (KIND == kEpiGated && row >= BM / 2 ? own : 0);
             const uint32_t to = mapa_shared(smem_u32(sums + at), static_cast<uint32_t>(dst));
             const uint32_t acc = tmem + (static_cast<uint32_t>(warp * 32) << 16);
 #pragma unroll 1
@@ -201,7 +231,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     const int pitch = KIND == kEpiGated ? 2 * own : own;
     const int base = n0 + rank * own;
     for (int i = threadIdx.x; i < T * own; i += kThreads) {
-        const int t = i / own, r = i % own, n = base + r;
+        const int t = i >> own_log, r = i & (own - 1), n = base + r;
         if (n >= p.epi.N) continue;
         float a0 = 0.0f, a1 = 0.0f;
         for (int s = 0; s < S; ++s) {
@@ -268,9 +298,13 @@ static int launch_form(const Product& p, int* status, int reset, int second, int
     return DTP_OK;
 }
 
-// Whether this kernel takes the product: both operands with k contiguous, few tokens.
+// Whether this kernel takes the product: both operands with k contiguous, few tokens.  Up to 32 always (4096 x 4096, 32 tokens:
+// 9.4 us here, 13.3 in the persistent tiles); from 33 to 64 where there are too few tiles to keep those busy (64 tokens: 4096 x
+// 4096 11.8 and 13.5 us, 4096 x 14336 31.7 and 24.5).
 bool takes(const Product& p) {
-    return p.M <= 128 && p.segments == 1 && p.A[0].ks == 1 && p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad;
+    const int cols = p.epi.kind == kEpiGated ? BM / 2 : BM;
+    return p.M <= (p.N > 64 * cols ? 32 : 64) && p.segments == 1 && p.A[0].ks == 1 && p.B[0].ks == 1 &&
+           p.epi.kind != kEpiGatedGrad;
 }
 
 // second: X was written by the launch before this one on the stream, which is this kernel too.
@@ -280,8 +314,7 @@ int launch(const Product& p, int* status, int reset, int second, cudaStream_t st
     DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     if (p.M <= 16) return launch_form<16>(p, status, reset, second, sms, stream);
     if (p.M <= 32) return launch_form<32>(p, status, reset, second, sms, stream);
-    if (p.M <= 64) return launch_form<64>(p, status, reset, second, sms, stream);
-    return launch_form<128>(p, status, reset, second, sms, stream);
+    return launch_form<64>(p, status, reset, second, sms, stream);
 }
 
 }  // namespace few

@@ -26,6 +26,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "dtp_common.cuh"
 #include "layer_common.cuh"
@@ -84,31 +85,6 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-
-// Shared-memory matrix descriptors (128-byte swizzle, version 1) as two words: the high word is the stride byte offset (1024
-// >> 4) and the layout, the same for both orders.  With k contiguous a tile is rows of 64 k, 8-row groups 1024 bytes apart.
-// With the rows contiguous it is 64-row blocks of [k][64 rows], 128 bytes per k: the stride byte offset leads from one group of
-// 8 k to the next, the leading byte offset (64 k x 128 bytes) from one 64-row block to the next.
-constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, bool rows_contiguous) {
-    return ((saddr & 0x3FFFFu) >> 4) | ((rows_contiguous ? (64u * 128u) >> 4 : 1u) << 16);
-}
-__device__ __forceinline__ uint64_t desc(uint32_t low) {
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
-    return d;
-}
-
-// One lane of the warp, the same every time.
-__device__ __forceinline__ bool elect_one() {
-    uint32_t p;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xFFFFFFFF;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}\n"
-        : "=r"(p));
-    return p != 0;
-}
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -371,9 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         uint8_t* stg = staging + (warp - kEpiWarp0) * kStageOut;
         const bool wide = (e.ldo & 7) == 0;
-        // 64 bytes of the thread's row through the staging buffer: a bulk store of a box of 32 rows, from column x
-        auto store_box = [&](const CUtensorMap* map, const uint32_t* w, int x, int row0) {
-            // the staging buffer is free once the store issued from it has read it
+        // 64 bytes of every lane's row into the staging buffer, once the store issued from it has read it
+        auto stage_box = [&](const uint32_t* w) {
             if (lane == 0) bulk_wait_read0();
             __syncwarp();
             uint8_t* sb = stg + lane * 64;
@@ -381,6 +356,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             for (int c = 0; c < 4; ++c)
                 *reinterpret_cast<uint4*>(sb + ((c ^ ((lane >> 1) & 3)) << 4)) =
                     make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        };
+        // a bulk store of the box of 32 rows, from column x
+        auto store_box = [&](const CUtensorMap* map, const uint32_t* w, int x, int row0) {
+            stage_box(w);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -388,19 +367,25 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 bulk_commit();
             }
         };
-        // 32 columns of the thread's row, from column n: a box or, where rows are not on 16-byte boundaries, one by one
-        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int64_t m, int row0) {
-            if (!p.direct) return store_box(map, w, n, row0);
-            if (m < e.M) {
-                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + m * e.ldo + n;
-#pragma unroll
-                for (int c = 0; c < 16; ++c) {
-                    float lo, hi;
-                    unpack_bf16(w[c], lo, hi);
-                    if (n + 2 * c < e.N) o[2 * c] = __float2bfloat16_rn(lo);
-                    if (n + 2 * c + 1 < e.N) o[2 * c + 1] = __float2bfloat16_rn(hi);
-                }
+        // the same where rows are not on 16-byte boundaries: element by element, the lanes along the rows
+        auto store_elements = [&](auto* out, int64_t ld, const uint32_t* w, int x, int row0) {
+            using V = std::remove_pointer_t<decltype(out)>;
+            constexpr int kPer = 64 / sizeof(V);          // columns of a box
+            stage_box(w);
+            __syncwarp();
+            const int c = lane % kPer;
+#pragma unroll 4
+            for (int r = lane / kPer; r < 32; r += 32 / kPer) {
+                const int at = r * 64 + ((((c * sizeof(V)) >> 4) ^ ((r >> 1) & 3)) << 4) + ((c * sizeof(V)) & 15);
+                if (row0 + r < e.M && x + c < e.N)
+                    out[(static_cast<int64_t>(row0) + r) * ld + x + c] = *reinterpret_cast<const V*>(stg + at);
             }
+            __syncwarp();
+        };
+        // 32 columns of the box's rows, from column n
+        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int row0) {
+            if (p.direct) store_elements(static_cast<__nv_bfloat16*>(out), e.ldo, w, n, row0);
+            else store_box(map, w, n, row0);
         };
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (int u = first + set * workers; u < p.units; u += 2 * workers, unit_count += 2) {
@@ -460,20 +445,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         }
                     }
                     if (e.Z) {
-                        if (!p.direct_z) {
 #pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                if (n + 16 * q < e.N) {
+                        for (int q = 0; q < 2; ++q) {
+                            if (n + 16 * q < e.N) {
 #pragma unroll
-                                    for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
-                                    store_box(&p.z, w, n + 16 * q, row0);
-                                }
+                                for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
+                                if (p.direct_z) store_elements(e.Z, e.N, w, n + 16 * q, row0);
+                                else store_box(&p.z, w, n + 16 * q, row0);
                             }
-                        } else if (m < e.M) {
-                            float* z = e.Z + m * e.N + n;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (n + i < e.N) z[i] = v[i];
                         }
                     }
                     act_values<true>(e.act, v);
@@ -489,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     }
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                    store32(&p.out, e.out, w, n, m, row0);
+                    store32(&p.out, e.out, w, n, row0);
                 } else if constexpr (KIND == kEpiGated) {
                     float* pre = e.pre ? e.pre + pre_index(m, n, e.N) : nullptr;
 #pragma unroll
@@ -513,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         for (int i = 0; i < 8; ++i)
                             w[8 * q + i] = pack_bf16(g[2 * i] * v[2 * i], g[2 * i + 1] * v[2 * i + 1]);
                     }
-                    store32(&p.out, e.out, w, n, m, row0);
+                    store32(&p.out, e.out, w, n, row0);
                 } else {
                     const float* pre = e.pre + pre_index(m, n, e.N);
                     uint32_t w2[16];
@@ -534,8 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         w2[2 * q] = pack_bf16(d[0] * value[0], d[1] * value[1]);
                         w2[2 * q + 1] = pack_bf16(d[2] * value[2], d[3] * value[3]);
                     }
-                    store32(&p.out, e.out, w, n, m, row0);
-                    store32(&p.out2, e.out2, w2, n, m, row0);
+                    store32(&p.out, e.out, w, n, row0);
+                    store32(&p.out2, e.out2, w2, n, row0);
                 }
             }
             if constexpr (!kSplit) {

@@ -86,6 +86,31 @@ __device__ __forceinline__ void act_both4(int act, float (&v)[4], float (&slope)
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Shared-memory matrix descriptors (128-byte swizzle, version 1) as two words: the high word is the stride byte offset (1024
+// >> 4) and the layout, the same for both orders.  With k contiguous a tile is rows of 64 k, 8-row groups 1024 bytes apart.
+// With the rows contiguous it is 64-row blocks of [k][64 rows], 128 bytes per k: the stride byte offset leads from one group of
+// 8 k to the next, the leading byte offset (64 k x 128 bytes) from one 64-row block to the next.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, bool rows_contiguous) {
+    return ((saddr & 0x3FFFFu) >> 4) | ((rows_contiguous ? (64u * 128u) >> 4 : 1u) << 16);
+}
+__device__ __forceinline__ uint64_t desc(uint32_t low) {
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
+    return d;
+}
+
+// One lane of the warp, the same every time.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "elect.sync _|p, 0xFFFFFFFF;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}\n"
+        : "=r"(p));
+    return p != 0;
+}
+
 // Element types of the operands.
 template <typename E>
 __device__ __forceinline__ float to_f32(E v) { return static_cast<float>(v); }

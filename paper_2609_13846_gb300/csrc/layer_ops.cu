@@ -19,6 +19,11 @@ bool takes(const layer::Product& p);
 int launch(const layer::Product& p, int* status, int reset, int second, cudaStream_t stream);
 }  // namespace few
 
+namespace fews {
+bool takes(const layer::Product& p, int dtype);
+int launch(const layer::Product& p, int dtype, int* status, int second, cudaStream_t stream);
+}  // namespace fews
+
 namespace layer {
 
 constexpr int kRowChunk = 32;     // tokens per partial sum of the bias gradient
@@ -216,13 +221,17 @@ struct Call {
     void* workspace;
     cudaStream_t stream;
     bool fresh = true;          // the status word is still an earlier call's
-    bool after_few = false;     // the last launch was the few-token kernel
+    bool after_few = false;     // the last launch was a few-token kernel
 
     int run(const Product& p) {
         int* status = static_cast<int*>(workspace);
         const int reset = fresh;
         const bool second = after_few;
         after_few = false;
+        if (p.K > 0 && p.M > 0 && fews::takes(p, dtype)) {
+            fresh = false, after_few = true;
+            return fews::launch(p, dtype, reset ? status : nullptr, second, stream);
+        }
         if (dtype == DTP_BF16 && p.K > 0) {
             fresh = false;
             if (few::takes(p)) {
