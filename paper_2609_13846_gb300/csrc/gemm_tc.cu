@@ -95,20 +95,6 @@ __device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
     b = __uint_as_float(v & 0xFFFF0000u);
 }
 
-// Eight consecutive bf16 of a row, n beyond the end as zero; `wide`: 16-byte loads are aligned.
-__device__ __forceinline__ void load8(const __nv_bfloat16* row, int n, int N, bool wide, float* v) {
-    if (wide && n + 8 <= N) {
-        const uint4 q = *reinterpret_cast<const uint4*>(row + n);
-        unpack_bf16(q.x, v[0], v[1]);
-        unpack_bf16(q.y, v[2], v[3]);
-        unpack_bf16(q.z, v[4], v[5]);
-        unpack_bf16(q.w, v[6], v[7]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = n + i < N ? to_f32(row[n + i]) : 0.0f;
-    }
-}
-
 // Units of a persistent worker: row tiles in groups of 8, column tile by column tile within a group, so that the
 // tiles in flight share their rows and columns in L2.
 constexpr int kGroupM = 8;
@@ -195,6 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     // An early launch works on other tiles than the one before it, which had itself waited: it waits at its end.
     if (!(kSplit && p.early)) grid_wait();
     grid_release();
+    asm volatile("fence.proxy.async;" ::: "memory");     // what was stored plainly is loaded by TMA
     // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
     // block 0, which starts first, has passed here.
     if (p.reset && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int*>(p.status) = DTP_OK;
@@ -394,15 +381,39 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
             const uint32_t buf = unit_count & 1u;
+            const int width = kSplit ? kCols / p.split : kCols;          // this CTA's columns of the tile, 32 at a time
+            const int base = tn * kCols + (kSplit ? part * width : 0);
+            // A box's residual (four lanes to a row's 64 bytes, eight rows at a time) and bias (a pair of columns in each
+            // of 16 lanes) are loaded one box ahead, the first before the accumulator is waited for.
+            uint4 rq[4];
+            uint32_t bq = 0;
+            auto fetch = [&](int c) {
+                const int n = base + c;
+                if (c >= width || n >= e.N || row0 >= e.M) return;
+                if (e.bias) {
+                    const __nv_bfloat16* b = reinterpret_cast<const __nv_bfloat16*>(e.bias) + n + 2 * (lane & 15);
+                    const int left = e.N - n - 2 * (lane & 15);
+                    bq = left >= 2 ? *reinterpret_cast<const uint32_t*>(b)
+                                   : left == 1 ? *reinterpret_cast<const uint16_t*>(b) : 0u;
+                }
+                if (e.residual && wide) {
+                    const int col = n + 8 * (lane & 3);
+                    const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + col;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int64_t row = static_cast<int64_t>(row0) + (lane >> 2) + 8 * i;
+                        rq[i] = row < e.M && col < e.N ? *reinterpret_cast<const uint4*>(r + row * e.ldo)
+                                                       : make_uint4(0, 0, 0, 0);
+                    }
+                }
+            };
+            if constexpr (KIND == kEpiLinear) fetch(32 * half);
             if constexpr (!kSplit) {
                 const uint32_t use = (unit_count >> 1) & 1u;
                 if (!mbar_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
                 tc_fence_after();
             }
             const uint32_t acc = lane_base + buf * BN;
-            // this CTA's columns of the tile, 32 at a time, shared by the two halves of the warps
-            const int width = kSplit ? kCols / p.split : kCols;
-            const int base = tn * kCols + (kSplit ? part * width : 0);
             // 16 columns from column col of accumulator q
             auto get16 = [&](int q, int col, float* v) {
                 if constexpr (kSplit) {
@@ -437,11 +448,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     got();
                     if (e.bias) {
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            float b[8];
-                            load8(reinterpret_cast<const __nv_bfloat16*>(e.bias), n + 8 * q, e.N, true, b);
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
+                        for (int i = 0; i < 16; ++i) {
+                            float lo, hi;
+                            unpack_bf16(__shfl_sync(0xFFFFFFFFu, bq, i), lo, hi);
+                            v[2 * i] += lo;
+                            v[2 * i + 1] += hi;
                         }
                     }
                     if (e.Z) {
@@ -456,16 +467,36 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         }
                     }
                     act_values<true>(e.act, v);
-                    if (e.residual && m < e.M) {
-                        const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + m * e.ldo;
+                    if (e.residual && wide) {
+                        // from the rows' quarters to the lane's row, through the staging buffer
+                        if (lane == 0) bulk_wait_read0();
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = (lane >> 2) + 8 * i;
+                            *reinterpret_cast<uint4*>(stg + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4)) = rq[i];
+                        }
+                        __syncwarp();
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            float b[8];
-                            load8(r, n + 8 * q, e.N, wide, b);
+                            const uint4 x = *reinterpret_cast<const uint4*>(stg + lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4));
+                            const uint32_t words[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) v[8 * q + i] += b[i];
+                            for (int i = 0; i < 4; ++i) {
+                                float lo, hi;
+                                unpack_bf16(words[i], lo, hi);
+                                v[8 * q + 2 * i] += lo;
+                                v[8 * q + 2 * i + 1] += hi;
+                            }
                         }
+                        __syncwarp();
+                    } else if (e.residual && m < e.M) {
+                        const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + m * e.ldo;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (n + i < e.N) v[i] += to_f32(r[n + i]);
                     }
+                    fetch(c + 64);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
                     store32(&p.out, e.out, w, n, row0);

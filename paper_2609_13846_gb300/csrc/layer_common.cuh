@@ -20,11 +20,33 @@ __device__ __forceinline__ float sigmoid(float z) {
     else return 1.0f / (1.0f + expf(-z));
 }
 
+// Phi(z) and e^(-z^2/2).  kFast: erf by Abramowitz and Stegun 7.1.26 (absolute error 1.5e-7), whose exponential is the one
+// of the density; the small side is computed and not subtracted from 1.
+template <bool kFast>
+__device__ __forceinline__ float normal_cdf(float z, float& bell) {
+    if constexpr (kFast) {
+        bell = __expf(-0.5f * z * z);
+        const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+        float p = fmaf(1.061405429f, t, -1.453152027f);
+        p = fmaf(p, t, 1.421413741f);
+        p = fmaf(p, t, -0.284496736f);
+        p = fmaf(p, t, 0.254829592f);
+        const float q = 0.5f * p * t * bell;
+        return z < 0.0f ? q : 1.0f - q;
+    } else {
+        bell = expf(-0.5f * z * z);
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f));
+    }
+}
+
 template <bool kFast>
 __device__ __forceinline__ float act_value(int act, float z) {
     switch (act) {
         case DTP_ACT_SILU: return z * sigmoid<kFast>(z);
-        case DTP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+        case DTP_ACT_GELU: {
+            float bell;
+            return z * normal_cdf<kFast>(z, bell);
+        }
         case DTP_ACT_RELU: return z <= 0.0f ? 0.0f : z;       // a NaN stays a NaN
         default: return z;
     }
@@ -41,10 +63,10 @@ __device__ __forceinline__ void act_both(int act, float z, float& value, float& 
             return;
         }
         case DTP_ACT_GELU: {
-            const float cdf = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
-            const float e = kFast ? __expf(-0.5f * z * z) : expf(-0.5f * z * z);
+            float bell;
+            const float cdf = normal_cdf<kFast>(z, bell);
+            slope = fmaf(z * 0.39894228040143268f, bell, cdf);
             value = z * cdf;
-            slope = fmaf(z * 0.39894228040143268f, e, cdf);
             return;
         }
         case DTP_ACT_RELU:
@@ -62,10 +84,13 @@ template <bool kFast, int N>
 __device__ __forceinline__ void act_values(int act, float (&v)[N]) {
     if (act == DTP_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] *= sigmoid<kFast>(v[i]);
-    } else if (act != DTP_ACT_NONE) {
+        for (int i = 0; i < N; ++i) v[i] = act_value<kFast>(DTP_ACT_SILU, v[i]);
+    } else if (act == DTP_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = act_value<kFast>(act, v[i]);
+        for (int i = 0; i < N; ++i) v[i] = act_value<kFast>(DTP_ACT_GELU, v[i]);
+    } else if (act == DTP_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = act_value<kFast>(DTP_ACT_RELU, v[i]);
     }
 }
 // act and act' of four values, the values in place.
@@ -74,6 +99,9 @@ __device__ __forceinline__ void act_both4(int act, float (&v)[4], float (&slope)
     if (act == DTP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) act_both<kFast>(DTP_ACT_SILU, v[i], v[i], slope[i]);
+    } else if (act == DTP_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) act_both<kFast>(DTP_ACT_GELU, v[i], v[i], slope[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) act_both<kFast>(act, v[i], v[i], slope[i]);

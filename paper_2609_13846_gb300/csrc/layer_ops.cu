@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "dtp_common.cuh"
 #include "layer_common.cuh"
 
@@ -27,10 +29,10 @@ int launch(const layer::Product& p, int dtype, int* status, int second, cudaStre
 namespace layer {
 
 constexpr int kRowChunk = 32;     // tokens per partial sum of the bias gradient
-constexpr int kPer = 8;           // columns per thread
+constexpr int kPer = 4;           // columns per thread
 
 // dZ = dY act'(Z), rounded once, and the partial sums over kRowChunk tokens of the unrounded values (the bias
-// gradient).  Bound by memory.  A block takes 256 columns x kRowChunk tokens, a thread 8 columns of every eighth token, two
+// gradient).  Bound by memory.  A block takes 128 columns x kRowChunk tokens, a thread 4 columns of every eighth token, two
 // tokens in flight; each of the 8 warps sums its tokens in order.  kWide: rows on 16-byte boundaries.
 template <typename E, bool kWide>
 __global__ void __launch_bounds__(256)
@@ -47,15 +49,14 @@ act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T
     const int64_t t0 = chunk * kRowChunk;
     const int64_t t1 = t0 + kRowChunk < T ? t0 + kRowChunk : T;
     const bool full = kWide && n0 + kPer <= N;
-    constexpr int kWords = kPer * sizeof(E) / 16;
-    union Row { uint4 q[kWords]; E e[kPer]; };
+    using W = std::conditional_t<sizeof(E) == 2, uint2, uint4>;       // the thread's columns of a token
+    union Row { W q; E e[kPer]; };
     float sum[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) sum[j] = 0.0f;
     auto load = [&](int64_t t, Row& g, float (&z)[kPer]) {
         if (full) {
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) g.q[j] = reinterpret_cast<const uint4*>(dY + t * N + n0)[j];
+            g.q = *reinterpret_cast<const W*>(dY + t * N + n0);
             if (act != DTP_ACT_NONE) {
 #pragma unroll
                 for (int j = 0; j < kPer / 4; ++j) {
@@ -87,8 +88,7 @@ act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T
         }
         if (!dZ) return;
         if (full) {
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) reinterpret_cast<uint4*>(dZ + t * ldz + n0)[j] = o.q[j];
+            *reinterpret_cast<W*>(dZ + t * ldz + n0) = o.q;
         } else {
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
@@ -117,7 +117,7 @@ act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T
     for (int j = 0; j < kPer; ++j) red[warp][lane * kPer + j] = sum[j];
     __syncthreads();
     const int n = block * 32 * kPer + threadIdx.x;
-    if (n < N) {
+    if (threadIdx.x < 32 * kPer && n < N) {
         float s = 0.0f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
@@ -136,6 +136,7 @@ bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* 
     const int n = blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (n < N)
+#pragma unroll 8
         for (int64_t c = warp; c < chunks; c += 8) s += partial[c * N + n];
     red[warp][lane] = s;
     __syncthreads();
