@@ -105,6 +105,8 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");    // this CTA runs
 
     constexpr int kBoxes = F::kBoxes;
+    // Before any bounded wait of this launch begins, the launch before it is over: it may run longer than their limit.
+    if (warp != 4) grid_wait();
     if (warp == 4) {
         // -------------------------------------------------------------------- producer: one lane issues
         const bool issuer = elect_one();
@@ -217,7 +219,6 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
         tc_fence_before();
     }
     cluster_sync();
-    grid_wait();            // of this thread's own accesses, long fulfilled
     if (warp == 5) {
         if (*abort_flag) {      // loads and MMAs already issued may still be under way: let them finish
             const uint64_t t0 = globaltimer_ns();

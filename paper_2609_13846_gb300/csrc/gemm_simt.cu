@@ -48,6 +48,7 @@ struct Args {
     int tiles_n;
     int split;
     int wide_a, wide_b;      // rows contiguous and on 16-byte boundaries
+    int* status;             // set: this launch clears it (nothing here can give up)
 };
 
 __device__ __forceinline__ void fma2(uint64_t& d, uint64_t a, uint64_t b) {
@@ -167,6 +168,7 @@ __global__ void __launch_bounds__(Tile<TY>::kThreads, Tile<TY>::kBlocks) gemm_f3
 
     const Copies<TM, S::kThreads> ca(p.A, p.segments, m0, p.M, g.wide_a, false);
     const Copies<TN, S::kThreads> cb(p.B, p.segments, n0, p.N, g.wide_b, kGated);
+    if (g.status && blockIdx.x == 0 && tid == 0) *g.status = DTP_OK;
     auto fetch = [&](int64_t b) {
         if (b < b1) {
             float* st = stages + (b % STAGES) * S::kStage;
@@ -262,11 +264,12 @@ __global__ void __launch_bounds__(Tile<TY>::kThreads, Tile<TY>::kBlocks) gemm_f3
 }
 
 template <int TY>
-static int launch_tiles(const Product& p, int sms, cudaStream_t stream) {
+static int launch_tiles(const Product& p, int* status, int sms, cudaStream_t stream) {
     using S = Tile<TY>;
     const int cols = p.epi.kind == kEpiGated ? TN / 2 : TN;
     Args g;
     g.p = p;
+    g.status = status;
     g.tiles_n = (p.N + cols - 1) / cols;
     const int64_t tiles = (p.M + S::TM - 1) / S::TM * g.tiles_n;
     // blocks per tile: as many as the chip holds of them, with at least 64 k for each
@@ -306,7 +309,8 @@ __global__ void zero_kernel(E* out, int64_t rows, int64_t cols, int64_t ld) {
         out[i / cols * ld + i % cols] = from_f32<E>(0.0f);
 }
 
-int launch(const Product& p, int dtype, cudaStream_t stream) {
+// status: set when this launch clears it.
+int launch(const Product& p, int dtype, int* status, cudaStream_t stream) {
     if (p.K == 0) {
         if (dtype == DTP_BF16)
             zero_kernel<<<256, 256, 0, stream>>>(static_cast<__nv_bfloat16*>(p.epi.out), p.M, p.N, p.epi.ldo);
@@ -321,7 +325,7 @@ int launch(const Product& p, int dtype, cudaStream_t stream) {
     DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
     const int64_t cols = p.epi.kind == kEpiGated ? TN / 2 : TN;
     const int64_t large = (p.M + 127) / 128 * ((p.N + cols - 1) / cols);
-    return large >= 8 * sms ? launch_tiles<16>(p, sms, stream) : launch_tiles<8>(p, sms, stream);
+    return large >= 8 * sms ? launch_tiles<16>(p, status, sms, stream) : launch_tiles<8>(p, status, sms, stream);
 }
 
 }  // namespace simt

@@ -11,7 +11,7 @@
 
 namespace dtp {
 namespace simt {
-int launch(const layer::Product& p, int dtype, cudaStream_t stream);
+int launch(const layer::Product& p, int dtype, int* status, cudaStream_t stream);
 }  // namespace simt
 namespace gtc {
 int launch(const layer::Product& p, int* status, int reset, cudaStream_t stream);
@@ -171,9 +171,13 @@ __global__ void __launch_bounds__(256)
 repitch_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t pitch, uint16_t* __restrict__ dst) {
     grid_wait();
     grid_release();
-    const int64_t total = rows * cols;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll)
-        dst[i / cols * pitch + i % cols] = src[i];
+    const int lane = threadIdx.x & 31;
+    for (int64_t r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8ll) {      // a warp per row
+        const uint16_t* from = src + r * cols;
+        uint16_t* to = dst + r * pitch;
+#pragma unroll 8
+        for (int c = lane; c < cols; c += 32) to[c] = from[c];
+    }
 }
 
 // Pieces of a workspace, in the order in which they are asked for.
@@ -208,8 +212,8 @@ static int aligned_rows(const void* p, int64_t rows, int cols, int dtype, Carver
     }
     void* to = c.take(bytes);
     *out = Rows{to, padded(cols)};
-    const int64_t blocks = (rows * cols + 1023) / 1024;
-    return launch_after(repitch_kernel, blocks < 4096 ? blocks : 4096, stream, static_cast<const uint16_t*>(p), rows, cols,
+    const int64_t blocks = (rows + 7) / 8;
+    return launch_after(repitch_kernel, blocks < 8192 ? blocks : 8192, stream, static_cast<const uint16_t*>(p), rows, cols,
                         padded(cols), static_cast<uint16_t*>(to));
 }
 
@@ -241,7 +245,9 @@ struct Call {
             }
             return gtc::launch(p, status, reset, stream);
         }
-        return simt::launch(p, dtype, stream);
+        if (p.K == 0) return simt::launch(p, dtype, nullptr, stream);
+        fresh = false;
+        return simt::launch(p, dtype, reset ? status : nullptr, stream);
     }
     // calls without such a launch
     int done() {
@@ -268,14 +274,18 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
                    int act, int dtype, void* Y, float* Z, void* workspace, cudaStream_t stream) {
     Call call{dtype, workspace, stream};
     Carver c(workspace);
-    Rows x, w;
-    int st = aligned_rows(X, T, K, dtype, c, stream, &x);
-    if (st == DTP_OK) st = aligned_rows(W, N, K, dtype, c, stream, &w);
-    if (st != DTP_OK) return st;
+    int st = DTP_OK;
     Product p;
-    p.A[0] = by_row(x.p, x.ld);
-    p.B[0] = by_row(w.p, w.ld);
+    p.A[0] = by_row(X, K);
+    p.B[0] = by_row(W, K);
     p.M = T, p.N = N, p.K = K;
+    if (!fews::takes(p, dtype)) {            // which reads rows at any pitch
+        Rows x, w;
+        if ((st = aligned_rows(X, T, K, dtype, c, stream, &x)) != DTP_OK) return st;
+        if ((st = aligned_rows(W, N, K, dtype, c, stream, &w)) != DTP_OK) return st;
+        p.A[0] = by_row(x.p, x.ld);
+        p.B[0] = by_row(w.p, w.ld);
+    }
     p.epi.act = act, p.epi.bias = bias, p.epi.residual = residual, p.epi.out = Y, p.epi.ldo = N, p.epi.Z = Z;
     p.epi.M = T, p.epi.N = N;
     if ((st = call.run(p)) != DTP_OK) return st;
@@ -358,16 +368,22 @@ int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd,
     Call call{dtype, workspace, stream};
     Carver c(workspace);
     void* h = H ? H : c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
-    Rows x, wg, wu, wd;
-    int st = aligned_rows(X, T, d, dtype, c, stream, &x);
-    if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
-    if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
-    if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
-    if (st != DTP_OK) return st;
+    int st = DTP_OK;
     Product p;
-    p.A[0] = by_row(x.p, x.ld);
-    p.B[0] = by_row(wg.p, wg.ld), p.B[1] = by_row(wu.p, wu.ld);
+    p.A[0] = by_row(X, d);
+    p.B[0] = by_row(Wg, d), p.B[1] = by_row(Wu, d);
     p.M = T, p.N = N, p.K = d;
+    Rows wd{Wd, N};
+    if (!fews::takes(p, dtype)) {            // which reads rows at any pitch
+        Rows x, wg, wu;
+        st = aligned_rows(X, T, d, dtype, c, stream, &x);
+        if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
+        if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
+        if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
+        if (st != DTP_OK) return st;
+        p.A[0] = by_row(x.p, x.ld);
+        p.B[0] = by_row(wg.p, wg.ld), p.B[1] = by_row(wu.p, wu.ld);
+    }
     p.epi.kind = kEpiGated, p.epi.act = act, p.epi.out = h, p.epi.ldo = padded(N), p.epi.pre = pre;
     p.epi.M = T, p.epi.N = N;
     if ((st = call.run(p)) != DTP_OK) return st;

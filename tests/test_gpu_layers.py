@@ -307,3 +307,74 @@ def test_refusals():
     with pytest.raises(dtp.DTPError) as e:      # not on a 16-byte boundary
         dtp.gated_ffn(flat[1:1 + 8 * 64].view(8, 64), Wg, Wu, Wd)
     assert e.value.status == dtp.DTP_ERR_ARG
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_gradients_that_are_not_wanted(dtype):
+    """Each gradient may be left out (NULL at the C ABI); the others keep their bits."""
+    T, d, N = 150, 72, 136
+    X, Wg, Wu, Wd = _gated_inputs(T, d, N, dtype, seed=30)
+    dY = _rand(31, T, d, dtype=dtype)
+    _, saved = dtp.gated_ffn(X, Wg, Wu, Wd, save=True)
+    full = dtp.gated_ffn_backward(dY, X, Wg, Wu, Wd, saved)
+    code = dtp.DTP_BF16 if dtype is BF16 else dtp.DTP_F32
+    ws = dtp.gated_ffn_workspace(T, d, N, dtype, DEV, backward=True)
+    stream = torch.cuda.current_stream().cuda_stream
+    for skip in range(4):
+        out = [None if i == skip else torch.empty_like(g) for i, g in enumerate(full)]
+        st = dtp.lib().dtp_gated_ffn_backward(*(t.data_ptr() for t in (dY, X, Wg, Wu, Wd, *saved)), T, d, N, 1, code,
+                                              *(None if t is None else t.data_ptr() for t in out), ws.data_ptr(), ws.numel(),
+                                              stream)
+        assert st == dtp.DTP_OK
+        assert all(t is None or torch.equal(t, g) for t, g in zip(out, full))
+    assert dtp.workspace_status(ws) == dtp.DTP_OK
+    R = _rand(32, T, N, dtype=dtype)
+    dX, dW, db = dtp.linear_backward(R, X, Wg, bias=True)
+    ws = dtp.linear_workspace(T, d, N, dtype, DEV, backward=True)
+    for skip in range(3):
+        out = [None if i == skip else torch.empty_like(g) for i, g in enumerate((dX, dW, db))]
+        st = dtp.lib().dtp_linear_backward(R.data_ptr(), X.data_ptr(), Wg.data_ptr(), None, T, d, N, 0, code,
+                                           *(None if t is None else t.data_ptr() for t in out), ws.data_ptr(), ws.numel(),
+                                           stream)
+        assert st == dtp.DTP_OK
+        assert all(t is None or torch.equal(t, g) for t, g in zip(out, (dX, dW, db)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("T", [1, 2, 5, 40, 200])
+def test_status_word_is_cleared(T, dtype):
+    """An old code in the workspace's status word does not outlive a call that went well."""
+    X, Wg, Wu, Wd = _gated_inputs(T, 136, 264, dtype, seed=33)
+    for backward in (False, True):
+        ws = dtp.gated_ffn_workspace(T, 136, 264, dtype, DEV, backward=backward)
+        _, saved = dtp.gated_ffn(X, Wg, Wu, Wd, save=True)
+        ws[:4].view(torch.int32).fill_(dtp.DTP_ERR_NOT_CONVERGED)
+        if backward:
+            dtp.gated_ffn_backward(X, X, Wg, Wu, Wd, saved, workspace=ws)
+        else:
+            dtp.gated_ffn(X, Wg, Wu, Wd, workspace=ws)
+        assert dtp.workspace_status(ws) == dtp.DTP_OK
+    ws = dtp.linear_workspace(T, 136, 264, dtype, DEV)
+    ws[:4].view(torch.int32).fill_(dtp.DTP_ERR_NOT_CONVERGED)
+    dtp.linear(X, Wg, workspace=ws)
+    assert dtp.workspace_status(ws) == dtp.DTP_OK
+
+
+def test_calls_in_a_row_on_one_workspace():
+    """Launches overlap their predecessors' ends: a chain of calls that read and write the same buffers keeps its order."""
+    X, Wg, Wu, Wd = _gated_inputs(300, 256, 512, BF16, seed=34)
+    small, _, _, _ = _gated_inputs(2, 256, 512, BF16, seed=35)
+    ws = dtp.gated_ffn_workspace(300, 256, 512, BF16, DEV, backward=True)
+    ref = X
+    for _ in range(4):
+        ref = dtp.gated_ffn(ref, Wg, Wu, Wd, ref)
+        torch.cuda.synchronize()
+    refs = dtp.gated_ffn(dtp.gated_ffn(small, Wg, Wu, Wd), Wg, Wu, Wd)
+    a, b = X.clone(), torch.empty_like(X)
+    for _ in range(30):
+        a.copy_(X)
+        for i in range(4):
+            dtp.gated_ffn(a, Wg, Wu, Wd, a, Y=b, workspace=ws)
+            a, b = b, a
+        s = dtp.gated_ffn(dtp.gated_ffn(small, Wg, Wu, Wd, workspace=ws), Wg, Wu, Wd, workspace=ws)
+        assert torch.equal(a, ref) and torch.equal(s, refs)
