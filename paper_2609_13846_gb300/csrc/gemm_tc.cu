@@ -76,11 +76,22 @@ struct Args {
     Epilogue epi;
 };
 
+// `leave`: out of L2 first, for what only the backward pass reads again (Z); the operands stay.
+template <bool kLeave>
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
-                     reinterpret_cast<uint64_t>(map)),
-                 "r"(src), "r"(x), "r"(y)
-                 : "memory");
+    if constexpr (kLeave) {
+        uint64_t policy;
+        asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group.L2::cache_hint [%0, {%2, %3}], [%1], %4;" ::"l"(
+                         reinterpret_cast<uint64_t>(map)),
+                     "r"(src), "r"(x), "r"(y), "l"(policy)
+                     : "memory");
+    } else {
+        asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                         reinterpret_cast<uint64_t>(map)),
+                     "r"(src), "r"(x), "r"(y)
+                     : "memory");
+    }
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
@@ -345,12 +356,12 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
         };
         // a bulk store of the box of 32 rows, from column x
-        auto store_box = [&](const CUtensorMap* map, const uint32_t* w, int x, int row0) {
+        auto store_box = [&](auto leave, const CUtensorMap* map, const uint32_t* w, int x, int row0) {
             stage_box(w);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
-                tma_store_2d(map, smem_u32(stg), x, row0);
+                tma_store_2d<decltype(leave)::value>(map, smem_u32(stg), x, row0);
                 bulk_commit();
             }
         };
@@ -372,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         // 32 columns of the box's rows, from column n
         auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int row0) {
             if (p.direct) store_elements(static_cast<__nv_bfloat16*>(out), e.ldo, w, n, row0);
-            else store_box(map, w, n, row0);
+            else store_box(std::false_type(), map, w, n, row0);
         };
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (int u = first + set * workers; u < p.units; u += 2 * workers, unit_count += 2) {
@@ -462,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
                                 if (p.direct_z) store_elements(e.Z, e.N, w, n + 16 * q, row0);
-                                else store_box(&p.z, w, n + 16 * q, row0);
+                                else store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
                             }
                         }
                     }
@@ -512,10 +523,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 float* to = pre + (4 * q + i) * kPreTile * 4;
-                                *reinterpret_cast<float4*>(to) =
-                                    make_float4(g[4 * i], g[4 * i + 1], g[4 * i + 2], g[4 * i + 3]);
-                                *reinterpret_cast<float4*>(to + kPreTile * kPreTile) =
-                                    make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                                __stcs(reinterpret_cast<float4*>(to),
+                                       make_float4(g[4 * i], g[4 * i + 1], g[4 * i + 2], g[4 * i + 3]));
+                                __stcs(reinterpret_cast<float4*>(to + kPreTile * kPreTile),
+                                       make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
                             }
                         }
                         act_values<true>(e.act, g);

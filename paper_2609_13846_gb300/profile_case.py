@@ -11,6 +11,10 @@ times, with nothing else in between, so that an ncu capture with
     python -m paper_2609_13846_gb300.profile_case --what gather --workload qwen3_0.6b_model --layers 28
     python -m paper_2609_13846_gb300.profile_case --what apply --workload qwen3_0.6b_model --layers 28
     python -m paper_2609_13846_gb300.profile_case --what add --workload qwen3_0.6b_layer
+    python -m paper_2609_13846_gb300.profile_case --what ffn --workload llama3.1_8b_layer --T 32
+    python -m paper_2609_13846_gb300.profile_case --what ffn_train --workload qwen3_0.6b_layer
+    python -m paper_2609_13846_gb300.profile_case --what linear_train --workload qwen3_0.6b_layer --T 8192
+    python -m paper_2609_13846_gb300.profile_case --what clip --workload qwen3_0.6b_model --layers 4
 """
 from __future__ import annotations
 
@@ -23,7 +27,8 @@ from . import ablation, dtp, synth
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--what", choices=["affinity", "search", "producer", "gather", "apply", "add"], default="affinity")
+    ap.add_argument("--what", choices=["affinity", "search", "producer", "gather", "apply", "add",
+                                           "ffn", "ffn_train", "linear_train", "clip"], default="affinity")
     ap.add_argument("--qrow", type=int, default=1, help="producer: query heads per output row")
     ap.add_argument("--workload", default="qwen3_0.6b_layer")
     ap.add_argument("--T", type=int, default=None, help="token count (default: the workload's)")
@@ -54,6 +59,36 @@ def main():
             dtp.affinity_add_accumulate(L["C"], L["W_gate"], L["W_up"], A_add=A)
         torch.cuda.synchronize()
         print(f"add {args.workload} T={T}: {args.launches} launches, A sum {float(A.sum()):.6e}")
+    elif args.what in ("ffn", "ffn_train", "linear_train"):
+        dt = torch.float32 if args.dtype == "f32" else torch.bfloat16
+        T = args.T or w.T
+        L = synth.make_layer(w.d, 1, w.N, T, w.layer_seed(0), dtype="f32" if args.dtype == "f32" else "bf16", device=dev,
+                             with_down=True)
+        X, Wg, Wu, Wd = (L[k] for k in ("X", "W_gate", "W_up", "W_down"))
+        ws = dtp.gated_ffn_workspace(T, w.d, w.N, dt, dev, backward=True)
+        dY = torch.randn_like(X)
+        b, dZ = torch.randn(w.N, device=dev).to(dt), torch.randn((T, w.N), device=dev).to(dt)
+        ws_l = dtp.linear_workspace(T, w.d, w.N, dt, dev, backward=True)
+        torch.cuda.synchronize()
+        for _ in range(args.launches):
+            if args.what == "linear_train":
+                Y, Z = dtp.linear(X, Wg, b, activation="silu", save=True, workspace=ws_l)
+                dtp.linear_backward(dZ, X, Wg, Z, activation="silu", bias=True, workspace=ws_l)
+                continue
+            Y, saved = dtp.gated_ffn(X, Wg, Wu, Wd, X, save=True, workspace=ws)
+            if args.what == "ffn_train":
+                dtp.gated_ffn_backward(dY, X, Wg, Wu, Wd, saved, workspace=ws)
+        torch.cuda.synchronize()
+        print(f"{args.what} {args.workload} T={T}: {args.launches} launches, Y sum {float(Y.double().sum()):.6e}")
+    elif args.what == "clip":
+        W = synth.make_dense_weights(args.layers, w.d, w.G * w.q_per_group, w.G, w.head_dim, w.N, w.seed, device=dev)
+        g = [t for v in W.values() for t in v]
+        out = [torch.empty_like(t) for t in g]
+        torch.cuda.synchronize()
+        for _ in range(args.launches):
+            n = dtp.clip_grad_norm(g, 1.0, out=out)
+        torch.cuda.synchronize()
+        print(f"clip {len(g)} tensors, {sum(t.numel() for t in g)} elements: {args.launches} launches, norm {float(n):.6e}")
     elif args.what == "producer":
         T = args.T or w.T
         P = synth.make_attention_inputs(T, w.d, w.G * w.q_per_group, w.head_dim, w.seed, device=dev)
