@@ -59,18 +59,26 @@ struct Form {
     static constexpr size_t kSmemBytes = 1024 + STAGES * kStageBytes + kEpiWarps * kStageOut + 512;
 };
 
+// A launch's products: one (of one or two segments, or with a second B or output), or up to three of the same K and
+// operand orders whose tiles follow one another, so that the last round of one is filled by the next.
+constexpr int kBatch = 3;
 struct Args {
-    CUtensorMap a[2], b[2], out, out2, z;
+    CUtensorMap a[kBatch], b[kBatch], out[kBatch], z;     // by product; by segment, or gate and up, in a single one
     int segments;
     int KB;               // k blocks of 64 per segment
     int a_mn, b_mn;       // operand stored with its rows contiguous
-    int tiles_m, tiles_n; // per CTA or pair
+    int tiles_m[kBatch], tiles_n[kBatch];     // per CTA or pair
+    int last[kBatch];     // tiles of the products up to this one
+    int64_t M[kBatch];
+    int N[kBatch];
+    int64_t ldo[kBatch];
+    void* dst[kBatch];
+    int direct[kBatch];   // out rows are not on 16-byte boundaries: plain stores
     int unit0, units;     // this launch's tiles: unit0 .. units - 1
     int split;            // pairs per tile (kSplit)
     int early;            // kSplit: begun while the launch before it, of the same product's other tiles, still runs
     uint32_t idesc;
-    int direct;           // out rows are not on 16-byte boundaries: plain stores
-    int direct_z;         // the same of Z
+    int direct_z;         // rows of Z are not on 16-byte boundaries
     int reset;            // this launch clears the status word
     int* status;
     Epilogue epi;
@@ -109,11 +117,13 @@ __device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
 // Units of a persistent worker: row tiles in groups of 8, column tile by column tile within a group, so that the
 // tiles in flight share their rows and columns in L2.
 constexpr int kGroupM = 8;
-__device__ __forceinline__ void decode(const Args& p, int u, int& tm, int& tn) {
-    const unsigned per = static_cast<unsigned>(kGroupM) * p.tiles_n;
+__device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, int& tn) {
+    job = (u >= p.last[0]) + (u >= p.last[1]);
+    if (job) u -= p.last[job - 1];
+    const unsigned per = static_cast<unsigned>(kGroupM) * p.tiles_n[job];
     const unsigned g = static_cast<unsigned>(u) / per, rest = static_cast<unsigned>(u) - g * per;
     const int m0 = static_cast<int>(g) * kGroupM;
-    const unsigned gm = p.tiles_m - m0 < kGroupM ? p.tiles_m - m0 : kGroupM;
+    const unsigned gm = p.tiles_m[job] - m0 < kGroupM ? p.tiles_m[job] - m0 : kGroupM;
     tn = static_cast<int>(rest / gm);
     tm = m0 + static_cast<int>(rest % gm);
 }
@@ -171,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         fence_mbar_init();
         tma_prefetch_desc(&p.a[0]);
         tma_prefetch_desc(&p.b[0]);
-        if (!p.direct) tma_prefetch_desc(&p.out);
+        if (!p.direct[0]) tma_prefetch_desc(&p.out[0]);
     }
     if (warp == 1) {
         if constexpr (kPair) {
@@ -206,8 +216,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         uint32_t phase = 0;
         bool ok = true;
         for (int u = first; ok && u < p.units; u += workers) {
-            int tm, tn;
-            decode(p, u, tm, tn);
+            int job, tm, tn;
+            decode(p, u, job, tm, tn);
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
             for (int kb = kb0; kb < kb1; kb += kBoxes) {
@@ -220,23 +230,23 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     for (int x = 0; x < kBoxes; ++x) {
                         if (x >= boxes) break;
                         const uint32_t sa = tiles0 + stage * kStageBytes + x * F::kBoxBytes, sb = sa + kTileA;
-                        const int seg = kb + x >= p.KB;
+                        const int seg = kb + x >= p.KB, at = seg + job;
                         const int k0 = (kb + x - seg * p.KB) * BK;
                         auto load = [&](uint32_t dst, const CUtensorMap* map, int cx, int cy) {
                             if constexpr (kPair) tma_load_2d_pair(dst, map, fb, cx, cy);
                             else tma_load_2d(dst, map, fb, cx, cy);
                         };
                         if (p.a_mn) {
-                            load(sa, &p.a[seg], m0, k0);
-                            load(sa + kTileA / 2, &p.a[seg], m0 + 64, k0);
+                            load(sa, &p.a[at], m0, k0);
+                            load(sa + kTileA / 2, &p.a[at], m0 + 64, k0);
                         } else {
-                            load(sa, &p.a[seg], k0, m0);
+                            load(sa, &p.a[at], k0, m0);
                         }
                         // rows of B: halves of BN / 2, which are gate and up in the gated kind
 #pragma unroll
                         for (int h = 0; h < F::kRowsB / (BN / 2); ++h) {
                             const int half = kPair ? static_cast<int>(rank) : h;
-                            const CUtensorMap* map = KIND == kEpiGated ? &p.b[half] : &p.b[seg];
+                            const CUtensorMap* map = KIND == kEpiGated ? &p.b[half] : &p.b[at];
                             const int r0 = KIND == kEpiGated ? n0 : n0 + half * (BN / 2);
                             const uint32_t dst = sb + h * (BN / 2) * BK * 2;
                             if (p.b_mn) {
@@ -344,7 +354,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         const int set = (warp - kEpiWarp0) >> 3;
         const uint32_t lane_base = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         uint8_t* stg = staging + (warp - kEpiWarp0) * kStageOut;
-        const bool wide = (e.ldo & 7) == 0;
+        // of the tile's product
+        int64_t M = p.M[0], ldo = p.ldo[0];
+        int N = p.N[0], job = 0;
+        const bool wide = (p.ldo[0] & 7) == 0;
         // 64 bytes of every lane's row into the staging buffer, once the store issued from it has read it
         auto stage_box = [&](const uint32_t* w) {
             if (lane == 0) bulk_wait_read0();
@@ -375,20 +388,21 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll 4
             for (int r = lane / kPer; r < 32; r += 32 / kPer) {
                 const int at = r * 64 + ((((c * sizeof(V)) >> 4) ^ ((r >> 1) & 3)) << 4) + ((c * sizeof(V)) & 15);
-                if (row0 + r < e.M && x + c < e.N)
+                if (row0 + r < M && x + c < N)
                     out[(static_cast<int64_t>(row0) + r) * ld + x + c] = *reinterpret_cast<const V*>(stg + at);
             }
             __syncwarp();
         };
-        // 32 columns of the box's rows, from column n
-        auto store32 = [&](const CUtensorMap* map, void* out, const uint32_t (&w)[16], int n, int row0) {
-            if (p.direct) store_elements(static_cast<__nv_bfloat16*>(out), e.ldo, w, n, row0);
-            else store_box(std::false_type(), map, w, n, row0);
+        // 32 columns of the box's rows, from column n, into output i
+        auto store32 = [&](int i, void* out, const uint32_t (&w)[16], int n, int row0) {
+            if (p.direct[job]) store_elements(static_cast<__nv_bfloat16*>(out), ldo, w, n, row0);
+            else store_box(std::false_type(), &p.out[i], w, n, row0);
         };
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (int u = first + set * workers; u < p.units; u += 2 * workers, unit_count += 2) {
             int tm, tn;
-            decode(p, u, tm, tn);
+            decode(p, u, job, tm, tn);
+            M = p.M[job], N = p.N[job], ldo = p.ldo[job];
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
             const uint32_t buf = unit_count & 1u;
@@ -400,10 +414,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             uint32_t bq = 0;
             auto fetch = [&](int c) {
                 const int n = base + c;
-                if (c >= width || n >= e.N || row0 >= e.M) return;
+                if (c >= width || n >= N || row0 >= M) return;
                 if (e.bias) {
                     const __nv_bfloat16* b = reinterpret_cast<const __nv_bfloat16*>(e.bias) + n + 2 * (lane & 15);
-                    const int left = e.N - n - 2 * (lane & 15);
+                    const int left = N - n - 2 * (lane & 15);
                     bq = left >= 2 ? *reinterpret_cast<const uint32_t*>(b)
                                    : left == 1 ? *reinterpret_cast<const uint16_t*>(b) : 0u;
                 }
@@ -413,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int64_t row = static_cast<int64_t>(row0) + (lane >> 2) + 8 * i;
-                        rq[i] = row < e.M && col < e.N ? *reinterpret_cast<const uint4*>(r + row * e.ldo)
+                        rq[i] = row < M && col < N ? *reinterpret_cast<const uint4*>(r + row * ldo)
                                                        : make_uint4(0, 0, 0, 0);
                     }
                 }
@@ -450,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll 1
             for (int c = 32 * half; c < width; c += 64) {
                 const int n = base + c;
-                if (n >= e.N || row0 >= e.M) continue;     // box entirely outside (warp-uniform)
+                if (n >= N || row0 >= M) continue;     // box entirely outside (warp-uniform)
                 uint32_t w[16];
                 if constexpr (KIND == kEpiLinear) {
                     float v[32];
@@ -469,10 +483,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     if (e.Z) {
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
-                            if (n + 16 * q < e.N) {
+                            if (n + 16 * q < N) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
-                                if (p.direct_z) store_elements(e.Z, e.N, w, n + 16 * q, row0);
+                                if (p.direct_z) store_elements(e.Z, static_cast<int64_t>(N), w, n + 16 * q, row0);
                                 else store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
                             }
                         }
@@ -501,18 +515,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             }
                         }
                         __syncwarp();
-                    } else if (e.residual && m < e.M) {
-                        const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + m * e.ldo;
+                    } else if (e.residual && m < M) {
+                        const __nv_bfloat16* r = reinterpret_cast<const __nv_bfloat16*>(e.residual) + m * ldo;
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (n + i < e.N) v[i] += to_f32(r[n + i]);
+                            if (n + i < N) v[i] += to_f32(r[n + i]);
                     }
                     fetch(c + 64);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                    store32(&p.out, e.out, w, n, row0);
+                    store32(job, p.dst[job], w, n, row0);
                 } else if constexpr (KIND == kEpiGated) {
-                    float* pre = e.pre ? e.pre + pre_index(m, n, e.N) : nullptr;
+                    float* pre = e.pre ? e.pre + pre_index(m, n, N) : nullptr;
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         float g[16], v[16];
@@ -534,9 +548,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         for (int i = 0; i < 8; ++i)
                             w[8 * q + i] = pack_bf16(g[2 * i] * v[2 * i], g[2 * i + 1] * v[2 * i + 1]);
                     }
-                    store32(&p.out, e.out, w, n, row0);
+                    store32(job, p.dst[job], w, n, row0);
                 } else {
-                    const float* pre = e.pre + pre_index(m, n, e.N);
+                    const float* pre = e.pre + pre_index(m, n, N);
                     uint32_t w2[16];
                     float dh[32];
                     get16(0, c, dh);
@@ -555,8 +569,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         w2[2 * q] = pack_bf16(d[0] * value[0], d[1] * value[1]);
                         w2[2 * q + 1] = pack_bf16(d[2] * value[2], d[3] * value[3]);
                     }
-                    store32(&p.out, e.out, w, n, row0);
-                    store32(&p.out2, e.out2, w2, n, row0);
+                    store32(job, p.dst[job], w, n, row0);
+                    store32(1, e.out2, w2, n, row0);
                 }
             }
             if constexpr (!kSplit) {
@@ -628,29 +642,42 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
                        int64_t most, cudaStream_t stream) {
     using F = Form<kPair, BN>;
     const bool gated = p.epi.kind == kEpiGated;
+    const int rows = kPair ? 2 * BM : BM, cols = gated ? BN / 2 : BN;
     Args a;
     for (int s = 0; s < 2; ++s) {            // only the maps that the kernel reads: an encoding is host time
         if (s < p.segments && !map_operand(&a.a[s], p.A[s], p.M, p.K, BM)) return DTP_ERR_CUDA;
         if ((s < p.segments || gated) && !map_operand(&a.b[s], p.B[s], p.N, p.K, BN / 2)) return DTP_ERR_CUDA;
     }
-    a.direct = (p.epi.ldo & 7) != 0;
-    if (!a.direct) {
-        if (!map_2d(&a.out, p.epi.out, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
-        if (p.epi.out2 && !map_2d(&a.out2, p.epi.out2, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+    int64_t all = 0;
+    for (int j = 0; j < kBatch; ++j) {
+        a.last[j] = 0x7FFFFFFF;
+        if (j >= p.batch) continue;
+        const Also& x = p.also[j > 0 ? j - 1 : 0];
+        if (j > 0 && (!map_operand(&a.a[j], x.A, x.M, p.K, BM) || !map_operand(&a.b[j], x.B, x.N, p.K, BN / 2)))
             return DTP_ERR_CUDA;
+        a.M[j] = j > 0 ? x.M : p.M;
+        a.N[j] = j > 0 ? x.N : p.N;
+        a.ldo[j] = j > 0 ? x.ldo : p.epi.ldo;
+        a.dst[j] = j > 0 ? x.out : p.epi.out;
+        a.direct[j] = (a.ldo[j] & 7) != 0;
+        if (!a.direct[j] && !map_2d(&a.out[j], a.dst[j], a.N[j], a.M[j], a.ldo[j], 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+            return DTP_ERR_CUDA;
+        a.tiles_m[j] = static_cast<int>((a.M[j] + rows - 1) / rows);
+        a.tiles_n[j] = (a.N[j] + cols - 1) / cols;
+        all += static_cast<int64_t>(a.tiles_m[j]) * a.tiles_n[j];
+        if (all > 0x3FFFFFFF) return DTP_ERR_UNSUPPORTED;
+        if (j + 1 < p.batch) a.last[j] = static_cast<int>(all);
     }
+    if (p.epi.out2 && !a.direct[0] &&
+        !map_2d(&a.out[1], p.epi.out2, p.N, p.M, p.epi.ldo, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
+        return DTP_ERR_CUDA;
     a.direct_z = (p.N & 3) != 0;
     if (p.epi.Z && !a.direct_z && !map_2d(&a.z, p.epi.Z, p.N, p.M, p.N, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B, true))
         return DTP_ERR_CUDA;
-    const int rows = kPair ? 2 * BM : BM, cols = gated ? BN / 2 : BN;
     a.segments = p.segments;
     a.KB = static_cast<int>((p.K + BK - 1) / BK);
     a.a_mn = p.A[0].ks != 1;
     a.b_mn = p.B[0].ks != 1;
-    a.tiles_m = static_cast<int>((p.M + rows - 1) / rows);
-    a.tiles_n = (p.N + cols - 1) / cols;
-    const int64_t all = static_cast<int64_t>(a.tiles_m) * a.tiles_n;
-    if (all > 0x3FFFFFFF) return DTP_ERR_UNSUPPORTED;
     a.unit0 = static_cast<int>(unit0);
     a.units = static_cast<int>(count < 0 ? all : unit0 + count);
     a.split = split;
@@ -732,7 +759,10 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
     const bool gated = p.epi.kind == kEpiGated;
     auto tiles = [&](int rows, int bn) {
         const int cols = gated ? bn / 2 : bn;
-        return (p.M + rows - 1) / rows * ((p.N + cols - 1) / cols);
+        int64_t n = (p.M + rows - 1) / rows * ((p.N + cols - 1) / cols);
+        for (int j = 0; j + 1 < p.batch; ++j)
+            n += (p.also[j].M + rows - 1) / rows * ((p.also[j].N + cols - 1) / cols);
+        return n;
     };
     auto whole = [&](int64_t n, int64_t workers, int clocks, int fixed) {
         const int64_t round = kb * clocks > fixed / 3 ? kb * clocks : fixed / 3;
@@ -752,7 +782,7 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
     };
     take(whole(tiles(2 * BM, 128), pairs, 400, 7000), 128, 1, 0);
     if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad) take(whole(tiles(2 * BM, 64), pairs, 280, 5500), 64, 1, 0);
-    if (p.M <= BM) take(whole(tiles(BM, 128), sms, 500, 7000), 0, 1, 0);
+    if (p.M <= BM && p.batch == 1) take(whole(tiles(BM, 128), sms, 500, 7000), 0, 1, 0);
     const int64_t left = n256 % pairs;
     for (int split : {2, 4}) {
         for (int bn : {256, 128})

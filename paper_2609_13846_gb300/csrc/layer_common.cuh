@@ -229,8 +229,18 @@ struct Mat {
 
 // sum over the segments s of A_s [M, K] B_s [N, K]^T, then the epilogue.  kEpiGated: one segment, whose
 // second accumulator takes B[1].
+// `also`: up to two more products of the same K and operand orders, without an epilogue, for the same launch (bf16 only).
+struct Also {
+    Mat A, B;
+    int64_t M = 0;
+    int N = 0;
+    void* out = nullptr;
+    int64_t ldo = 0;
+};
 struct Product {
     int segments = 1;
+    int batch = 1;
+    Also also[2];
     Mat A[2], B[2];
     int64_t M = 0;
     int N = 0;

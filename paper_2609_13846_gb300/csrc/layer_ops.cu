@@ -429,18 +429,28 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
         p.epi.out = dX, p.epi.ldo = d, p.epi.M = T, p.epi.N = d;
         if ((st = call.run(p)) != DTP_OK) return st;
     }
+    // the weights' gradients share their K: one launch for all that are wanted (bf16), so that their tiles fill the rounds
+    Also w[3];
+    int count = 0;
     auto weight = [&](const void* a, int64_t lda, int64_t rows, const void* b, int64_t ldb, int cols, void* out) {
-        if (!out) return static_cast<int>(DTP_OK);
-        Product p;
-        p.A[0] = by_col(a, lda);
-        p.B[0] = by_col(b, ldb);
-        p.M = rows, p.N = cols, p.K = T;
-        p.epi.out = out, p.epi.ldo = cols, p.epi.M = rows, p.epi.N = cols;
-        return call.run(p);
+        if (out) w[count++] = Also{by_col(a, lda), by_col(b, ldb), rows, cols, out, cols};
     };
-    if ((st = weight(dg, ld, N, x.p, x.ld, d, dWg)) != DTP_OK) return st;
-    if ((st = weight(du, ld, N, x.p, x.ld, d, dWu)) != DTP_OK) return st;
-    if ((st = weight(dy.p, dy.ld, d, H, ld, N, dWd)) != DTP_OK) return st;
+    weight(dg, ld, N, x.p, x.ld, d, dWg);
+    weight(du, ld, N, x.p, x.ld, d, dWu);
+    weight(dy.p, dy.ld, d, H, ld, N, dWd);
+    const bool together = dtype == DTP_BF16 && T > 0;
+    for (int i = 0; i < count; i += together ? count : 1) {
+        Product p;
+        p.A[0] = w[i].A;
+        p.B[0] = w[i].B;
+        p.M = w[i].M, p.N = w[i].N, p.K = T;
+        p.epi.out = w[i].out, p.epi.ldo = w[i].ldo, p.epi.M = w[i].M, p.epi.N = w[i].N;
+        if (together) {
+            p.batch = count;
+            for (int j = 1; j < count; ++j) p.also[j - 1] = w[j];
+        }
+        if ((st = call.run(p)) != DTP_OK) return st;
+    }
     return call.done();
 }
 
