@@ -550,27 +550,47 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     }
                     store32(job, p.dst[job], w, n, row0);
                 } else {
+                    // 16 columns at a time with all their saved values in flight (a row's four columns after the other: 192
+                    // us for 1024 x 3072 on 16384 tokens, the loads' latency 32 times a tile; so 144); dG goes to the staging buffer
+                    // as it is computed, dU waits in registers.  Both have rows on 16-byte boundaries.
                     const float* pre = e.pre + pre_index(m, n, N);
                     uint32_t w2[16];
-                    float dh[32];
-                    get16(0, c, dh);
-                    get16(0, c + 16, dh + 16);
-                    got();
+                    if (lane == 0) bulk_wait_read0();
+                    __syncwarp();
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        const float* from = pre + q * kPreTile * 4;
-                        const float4 g = __ldcs(reinterpret_cast<const float4*>(from));
-                        const float4 v = __ldcs(reinterpret_cast<const float4*>(from + kPreTile * kPreTile));
-                        float value[4] = {g.x, g.y, g.z, g.w}, slope[4];
-                        act_both4<true>(e.act, value, slope);
-                        const float* d = dh + 4 * q;
-                        w[2 * q] = pack_bf16(d[0] * v.x * slope[0], d[1] * v.y * slope[1]);
-                        w[2 * q + 1] = pack_bf16(d[2] * v.z * slope[2], d[3] * v.w * slope[3]);
-                        w2[2 * q] = pack_bf16(d[0] * value[0], d[1] * value[1]);
-                        w2[2 * q + 1] = pack_bf16(d[2] * value[2], d[3] * value[3]);
+                    for (int q = 0; q < 2; ++q) {
+                        float4 g[4], v[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float* from = pre + (4 * q + i) * kPreTile * 4;
+                            g[i] = __ldcs(reinterpret_cast<const float4*>(from));
+                            v[i] = __ldcs(reinterpret_cast<const float4*>(from + kPreTile * kPreTile));
+                        }
+                        float dh[16];
+                        get16(0, c + 16 * q, dh);
+                        got();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float value[4] = {g[i].x, g[i].y, g[i].z, g[i].w}, slope[4];
+                            act_both4<true>(e.act, value, slope);
+                            const float* d = dh + 4 * i;
+                            w[2 * i] = pack_bf16(d[0] * v[i].x * slope[0], d[1] * v[i].y * slope[1]);
+                            w[2 * i + 1] = pack_bf16(d[2] * v[i].z * slope[2], d[3] * v[i].w * slope[3]);
+                            w2[8 * q + 2 * i] = pack_bf16(d[0] * value[0], d[1] * value[1]);
+                            w2[8 * q + 2 * i + 1] = pack_bf16(d[2] * value[2], d[3] * value[3]);
+                        }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            *reinterpret_cast<uint4*>(stg + lane * 64 + (((2 * q + h) ^ ((lane >> 1) & 3)) << 4)) =
+                                make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
                     }
-                    store32(job, p.dst[job], w, n, row0);
-                    store32(1, e.out2, w2, n, row0);
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        tma_store_2d<false>(&p.out[0], smem_u32(stg), n, row0);
+                        bulk_commit();
+                    }
+                    store_box(std::false_type(), &p.out[1], w2, n, row0);
                 }
             }
             if constexpr (!kSplit) {
