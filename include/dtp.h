@@ -629,7 +629,9 @@ typedef enum {
  *   act      a dtp_activation
  *   Y        [T, N]   out
  *   Z        [T, N] fp32 out or NULL: the pre-activations that
- *            dtp_linear_backward needs when act is not DTP_ACT_NONE
+ *            dtp_linear_backward needs when act is not DTP_ACT_NONE.  With
+ *            DTP_ACT_RELU and bf16 its values near zero are summed again in 64
+ *            bits: the gradient's mask is the exact sums' sign
  * T == 0 returns DTP_OK.  Workspace from dtp_linear_workspace_size (backward:
  * nonzero for the size that both directions need).  Asynchronous.
  */

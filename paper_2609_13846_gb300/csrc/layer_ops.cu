@@ -165,6 +165,74 @@ static int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t strea
     return DTP_OK;
 }
 
+// relu has a kink where its gradient jumps, and the tensor cores' sums are off by about 2^-26 of the running sum for every 16 k
+// (they cut the sum off instead of rounding it): a pre-activation nearer to zero than that may come out on the wrong side.  The
+// saved values within 2^-15 (more for sums of more than 16384 terms) of their neighbourhood's largest, more than ten times
+// those sums' error, are summed again: the products are exact in fp32, each lane carries its additions' errors along, and the
+// lanes meet in fp64, so that the backward pass uses the sign of the exact sum.  Few of them: a warp reads 128 columns of four
+// tokens and takes its lanes' candidates one by one.  Exact zeros stay: the gradient there is zero.  Bound by reading Z once.
+__global__ void __launch_bounds__(256)
+relu_sign_kernel(const __nv_bfloat16* __restrict__ X, int64_t ldx, const __nv_bfloat16* __restrict__ W, int64_t ldw,
+                 const __nv_bfloat16* __restrict__ bias, int64_t T, int K, int N, float* __restrict__ Z) {
+    grid_wait();
+    grid_release();
+    const int lane = threadIdx.x & 31;
+    const int per_row = (N + 127) / 128;
+    const int64_t pieces = (T + 3) / 4 * per_row;
+    const float share = 3.0517578125e-5f * (1.0f + K * (1.0f / 16384.0f));
+    const bool wide = (ldx & 7) == 0 && (ldw & 7) == 0;      // rows on 16-byte boundaries
+    for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < pieces; i += gridDim.x * 8ll) {
+        const int64_t g = i / per_row, t0 = g * 4;
+        const int n0 = static_cast<int>(i - g * per_row) * 128;
+        float z[16], top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const int n = n0 + 32 * (j & 3) + lane;
+            const int64_t t = t0 + (j >> 2);
+            z[j] = n < N && t < T ? Z[t * N + n] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(z[j]));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        unsigned mine = 0;                                   // the lane's candidates
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mine |= (z[j] != 0.0f && fabsf(z[j]) < share * top ? 1u : 0u) << j;
+        if (!__any_sync(0xFFFFFFFFu, mine != 0)) continue;
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) {
+            const int64_t t = t0 + (j >> 2);
+            unsigned todo = __ballot_sync(0xFFFFFFFFu, (mine >> j) & 1u);
+            while (todo) {
+                const int at = __ffs(todo) - 1, n = n0 + 32 * (j & 3) + at;
+                todo &= todo - 1;
+                const __nv_bfloat16 *x = X + t * ldx, *w = W + n * ldw;
+                float hi = 0.0f, lo = 0.0f;
+                auto add = [&](float p) {                    // hi + lo is the sum: the error of each addition, exactly
+                    const float s = hi + p, b = s - hi;
+                    lo += (hi - (s - b)) + (p - b);
+                    hi = s;
+                };
+                const int words = wide ? K / 8 : 0;
+                for (int k = lane; k < words; k += 32) {
+                    const uint4 a = reinterpret_cast<const uint4*>(x)[k], c = reinterpret_cast<const uint4*>(w)[k];
+                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        add(__uint_as_float(aw[q] << 16) * __uint_as_float(cw[q] << 16));
+                        add(__uint_as_float(aw[q] & 0xFFFF0000u) * __uint_as_float(cw[q] & 0xFFFF0000u));
+                    }
+                }
+                for (int k = 8 * words + lane; k < K; k += 32) add(to_f32(x[k]) * to_f32(w[k]));
+                double sum = static_cast<double>(hi) + static_cast<double>(lo);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                if (lane == at) Z[t * N + n] = static_cast<float>(sum + (bias ? static_cast<double>(to_f32(bias[n])) : 0.0));
+            }
+        }
+    }
+}
+
 // Rows copied to a pitch of whole 16 bytes, for the tensor cores' loads; the pitch's spare entries stay unwritten
 // (the loads' extents end before them).
 __global__ void __launch_bounds__(256)
@@ -289,6 +357,13 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
     p.epi.act = act, p.epi.bias = bias, p.epi.residual = residual, p.epi.out = Y, p.epi.ldo = N, p.epi.Z = Z;
     p.epi.M = T, p.epi.N = N;
     if ((st = call.run(p)) != DTP_OK) return st;
+    if (dtype == DTP_BF16 && act == DTP_ACT_RELU && Z) {
+        const int64_t blocks = ((T + 3) / 4 * ((N + 127) / 128) + 7) / 8;
+        st = launch_after(relu_sign_kernel, blocks < 8192 ? blocks : 8192, stream,
+                          static_cast<const __nv_bfloat16*>(p.A[0].p), p.A[0].rs, static_cast<const __nv_bfloat16*>(p.B[0].p),
+                          p.B[0].rs, static_cast<const __nv_bfloat16*>(bias), T, K, N, Z);
+        if (st != DTP_OK) return st;
+    }
     return call.done();
 }
 

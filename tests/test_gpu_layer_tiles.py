@@ -108,3 +108,18 @@ def test_f32_few_tokens_and_long_sums(T, K, N):
     terms = X.double().abs() @ W.double().t().abs() + b.double().abs()
     # K sequential additions at the very most: K 2^-24 of the terms; a hundredth of it is held (sqrt(K) and less in practice)
     assert ((Y.double() - ref).abs() <= max(4, K / 100) * 2.0 ** -24 * terms).all()
+
+
+@pytest.mark.parametrize("T,K,N,bias", [(600, 4096, 520, True), (40, 2048, 1001, False), (1500, 777, 300, True), (2, 512, 999, True)])
+def test_relu_mask_is_the_exact_signs(T, K, N, bias):
+    """Saved pre-activations have the sign of the exact sum, outlier channels and all.  Left out is what the kernel's own
+    compensated sums leave open: K / 32 additions of errors of 2^-24 of 2^-24 of the terms, below 2^-40 of them."""
+    X, W = _rand(1, T, K), _rand(2, N, K, std=0.02)
+    X[:, :4] *= 20
+    b = _rand(3, N, std=0.5) if bias else None
+    _, Z = dtp.linear(X, W, b, activation="relu", save=True)
+    z = X.double() @ W.double().t() + (b.double() if bias else 0)
+    size = X.double().abs() @ W.double().t().abs() + (b.double().abs() if bias else 0)
+    clear = z.abs() > 2.0 ** -40 * size
+    assert torch.equal((Z > 0) & clear, (z > 0) & clear)
+    assert ((Z.double() - z).abs() <= 2.0 ** -16 * size).all()
