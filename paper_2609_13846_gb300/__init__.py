@@ -9,7 +9,11 @@ Sharding for Delayed Tensor Parallelism" (arXiv 2609.13846), Sec. 3:
 * the coordinate-ascent layout optimiser (exact balanced neuron assignment,
   exhaustive labelled head-partition search, exact integer objective).
 
-Both live in the C-ABI library ``libdtp.so`` (declared in ``include/dtp.h``);
+Beside them are the layers that a layout permutes, run forward and backward
+(Sec. 4): a linear layer with its epilogue, the gated feed-forward block, and
+gradient clipping; :mod:`paper_2609_13846_gb300.distill` runs them together.
+
+All of it lives in the C-ABI library ``libdtp.so`` (declared in ``include/dtp.h``);
 :mod:`paper_2609_13846_gb300.dtp` is the thin ctypes binding.  Import of the
 binding is lazy so that :mod:`paper_2609_13846_gb300.synth` (seeded inputs)
 can be used without the compiled library.
