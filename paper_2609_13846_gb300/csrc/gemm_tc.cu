@@ -117,9 +117,13 @@ __device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
 // Units of a persistent worker: row tiles in groups of 8, column tile by column tile within a group, so that the
 // tiles in flight share their rows and columns in L2.
 constexpr int kGroupM = 8;
+template <int JOBS>
 __device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, int& tn) {
-    job = (u >= p.last[0]) + (u >= p.last[1]);
-    if (job) u -= p.last[job - 1];
+    job = 0;
+    if constexpr (JOBS > 1) {
+        job = (u >= p.last[0]) + (u >= p.last[1]);
+        if (job) u -= p.last[job - 1];
+    }
     const unsigned per = static_cast<unsigned>(kGroupM) * p.tiles_n[job];
     const unsigned g = static_cast<unsigned>(u) / per, rest = static_cast<unsigned>(u) - g * per;
     const int m0 = static_cast<int>(g) * kGroupM;
@@ -133,7 +137,8 @@ __device__ __forceinline__ void st_shared_cluster_f32x4(uint32_t cluster_addr, f
                  : "memory");
 }
 
-template <bool kPair, int BN, int KIND, bool kSplit>
+// JOBS: products that the launch may hold.
+template <bool kPair, int BN, int KIND, bool kSplit, int JOBS>
 __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_constant__ Args p) {
     using F = Form<kPair, BN>;
     constexpr int STAGES = F::STAGES;
@@ -217,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         bool ok = true;
         for (int u = first; ok && u < p.units; u += workers) {
             int job, tm, tn;
-            decode(p, u, job, tm, tn);
+            decode<JOBS>(p, u, job, tm, tn);
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
             for (int kb = kb0; kb < kb1; kb += kBoxes) {
@@ -401,8 +406,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (int u = first + set * workers; u < p.units; u += 2 * workers, unit_count += 2) {
             int tm, tn;
-            decode(p, u, job, tm, tn);
-            M = p.M[job], N = p.N[job], ldo = p.ldo[job];
+            decode<JOBS>(p, u, job, tm, tn);
+            if constexpr (JOBS > 1) M = p.M[job], N = p.N[job], ldo = p.ldo[job];
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
             const uint32_t buf = unit_count & 1u;
@@ -707,9 +712,11 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     a.reset = reset;
     a.status = status;
     a.epi = p.epi;
-    auto kernel = gated ? gemm_tc_kernel<kPair, BN, kEpiGated, kSplit> : gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit>;
+    auto kernel = gated ? gemm_tc_kernel<kPair, BN, kEpiGated, kSplit, 1> : gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit, 1>;
     if constexpr (BN >= 128)
-        if (p.epi.kind == kEpiGatedGrad) kernel = gemm_tc_kernel<kPair, BN, kEpiGatedGrad, kSplit>;
+        if (p.epi.kind == kEpiGatedGrad) kernel = gemm_tc_kernel<kPair, BN, kEpiGatedGrad, kSplit, 1>;
+    if constexpr (kPair && BN >= 128)
+        if (p.batch > 1) kernel = gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit, kBatch>;
     DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       static_cast<int>(F::kSmemBytes)));
     const int64_t per = kSplit ? 2 * split : kPair ? 2 : 1;
@@ -742,7 +749,7 @@ static int cluster_room(int split, int sms) {
     int n = slot ? slot->load(std::memory_order_relaxed) : 0;
     if (n) return n - 1;
     using F = Form<true, 256>;
-    auto kernel = gemm_tc_kernel<true, 256, kEpiLinear, true>;
+    auto kernel = gemm_tc_kernel<true, 256, kEpiLinear, true, 1>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(F::kSmemBytes)) !=
         cudaSuccess)
         return 0;
