@@ -216,9 +216,10 @@ static int launch_typed(const Product& p, int* status, int second, cudaStream_t 
     return DTP_ERR_UNSUPPORTED;
 }
 
-// Whether this kernel takes the product: both operands with k contiguous, and few tokens.  bf16, 4096 x 4096, one and two
-// tokens: 8.3 us here, 8.6 on the tensor cores, 3.1 and 4.1 with 1024 x 3072; from three tokens on the tensor cores win.  fp32:
-// up to 32, beyond them the tiles.
+// Whether this kernel takes the product: both operands with k contiguous, and few tokens.  bf16, one token and two: 4096 x 4096
+// 7.5 and 8.1 us here, 7.8 on the tensor cores for three, 1024 x 3072 3.0 and 3.4, and 3.5 (before the tensor-core form took two
+// k blocks a stage, 4.1); from three tokens on the tensor cores win.  fp32, up to 32: 4096 x 4096 12 us for one token (5.4
+// TB/s), 50 for 32, 61 in the tiles.
 bool takes(const Product& p, int dtype) {
     return p.M <= (dtype == DTP_BF16 ? 2 : 32) && p.segments == 1 && p.A[0].ks == 1 && p.B[0].ks == 1 &&
            p.epi.kind != kEpiGatedGrad;

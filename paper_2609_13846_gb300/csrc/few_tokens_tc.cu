@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
         int stage = 0;
         uint32_t phase = 0;                      // of the stage's reuse
         for (int kb = kb0 + first * kBoxes; kb < kb1; kb += kBoxes) {
-            if (!mbar_wait(empty0 + stage * 8u, phase, abort_flag)) break;
+            if (!warp_wait(empty0 + stage * 8u, phase, abort_flag)) break;
             load_w(kb, stage);
             load_x(kb, stage);
             if (++stage == STAGES) { stage = 0; phase ^= 1u; }
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
         int stage = 0;
         uint32_t phase = 0;
         for (int kb = kb0; kb < kb1; kb += kBoxes) {
-            if (!mbar_wait(full0 + stage * 8u, phase, abort_flag)) break;
+            if (!warp_wait(full0 + stage * 8u, phase, abort_flag)) break;
             tc_fence_after();
             const int boxes = kb1 - kb < kBoxes ? kb1 - kb : kBoxes;
             if (issuer) {
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(kThreads) few_tokens_kernel(const __grid_const
     const int own_log = (KIND == kEpiGated ? 6 : 7) - (31 - __clz(S)), own = 1 << own_log;
     if (warp < 4) {
         // ------------------------------------------------- partial sums to the CTAs that finish them
-        const bool ok = mbar_wait(smem_u32(acc_full), 0, abort_flag);
+        const bool ok = warp_wait(smem_u32(acc_full), 0, abort_flag);
         tc_fence_after();
         if (ok) {
             const int row = warp * 32 + lane;            // of the tile

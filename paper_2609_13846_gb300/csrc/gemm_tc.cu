@@ -9,16 +9,17 @@
 // 128-byte-swizzled tiles and described to the tensor core in their own order, so nothing is transposed in
 // memory.
 //
-// Structure: persistent grid, one CTA per SM, twelve warps: warp 0 loads tiles by TMA, warp 1 issues the MMAs,
+// Structure: persistent grid, one CTA per SM, twenty warps: warp 0 loads tiles by TMA, warp 1 issues the MMAs,
 // sixteen warps in two sets drain the accumulator, which is double-buffered in TMEM: a set takes every second tile, so that
-// it has two tiles' time for its epilogue (eight warps and one tile's time: the layer of 1024 x 4096 with bias, silu and Z
-// 66 us on 8192 tokens, the gate and up products of 1024 x 3072 120 us on 16384).  Two forms: CTA pairs share 256 x BN x 16 tcgen05.mma of cta_group::2 (each CTA stages 128
-// rows of A and half of B), single CTAs issue 128 x BN x 16 ones (up to 128 rows).  Shared memory bounds both: a 64-wide k
+// it has two tiles' time for its epilogue (the block of 1024 x 3072 on 16384 tokens 173 us, with eight warps and one tile's
+// time 193).  Two forms: CTA pairs share 256 x BN x 16 tcgen05.mma of cta_group::2 (each CTA stages 128 rows of A and half of
+// B), single CTAs issue 128 x BN x 16 ones (up to 128 rows).  Shared memory bounds both: a 64-wide k
 // block is written once and read once by the tensor core, 64 KB per CTA at 128 bytes a clock for 256 x 256 pairs, as long as
 // its MMAs take (512 clocks), 384 clocks against 256 for 256 x 128 ones, 512 against 256 for single 128 x 128 tiles.
 // Where tiles are fewer than the pairs that the chip holds, a cluster of two or four pairs shares a tile, each pair with its
 // own range of k (kSplit): the partial sums meet in the shared memory that the stages leave free, are added in the order of
-// the ranges, and each CTA finishes a slice of the columns.
+// the ranges, and each CTA finishes a slice of the columns.  Measured: 4096 x 14336 x 4096 1.83 PFLOP/s (254 us; 293 with whole
+// left-over tiles), 8192^3 1.82, 1003 x 2048 x 1024 with a residual 9.6 us, 200 x 1024 x 1024 5.5 us.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -226,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
             for (int kb = kb0; kb < kb1; kb += kBoxes) {
-                if (!mbar_wait(empty0 + stage * 8u, phase ^ 1u, abort_flag)) { ok = false; break; }
+                if (!warp_wait(empty0 + stage * 8u, phase ^ 1u, abort_flag)) { ok = false; break; }
                 const int boxes = kb1 - kb < kBoxes ? kb1 - kb : kBoxes;      // the last stage may hold one block
                 const uint32_t fb = full_lead + stage * 8u;
                 if (issuer) {
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         const uint32_t low_a = desc_low(smem_u32(tiles), p.a_mn), low_b = desc_low(smem_u32(tiles) + kTileA, p.b_mn);
         const uint32_t idesc = p.idesc;
         auto wait = [&](uint32_t bar, uint32_t parity) {
-            return kPair ? mbar_wait_cluster(bar, parity, abort_flag) : mbar_wait(bar, parity, abort_flag);
+            return kPair ? warp_wait_cluster(bar, parity, abort_flag) : warp_wait(bar, parity, abort_flag);
         };
         for (int u = first; ok && u < p.units; u += workers, ++unit_count) {
             const uint32_t buf = unit_count & 1u;
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         const bool epi_warp = warp >= kEpiWarp0;
         bool ok = true;
         if (epi_warp) {
-            ok = mbar_wait(smem_u32(&acc_full[0]), 0, abort_flag);
+            ok = warp_wait(smem_u32(&acc_full[0]), 0, abort_flag);
             tc_fence_after();
         }
         cluster_sync();                  // every pair's MMAs are done: the stages may be written over
@@ -440,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             if constexpr (KIND == kEpiLinear) fetch(32 * half);
             if constexpr (!kSplit) {
                 const uint32_t use = (unit_count >> 1) & 1u;
-                if (!mbar_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
+                if (!warp_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
                 tc_fence_after();
             }
             const uint32_t acc = lane_base + buf * BN;
@@ -555,9 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     }
                     store32(job, p.dst[job], w, n, row0);
                 } else {
-                    // 16 columns at a time with all their saved values in flight (a row's four columns after the other: 192
-                    // us for 1024 x 3072 on 16384 tokens, the loads' latency 32 times a tile; so 144); dG goes to the staging buffer
-                    // as it is computed, dU waits in registers.  Both have rows on 16-byte boundaries.
+                    // 16 columns at a time with all their saved values in flight: 144 us for 1024 x 3072 on 16384 tokens (four
+                    // columns at a time 192 us, the loads' latency 32 times a tile).  dG goes to the staging buffer as it
+                    // is computed, dU waits in registers.  Both have rows on 16-byte boundaries.
                     const float* pre = e.pre + pre_index(m, n, N);
                     uint32_t w2[16];
                     if (lane == 0) bulk_wait_read0();

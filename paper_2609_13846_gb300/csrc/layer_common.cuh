@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "dtp.h"
+#include "dtp_common.cuh"
 
 namespace dtp {
 namespace layer {
@@ -126,6 +127,15 @@ __device__ __forceinline__ uint64_t desc(uint32_t low) {
     uint64_t d;
     asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low), "r"(kDescHigh));
     return d;
+}
+
+// A whole warp's bounded wait, with one outcome for all lanes: where some saw the phase complete and others the abort flag,
+// all give up, so that none waits for the others at a warp barrier.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort)) != 0;
+}
+__device__ __forceinline__ bool warp_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait_cluster(bar, parity, abort)) != 0;
 }
 
 // One lane of the warp, the same every time.
