@@ -646,7 +646,8 @@ int dtp_linear(const void* X, const void* W, const void* bias, const void* resid
  *   Z      as dtp_linear wrote it; NULL when act is DTP_ACT_NONE
  *   dX     [T, K], dW [N, K], dbias [N]: each out or NULL (not computed)
  * dZ is rounded once to dtype before the products; dbias sums the unrounded
- * values.  T == 0 writes zeros to dW and dbias.  Asynchronous.
+ * values.  T == 0 writes zeros to dW and dbias and reads no input (they may
+ * be NULL).  Asynchronous.
  */
 int dtp_linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N,
                         int act, int dtype, void* dX, void* dW, void* dbias, void* workspace,
@@ -680,7 +681,8 @@ int dtp_gated_ffn(const void* X, const void* W_gate, const void* W_up, const voi
  *   H, pre   as dtp_gated_ffn wrote them for the same X, weights and act
  *   dX [T, d], dW_gate, dW_up [N, d], dW_down [d, N]: each out or NULL
  * dG and dU are rounded once to dtype before the products.  T == 0 writes
- * zeros to the weights' gradients.  Asynchronous.
+ * zeros to the weights' gradients and reads no input (they may be NULL).
+ * Asynchronous.
  */
 int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, const void* W_up, const void* W_down,
                            const void* H, const float* pre, int64_t T, int d, int N, int act, int dtype, void* dX,

@@ -487,14 +487,15 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
     const int64_t ld = padded(N);
     void* dg = c.take(static_cast<size_t>(T) * ld * elem(dtype));
     void* du = c.take(static_cast<size_t>(T) * ld * elem(dtype));
-    Rows x, wg, wu, wd, dy;
-    int st = aligned_rows(X, T, d, dtype, c, stream, &x);
-    if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
-    if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
-    if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
-    if (st == DTP_OK) st = aligned_rows(dY, T, d, dtype, c, stream, &dy);
-    if (st != DTP_OK) return st;
-    if (T > 0) {
+    int st = DTP_OK;
+    Rows x{}, wg{}, wu{}, wd{}, dy{};
+    if (T > 0) {                             // without tokens no input is read, and they may be NULL
+        st = aligned_rows(X, T, d, dtype, c, stream, &x);
+        if (st == DTP_OK) st = aligned_rows(Wg, N, d, dtype, c, stream, &wg);
+        if (st == DTP_OK) st = aligned_rows(Wu, N, d, dtype, c, stream, &wu);
+        if (st == DTP_OK) st = aligned_rows(Wd, d, N, dtype, c, stream, &wd);
+        if (st == DTP_OK) st = aligned_rows(dY, T, d, dtype, c, stream, &dy);
+        if (st != DTP_OK) return st;
         Product p;
         p.A[0] = by_row(dy.p, dy.ld);
         p.B[0] = by_col(wd.p, wd.ld);
