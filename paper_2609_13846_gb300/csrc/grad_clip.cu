@@ -119,12 +119,13 @@ __device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(E)]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A sum of many fp32 terms with the rounding errors of the additions carried along.
+// A sum of many fp32 terms with the rounding errors of the additions carried along.  An infinite sum stays infinite: the error of
+// an addition to it would be inf - inf.
 struct Total {
     float sum = 0.0f, lost = 0.0f;
     __device__ __forceinline__ void add(float x) {
         const float y = x - lost, t = sum + y;
-        lost = (t - sum) - y;
+        lost = isinf(t) ? 0.0f : (t - sum) - y;
         sum = t;
     }
 };

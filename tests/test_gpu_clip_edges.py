@@ -1,0 +1,47 @@
+"""The gradient norm with infinities, norms beyond fp32, and coefficients below fp32's normal numbers."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_13846_gb300 import dtp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+TYPES = pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+BAD = pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+
+
+def _expect(norm, bad):
+    assert math.isnan(norm.item()) if math.isnan(bad) else norm.item() == math.inf
+
+
+@TYPES
+@BAD
+@pytest.mark.parametrize("n", [100, 5000, 300_001, 100_000_003])
+def test_bad_element_anywhere(n, bad, dtype):
+    """An infinity makes the norm +inf and a NaN makes it NaN, wherever it lies: before the first 16-byte word (the views
+    start one element past one), in the first words, in the middle, after the last word.  The gradients stay."""
+    g = torch.full((n + 1,), 0.5, device=DEV, dtype=dtype)[1:]
+    for at in (0, 9, n // 2, n - 10, n - 1):
+        g[at] = bad
+        _expect(dtp.clip_grad_norm([g], 1.0), bad)
+        g[at] = 0.5
+        assert (g == 0.5).all()
+
+
+@BAD
+@pytest.mark.parametrize("at", [0, 1, 750, 1499])
+def test_bad_element_among_many_tensors(at, bad):
+    ts = [torch.full((3,), 0.5, device=DEV, dtype=F32 if i % 3 else BF16) for i in range(1500)]
+    ts[at][1] = bad
+    _expect(dtp.clip_grad_norm(ts, 1.0), bad)
+
+
+def test_infinities_of_both_signs():
+    g = torch.full((500_000,), 0.5, device=DEV)
+    g[3], g[400_000] = math.inf, -math.inf
+    _expect(dtp.clip_grad_norm([g], 1.0), math.inf)
+    g[499_999] = math.nan
+    _expect(dtp.clip_grad_norm([g], 1.0), math.nan)
