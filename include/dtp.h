@@ -701,8 +701,9 @@ int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, co
  *   dtypes  host array: DTP_BF16 or DTP_F32 of each (out has the same)
  *   max_norm  >= 0, may be infinite (the norm alone)
  *   norm    device fp32 out: n
- * A norm that is not finite leaves the gradients as they are (out receives
- * copies); the caller reads it and skips the step.  Squares are summed in fp32
+ * A norm that is not finite in fp32 (NaN, infinite, or above 3.4e38) leaves the
+ * gradients as they are (out receives copies); the caller reads it and skips
+ * the step.  Squares are summed in fp32
  * by each thread (with compensation) and block, with a power of two taken out
  * where they would leave fp32's range, and in fp64 over the blocks.
  * Deterministic.  The host arrays are read before the call returns.  At most

@@ -245,9 +245,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clip_kernel(const __gr
             for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
             if (threadIdx.x == 0) {
                 const double r = sqrt(s);
-                // a norm that is not finite leaves the gradients as they are
-                coef = isfinite(r) && r > static_cast<double>(t.max_norm) ? static_cast<float>(t.max_norm / r) : 1.0f;
-                if (blockIdx.x == 0) *t.norm = static_cast<float>(r);
+                const float n = static_cast<float>(r);
+                // a norm that is not finite, as the caller reads it, leaves the gradients as they are
+                coef = isfinite(n) && r > static_cast<double>(t.max_norm) ? static_cast<float>(t.max_norm / r) : 1.0f;
+                if (blockIdx.x == 0) *t.norm = n;
             }
         }
         __syncthreads();

@@ -45,3 +45,15 @@ def test_infinities_of_both_signs():
     _expect(dtp.clip_grad_norm([g], 1.0), math.inf)
     g[499_999] = math.nan
     _expect(dtp.clip_grad_norm([g], 1.0), math.nan)
+
+
+@TYPES
+@pytest.mark.parametrize("inplace", [True, False])
+def test_finite_gradients_whose_norm_is_not(dtype, inplace):
+    """sqrt(1000) 3e38 is no fp32 number: the norm reads infinite, and what the caller will skip is not scaled."""
+    ts = [torch.full((n,), 3e38, device=DEV, dtype=dtype) for n in (990, 10)]
+    keep = [t.clone() for t in ts]
+    out = None if inplace else [torch.zeros_like(t) for t in ts]
+    assert dtp.clip_grad_norm(ts, 1.0, out=out).item() == math.inf
+    assert all(torch.equal(a, b) for a, b in zip(ts, keep))
+    assert inplace or all(torch.equal(a, b) for a, b in zip(out, keep))
