@@ -164,12 +164,24 @@ constexpr float kTiny = 8.271806e-25f;         // 2^-80
 constexpr float kUp = 1.2676506e30f;           // 2^100
 constexpr float kDown = 7.888609e-31f;         // 2^-100
 
-// dst = c src, last words first.  Words where both are equally aligned; c == 1 copies bit for bit, NaNs too.
+// A factor c down down.  `down` is 1, or a power of two where the factor would leave few bits of c, or none, among fp32's subnormal
+// numbers (large gradients, a small limit).
+struct Factor {
+    float c, down;
+    __device__ __forceinline__ float operator()(float v) const { return v * c * down * down; }
+};
+// below 1, above 0
+__device__ __forceinline__ Factor factor_of(double ratio) {
+    const int half = ratio < 7.888609052210118e-31 ? (-ilogb(ratio) - 1) / 2 : 0;       // 2^-100; then c is in [1/4, 1)
+    return Factor{static_cast<float>(ldexp(ratio, 2 * half)), ldexpf(1.0f, -half)};
+}
+
+// dst = f src, last words first.  Words where both are equally aligned; a factor of 1 copies bit for bit, NaNs too.
 template <typename E>
-__device__ __forceinline__ void scale_run(const E* src, E* dst, int64_t n, float c) {
-    const bool copy = c == 1.0f;
+__device__ __forceinline__ void scale_run(const E* src, E* dst, int64_t n, const Factor f) {
+    const bool copy = f.c == 1.0f;
     if (copy && src == dst) return;
-    auto one = [&](int64_t i) { dst[i] = copy ? src[i] : from_f32<E>(to_f32(src[i]) * c); };
+    auto one = [&](int64_t i) { dst[i] = copy ? src[i] : from_f32<E>(f(to_f32(src[i]))); };
     if ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15) {
         for (int64_t i = threadIdx.x; i < n; i += kThreads) one(i);
         return;
@@ -182,7 +194,7 @@ __device__ __forceinline__ void scale_run(const E* src, E* dst, int64_t n, float
         float v[Span<E>::kPer];
         unpack<E>(q, v);
 #pragma unroll
-        for (int i = 0; i < Span<E>::kPer; ++i) v[i] *= c;
+        for (int i = 0; i < Span<E>::kPer; ++i) v[i] = f(v[i]);
         return pack<E>(v);
     };
     const int64_t rounds = s.words / (R * kThreads) * (R * kThreads);
@@ -204,7 +216,7 @@ enum Mode { kNorm = 0, kScale = 1 };
 template <int CAP, int MODE>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clip_kernel(const __grid_constant__ Table<CAP> t) {
     __shared__ float red[kWarps];
-    __shared__ float coef;
+    __shared__ Factor coef;
     // this block's chunks, and elements [a, b) of tensor i among them
     const int c0 = static_cast<int>(static_cast<int64_t>(t.chunks) * blockIdx.x / gridDim.x);
     const int c1 = static_cast<int>(static_cast<int64_t>(t.chunks) * (blockIdx.x + 1) / gridDim.x);
@@ -247,12 +259,14 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) clip_kernel(const __gr
                 const double r = sqrt(s);
                 const float n = static_cast<float>(r);
                 // a norm that is not finite, as the caller reads it, leaves the gradients as they are
-                coef = isfinite(n) && r > static_cast<double>(t.max_norm) ? static_cast<float>(t.max_norm / r) : 1.0f;
+                coef = !isfinite(n) || r <= static_cast<double>(t.max_norm) ? Factor{1.0f, 1.0f}
+                       : t.max_norm > 0.0f                                  ? factor_of(t.max_norm / r)
+                                                                            : Factor{0.0f, 1.0f};
                 if (blockIdx.x == 0) *t.norm = n;
             }
         }
         __syncthreads();
-        const float f = coef;
+        const Factor f = coef;
         if (c0 < c1) {
             for (int i = tensor_of(t, c1 - 1); i >= 0 && t.first[i + 1] > c0; --i) {
                 int64_t a, b;

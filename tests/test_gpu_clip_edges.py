@@ -57,3 +57,21 @@ def test_finite_gradients_whose_norm_is_not(dtype, inplace):
     assert dtp.clip_grad_norm(ts, 1.0, out=out).item() == math.inf
     assert all(torch.equal(a, b) for a, b in zip(ts, keep))
     assert inplace or all(torch.equal(a, b) for a, b in zip(out, keep))
+
+
+@TYPES
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e-20, 1e-35])
+@pytest.mark.parametrize("scale", [1.0, 1e20, 1e36])
+def test_small_factors(max_norm, scale, dtype):
+    """max_norm / n from 1e-3 to 1e-74: below fp32's normal numbers and below all of them.  The norm is held to 2e-6 as in the
+    other tests; a scaled value is off by the norm's error and one rounding (2^-8, 2^-23), or half of the smallest
+    subnormal number of its type."""
+    g = torch.Generator(device=DEV).manual_seed(3)
+    ts = [(torch.rand(n, generator=g, device=DEV) * scale).to(dtype) for n in (1000, 37)]
+    src = [t.double() for t in ts]
+    n = math.sqrt(sum((t ** 2).sum().item() for t in src))
+    assert abs(dtp.clip_grad_norm(ts, max_norm).item() - n) <= 2e-6 * n
+    u, least = (2.0 ** -8, 2.0 ** -133) if dtype is BF16 else (2.0 ** -23, 2.0 ** -149)
+    for a, b in zip(ts, src):
+        ref = b * (torch.tensor(max_norm, dtype=F32).item() / n)
+        assert ((a.double() - ref).abs() <= (u + 2.1e-6) * ref + 0.51 * least).all()
