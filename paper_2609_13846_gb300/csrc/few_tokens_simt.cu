@@ -36,14 +36,16 @@ struct Args {
     Epilogue epi;
 };
 
-// PER consecutive elements from k, zero beyond K.
+// PER consecutive elements from k, zero beyond K.  Plain loads, not those of the read-only path: this kernel starts while the launch
+// before it may still be writing the tokens (or, in a call of its own, the weights), and what that path reads must not
+// change while the kernel lives.
 template <typename E, bool kWide>
 struct Word {
     static constexpr int PER = kWide ? 16 / static_cast<int>(sizeof(E)) : 1;
     uint4 q;
     __device__ __forceinline__ void load(const E* row, int64_t k, int64_t K) {
         if constexpr (kWide) {
-            q = k < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0, 0, 0, 0);
+            q = k < K ? *reinterpret_cast<const uint4*>(row + k) : make_uint4(0, 0, 0, 0);
         } else {
             const float v = k < K ? to_f32(row[k]) : 0.0f;
             q.x = __float_as_uint(v);

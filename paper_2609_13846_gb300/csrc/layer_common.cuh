@@ -111,7 +111,8 @@ __device__ __forceinline__ void act_both4(int act, float (&v)[4], float (&slope)
 
 // The layer kernels are launched so that a kernel's set-up overlaps the end of the one before it on the stream.  Each waits
 // for that one (grid_wait) before it touches global memory, and only then lets the next one begin (grid_release): what
-// begins early may rely on everything before its predecessor.
+// begins early may rely on everything before its predecessor.  Memory may thus change while a kernel lives: these kernels
+// take no __restrict__ pointers and read nothing through the read-only path (__ldg), whose loads need not stay behind the wait.
 __device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 

@@ -36,8 +36,7 @@ constexpr int kPer = 4;           // columns per thread
 // tokens in flight; each of the 8 warps sums its tokens in order.  kWide: rows on 16-byte boundaries.
 template <typename E, bool kWide>
 __global__ void __launch_bounds__(256)
-act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T, int N, int64_t ldz, int act,
-                E* __restrict__ dZ, float* __restrict__ partial) {
+act_grad_kernel(const E* dY, const float* Z, int64_t T, int N, int64_t ldz, int act, E* dZ, float* partial) {
     __shared__ float red[8][32 * kPer + 1];
     grid_wait();
     grid_release();
@@ -128,7 +127,7 @@ act_grad_kernel(const E* __restrict__ dY, const float* __restrict__ Z, int64_t T
 // out[n] = sum over the chunks: each of 8 warps sums every eighth in order, then the warps' sums in order.
 template <typename E>
 __global__ void __launch_bounds__(256)
-bias_reduce_kernel(const float* __restrict__ partial, int64_t chunks, int N, E* __restrict__ out) {
+bias_reduce_kernel(const float* partial, int64_t chunks, int N, E* out) {
     __shared__ float red[8][32];
     grid_wait();
     grid_release();
@@ -172,8 +171,8 @@ static int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t strea
 // lanes meet in fp64, so that the backward pass uses the sign of the exact sum.  Few of them: a warp reads 128 columns of four
 // tokens and takes its lanes' candidates one by one.  Exact zeros stay: the gradient there is zero.  Bound by reading Z once.
 __global__ void __launch_bounds__(256)
-relu_sign_kernel(const __nv_bfloat16* __restrict__ X, int64_t ldx, const __nv_bfloat16* __restrict__ W, int64_t ldw,
-                 const __nv_bfloat16* __restrict__ bias, int64_t T, int K, int N, float* __restrict__ Z) {
+relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, int64_t ldw, const __nv_bfloat16* bias, int64_t T,
+                 int K, int N, float* Z) {
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31;
@@ -236,7 +235,7 @@ relu_sign_kernel(const __nv_bfloat16* __restrict__ X, int64_t ldx, const __nv_bf
 // Rows copied to a pitch of whole 16 bytes, for the tensor cores' loads; the pitch's spare entries stay unwritten
 // (the loads' extents end before them).
 __global__ void __launch_bounds__(256)
-repitch_kernel(const uint16_t* __restrict__ src, int64_t rows, int cols, int64_t pitch, uint16_t* __restrict__ dst) {
+repitch_kernel(const uint16_t* src, int64_t rows, int cols, int64_t pitch, uint16_t* dst) {
     grid_wait();
     grid_release();
     // a warp per 512 entries of a row, all of them in flight (3162 x 3854: 10 us; a warp per row 13, and 12 for 640 rows, now 5)

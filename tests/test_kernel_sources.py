@@ -65,3 +65,13 @@ def test_shared_memory_budget_and_workspace_rule_agree(tmp_path, budget, builds)
     r = subprocess.run(cmd, capture_output=True, text=True)
     assert (r.returncode == 0) == builds, r.stderr
     assert builds or "layers without a workspace fit one block" in r.stderr
+
+
+@pytest.mark.parametrize("name", ["few_tokens_simt.cu", "few_tokens_tc.cu", "gemm_tc.cu", "layer_ops.cu", "grad_clip.cu",
+                                  "layer_common.cuh"])
+def test_overlapped_launches_read_coherently(name):
+    """A kernel that starts before its predecessor on the stream has ended sees memory change while it lives: loads of the
+    read-only path, and any load from a pointer declared free of aliases, may be moved before its wait."""
+    text = _source(name)
+    assert "griddepcontrol.wait" in text or "grid_wait()" in text
+    assert "__ldg(" not in text and "__restrict__" not in text and "ld.global.nc" not in text
