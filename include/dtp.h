@@ -630,8 +630,10 @@ typedef enum {
  *   Y        [T, N]   out
  *   Z        [T, N] fp32 out or NULL: the pre-activations that
  *            dtp_linear_backward needs when act is not DTP_ACT_NONE.  With
- *            DTP_ACT_RELU and bf16 its values near zero are summed again in 64
- *            bits: the gradient's mask is the exact sums' sign
+ *            DTP_ACT_RELU and bf16 a value that fp32 sums may have put on the
+ *            wrong side of zero is summed again: its sign, the gradient's mask,
+ *            is that of the sum in 64 bits.  (With fp32 operands it is that of
+ *            the fp32 sum.)
  * T == 0 returns DTP_OK.  Workspace from dtp_linear_workspace_size (backward:
  * nonzero for the size that both directions need).  Asynchronous.
  */

@@ -164,39 +164,145 @@ static int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t strea
     return DTP_OK;
 }
 
-// relu has a kink where its gradient jumps, and the tensor cores' sums are off by about 2^-26 of the running sum for every 16 k
-// (they cut the sum off instead of rounding it): a pre-activation nearer to zero than that may come out on the wrong side.  The
-// saved values within 2^-15 (more for sums of more than 16384 terms) of their neighbourhood's largest, more than ten times
-// those sums' error, are summed again: the products are exact in fp32, each lane carries its additions' errors along, and the
-// lanes meet in fp64, so that the backward pass uses the sign of the exact sum.  Few of them: a warp reads 128 columns of four
-// tokens and takes its lanes' candidates one by one.  Exact zeros stay: the gradient there is zero.  Bound by reading Z once.
+// relu has a kink where its gradient jumps: the gradient's mask wants the sign of the sum, and a sum near zero may come out on
+// the wrong side.  How near goes by the terms, not by the sum.  An MMA of 16 k aligns its products and the accumulator to
+// the largest of them, cuts each of the 17 off at 2^-25 of it and their sum at 2^-23 (measured: 1 + p - 1 with p in the same step and
+// in others), and while a sum of terms of sizes S and a bias b comes back to zero no partial sum is above (S + |b|) / 2: 21/16 2^-22
+// (S + |b|) for every 16 k.  S is at most |x| |w|, the norms of the two rows.  So every saved value below kSignShare (K + 64)
+// (|x| |w| + |b|) is summed again, computed zeros too (64: the partial sums of a split range).
+constexpr float kSignShare = 1.9557774e-8f;      // 21/16 2^-26
+
+// Upper bounds of the 2-norms of T rows of X, then of N rows of W: a warp per row, fp32 sums of squares, with a power of two taken
+// out where they leave fp32's range; a 32nd covers their roundings (K / 32 additions a lane, K to 2^24, and the root halves
+// the error).  Two bytes a row, rounded up.  A row of zeros gives 0, one with an infinity an infinity, a NaN a NaN.
 __global__ void __launch_bounds__(256)
-relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, int64_t ldw, const __nv_bfloat16* bias, int64_t T,
-                 int K, int N, float* Z) {
+row_norms_kernel(const __nv_bfloat16* X, int64_t ldx, int64_t T, const __nv_bfloat16* W, int64_t ldw, int N, int K,
+                 __nv_bfloat16* norms) {
+    grid_wait();
+    grid_release();
+    const int lane = threadIdx.x & 31;
+    for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < T + N; i += gridDim.x * 8ll) {
+        const int64_t ld = i < T ? ldx : ldw;
+        const __nv_bfloat16* row = i < T ? X + i * ldx : W + (i - T) * ldw;
+        const int words = (ld & 7) == 0 ? K / 8 : 0;
+        auto squares = [&](float scale) {
+            float s = 0.0f;
+            auto add = [&](float v) { v *= scale, s = fmaf(v, v, s); };
+#pragma unroll 4
+            for (int k = lane; k < words; k += 32) {
+                const uint4 a = reinterpret_cast<const uint4*>(row)[k];
+                const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) add(__uint_as_float(w[q] << 16)), add(__uint_as_float(w[q] & 0xFFFF0000u));
+            }
+            for (int k = 8 * words + lane; k < K; k += 32) add(to_f32(row[k]));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            return s;
+        };
+        float s = squares(1.0f), back = 1.0f;
+        if (!(s >= 8.271806e-25f && s <= 3.0e38f)) {                             // 2^-80
+            back = s < 8.271806e-25f ? 7.888609e-31f : 1.2676506e30f;            // 2^-100, 2^100
+            s = squares(1.0f / back);
+        }
+        if (lane == 0) norms[i] = __float2bfloat16_ru(1.03125f * sqrtf(s) * back);
+    }
+}
+
+// The product of two rows by a whole warp, in up to three steps, until the sum is larger than the step's error: fp32 in eight sums a lane;
+// products in fp32 (exact) with each lane carrying its additions' errors along and the lanes meeting in fp64; and fp64, which is
+// the result whatever it is (it may be zero).  `size` bounds the sum of the terms' sizes and the bias.
+struct Dot {
+    int K, words;            // words of eight that may be loaded at once
+    float fp32, carried, least;
+    __device__ __forceinline__ Dot(int K, bool wide) : K(K), words(wide ? K / 8 : 0) {
+        const float most = (K + 31) / 32;                                    // a lane's terms
+        fp32 = (K / (wide ? 256 : 32) + 24.0f) * 5.9604645e-8f;              // 2^-24: a sum's additions, then the tree's
+        carried = most * most * 3.5527137e-15f;                              // 2^-48: the errors' own roundings
+        least = K * 1.4012985e-45f;                                          // among fp32's subnormal numbers
+    }
+    template <typename V>
+    __device__ __forceinline__ static V lanes(V s) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        return s;
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(const __nv_bfloat16* x, const __nv_bfloat16* w, F add) const {
+        const int lane = threadIdx.x & 31;
+#pragma unroll 4
+        for (int k = lane; k < words; k += 32) {
+            const uint4 a = reinterpret_cast<const uint4*>(x)[k], c = reinterpret_cast<const uint4*>(w)[k];
+            const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                add(2 * q, __uint_as_float(aw[q] << 16), __uint_as_float(cw[q] << 16));
+                add(2 * q + 1, __uint_as_float(aw[q] & 0xFFFF0000u), __uint_as_float(cw[q] & 0xFFFF0000u));
+            }
+        }
+        for (int k = 8 * words + lane; k < K; k += 32) add(0, to_f32(x[k]), to_f32(w[k]));
+    }
+    __device__ __forceinline__ float operator()(const __nv_bfloat16* x, const __nv_bfloat16* w, float bias, float size) const {
+        float s[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        each(x, w, [&](int i, float a, float c) { s[i] = fmaf(a, c, s[i]); });
+        const float plain = lanes(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]))) + bias;
+        if (fabsf(plain) > fmaxf(fp32 * size, least) && isfinite(plain)) return plain;
+        float hi = 0.0f, lo = 0.0f;
+        each(x, w, [&](int, float a, float c) {      // hi + lo is the sum: the error of each addition, exactly
+            const float p = a * c, t = hi + p, b = t - hi;
+            lo += (hi - (t - b)) + (p - b);
+            hi = t;
+        });
+        double sum = lanes(static_cast<double>(hi) + static_cast<double>(lo)) + static_cast<double>(bias);
+        if (!(fabs(sum) > fmaxf(carried * size, least)) || isinf(sum)) {
+            sum = 0.0;
+            each(x, w, [&](int, float a, float c) { sum = fma(static_cast<double>(a), static_cast<double>(c), sum); });
+            sum = lanes(sum) + static_cast<double>(bias);
+        }
+        return static_cast<float>(sum);
+    }
+};
+
+// The saved values that may have the wrong sign, summed again.  A warp reads 128 columns of four tokens and takes its lanes' candidates one
+// by one.  Where the terms are all zero the sum is, and nothing is a candidate; where a norm is infinite everything finite is,
+// and beside a NaN nothing.  Candidates go with K sqrt(K) (random rows: 0.05% of the values at K = 1024, 0.4% at 4096, 1.2% at
+// 8192), the rows that they read with K times that.  With the norms, 8192 x 4096 values of K = 1024: 62 us, reading Z and the
+// candidates' latency; 4096 x 4096: 146 us at K = 4096, 558 at 8192, their rows from L2.
+__global__ void __launch_bounds__(256)
+relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, int64_t ldw, const __nv_bfloat16* bias,
+                 const __nv_bfloat16* norms, int64_t T, int K, int N, float* Z) {
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31;
     const int per_row = (N + 127) / 128;
     const int64_t pieces = (T + 3) / 4 * per_row;
-    const float share = 3.0517578125e-5f * (1.0f + K * (1.0f / 16384.0f));
-    const bool wide = (ldx & 7) == 0 && (ldw & 7) == 0;      // rows on 16-byte boundaries
+    const float share = kSignShare * (K + 64.0f);
+    const Dot dot(K, (ldx & 7) == 0 && (ldw & 7) == 0);
     for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < pieces; i += gridDim.x * 8ll) {
         const int64_t g = i / per_row, t0 = g * 4;
         const int n0 = static_cast<int>(i - g * per_row) * 128;
-        float z[16], top = 0.0f;
+        float z[16], nx[4], nw[4], nb[4];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const int n = n0 + 32 * (j & 3) + lane;
             const int64_t t = t0 + (j >> 2);
-            z[j] = n < N && t < T ? Z[t * N + n] : 0.0f;
+            z[j] = n < N && t < T ? Z[t * N + n] : __int_as_float(0x7FC00000);     // a NaN is no candidate
         }
 #pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(z[j]));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        for (int j = 0; j < 4; ++j) {
+            const int n = n0 + 32 * j + lane;
+            nx[j] = t0 + j < T ? to_f32(norms[t0 + j]) : 0.0f;
+            nw[j] = n < N ? to_f32(norms[T + n]) : 0.0f;
+            nb[j] = n < N && bias ? fabsf(to_f32(bias[n])) : 0.0f;
+        }
         unsigned mine = 0;                                   // the lane's candidates
+        float top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) mine |= (z[j] != 0.0f && fabsf(z[j]) < share * top ? 1u : 0u) << j;
+        for (int j = 0; j < 16; ++j) {
+            const float s = fmaf(nx[j >> 2], nw[j & 3], nb[j & 3]), a = fabsf(z[j]);
+            mine |= (a < share * s || (a < dot.least && s > 0.0f) ? 1u : 0u) << j;
+            top = fmaxf(top, s);
+        }
         if (!__any_sync(0xFFFFFFFFu, mine != 0)) continue;
 #pragma unroll 1
         for (int j = 0; j < 16; ++j) {
@@ -205,28 +311,8 @@ relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, in
             while (todo) {
                 const int at = __ffs(todo) - 1, n = n0 + 32 * (j & 3) + at;
                 todo &= todo - 1;
-                const __nv_bfloat16 *x = X + t * ldx, *w = W + n * ldw;
-                float hi = 0.0f, lo = 0.0f;
-                auto add = [&](float p) {                    // hi + lo is the sum: the error of each addition, exactly
-                    const float s = hi + p, b = s - hi;
-                    lo += (hi - (s - b)) + (p - b);
-                    hi = s;
-                };
-                const int words = wide ? K / 8 : 0;
-                for (int k = lane; k < words; k += 32) {
-                    const uint4 a = reinterpret_cast<const uint4*>(x)[k], c = reinterpret_cast<const uint4*>(w)[k];
-                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w}, cw[4] = {c.x, c.y, c.z, c.w};
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        add(__uint_as_float(aw[q] << 16) * __uint_as_float(cw[q] << 16));
-                        add(__uint_as_float(aw[q] & 0xFFFF0000u) * __uint_as_float(cw[q] & 0xFFFF0000u));
-                    }
-                }
-                for (int k = 8 * words + lane; k < K; k += 32) add(to_f32(x[k]) * to_f32(w[k]));
-                double sum = static_cast<double>(hi) + static_cast<double>(lo);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                if (lane == at) Z[t * N + n] = static_cast<float>(sum + (bias ? static_cast<double>(to_f32(bias[n])) : 0.0));
+                const float sum = dot(X + t * ldx, W + n * ldw, bias ? to_f32(bias[n]) : 0.0f, __shfl_sync(0xFFFFFFFFu, top, at));
+                if (lane == at) Z[t * N + n] = sum;
             }
         }
     }
@@ -278,6 +364,10 @@ struct Rows {
 };
 static size_t repitch_bytes(int64_t rows, int cols, int dtype) {
     return dtype == DTP_BF16 && cols % 8 ? static_cast<size_t>(rows) * padded(cols) * 2 : 0;
+}
+// the row norms for relu's signs
+static size_t norms_bytes(int64_t T, int N, int dtype) {
+    return dtype == DTP_BF16 ? static_cast<size_t>(T + N) * sizeof(__nv_bfloat16) : 0;
 }
 static int aligned_rows(const void* p, int64_t rows, int cols, int dtype, Carver& c, cudaStream_t stream, Rows* out) {
     const size_t bytes = repitch_bytes(rows, cols, dtype);
@@ -338,11 +428,25 @@ size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) 
     Carver c(nullptr);
     c.take(repitch_bytes(T, K, dtype));
     c.take(repitch_bytes(N, K, dtype));
+    c.take(norms_bytes(T, N, dtype));
     if (backward) {
         c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
         c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float));
     }
     return c.used;
+}
+
+// The saved values of a bf16 product with relu get the sums' signs.
+static int relu_signs(const Product& p, const __nv_bfloat16* bias, float* Z, Carver& c, cudaStream_t stream) {
+    const auto* X = static_cast<const __nv_bfloat16*>(p.A[0].p);
+    const auto* W = static_cast<const __nv_bfloat16*>(p.B[0].p);
+    const int K = static_cast<int>(p.K);
+    auto* norms = static_cast<__nv_bfloat16*>(c.take(norms_bytes(p.M, p.N, DTP_BF16)));
+    const int64_t rows = (p.M + p.N + 7) / 8, pieces = ((p.M + 3) / 4 * ((p.N + 127) / 128) + 7) / 8;
+    const int st = launch_after(row_norms_kernel, rows < 8192 ? rows : 8192, stream, X, p.A[0].rs, p.M, W, p.B[0].rs, p.N, K, norms);
+    if (st != DTP_OK) return st;
+    return launch_after(relu_sign_kernel, pieces < 8192 ? pieces : 8192, stream, X, p.A[0].rs, W, p.B[0].rs, bias,
+                        static_cast<const __nv_bfloat16*>(norms), p.M, K, p.N, Z);
 }
 
 int linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
@@ -364,13 +468,9 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
     p.epi.act = act, p.epi.bias = bias, p.epi.residual = residual, p.epi.out = Y, p.epi.ldo = N, p.epi.Z = Z;
     p.epi.M = T, p.epi.N = N;
     if ((st = call.run(p)) != DTP_OK) return st;
-    if (dtype == DTP_BF16 && act == DTP_ACT_RELU && Z) {
-        const int64_t blocks = ((T + 3) / 4 * ((N + 127) / 128) + 7) / 8;
-        st = launch_after(relu_sign_kernel, blocks < 8192 ? blocks : 8192, stream,
-                          static_cast<const __nv_bfloat16*>(p.A[0].p), p.A[0].rs, static_cast<const __nv_bfloat16*>(p.B[0].p),
-                          p.B[0].rs, static_cast<const __nv_bfloat16*>(bias), T, K, N, Z);
-        if (st != DTP_OK) return st;
-    }
+    if (dtype == DTP_BF16 && act == DTP_ACT_RELU && Z)
+        st = relu_signs(p, static_cast<const __nv_bfloat16*>(bias), Z, c, stream);
+    if (st != DTP_OK) return st;
     return call.done();
 }
 
