@@ -664,7 +664,8 @@ int dtp_linear_backward(const void* dY, const void* X, const void* W, const floa
  *            pitch of N rounded up to a multiple of 8 (entries beyond N are
  *            not written)
  *   pre      NULL, or out for dtp_gated_ffn_backward: G and U in fp32 in the
- *            library's own order, dtp_gated_ffn_saved_size bytes
+ *            library's own order, dtp_gated_ffn_saved_size bytes.  With
+ *            DTP_ACT_RELU the signs of G are as dtp_linear's of Z
  * H is rounded once to dtype before the down projection.  T == 0 returns
  * DTP_OK.  Workspace from dtp_gated_ffn_workspace_size (backward: nonzero for
  * the size that both directions need).  Asynchronous.

@@ -263,35 +263,52 @@ struct Dot {
     }
 };
 
-// The saved values that may have the wrong sign, summed again.  A warp reads 128 columns of four tokens and takes its lanes' candidates one
-// by one.  Where the terms are all zero the sum is, and nothing is a candidate; where a norm is infinite everything finite is,
-// and beside a NaN nothing.  Candidates go with K sqrt(K) (random rows: 0.05% of the values at K = 1024, 0.4% at 4096, 1.2% at
-// 8192), the rows that they read with K times that.  With the norms, 8192 x 4096 values of K = 1024: 62 us, reading Z and the
-// candidates' latency; 4096 x 4096: 146 us at K = 4096, 558 at 8192, their rows from L2.
-__global__ void __launch_bounds__(256)
+// The saved values that may have the wrong sign, summed again.  A warp reads 128 columns of four tokens, or where they are the block's
+// saved gate (kPre) 16 neurons of 32 tokens, and takes its lanes' candidates one by one.  Where the terms are all zero the sum
+// is, and nothing is a candidate; where a norm is infinite everything finite is, and beside a NaN nothing.  Candidates go
+// with K sqrt(K) (random rows: 0.05% of the values at K = 1024, 0.4% at 4096, 1.2% at 8192), the rows that they read with K times
+// that.  With the norms, 8192 x 4096 values of K = 1024: 69 us, reading Z and the candidates' latency (8192 x 3072 of the gate 71); 4096
+// x 4096: 118 us at K = 4096, 453 at 8192, their rows from L2.
+template <bool kPre>
+__global__ void __launch_bounds__(256, 4)
 relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, int64_t ldw, const __nv_bfloat16* bias,
-                 const __nv_bfloat16* norms, int64_t T, int K, int N, float* Z) {
+                 const __nv_bfloat16* norms, int64_t T, int K, int N, float* values) {
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31;
-    const int per_row = (N + 127) / 128;
-    const int64_t pieces = (T + 3) / 4 * per_row;
+    constexpr int kTokens = kPre ? 32 : 4, kCols = kPre ? 16 : 128;      // of a warp; 16 values a lane
+    const int per_row = (N + kCols - 1) / kCols;
+    const int64_t pieces = (T + kTokens - 1) / kTokens * per_row;
     const float share = kSignShare * (K + 64.0f);
     const Dot dot(K, (ldx & 7) == 0 && (ldw & 7) == 0);
     for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < pieces; i += gridDim.x * 8ll) {
-        const int64_t g = i / per_row, t0 = g * 4;
-        const int n0 = static_cast<int>(i - g * per_row) * 128;
-        float z[16], nx[4], nw[4], nb[4];
+        const int64_t g = i / per_row, t0 = g * kTokens;
+        const int n0 = static_cast<int>(i - g * per_row) * kCols;
+        // of value j of lane l
+        auto token = [&](int j, int l) { return kPre ? t0 + l : t0 + (j >> 2); };
+        auto column = [&](int j, int l) { return kPre ? n0 + j : n0 + 32 * (j & 3) + l; };
+        auto inside = [&](int j) { return column(j, lane) < N && token(j, lane) < T; };
+        const float kNone = __int_as_float(0x7FC00000);      // beyond the edges: a NaN is no candidate
+        float z[16];
+        if constexpr (kPre) {                                // groups of four neurons; beyond the edges there is room
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const int n = n0 + 32 * (j & 3) + lane;
-            const int64_t t = t0 + (j >> 2);
-            z[j] = n < N && t < T ? Z[t * N + n] : __int_as_float(0x7FC00000);     // a NaN is no candidate
+            for (int q = 0; q < 4; ++q) {
+                float4 v = make_float4(kNone, kNone, kNone, kNone);
+                if (inside(4 * q)) v = *reinterpret_cast<const float4*>(values + pre_index(t0 + lane, n0 + 4 * q, N));
+                z[4 * q] = v.x, z[4 * q + 1] = inside(4 * q + 1) ? v.y : kNone;
+                z[4 * q + 2] = inside(4 * q + 2) ? v.z : kNone, z[4 * q + 3] = inside(4 * q + 3) ? v.w : kNone;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z[j] = inside(j) ? values[token(j, lane) * N + column(j, lane)] : kNone;
         }
+        constexpr int kX = kPre ? 1 : 4, kW = kPre ? 16 : 4;      // the lane's tokens and columns: value j is of j / kW and j % kW
+        float nx[kX], nw[kW], nb[kW];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = n0 + 32 * j + lane;
-            nx[j] = t0 + j < T ? to_f32(norms[t0 + j]) : 0.0f;
+        for (int j = 0; j < kX; ++j) nx[j] = token(kW * j, lane) < T ? to_f32(norms[token(kW * j, lane)]) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < kW; ++j) {
+            const int n = column(j, lane);
             nw[j] = n < N ? to_f32(norms[T + n]) : 0.0f;
             nb[j] = n < N && bias ? fabsf(to_f32(bias[n])) : 0.0f;
         }
@@ -299,20 +316,20 @@ relu_sign_kernel(const __nv_bfloat16* X, int64_t ldx, const __nv_bfloat16* W, in
         float top = 0.0f;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            const float s = fmaf(nx[j >> 2], nw[j & 3], nb[j & 3]), a = fabsf(z[j]);
+            const float s = fmaf(nx[j / kW], nw[j % kW], nb[j % kW]), a = fabsf(z[j]);
             mine |= (a < share * s || (a < dot.least && s > 0.0f) ? 1u : 0u) << j;
             top = fmaxf(top, s);
         }
         if (!__any_sync(0xFFFFFFFFu, mine != 0)) continue;
 #pragma unroll 1
         for (int j = 0; j < 16; ++j) {
-            const int64_t t = t0 + (j >> 2);
             unsigned todo = __ballot_sync(0xFFFFFFFFu, (mine >> j) & 1u);
             while (todo) {
-                const int at = __ffs(todo) - 1, n = n0 + 32 * (j & 3) + at;
+                const int at = __ffs(todo) - 1, n = column(j, at);
+                const int64_t t = token(j, at);
                 todo &= todo - 1;
                 const float sum = dot(X + t * ldx, W + n * ldw, bias ? to_f32(bias[n]) : 0.0f, __shfl_sync(0xFFFFFFFFu, top, at));
-                if (lane == at) Z[t * N + n] = sum;
+                if (lane == at) values[kPre ? pre_index(t, n, N) : t * N + n] = sum;
             }
         }
     }
@@ -436,17 +453,19 @@ size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) 
     return c.used;
 }
 
-// The saved values of a bf16 product with relu get the sums' signs.
-static int relu_signs(const Product& p, const __nv_bfloat16* bias, float* Z, Carver& c, cudaStream_t stream) {
+// The saved values of a bf16 product with relu (Z, or the block's gate) get the sums' signs.
+template <bool kPre>
+static int relu_signs(const Product& p, const __nv_bfloat16* bias, float* values, Carver& c, cudaStream_t stream) {
     const auto* X = static_cast<const __nv_bfloat16*>(p.A[0].p);
     const auto* W = static_cast<const __nv_bfloat16*>(p.B[0].p);
     const int K = static_cast<int>(p.K);
     auto* norms = static_cast<__nv_bfloat16*>(c.take(norms_bytes(p.M, p.N, DTP_BF16)));
-    const int64_t rows = (p.M + p.N + 7) / 8, pieces = ((p.M + 3) / 4 * ((p.N + 127) / 128) + 7) / 8;
+    const int64_t rows = (p.M + p.N + 7) / 8;
+    const int64_t warps = kPre ? (p.M + 31) / 32 * ((p.N + 15) / 16) : (p.M + 3) / 4 * ((p.N + 127) / 128), blocks = (warps + 7) / 8;
     const int st = launch_after(row_norms_kernel, rows < 8192 ? rows : 8192, stream, X, p.A[0].rs, p.M, W, p.B[0].rs, p.N, K, norms);
     if (st != DTP_OK) return st;
-    return launch_after(relu_sign_kernel, pieces < 8192 ? pieces : 8192, stream, X, p.A[0].rs, W, p.B[0].rs, bias,
-                        static_cast<const __nv_bfloat16*>(norms), p.M, K, p.N, Z);
+    return launch_after(relu_sign_kernel<kPre>, blocks < 8192 ? blocks : 8192, stream, X, p.A[0].rs, W, p.B[0].rs, bias,
+                        static_cast<const __nv_bfloat16*>(norms), p.M, K, p.N, values);
 }
 
 int linear_forward(const void* X, const void* W, const void* bias, const void* residual, int64_t T, int K, int N,
@@ -469,7 +488,7 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
     p.epi.M = T, p.epi.N = N;
     if ((st = call.run(p)) != DTP_OK) return st;
     if (dtype == DTP_BF16 && act == DTP_ACT_RELU && Z)
-        st = relu_signs(p, static_cast<const __nv_bfloat16*>(bias), Z, c, stream);
+        st = relu_signs<false>(p, static_cast<const __nv_bfloat16*>(bias), Z, c, stream);
     if (st != DTP_OK) return st;
     return call.done();
 }
@@ -535,6 +554,7 @@ size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward) {
     c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
     for (int64_t rows : {T, static_cast<int64_t>(N), static_cast<int64_t>(N)}) c.take(repitch_bytes(rows, d, dtype));
     c.take(repitch_bytes(d, N, dtype));
+    c.take(norms_bytes(T, N, dtype));
     if (backward) {
         c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
         c.take(repitch_bytes(T, d, dtype));
@@ -575,6 +595,8 @@ int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd,
     q.M = T, q.N = d, q.K = N;
     q.epi.residual = residual, q.epi.out = Y, q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
     if ((st = call.run(q)) != DTP_OK) return st;
+    if (dtype == DTP_BF16 && act == DTP_ACT_RELU && pre) st = relu_signs<true>(p, nullptr, pre, c, stream);
+    if (st != DTP_OK) return st;
     return call.done();
 }
 

@@ -109,3 +109,40 @@ def test_nothing_beyond_the_rows_is_touched(T, N):
                               torch.cuda.current_stream().cuda_stream)
     assert st == dtp.DTP_OK and dtp.workspace_status(ws) == dtp.DTP_OK
     assert (store[T * N:] == 7).all() and (store[:T * N] > 0.9).all()
+
+
+@pytest.mark.parametrize("T,K,N", [(1, 1025, 1), (1, 777, 40), (2, 2049, 333), (33, 1025, 200), (40, 1001, 17), (200, 2049, 300),
+                                   (600, 1032, 136), (1100, 505, 130)])
+def test_gate_of_the_block(T, K, N):
+    """The mask of the block's gate, read off its gradient: a one in a column of its own for every token makes dW_gate's column
+    that token's dG, which is dH U where the gate's sum is positive and zero elsewhere."""
+    X, W_gate, z = _cancelling(T, K, N, seed=17)
+    X = torch.cat([X, torch.eye(T, device=DEV, dtype=BF16)], 1).contiguous()
+    W_gate = torch.cat([W_gate, torch.zeros((N, T), device=DEV, dtype=BF16)], 1).contiguous()
+    W_up = torch.zeros_like(W_gate)
+    W_up[:, K - 1] = 1.0
+    W_down = torch.ones((K + T, N), device=DEV, dtype=BF16)
+    Y, saved = dtp.gated_ffn(X, W_gate, W_up, W_down, activation="relu", save=True)
+    _, dW_gate, _, _ = dtp.gated_ffn_backward(torch.ones_like(Y), X, W_gate, W_up, W_down, saved, activation="relu")
+    assert torch.equal(dW_gate[:, K:].t().double(), torch.where(z > 0, float(K + T), 0.0).to(BF16).double())
+
+
+@pytest.mark.parametrize("T,d,N", [(1, 64, 128), (2, 72, 200), (3, 520, 1001), (40, 136, 200), (300, 520, 333), (1000, 256, 640)])
+def test_block_with_relu(T, d, N):
+    """Value and gradients against the formulas in 64 bits; an element is off by at most its own rounding (2^-8) and, with the
+    rounded factors H, dG and dU, 1.1 2^-8 of its terms' sizes."""
+    def rand(seed, *shape, std=1.0):
+        return (torch.randn(shape, generator=_gen(seed), device=DEV) * std).to(BF16)
+
+    X, dY = rand(1, T, d), rand(2, T, d)
+    Wg, Wu, Wd = rand(3, N, d, std=d ** -0.5), rand(4, N, d, std=d ** -0.5), rand(5, d, N, std=N ** -0.5)
+    Y, saved = dtp.gated_ffn(X, Wg, Wu, Wd, activation="relu", save=True)
+    got = (Y, *dtp.gated_ffn_backward(dY, X, Wg, Wu, Wd, saved, activation="relu"))
+    x, wg, wu, wd, dy = (t.double() for t in (X, Wg, Wu, Wd, dY))
+    g, u, dh = x @ wg.t(), x @ wu.t(), dy @ wd
+    h, du, dg = g.clamp(min=0) * u, dh * g.clamp(min=0), dh * u * (g > 0)
+    ref = (h @ wd.t(), dg @ wg + du @ wu, dg.t() @ x, du.t() @ x, dy.t() @ h)
+    a = [t.abs() for t in (x, wg, wu, wd, h, dg, du, dy)]
+    size = (a[4] @ a[3].t(), a[5] @ a[1] + a[6] @ a[2], a[5].t() @ a[0], a[6].t() @ a[0], a[7].t() @ a[4])
+    for name, v, r, s in zip(("Y", "dX", "dW_gate", "dW_up", "dW_down"), got, ref, size):
+        assert ((v.double() - r).abs() <= 2.0 ** -8 * (r.abs() + 1.1 * s)).all(), name
