@@ -605,8 +605,10 @@ int dtp_apply_layout(const int32_t* head_part, const int32_t* neuron_dev, int la
  * serving) and backward (the distillation of Sec. 4).  dtype is that of every
  * tensor without a stated type: DTP_BF16 (tensor cores, fp32 accumulation,
  * each output rounded once) or DTP_F32 (CUDA cores, fp32 throughout).
- * Sizes: 0 <= T <= 2^31 - 256, every width 1 <= . <= 2^24.  Widths need not be
- * multiples of anything; rows of bf16 matrices that are no multiple of 16
+ * Sizes: 0 <= T <= 2^31 - 256, every width 1 <= . <= 2^20.  A bf16 sum loses
+ * about 2^-26 of its running value for every 16 terms (the tensor cores cut
+ * sums off); sums over the tokens are made in runs of at most 2^18, which are
+ * added in 64 bits.  Widths need not be multiples of anything; rows of bf16 matrices that are no multiple of 16
  * bytes cost a copy to an aligned pitch in the workspace.  Outputs must not
  * overlap inputs (Y may be `residual` itself).  Results are deterministic: no
  * floating-point atomics, and sums whose order depends on the sizes alone.  A

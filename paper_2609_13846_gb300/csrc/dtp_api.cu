@@ -136,7 +136,8 @@ bool search_sizes_ok(int layers, int H, int N, int D, int iters) {
 
 bool layer_sizes_ok(int64_t T, int K, int N, int dtype) {
     if (dtype != DTP_BF16 && dtype != DTP_F32) return false;
-    return T >= 0 && T <= (int64_t(1) << 31) - 256 && K >= 1 && K <= (1 << 24) && N >= 1 && N <= (1 << 24);
+    constexpr int widest = 1 << 20;          // a sum over a width is one accumulator's, which loses about 2^-26 for every 16 terms
+    return T >= 0 && T <= (int64_t(1) << 31) - 256 && K >= 1 && K <= widest && N >= 1 && N <= widest;
 }
 
 bool act_ok(int act) { return act >= DTP_ACT_NONE && act <= DTP_ACT_RELU; }

@@ -173,7 +173,7 @@ static int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t strea
 constexpr float kSignShare = 1.9557774e-8f;      // 21/16 2^-26
 
 // Upper bounds of the 2-norms of T rows of X, then of N rows of W: a warp per row, fp32 sums of squares, with a power of two taken
-// out where they leave fp32's range; a 32nd covers their roundings (K / 32 additions a lane, K to 2^24, and the root halves
+// out where they leave fp32's range; a 128th covers their roundings (K / 32 additions a lane, K to 2^20, and the root halves
 // the error).  Two bytes a row, rounded up.  A row of zeros gives 0, one with an infinity an infinity, a NaN a NaN.
 __global__ void __launch_bounds__(256)
 row_norms_kernel(const __nv_bfloat16* X, int64_t ldx, int64_t T, const __nv_bfloat16* W, int64_t ldw, int N, int K,
@@ -205,7 +205,7 @@ row_norms_kernel(const __nv_bfloat16* X, int64_t ldx, int64_t T, const __nv_bflo
             back = s < 8.271806e-25f ? 7.888609e-31f : 1.2676506e30f;            // 2^-100, 2^100
             s = squares(1.0f / back);
         }
-        if (lane == 0) norms[i] = __float2bfloat16_ru(1.03125f * sqrtf(s) * back);
+        if (lane == 0) norms[i] = __float2bfloat16_ru(1.0078125f * sqrtf(s) * back);
     }
 }
 
@@ -358,6 +358,20 @@ repitch_kernel(const uint16_t* src, int64_t rows, int cols, int64_t pitch, uint1
     }
 }
 
+// The runs' sums of a weight gradient (see kRun), added in their order.
+template <typename E>
+__global__ void __launch_bounds__(256)
+sum_runs_kernel(const float* runs, int64_t count, int64_t values, E* out) {
+    grid_wait();
+    grid_release();
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < values; i += gridDim.x * 256ll) {
+        double s = 0.0;
+#pragma unroll 4
+        for (int64_t r = 0; r < count; ++r) s += static_cast<double>(runs[r * values + i]);
+        out[i] = from_f32<E>(static_cast<float>(s));
+    }
+}
+
 // Pieces of a workspace, in the order in which they are asked for.
 struct Carver {
     uint8_t* base;
@@ -439,6 +453,40 @@ struct Call {
     }
 };
 
+// The weights' gradients are sums over the tokens, of which there may be 2^31, and an fp32 accumulator loses about 2^-26 of its sum for
+// every 16 of them on the tensor cores (it cuts off: 10% of a sum of 2^26 terms of one sign) and what rounding leaves on the
+// CUDA cores (0.1%).  So such a sum is made in runs of at most 2^18 tokens (2^-12), each a product of its own whose fp32 sums go
+// to the workspace, and the runs are added in 64 bits.
+constexpr int64_t kRun = 1 << 18;
+static size_t runs_bytes(int64_t T, int64_t rows, int64_t cols) {
+    return T > kRun ? static_cast<size_t>((T + kRun - 1) / kRun) * rows * cols * sizeof(float) : 0;
+}
+
+// out [rows, cols] = sum over T tokens of A's rows times B's columns, both stored token by token
+static int weight_gradient(Call& call, const Also& w, int64_t T, float* runs) {
+    const int64_t values = w.M * w.N, count = T > kRun ? (T + kRun - 1) / kRun : 1;
+    for (int64_t r = 0; r < count; ++r) {
+        const int64_t t0 = r * kRun;
+        auto from = [&](const Mat& m) {
+            return by_col(static_cast<const uint8_t*>(m.p) + static_cast<size_t>(t0 * m.ks) * elem(call.dtype), m.ks);
+        };
+        Product p;
+        p.A[0] = count > 1 ? from(w.A) : w.A;
+        p.B[0] = count > 1 ? from(w.B) : w.B;
+        p.M = w.M, p.N = w.N, p.K = count > 1 && T - t0 > kRun ? kRun : T - t0;
+        p.epi.out = w.out, p.epi.ldo = w.ldo, p.epi.M = w.M, p.epi.N = w.N;
+        if (count > 1) p.epi.Z = runs + r * values;
+        const int st = call.run(p);
+        if (st != DTP_OK) return st;
+    }
+    if (count == 1) return DTP_OK;
+    const int64_t blocks = (values + 255) / 256 < 8192 ? (values + 255) / 256 : 8192;
+    return call.dtype == DTP_BF16 ? launch_after(sum_runs_kernel<__nv_bfloat16>, blocks, call.stream, static_cast<const float*>(runs),
+                                                 count, values, static_cast<__nv_bfloat16*>(w.out))
+                                  : launch_after(sum_runs_kernel<float>, blocks, call.stream, static_cast<const float*>(runs), count,
+                                                 values, static_cast<float*>(w.out));
+}
+
 // ------------------------------------------------------------------------------- linear layer
 
 size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) {
@@ -449,6 +497,7 @@ size_t linear_workspace_bytes(int64_t T, int K, int N, int dtype, int backward) 
     if (backward) {
         c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
         c.take(static_cast<size_t>(chunks_of(T)) * N * sizeof(float));
+        c.take(runs_bytes(T, N, K));
     }
     return c.used;
 }
@@ -537,12 +586,9 @@ int linear_backward(const void* dY, const void* X, const void* W, const float* Z
     if (dW) {
         Rows x;
         if ((st = aligned_rows(X, T, K, dtype, c, stream, &x)) != DTP_OK) return st;
-        Product p;
-        p.A[0] = by_col(g, ldz);
-        p.B[0] = by_col(x.p, x.ld);
-        p.M = N, p.N = K, p.K = T;
-        p.epi.out = dW, p.epi.ldo = K, p.epi.M = N, p.epi.N = K;
-        if ((st = call.run(p)) != DTP_OK) return st;
+        auto* runs = static_cast<float*>(c.take(runs_bytes(T, N, K)));
+        st = weight_gradient(call, Also{by_col(g, ldz), by_col(x.p, x.ld), N, K, dW, K}, T, runs);
+        if (st != DTP_OK) return st;
     }
     return call.done();
 }
@@ -558,6 +604,7 @@ size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward) {
     if (backward) {
         c.take(static_cast<size_t>(T) * padded(N) * elem(dtype));
         c.take(repitch_bytes(T, d, dtype));
+        c.take(runs_bytes(T, N, d));
     }
     return c.used;
 }
@@ -634,7 +681,6 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
         p.epi.out = dX, p.epi.ldo = d, p.epi.M = T, p.epi.N = d;
         if ((st = call.run(p)) != DTP_OK) return st;
     }
-    // the weights' gradients share their K: one launch for all that are wanted (bf16), so that their tiles fill the rounds
     Also w[3];
     int count = 0;
     auto weight = [&](const void* a, int64_t lda, int64_t rows, const void* b, int64_t ldb, int cols, void* out) {
@@ -643,19 +689,21 @@ int gated_backward(const void* dY, const void* X, const void* Wg, const void* Wu
     weight(dg, ld, N, x.p, x.ld, d, dWg);
     weight(du, ld, N, x.p, x.ld, d, dWu);
     weight(dy.p, dy.ld, d, H, ld, N, dWd);
-    const bool together = dtype == DTP_BF16 && T > 0;
-    for (int i = 0; i < count; i += together ? count : 1) {
+    // they share their K: one launch for all that are wanted (bf16), so that their tiles fill the rounds
+    if (dtype == DTP_BF16 && T > 0 && T <= kRun && count > 0) {
         Product p;
-        p.A[0] = w[i].A;
-        p.B[0] = w[i].B;
-        p.M = w[i].M, p.N = w[i].N, p.K = T;
-        p.epi.out = w[i].out, p.epi.ldo = w[i].ldo, p.epi.M = w[i].M, p.epi.N = w[i].N;
-        if (together) {
-            p.batch = count;
-            for (int j = 1; j < count; ++j) p.also[j - 1] = w[j];
-        }
+        p.A[0] = w[0].A;
+        p.B[0] = w[0].B;
+        p.M = w[0].M, p.N = w[0].N, p.K = T;
+        p.epi.out = w[0].out, p.epi.ldo = w[0].ldo, p.epi.M = w[0].M, p.epi.N = w[0].N;
+        p.batch = count;
+        for (int j = 1; j < count; ++j) p.also[j - 1] = w[j];
         if ((st = call.run(p)) != DTP_OK) return st;
+        return call.done();
     }
+    auto* runs = static_cast<float*>(c.take(runs_bytes(T, N, d)));
+    for (int i = 0; i < count; ++i)
+        if ((st = weight_gradient(call, w[i], T, runs)) != DTP_OK) return st;
     return call.done();
 }
 

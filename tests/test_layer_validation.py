@@ -114,3 +114,24 @@ def test_clip_rejects_before_launch(lib):
     assert lib.dtp_clip_grad_norm_workspace_size(1, None, ctypes.byref(n)) == -1
     assert lib.dtp_clip_grad_norm_workspace_size(3000, (ctypes.c_int64 * 3000)(*[7] * 3000), ctypes.byref(n)) == 0
     assert n.value >= 256
+
+
+@pytest.mark.parametrize("fn", ["dtp_linear_workspace_size", "dtp_gated_ffn_workspace_size"])
+def test_widths_whose_sums_one_accumulator_holds(lib, fn):
+    """2^20 terms lose about 2^-10 of their sum in one accumulator; wider sums are refused."""
+    n = ctypes.c_size_t(0)
+    for K, N, want in ((1 << 20, 8, 0), (8, 1 << 20, 0), ((1 << 20) + 1, 8, -1), (8, (1 << 20) + 1, -1)):
+        assert getattr(lib, fn)(4, K, N, dtp.DTP_BF16, 1, ctypes.byref(n)) == want
+    assert lib.dtp_gated_ffn_saved_size(4, (1 << 20) + 1, ctypes.byref(n)) == -1
+
+
+def test_workspace_of_long_sums(lib):
+    """A slot of fp32 sums for every 2^18 tokens of a weight gradient, none below."""
+    def bytes_of(fn, T, K, N):
+        return dtp._size_query(fn, T, K, N, dtp.DTP_F32, 1)
+
+    T, K, N = 3 << 18, 24, 40
+    for fn, per_token in (("dtp_linear_workspace_size", 4 * N + N / 8), ("dtp_gated_ffn_workspace_size", 8 * N)):
+        more = bytes_of(fn, T, K, N) - T * per_token
+        assert 3 * K * N * 4 <= more <= 3 * K * N * 4 + 5 * 256
+        assert bytes_of(fn, 1 << 18, K, N) - (1 << 18) * per_token <= 5 * 256
