@@ -146,6 +146,8 @@ def _check(fn: str, status: int):
 # The raw handle of a device's current stream: building a torch.cuda.Stream for it takes 3 us of every
 # call.  Not a documented name, so the documented way stays for a torch without it.
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# The current device's index, where CUDA is known to be initialised (there are tensors on it).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream=None) -> int:
@@ -851,9 +853,14 @@ def _layer_check(name: str, t: torch.Tensor, shape, dtype, index: int):
 
 
 def _layer_stream(stream, index: int) -> int:
-    """The raw handle of ``stream``, or of device ``index``'s current one."""
-    if stream is None and _current_raw_stream is not None:
-        return _current_raw_stream(index)
+    """The raw handle of ``stream``, or of the current one.  The library launches on the current device, which has to be the
+    tensors' and the stream's."""
+    if index != _current_device():
+        raise ValueError(f"the tensors are on cuda:{index}, the current device is cuda:{_current_device()}")
+    if stream is None:
+        return _current_raw_stream(index) if _current_raw_stream is not None else _stream()
+    if stream.device_index != index:
+        raise ValueError(f"stream must be on cuda:{index}, got cuda:{stream.device_index}")
     return _stream(stream)
 
 

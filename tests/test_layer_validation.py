@@ -1,6 +1,7 @@
 """Host-side checks of the layer operators and of gradient clipping, in the binding and at the C ABI, before any CUDA
 call (no GPU needed)."""
 import ctypes
+import types
 
 import pytest
 import torch
@@ -135,3 +136,15 @@ def test_workspace_of_long_sums(lib):
         more = bytes_of(fn, T, K, N) - T * per_token
         assert 3 * K * N * 4 <= more <= 3 * K * N * 4 + 5 * 256
         assert bytes_of(fn, 1 << 18, K, N) - (1 << 18) * per_token <= 5 * 256
+
+
+def test_tensors_and_streams_of_another_device(monkeypatch):
+    """The library launches on the current device: tensors or a stream of another one are refused."""
+    monkeypatch.setattr(dtp, "_current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        dtp._layer_stream(None, 1)
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        dtp._layer_stream(types.SimpleNamespace(device_index=1, cuda_stream=16), 1)
+    with pytest.raises(ValueError, match="stream must be on cuda:0"):
+        dtp._layer_stream(types.SimpleNamespace(device_index=1, cuda_stream=16), 0)
+    assert dtp._layer_stream(types.SimpleNamespace(device_index=0, cuda_stream=16), 0) == 16
