@@ -852,6 +852,12 @@ def _layer_check(name: str, t: torch.Tensor, shape, dtype, index: int):
     raise ValueError(f"{name} must be a contiguous CUDA tensor on the inputs' device")
 
 
+def _workspace_check(t: torch.Tensor, index: int):
+    """``t`` is a workspace whose size in bytes is its numel, on device ``index``."""
+    if not (t.dtype is torch.uint8 and t.get_device() == index and t.is_contiguous()):
+        raise ValueError("workspace must be a contiguous uint8 tensor on the inputs' device")
+
+
 def _layer_stream(stream, index: int) -> int:
     """The raw handle of ``stream``, or of the current one.  The library launches on the current device, which has to be the
     tensors' and the stream's."""
@@ -914,6 +920,8 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, r
     Z = _keep(torch.empty((T, N), dtype=torch.float32, device=X.device), stream) if save else None
     if workspace is None:
         workspace = _keep(linear_workspace(T, K, N, dtype, X.device), stream)
+    else:
+        _workspace_check(workspace, index)
     st = lib().dtp_linear(X.data_ptr(), W.data_ptr(), _ptr(bias), _ptr(residual), T, K, N, act, code, Y.data_ptr(),
                           _ptr(Z), workspace.data_ptr(), workspace.numel(), _layer_stream(stream, index))
     if st:
@@ -941,6 +949,8 @@ def linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: torch
     db = _keep(torch.empty(N, dtype=X.dtype, device=X.device), stream) if bias else None
     if workspace is None:
         workspace = _keep(linear_workspace(T, K, N, dtype, X.device, backward=True), stream)
+    else:
+        _workspace_check(workspace, index)
     _check("dtp_linear_backward",
            lib().dtp_linear_backward(_ptr(dY), _ptr(X), _ptr(W), _ptr(Z), T, K, N, act, code, _ptr(dX), _ptr(dW),
                                      _ptr(db), _ptr(workspace), workspace.numel(), _layer_stream(stream, index)))
@@ -995,6 +1005,8 @@ def gated_ffn(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down:
         pre = _keep(torch.empty(n, dtype=torch.float32, device=X.device), stream)
     if workspace is None:
         workspace = _keep(gated_ffn_workspace(T, d, N, dtype, X.device), stream)
+    else:
+        _workspace_check(workspace, index)
     st = lib().dtp_gated_ffn(X.data_ptr(), W_gate.data_ptr(), W_up.data_ptr(), W_down.data_ptr(), _ptr(residual), T, d, N,
                              act, code, Y.data_ptr(), _ptr(H), _ptr(pre), workspace.data_ptr(), workspace.numel(),
                              _layer_stream(stream, index))
@@ -1020,6 +1032,8 @@ def gated_ffn_backward(dY: torch.Tensor, X: torch.Tensor, W_gate: torch.Tensor, 
     dX, dWg, dWu, dWd = (_keep(torch.empty_like(t), stream) for t in (X, W_gate, W_up, W_down))
     if workspace is None:
         workspace = _keep(gated_ffn_workspace(T, d, N, dtype, X.device, backward=True), stream)
+    else:
+        _workspace_check(workspace, index)
     _check("dtp_gated_ffn_backward",
            lib().dtp_gated_ffn_backward(_ptr(dY), _ptr(X), _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(H), _ptr(pre),
                                         T, d, N, act, code, _ptr(dX), _ptr(dWg), _ptr(dWu), _ptr(dWd),
@@ -1081,6 +1095,8 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
         raise ValueError("norm must be one fp32 value on the gradients' device")
     if workspace is None:
         workspace = _keep(_clip_workspace(numel, grads[0].device), stream)
+    else:
+        _workspace_check(workspace, index)
     st = lib().dtp_clip_grad_norm(src.buffer_info()[0], None if dst is None else dst.buffer_info()[0],
                                   numel.buffer_info()[0], codes.buffer_info()[0], count, float(max_norm), _ptr(norm),
                                   _ptr(workspace), workspace.numel(), _layer_stream(stream, index))

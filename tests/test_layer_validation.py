@@ -148,3 +148,10 @@ def test_tensors_and_streams_of_another_device(monkeypatch):
     with pytest.raises(ValueError, match="stream must be on cuda:0"):
         dtp._layer_stream(types.SimpleNamespace(device_index=1, cuda_stream=16), 0)
     assert dtp._layer_stream(types.SimpleNamespace(device_index=0, cuda_stream=16), 0) == 16
+
+
+def test_workspaces_that_are_none():
+    """Anything but bytes on the inputs' device: its pointer and its number of elements go to the library as they are."""
+    for t in (torch.empty(4096, dtype=torch.uint8), torch.empty(4096, dtype=torch.uint8, device="meta")):
+        with pytest.raises(ValueError, match="workspace must be"):
+            dtp._workspace_check(t, 0)
