@@ -852,6 +852,12 @@ def _layer_check(name: str, t: torch.Tensor, shape, dtype, index: int):
     raise ValueError(f"{name} must be a contiguous CUDA tensor on the inputs' device")
 
 
+def _widths_check(*widths: int):
+    """Widths are C ints, into which ctypes would fold larger ones."""
+    if max(widths) > 0x7FFFFFFF:
+        raise ValueError(f"widths must be below 2^31, got {max(widths)}")
+
+
 def _workspace_check(t: torch.Tensor, index: int):
     """``t`` is a workspace whose size in bytes is its numel, on device ``index``."""
     if not (t.dtype is torch.uint8 and t.get_device() == index and t.is_contiguous()):
@@ -883,6 +889,7 @@ def _size_query(fn: str, *args) -> int:
 
 def linear_workspace(T: int, K: int, N: int, dtype: torch.dtype, device, backward: bool = False) -> torch.Tensor:
     """A device workspace for linear (and, with ``backward``, linear_backward) of these sizes."""
+    _widths_check(K, N)
     n = _size_query("dtp_linear_workspace_size", T, K, N, _torch_code(dtype), int(backward))
     return torch.empty(n, dtype=torch.uint8, device=device)
 
@@ -893,6 +900,7 @@ def _linear_shapes(X, W):
         raise ValueError("shapes must be X [T,K], W [N,K]")
     T, K = shape = X.shape
     N, dtype, index = W.shape[0], X.dtype, X.get_device()
+    _widths_check(K, N)
     _layer_check("X", X, shape, dtype, index)
     _layer_check("W", W, (N, K), dtype, index)
     return T, K, N, dtype, index
@@ -959,6 +967,7 @@ def linear_backward(dY: torch.Tensor, X: torch.Tensor, W: torch.Tensor, Z: torch
 
 def gated_ffn_workspace(T: int, d: int, N: int, dtype: torch.dtype, device, backward: bool = False) -> torch.Tensor:
     """A device workspace for gated_ffn (and, with ``backward``, gated_ffn_backward) of these sizes."""
+    _widths_check(d, N)
     n = _size_query("dtp_gated_ffn_workspace_size", T, d, N, _torch_code(dtype), int(backward))
     return torch.empty(n, dtype=torch.uint8, device=device)
 
@@ -969,6 +978,7 @@ def _gated_shapes(X, W_gate, W_up, W_down):
         raise ValueError("shapes must be X [T,d], W_gate/W_up [N,d], W_down [d,N]")
     T, d = shape = X.shape
     N, dtype, index = W_gate.shape[0], X.dtype, X.get_device()
+    _widths_check(d, N)
     _layer_check("X", X, shape, dtype, index)
     _layer_check("W_gate", W_gate, (N, d), dtype, index)
     _layer_check("W_up", W_up, (N, d), dtype, index)

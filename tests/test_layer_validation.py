@@ -155,3 +155,21 @@ def test_workspaces_that_are_none():
     for t in (torch.empty(4096, dtype=torch.uint8), torch.empty(4096, dtype=torch.uint8, device="meta")):
         with pytest.raises(ValueError, match="workspace must be"):
             dtp._workspace_check(t, 0)
+
+
+def test_widths_that_are_no_c_int(lib):
+    """2^32 + 8 columns are not 8."""
+    wide = (1 << 32) + 8
+    for fn in (dtp.linear_workspace, dtp.gated_ffn_workspace):
+        for K, N in ((wide, 8), (8, wide), (1 << 31, 8)):
+            with pytest.raises(ValueError, match="below 2\\^31"):
+                fn(4, K, N, torch.bfloat16, "cpu")
+
+    def meta(*shape):
+        return torch.empty(shape, dtype=torch.bfloat16, device="meta")
+
+    for K, N in ((wide, 8), (8, wide)):
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            dtp.linear(meta(4, K), meta(N, K))
+        with pytest.raises(ValueError, match="below 2\\^31"):
+            dtp.gated_ffn(meta(4, K), meta(N, K), meta(N, K), meta(K, N))
