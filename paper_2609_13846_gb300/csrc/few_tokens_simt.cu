@@ -230,10 +230,11 @@ static int launch_typed(const Product& p, int* status, int second, cudaStream_t 
     return DTP_ERR_UNSUPPORTED;
 }
 
-// Whether this kernel takes the product: both operands with k contiguous, and few tokens.  bf16, one token and two: 4096 x 4096
-// 7.5 and 8.1 us here, 7.8 on the tensor cores for three, 1024 x 3072 3.0 and 3.4, and 3.5 (before the tensor-core form took two
-// k blocks a stage, 4.1); from three tokens on the tensor cores win.  fp32, up to 32: 4096 x 4096 12 us for one token (5.4
-// TB/s), 50 for 32, 61 in the tiles.
+// Whether this kernel takes the product: both operands with k contiguous, and few tokens.  bf16, one token and two, this kernel and the
+// tensor cores: the block of 1024 x 3072 8.5 and 9.3 us for one (weights in L2 6.7 and 7.5), 7.4 and 7.7 for two (in L2);
+// a layer of 4096 x 4096 by itself 5.3 and 6.0 us for one with the weights in L2, 8.3 and 7.8 from HBM, for two 6.1 and 6.0, 8.7
+// and 8.0; odd widths are read here as they are, without a copy.  From three tokens on the tensor cores win.  fp32, up to 32:
+// 4096 x 4096 12.6 us for one token (5.3 TB/s), 49 for 32, 62 in the tiles for 33.
 bool takes(const Product& p, int dtype) {
     return p.M <= (dtype == DTP_BF16 ? 2 : 32) && p.segments == 1 && p.A[0].ks == 1 && p.B[0].ks == 1 &&
            p.epi.kind != kEpiGatedGrad;
