@@ -216,7 +216,7 @@ struct Dot {
     int K, words;            // words of eight that may be loaded at once
     float fp32, carried, least;
     __device__ __forceinline__ Dot(int K, bool wide) : K(K), words(wide ? K / 8 : 0) {
-        const float most = (K + 31) / 32;                                    // a lane's terms
+        const float most = (K + 31) / 32 + 8;                                // a lane's terms, of which a word has eight
         fp32 = (K / (wide ? 256 : 32) + 24.0f) * 5.9604645e-8f;              // 2^-24: a sum's additions, then the tree's
         carried = most * most * 3.5527137e-15f;                              // 2^-48: the errors' own roundings
         least = K * 1.4012985e-45f;                                          // among fp32's subnormal numbers
