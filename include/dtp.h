@@ -9,7 +9,9 @@
  *      and neuron assignments ("Objective", "Optimiser"),
  *   3. the linear layer and the gated feed-forward block, forward and
  *      backward, and gradient clipping: calibration, serving and distillation
- *      (Sec. 4) of the permuted layers.
+ *      (Sec. 4) of the permuted layers,
+ *   4. what else a training step of them takes: the RMS norm, the loss over
+ *      the vocabulary and the AdamW update.
  *
  * Conventions for every entry point:
  *   - Tensor arguments are DEVICE pointers owned by the caller; the library
@@ -718,6 +720,123 @@ int dtp_gated_ffn_backward(const void* dY, const void* X, const void* W_gate, co
 int dtp_clip_grad_norm_workspace_size(int count, const int64_t* numel, size_t* bytes);
 int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t* numel, const int* dtypes, int count,
                        float max_norm, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* 4. Norm, loss and update of a training step (Sec. 4)                       */
+/* ------------------------------------------------------------------------ */
+
+/*
+ * Sizes as in part 3: 0 <= T <= 2^31 - 256, widths 1 <= . <= 2^20.  The
+ * tensors of the norm and of the update, and the vectors over tokens, need
+ * only be aligned to their elements (views into larger ones are fine).
+ * Deterministic: no floating-point atomics.  Asynchronous.
+ *
+ * RMS norm of rows:
+ *     rms_t = sqrt(mean_i x_ti^2 + eps),  y_ti = gamma_i x_ti / rms_t
+ *   X     [T, d], Y [T, d] out (may be X): dtype
+ *   gamma [d] fp32
+ *   eps   > 0
+ *   rms   [T] fp32 out, or NULL: what dtp_rms_norm_backward and
+ *         dtp_head_writes take
+ * Sums in fp32, the output rounded once.  A row whose squares leave fp32's
+ * range is summed at a smaller scale.  T == 0 returns DTP_OK.
+ */
+int dtp_rms_norm(const void* X, const float* gamma, int64_t T, int d, float eps, int dtype, void* Y, float* rms,
+                 void* stream);
+
+/*
+ * Gradients of dtp_rms_norm for dY [T, d], with n = x / rms, dn = gamma dY:
+ *     dX = (dn - n mean_i(dn n)) / rms + dresidual,  dgamma_i = sum_t dY_ti n_ti
+ *   rms       [T] as dtp_rms_norm wrote it
+ *   dresidual [T, d] or NULL: a gradient of X by another way (a residual stream's)
+ *   dX        [T, d] out or NULL (may be dY or dresidual)
+ *   dgamma    [d] fp32 out or NULL
+ * T == 0 writes zeros to dgamma and reads no input.  Workspace from
+ * dtp_rms_norm_backward_workspace_size.
+ */
+int dtp_rms_norm_backward_workspace_size(int64_t T, int d, size_t* bytes);
+int dtp_rms_norm_backward(const void* dY, const void* X, const float* gamma, const float* rms, const void* dresidual,
+                          int64_t T, int d, int dtype, void* dX, float* dgamma, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Softmax cross entropy over a vocabulary, from the hidden states:
+ *     z_t = W x_t,  lse_t = log sum_v exp z_tv,  loss_t = lse_t - z_t[targets_t]
+ *   X       [T, d] hidden states, W [V, d] the output layer's rows: dtype,
+ *           16-byte aligned
+ *   targets [T] int64: token ids, or ignore_index (any value) for tokens that do
+ *           not count: their loss is 0
+ *   loss    [T] fp32 out;  lse [T] fp32 out (of every token)
+ * The logits are made in pieces and not kept.  A target outside [0, V) that is
+ * not ignore_index is reported as DTP_ERR_ARG through the workspace status word;
+ * its loss is NaN.  T == 0 returns DTP_OK.  Workspace from
+ * dtp_linear_cross_entropy_workspace_size (backward: nonzero for the size that
+ * both directions need).
+ */
+int dtp_linear_cross_entropy_workspace_size(int64_t T, int d, int V, int dtype, int backward, size_t* bytes);
+int dtp_linear_cross_entropy(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V,
+                             int64_t ignore_index, int dtype, float* loss, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum_t dloss_t loss_t:
+ *     dz_t = dloss_t (exp(z_t - lse_t) - onehot(targets_t)),  dX = dZ W,  dW = dZ^T X
+ *   dloss [T] fp32;  lse [T] as dtp_linear_cross_entropy wrote it
+ *   dX    [T, d], dW [V, d]: each out or NULL
+ * dZ is rounded once to dtype before the products.  Tokens that do not count
+ * (and targets out of range, reported as in the forward direction) have zero
+ * rows in dX and add nothing to dW, whatever stands in their rows of X and in
+ * dloss.  T == 0 writes zeros to dW.
+ */
+int dtp_linear_cross_entropy_backward(const float* dloss, const void* X, const void* W, const int64_t* targets,
+                                      const float* lse, int64_t T, int d, int V, int64_t ignore_index, int dtype,
+                                      void* dX, void* dW, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One AdamW step over many tensors:
+ *     t = *step + 1;  g = c grad, c = max_norm / norm where norm > max_norm, else 1
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     p = (1 - lr weight_decay) p - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *     *step = t
+ *   params       host array of `count` device pointers, updated; param_dtypes
+ *                (host): DTP_F32 or DTP_BF16 each.  bf16 ones are rounded up or
+ *                down with the probability of the distance, so that updates
+ *                below half a step are not lost
+ *   grads        host array of device pointers; grad_dtypes (host)
+ *   m, v         host arrays of device pointers, updated.  state_bits 32: fp32
+ *                moments.  state_bits 8: e4m3 codes, of m and of sqrt(v), of
+ *                blocks of 256 consecutive elements whose scales (largest
+ *                size / 448) are in m_scale and v_scale (host arrays of device
+ *                pointers to ceil(numel / 256) floats; NULL with 32 bits).
+ *                Codes are rounded up with the probability of the distance (a
+ *                hash of element and step: the same every time), a v above 0 is
+ *                never held as 0, what is not finite is held as NaN, and
+ *                blocks whose largest size is below 2^-100 as zeros
+ *   copies       NULL, or host array of device pointers, each NULL or to bf16
+ *                out: the updated parameters, rounded to the nearest (fp32
+ *                parameters only)
+ *   numel        host array: elements of each (0 allowed, pointers may be NULL)
+ *   opts         read on the host before the call returns
+ *   lr           device fp32, or NULL: the rate of opts
+ *   norm         device fp32, or NULL (c = 1): the gradients' global norm
+ *                (dtp_clip_grad_norm's).  One that is not finite leaves
+ *                everything as it is, the counter too
+ *   step         device int64: steps done, counted up
+ * No two tensors overlap.  The host arrays are read before the call returns.
+ * At most 2^46 elements in all.
+ */
+typedef struct dtp_adamw_opts {
+    double lr, beta1, beta2;     /* lr finite; 0 <= beta < 1 */
+    double eps, weight_decay;    /* eps > 0 (2^-126 or more in fp32); weight_decay finite */
+    double max_norm;             /* >= 0, may be infinite */
+    int state_bits;              /* 32 or 8 */
+    int reserved[5];             /* zero */
+} dtp_adamw_opts;
+int dtp_adamw_workspace_size(int count, const int64_t* numel, size_t* bytes);
+int dtp_adamw(void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes,
+              void* const* m, void* const* v, float* const* m_scale, float* const* v_scale, void* const* copies,
+              const int64_t* numel, int count, const dtp_adamw_opts* opts, const float* lr, const float* norm,
+              int64_t* step, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -3,6 +3,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+
 #include "dtp_common.cuh"
 
 namespace dtp {
@@ -49,6 +51,21 @@ int launch_layout(const int32_t* head_part, const int32_t* neuron_dev, int layer
                   int q_per_group, int head_dim, int d, int elem_bytes, const void* const* src, void* const* dst,
                   int32_t* head_order, int32_t* neuron_order, void* workspace, cudaStream_t stream);
 }  // namespace apply
+namespace norm {
+size_t backward_workspace_bytes(int64_t T, int d);
+int launch_forward(const void* X, const float* gamma, int64_t T, int d, float eps, int dtype, void* Y, float* rms,
+                   cudaStream_t stream);
+int launch_backward(const void* dY, const void* X, const float* gamma, const float* rms, const void* dres, int64_t T, int d,
+                    int dtype, void* dX, float* dgamma, void* workspace, cudaStream_t stream);
+}  // namespace norm
+namespace adamw {
+bool sizes_ok(int count, const int64_t* numel);
+size_t workspace_bytes();
+int launch(void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes, void* const* m,
+           void* const* v, float* const* m_scale, float* const* v_scale, void* const* copies, const int64_t* numel, int count,
+           const dtp_adamw_opts* opts, const float* lr, const float* norm, int64_t* step, void* workspace,
+           cudaStream_t stream);
+}  // namespace adamw
 int launch_finalize(float* A, int G, int N, int64_t T_total, const float* wd, cudaStream_t stream);
 int launch_top_share(const float* A, int layers, int G, int N, double* share, cudaStream_t stream);
 int launch_down_finalize(const float* act2, const float* bn, int G, int N, int64_t T_total, float* S,
@@ -77,6 +94,11 @@ int linear_forward(const void* X, const void* W, const void* bias, const void* r
                    int act, int dtype, void* Y, float* Z, void* workspace, cudaStream_t stream);
 int linear_backward(const void* dY, const void* X, const void* W, const float* Z, int64_t T, int K, int N, int act,
                     int dtype, void* dX, void* dW, void* dbias, void* workspace, cudaStream_t stream);
+size_t loss_workspace_bytes(int64_t T, int d, int V, int dtype, int backward);
+int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V, int64_t ignore, int dtype,
+                 float* loss, float* lse, void* workspace, cudaStream_t stream);
+int loss_backward(const float* dloss, const void* X, const void* W, const int64_t* targets, const float* lse, int64_t T, int d,
+                  int V, int64_t ignore, int dtype, void* dX, void* dW, void* workspace, cudaStream_t stream);
 size_t gated_workspace_bytes(int64_t T, int d, int N, int dtype, int backward);
 size_t gated_saved_bytes(int64_t T, int N);
 int gated_forward(const void* X, const void* Wg, const void* Wu, const void* Wd, const void* residual, int64_t T,
@@ -141,6 +163,11 @@ bool layer_sizes_ok(int64_t T, int K, int N, int dtype) {
 }
 
 bool act_ok(int act) { return act >= DTP_ACT_NONE && act <= DTP_ACT_RELU; }
+
+// An argument that need only be aligned to its elements.
+bool elem_ok(const void* p, size_t bytes, bool needed = true) {
+    return p ? (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0 : !needed;
+}
 
 // A tensor argument: set unless it may be left out, and on a 16-byte boundary.
 bool arg_ok(const void* p, bool needed = true) { return p ? aligned16(p) : !needed; }
@@ -644,6 +671,104 @@ int dtp_clip_grad_norm(const void* const* grads, void* const* out, const int64_t
     if (!workspace_ok(workspace, workspace_bytes, clip::workspace_bytes(count))) return DTP_ERR_WORKSPACE;
     return clip::launch(grads, out, numel, dtypes, count, max_norm, norm, workspace,
                         static_cast<cudaStream_t>(stream));
+}
+
+int dtp_rms_norm(const void* X, const float* gamma, int64_t T, int d, float eps, int dtype, void* Y, float* rms,
+                 void* stream) {
+    if (!layer_sizes_ok(T, d, 1, dtype) || !(eps >= 1.17549435e-38f && eps <= 3.4e38f)) return DTP_ERR_ARG;
+    if (T == 0) return DTP_OK;
+    const size_t e = dtype == DTP_BF16 ? 2 : 4;
+    if (!elem_ok(X, e) || !elem_ok(gamma, 4) || !elem_ok(Y, e) || !elem_ok(rms, 4, false)) return DTP_ERR_ARG;
+    return norm::launch_forward(X, gamma, T, d, eps, dtype, Y, rms, static_cast<cudaStream_t>(stream));
+}
+
+int dtp_rms_norm_backward_workspace_size(int64_t T, int d, size_t* bytes) {
+    if (!bytes || !layer_sizes_ok(T, d, 1, DTP_F32)) return DTP_ERR_ARG;
+    *bytes = norm::backward_workspace_bytes(T, d);
+    return DTP_OK;
+}
+
+int dtp_rms_norm_backward(const void* dY, const void* X, const float* gamma, const float* rms, const void* dresidual,
+                          int64_t T, int d, int dtype, void* dX, float* dgamma, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+    if (!layer_sizes_ok(T, d, 1, dtype)) return DTP_ERR_ARG;
+    const size_t e = dtype == DTP_BF16 ? 2 : 4;
+    const bool some = T > 0;
+    if (!elem_ok(dY, e, some) || !elem_ok(X, e, some) || !elem_ok(gamma, 4, some && dX) || !elem_ok(rms, 4, some) ||
+        !elem_ok(dresidual, e, false) || !elem_ok(dX, e, false) || !elem_ok(dgamma, 4, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, norm::backward_workspace_bytes(T, d))) return DTP_ERR_WORKSPACE;
+    return norm::launch_backward(dY, X, gamma, rms, dresidual, T, d, dtype, dX, dgamma, workspace,
+                                 static_cast<cudaStream_t>(stream));
+}
+
+int dtp_linear_cross_entropy_workspace_size(int64_t T, int d, int V, int dtype, int backward, size_t* bytes) {
+    if (!bytes || !layer_sizes_ok(T, d, V, dtype)) return DTP_ERR_ARG;
+    *bytes = layer::loss_workspace_bytes(T, d, V, dtype, backward);
+    return DTP_OK;
+}
+
+int dtp_linear_cross_entropy(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V,
+                             int64_t ignore_index, int dtype, float* loss, float* lse, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    if (!layer_sizes_ok(T, d, V, dtype)) return DTP_ERR_ARG;
+    if (T == 0) return DTP_OK;
+    if (!arg_ok(X) || !arg_ok(W) || !elem_ok(targets, 8) || !elem_ok(loss, 4) || !elem_ok(lse, 4)) return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::loss_workspace_bytes(T, d, V, dtype, 0))) return DTP_ERR_WORKSPACE;
+    return layer::loss_forward(X, W, targets, T, d, V, ignore_index, dtype, loss, lse, workspace,
+                               static_cast<cudaStream_t>(stream));
+}
+
+int dtp_linear_cross_entropy_backward(const float* dloss, const void* X, const void* W, const int64_t* targets,
+                                      const float* lse, int64_t T, int d, int V, int64_t ignore_index, int dtype,
+                                      void* dX, void* dW, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!layer_sizes_ok(T, d, V, dtype)) return DTP_ERR_ARG;
+    const bool some = T > 0;
+    if (!elem_ok(dloss, 4, some) || !arg_ok(X, some) || !arg_ok(W, some) || !elem_ok(targets, 8, some) ||
+        !elem_ok(lse, 4, some) || !arg_ok(dX, false) || !arg_ok(dW, false))
+        return DTP_ERR_ARG;
+    if (!workspace_ok(workspace, workspace_bytes, layer::loss_workspace_bytes(T, d, V, dtype, 1))) return DTP_ERR_WORKSPACE;
+    return layer::loss_backward(dloss, X, W, targets, lse, T, d, V, ignore_index, dtype, dX, dW, workspace,
+                                static_cast<cudaStream_t>(stream));
+}
+
+int dtp_adamw_workspace_size(int count, const int64_t* numel, size_t* bytes) {
+    if (!bytes || count < 0 || (count > 0 && !numel) || !adamw::sizes_ok(count, numel)) return DTP_ERR_ARG;
+    *bytes = adamw::workspace_bytes();
+    return DTP_OK;
+}
+
+int dtp_adamw(void* const* params, const int* param_dtypes, const void* const* grads, const int* grad_dtypes,
+              void* const* m, void* const* v, float* const* m_scale, float* const* v_scale, void* const* copies,
+              const int64_t* numel, int count, const dtp_adamw_opts* opts, const float* lr, const float* norm,
+              int64_t* step, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!opts || count < 0 || (count > 0 && (!params || !param_dtypes || !grads || !grad_dtypes || !m || !v || !numel)))
+        return DTP_ERR_ARG;
+    const dtp_adamw_opts& o = *opts;
+    auto beta_ok = [](double b) { return b >= 0.0 && b < 1.0; };
+    if (!std::isfinite(o.lr) || !beta_ok(o.beta1) || !beta_ok(o.beta2) || !(o.eps >= 1.17549435e-38 && o.eps <= 3.4e38) ||
+        !std::isfinite(o.weight_decay) || !(o.max_norm >= 0.0) || (o.state_bits != 32 && o.state_bits != 8))
+        return DTP_ERR_ARG;
+    for (int r : o.reserved)
+        if (r) return DTP_ERR_ARG;
+    const bool eight = o.state_bits == 8;
+    if (eight && count > 0 && (!m_scale || !v_scale)) return DTP_ERR_ARG;
+    if (!adamw::sizes_ok(count, numel) || !elem_ok(step, 8) || !elem_ok(lr, 4, false) || !elem_ok(norm, 4, false))
+        return DTP_ERR_ARG;
+    auto size_of = [](int dtype) -> size_t { return dtype == DTP_BF16 ? 2 : 4; };
+    for (int i = 0; i < count; ++i) {
+        for (int dtype : {param_dtypes[i], grad_dtypes[i]})
+            if (dtype != DTP_BF16 && dtype != DTP_F32) return DTP_ERR_ARG;
+        if (numel[i] == 0) continue;
+        const size_t s = eight ? 1 : 4;
+        if (!elem_ok(params[i], size_of(param_dtypes[i])) || !elem_ok(grads[i], size_of(grad_dtypes[i])) ||
+            !elem_ok(m[i], s) || !elem_ok(v[i], s) || (eight && (!elem_ok(m_scale[i], 4) || !elem_ok(v_scale[i], 4))))
+            return DTP_ERR_ARG;
+        if (copies && copies[i] && (param_dtypes[i] != DTP_F32 || !elem_ok(copies[i], 2))) return DTP_ERR_ARG;
+    }
+    if (!workspace_ok(workspace, workspace_bytes, adamw::workspace_bytes())) return DTP_ERR_WORKSPACE;
+    return adamw::launch(params, param_dtypes, grads, grad_dtypes, m, v, m_scale, v_scale, copies, numel, count, opts, lr,
+                         norm, step, workspace, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

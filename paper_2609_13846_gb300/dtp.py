@@ -41,6 +41,12 @@ class AffinityOpts(ctypes.Structure):
     _fields_ = [("max_ctas", ctypes.c_int), ("flags", ctypes.c_int), ("reserved", ctypes.c_int * 6)]
 
 
+class AdamWOpts(ctypes.Structure):
+    """dtp_adamw_opts."""
+    _fields_ = [(k, ctypes.c_double) for k in ("lr", "beta1", "beta2", "eps", "weight_decay", "max_norm")] + \
+        [("state_bits", ctypes.c_int), ("reserved", ctypes.c_int * 5)]
+
+
 class DTPError(RuntimeError):
     """A libdtp call returned a non-zero dtp_status."""
 
@@ -113,7 +119,20 @@ def lib():
                                          _vp, _vp, _vp, _sz, _vp]
     L.dtp_clip_grad_norm_workspace_size.argtypes = [_i32, _vp, ctypes.POINTER(_sz)]
     L.dtp_clip_grad_norm.argtypes = [_vp, _vp, _vp, _vp, _i32, ctypes.c_float, _vp, _vp, _sz, _vp]
-    for fn in ("dtp_linear_workspace_size", "dtp_linear", "dtp_linear_backward", "dtp_gated_ffn_workspace_size",
+    L.dtp_rms_norm.argtypes = [_vp, _vp, _i64, _i32, ctypes.c_float, _i32, _vp, _vp, _vp]
+    L.dtp_rms_norm_backward_workspace_size.argtypes = [_i64, _i32, ctypes.POINTER(_sz)]
+    L.dtp_rms_norm_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.dtp_linear_cross_entropy_workspace_size.argtypes = [_i64, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]
+    L.dtp_linear_cross_entropy.argtypes = [_vp, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _sz, _vp]
+    L.dtp_linear_cross_entropy_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp,
+                                                    _sz, _vp]
+    L.dtp_adamw_workspace_size.argtypes = [_i32, _vp, ctypes.POINTER(_sz)]
+    L.dtp_adamw.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, ctypes.POINTER(AdamWOpts), _vp, _vp, _vp,
+                            _vp, _sz, _vp]
+    for fn in ("dtp_rms_norm", "dtp_rms_norm_backward_workspace_size", "dtp_rms_norm_backward",
+               "dtp_linear_cross_entropy_workspace_size", "dtp_linear_cross_entropy",
+               "dtp_linear_cross_entropy_backward", "dtp_adamw_workspace_size", "dtp_adamw",
+               "dtp_linear_workspace_size", "dtp_linear", "dtp_linear_backward", "dtp_gated_ffn_workspace_size",
                "dtp_gated_ffn_saved_size", "dtp_gated_ffn", "dtp_gated_ffn_backward",
                "dtp_clip_grad_norm_workspace_size", "dtp_clip_grad_norm",
                "dtp_search_chain_workspace_size", "dtp_search_chain", "dtp_search_chain_ex", "dtp_chain_score",
@@ -1112,3 +1131,272 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
                                   _ptr(workspace), workspace.numel(), _layer_stream(stream, index))
     _check("dtp_clip_grad_norm", st)
     return norm
+
+
+# ------------------------------------------------------ norm, loss and update of a training step (Sec. 4) --
+
+def _norm_shapes(X, gamma):
+    """(T, d, dtype, device index) of X [T,d] and gamma [d] fp32."""
+    if X.dim() != 2:
+        raise ValueError("X must be [T,d]")
+    T, d = shape = X.shape
+    dtype, index = X.dtype, X.get_device()
+    _widths_check(d)
+    _layer_check("X", X, shape, dtype, index)
+    _layer_check("gamma", gamma, (d,), torch.float32, index)
+    return T, d, dtype, index
+
+
+def rms_norm(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, Y: torch.Tensor | None = None, stream=None):
+    """(Y, rms): Y = gamma X / rms in X's dtype (bf16 or fp32), rms = sqrt(mean X^2 + eps) [T] fp32.
+
+    X [T,d], gamma [d] fp32.  ``Y`` receives the result if given (it may be ``X``).  rms is what rms_norm_backward and
+    head_writes take.
+    """
+    T, d, dtype, index = _norm_shapes(X, gamma)
+    code = _code_of(dtype)
+    if Y is None:
+        Y = _keep(torch.empty((T, d), dtype=dtype, device=X.device), stream)
+    else:
+        _layer_check("Y", Y, (T, d), dtype, index)
+    rms = _keep(torch.empty(T, dtype=torch.float32, device=X.device), stream)
+    st = lib().dtp_rms_norm(X.data_ptr(), gamma.data_ptr(), T, d, eps, code, Y.data_ptr(), rms.data_ptr(),
+                            _layer_stream(stream, index))
+    if st:
+        _check("dtp_rms_norm", st)
+    return Y, rms
+
+
+def rms_norm_workspace(T: int, d: int, dtype: torch.dtype, device) -> torch.Tensor:
+    """A device workspace for rms_norm_backward of these sizes (the same for either dtype)."""
+    _widths_check(d)
+    _torch_code(dtype)
+    n = _size_query("dtp_rms_norm_backward_workspace_size", T, d)
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def rms_norm_backward(dY: torch.Tensor, X: torch.Tensor, gamma: torch.Tensor, rms: torch.Tensor,
+                      dresidual: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Gradients (dX [T,d] in X's dtype, dgamma [d] fp32) of rms_norm for dY [T,d]; ``dresidual`` [T,d] is added to dX."""
+    T, d, dtype, index = _norm_shapes(X, gamma)
+    code = _code_of(dtype)
+    _layer_check("dY", dY, (T, d), dtype, index)
+    _layer_check("rms", rms, (T,), torch.float32, index)
+    if dresidual is not None:
+        _layer_check("dresidual", dresidual, (T, d), dtype, index)
+    dX = _keep(torch.empty_like(X), stream)
+    dgamma = _keep(torch.empty_like(gamma), stream)
+    if workspace is None:
+        workspace = _keep(rms_norm_workspace(T, d, dtype, X.device), stream)
+    else:
+        _workspace_check(workspace, index)
+    st = lib().dtp_rms_norm_backward(_ptr(dY), _ptr(X), _ptr(gamma), _ptr(rms), _ptr(dresidual), T, d, code, _ptr(dX),
+                                     _ptr(dgamma), _ptr(workspace), workspace.numel(), _layer_stream(stream, index))
+    if st:
+        _check("dtp_rms_norm_backward", st)
+    return dX, dgamma
+
+
+def linear_cross_entropy_workspace(T: int, d: int, V: int, dtype: torch.dtype, device, backward: bool = False) -> torch.Tensor:
+    """A device workspace for linear_cross_entropy (and, with ``backward``, its backward pass) of these sizes."""
+    _widths_check(d, V)
+    n = _size_query("dtp_linear_cross_entropy_workspace_size", T, d, V, _torch_code(dtype), int(backward))
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _loss_shapes(X, W, targets, ignore_index):
+    """(T, d, V, dtype, device index) of X [T,d], W [V,d] and targets [T] int64."""
+    T, d, V, dtype, index = _linear_shapes(X, W)
+    _layer_check("targets", targets, (T,), torch.int64, index)
+    if not -(1 << 63) <= ignore_index < 1 << 63:
+        raise ValueError("ignore_index must be a 64-bit integer")
+    return T, d, V, dtype, index
+
+
+def linear_cross_entropy(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, ignore_index: int = -100,
+                         workspace: torch.Tensor | None = None, stream=None, check: bool = False):
+    """(loss, lse), both [T] fp32: lse_t = logsumexp(W X_t), loss_t = lse_t - (W X_t)[targets_t], 0 where the target is
+    ignore_index.
+
+    X [T,d] and W [V,d] bf16 or fp32, targets [T] int64.  The logits are made in pieces and not kept.  Any other target
+    outside [0, V) makes its loss NaN and is reported through the workspace status word, which ``check`` reads.
+    """
+    T, d, V, dtype, index = _loss_shapes(X, W, targets, ignore_index)
+    code = _code_of(dtype)
+    loss = _keep(torch.empty(T, dtype=torch.float32, device=X.device), stream)
+    lse = _keep(torch.empty(T, dtype=torch.float32, device=X.device), stream)
+    if workspace is None:
+        workspace = _keep(linear_cross_entropy_workspace(T, d, V, dtype, X.device), stream)
+    else:
+        _workspace_check(workspace, index)
+    st = lib().dtp_linear_cross_entropy(_ptr(X), _ptr(W), _ptr(targets), T, d, V, ignore_index, code, _ptr(loss), _ptr(lse),
+                                        _ptr(workspace), workspace.numel(), _layer_stream(stream, index))
+    if st:
+        _check("dtp_linear_cross_entropy", st)
+    if check and T:
+        _check("dtp_linear_cross_entropy (device status)", workspace_status(workspace, stream))
+    return loss, lse
+
+
+def linear_cross_entropy_backward(dloss: torch.Tensor, X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor,
+                                  lse: torch.Tensor, ignore_index: int = -100, workspace: torch.Tensor | None = None,
+                                  stream=None, check: bool = False):
+    """Gradients (dX [T,d], dW [V,d]) of linear_cross_entropy for dloss [T] fp32, the gradient of each token's loss.
+
+    ``lse`` as linear_cross_entropy returned it.  Tokens whose target is ignore_index (or out of range, see there) have
+    zero gradients, whatever stands in their rows of X and in dloss.
+    """
+    T, d, V, dtype, index = _loss_shapes(X, W, targets, ignore_index)
+    code = _code_of(dtype)
+    _layer_check("dloss", dloss, (T,), torch.float32, index)
+    _layer_check("lse", lse, (T,), torch.float32, index)
+    dX, dW = (_keep(torch.empty_like(t), stream) for t in (X, W))
+    if workspace is None:
+        workspace = _keep(linear_cross_entropy_workspace(T, d, V, dtype, X.device, backward=True), stream)
+    else:
+        _workspace_check(workspace, index)
+    st = lib().dtp_linear_cross_entropy_backward(_ptr(dloss), _ptr(X), _ptr(W), _ptr(targets), _ptr(lse), T, d, V, ignore_index,
+                                                 code, _ptr(dX), _ptr(dW), _ptr(workspace), workspace.numel(),
+                                                 _layer_stream(stream, index))
+    if st:
+        _check("dtp_linear_cross_entropy_backward", st)
+    if check:
+        _check("dtp_linear_cross_entropy_backward (device status)", workspace_status(workspace, stream))
+    return dX, dW
+
+
+ADAMW_BLOCK = 256        # elements that share a scale in the 8-bit states
+
+
+def adamw_state(params, bits: int = 32) -> dict:
+    """The state of adamw_step for ``params``, at step 0: bits; m and v, lists of flat tensors like the parameters, fp32
+    (32 bits) or float8_e4m3fn (8 bits, v as its root); m_scale and v_scale, lists of fp32 tensors with a value for each
+    256 elements (None with 32 bits); step, the number of steps done, a 0-d int64 tensor on the parameters' device.
+    """
+    params = list(params)
+    if bits not in (8, 32):
+        raise ValueError(f"bits must be 8 or 32, got {bits}")
+    if not params:
+        raise ValueError("params must hold at least one tensor")
+    dev = params[0].device
+
+    def moments():
+        if bits == 32:
+            return [torch.zeros(p.numel(), dtype=torch.float32, device=dev) for p in params]
+        return [torch.zeros(p.numel(), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn) for p in params]
+
+    def scales():
+        if bits == 32:
+            return None
+        return [torch.zeros(-(-p.numel() // ADAMW_BLOCK), dtype=torch.float32, device=dev) for p in params]
+
+    return dict(bits=bits, m=moments(), v=moments(), m_scale=scales(), v_scale=scales(),
+                step=torch.zeros((), dtype=torch.int64, device=dev))
+
+
+def adamw_moments(state: dict):
+    """(m, v): the moments that a state of adamw_step holds, as lists of flat fp32 tensors (copies with 8 bits)."""
+    if state["bits"] == 32:
+        return state["m"], state["v"]
+
+    def values(code, scale):
+        return code.float() * scale.repeat_interleave(ADAMW_BLOCK)[:code.numel()]
+
+    return ([values(*x) for x in zip(state["m"], state["m_scale"])],
+            [values(*x).square() for x in zip(state["v"], state["v_scale"])])
+
+
+def adamw_workspace(params) -> torch.Tensor:
+    """A device workspace for adamw_step of these tensors."""
+    params = list(params)
+    if not params:
+        raise ValueError("params must hold at least one tensor")
+    numel = array.array("q", list(map(_numel_of, params)))
+    n = _size_query("dtp_adamw_workspace_size", len(params), numel.buffer_info()[0])
+    return torch.empty(n, dtype=torch.uint8, device=params[0].device)
+
+
+def _scalar_on(name, t, dtype, index):
+    if t.dtype is not dtype or t.numel() != 1 or t.get_device() != index:
+        raise ValueError(f"{name} must be one {dtype} value on the parameters' device")
+    return t.data_ptr()
+
+
+def _codes_of(name, dtypes):
+    try:
+        return array.array("i", [_LAYER_CODES[d] for d in dtypes])
+    except KeyError:
+        raise TypeError(f"{name} must be bfloat16 or float32") from None
+
+
+def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+               norm: torch.Tensor | None = None, max_norm: float = float("inf"), copies=None,
+               workspace: torch.Tensor | None = None, stream=None) -> None:
+    """One AdamW step over all tensors, in place: parameters, the state's moments and its counter.
+
+    params: contiguous CUDA tensors, each fp32 or bf16 (bf16 ones are rounded up or down at random, by a hash of element
+    and step, so that small updates count); grads: like them, each bf16 or fp32; state: adamw_state's.  lr: a number, or a
+    0-d fp32 tensor on the device (a schedule under a captured graph).  norm: clip_grad_norm's result; gradients are then
+    taken times max_norm / norm where that is below 1 (call it with max_norm=inf: the clipped ones need not be
+    written), and a norm that is not finite leaves everything as it is.  copies: bf16 tensors like fp32 params, which
+    receive the updated parameters (None for those without).
+    """
+    params, grads = list(params), list(grads)
+    count = len(params)
+    if count == 0:
+        raise ValueError("params must hold at least one tensor")
+    index = params[0].get_device()
+    p, numel, pd = _flat_tensors("params", params, index)
+    g, g_numel, gd = _flat_tensors("grads", grads, index)
+    if g_numel != numel:
+        raise ValueError("grads must have the sizes of params")
+    held_at = [a for a, n in zip(p, numel) if n]
+    if len(set(held_at)) != len(held_at):
+        raise ValueError("params must not hold a tensor twice")
+    pc, gc = _codes_of("params", pd), _codes_of("grads", gd)
+    bits = state["bits"]
+    if bits not in (8, 32):
+        raise ValueError(f"the state's bits must be 8 or 32, got {bits}")
+    held = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    at = [p, g]
+    for k in ("m", "v"):
+        a, n, d = _flat_tensors(f"the state's {k}", state[k], index)
+        if n != numel or d.count(held) != count:
+            raise ValueError(f"the state's {k} must be {held} tensors of the sizes of params")
+        at.append(a)
+    blocks = array.array("q", [-(-n // ADAMW_BLOCK) for n in numel])
+    for k in ("m_scale", "v_scale"):
+        if bits == 32:
+            at.append(None)
+            continue
+        a, n, d = _flat_tensors(f"the state's {k}", state[k], index)
+        if n != blocks or d.count(torch.float32) != count:
+            raise ValueError(f"the state's {k} must be fp32 tensors with a value for each {ADAMW_BLOCK} elements")
+        at.append(a)
+    if copies is not None:
+        copies = list(copies)
+        some = [(i, c) for i, c in enumerate(copies) if c is not None]
+        a, n, d = _flat_tensors("copies", [c for _, c in some], index)
+        if len(copies) != count or d.count(torch.bfloat16) != len(some) or any(
+                n[j] != numel[i] or pc[i] != DTP_F32 for j, (i, _) in enumerate(some)):
+            raise ValueError("copies must be bfloat16 tensors like params, which are float32, or None")
+        full = array.array("Q", bytes(8 * count))
+        for j, (i, _) in enumerate(some):
+            full[i] = a[j]
+        copies = full
+    at.append(copies)
+    step = _scalar_on("the state's step", state["step"], torch.int64, index)
+    lr_at = _scalar_on("lr", lr, torch.float32, index) if isinstance(lr, torch.Tensor) else None
+    norm_at = None if norm is None else _scalar_on("norm", norm, torch.float32, index)
+    opts = AdamWOpts(0.0 if lr_at else lr, betas[0], betas[1], eps, weight_decay, max_norm, bits)
+    if workspace is None:
+        workspace = _keep(adamw_workspace(params), stream)
+    else:
+        _workspace_check(workspace, index)
+    # the arrays themselves stay in `at` until the call has read them
+    first = [None if a is None else a.buffer_info()[0] for a in at]
+    st = lib().dtp_adamw(first[0], pc.buffer_info()[0], first[1], gc.buffer_info()[0], *first[2:], numel.buffer_info()[0], count,
+                         ctypes.byref(opts), lr_at, norm_at, step, _ptr(workspace), workspace.numel(),
+                         _layer_stream(stream, index))
+    if st:
+        _check("dtp_adamw", st)
