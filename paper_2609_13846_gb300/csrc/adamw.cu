@@ -90,8 +90,8 @@ __global__ void factors_kernel(const Step s) {
     f.skip = s.norm && !isfinite(n);
     f.clip = 1.0f, f.down = 1.0f;
     if (!f.skip && static_cast<double>(n) > s.max_norm) {
-        const float c = static_cast<float>(s.max_norm) / n;
-        if (c >= 1.0e-30f || s.max_norm == 0.0) {
+        const float c = __frcp_rn(n) * static_cast<float>(s.max_norm);
+        if (n <= 1.0e37f && (c >= 1.0e-30f || s.max_norm == 0.0)) {
             f.clip = c;
         } else {                       // a factor among fp32's subnormal numbers would lose bits: in two parts
             const double r = s.max_norm / static_cast<double>(n);
@@ -219,10 +219,11 @@ __device__ __forceinline__ void update(const Table<CAP>& t, int i, int64_t b, co
             mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, o));
             vt = fmaxf(vt, __shfl_xor_sync(0xFFFFFFFFu, vt, o));
         }
-        const float mu = mt >= kLeast ? __fdiv_rn(448.0f, mt) : 0.0f, vu = vt >= kLeast ? __fdiv_rn(448.0f, vt) : 0.0f;
+        const float mu = mt >= kLeast ? __fmul_rn(__frcp_rn(mt), 448.0f) : 0.0f;
+        const float vu = vt >= kLeast ? __fmul_rn(__frcp_rn(vt), 448.0f) : 0.0f;
         if (lane == 0) {
-            t.ms[i][b] = mt >= kLeast ? __fdiv_rn(mt, 448.0f) : 0.0f;
-            t.vs[i][b] = vt >= kLeast ? __fdiv_rn(vt, 448.0f) : 0.0f;
+            t.ms[i][b] = mt >= kLeast ? __fmul_rn(mt, 1.0f / 448.0f) : 0.0f;
+            t.vs[i][b] = vt >= kLeast ? __fmul_rn(vt, 1.0f / 448.0f) : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

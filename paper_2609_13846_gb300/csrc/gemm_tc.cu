@@ -102,6 +102,13 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                      : "memory");
     }
 }
+// the same, added to what is there
+__device__ __forceinline__ void tma_add_2d(const CUtensorMap* map, uint32_t src, int32_t x, int32_t y) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.bulk_group [%0, {%2, %3}], [%1];" ::"l"(
+                     reinterpret_cast<uint64_t>(map)),
+                 "r"(src), "r"(x), "r"(y)
+                 : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -385,7 +392,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             }
         };
         // the same where rows are not on 16-byte boundaries: element by element, the lanes along the rows
-        auto store_elements = [&](auto* out, int64_t ld, const uint32_t* w, int x, int row0) {
+        auto store_elements = [&](auto* out, int64_t ld, const uint32_t* w, int x, int row0, bool add) {
             using V = std::remove_pointer_t<decltype(out)>;
             constexpr int kPer = 64 / sizeof(V);          // columns of a box
             stage_box(w);
@@ -394,14 +401,18 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll 4
             for (int r = lane / kPer; r < 32; r += 32 / kPer) {
                 const int at = r * 64 + ((((c * sizeof(V)) >> 4) ^ ((r >> 1) & 3)) << 4) + ((c * sizeof(V)) & 15);
-                if (row0 + r < M && x + c < N)
-                    out[(static_cast<int64_t>(row0) + r) * ld + x + c] = *reinterpret_cast<const V*>(stg + at);
+                if (row0 + r < M && x + c < N) {
+                    V* to = out + (static_cast<int64_t>(row0) + r) * ld + x + c;
+                    const V value = *reinterpret_cast<const V*>(stg + at);
+                    if constexpr (sizeof(V) == 4) *to = add ? *to + value : value;
+                    else *to = value;
+                }
             }
             __syncwarp();
         };
         // 32 columns of the box's rows, from column n, into output i
         auto store32 = [&](int i, void* out, const uint32_t (&w)[16], int n, int row0) {
-            if (p.direct[job]) store_elements(static_cast<__nv_bfloat16*>(out), ldo, w, n, row0);
+            if (p.direct[job]) store_elements(static_cast<__nv_bfloat16*>(out), ldo, w, n, row0, false);
             else store_box(std::false_type(), &p.out[i], w, n, row0);
         };
         uint32_t unit_count = static_cast<uint32_t>(set);
@@ -439,12 +450,27 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 }
             };
             if constexpr (KIND == kEpiLinear) fetch(32 * half);
+            // the row's target as a column, its lse times log2 e and its gradient: a row that does not count gets zeros
+            int target = -1;
+            float lse2 = INFINITY, grad = 0.0f;
+            if constexpr (KIND == kEpiParts || KIND == kEpiProb) {
+                if (m < M) {
+                    const int64_t y = e.vocab.targets[m];
+                    if (e.vocab.live(y)) {
+                        target = static_cast<int>(y) - e.vocab.v0;
+                        if constexpr (KIND == kEpiProb) lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m];
+                    } else if (KIND == kEpiProb && tn == 0 && half == 0 && e.vocab.bad(y)) {
+                        atomicCAS(p.status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
+                    }
+                }
+            }
             if constexpr (!kSplit) {
                 const uint32_t use = (unit_count >> 1) & 1u;
                 if (!warp_wait(smem_u32(&acc_full[buf]), use, abort_flag)) break;
                 tc_fence_after();
             }
             const uint32_t acc = lane_base + buf * BN;
+            float top = -INFINITY, sum = 0.0f;            // of the row's columns so far
             // 16 columns from column col of accumulator q
             auto get16 = [&](int q, int col, float* v) {
                 if constexpr (kSplit) {
@@ -492,11 +518,23 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             if (n + 16 * q < N) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
-                                if (p.direct_z) store_elements(e.Z, static_cast<int64_t>(N), w, n + 16 * q, row0);
-                                else store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
+                                if (p.direct_z) {
+                                    store_elements(e.Z, static_cast<int64_t>(N), w, n + 16 * q, row0, e.add != 0);
+                                } else if (e.add) {
+                                    stage_box(w);
+                                    fence_async_smem();
+                                    __syncwarp();
+                                    if (lane == 0) {
+                                        tma_add_2d(&p.z, smem_u32(stg), n + 16 * q, row0);
+                                        bulk_commit();
+                                    }
+                                } else {
+                                    store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
+                                }
                             }
                         }
                     }
+                    if (!e.out) continue;
                     act_values<true>(e.act, v);
                     if (e.residual && wide) {
                         // from the rows' quarters to the lane's row, through the staging buffer
@@ -555,6 +593,51 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             w[8 * q + i] = pack_bf16(g[2 * i] * v[2 * i], g[2 * i + 1] * v[2 * i + 1]);
                     }
                     store32(job, p.dst[job], w, n, row0);
+                } else if constexpr (KIND == kEpiParts) {
+                    float v[32];
+                    get16(0, c, v);
+                    get16(0, c + 16, v + 16);
+                    got();
+                    if (N - n < 32) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (n + i >= N) v[i] = -INFINITY;
+                    }
+                    const int at = target - n;
+                    if (__any_sync(0xFFFFFFFFu, at >= 0 && at < 32)) {
+                        float z = 0.0f;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) z = at == i ? v[i] : z;
+                        if (at >= 0 && at < 32) e.vocab.hit[m] = z;
+                    }
+                    float most = v[0];
+#pragma unroll
+                    for (int i = 1; i < 32; ++i) most = fmaxf(most, v[i]);
+                    most *= kLog2e;
+                    if (most > top) {
+                        sum *= exp2_fast(top - most);
+                        top = most;
+                    }
+                    const float shift = top == -INFINITY ? 0.0f : top;      // of a row of -inf alone: its sum is 0
+                    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast(fmaf(v[i], kLog2e, -shift));
+                    sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                } else if constexpr (KIND == kEpiProb) {
+                    float v[32];
+                    get16(0, c, v);
+                    get16(0, c + 16, v + 16);
+                    got();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], kLog2e, -lse2));
+                    const int at = target - n;
+                    if (__any_sync(0xFFFFFFFFu, at >= 0 && at < 32)) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] -= at == i ? 1.0f : 0.0f;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i] * grad, v[2 * i + 1] * grad);
+                    store32(job, p.dst[job], w, n, row0);
                 } else {
                     // 16 columns at a time with all their saved values in flight: 144 us for 1024 x 3072 on 16384 tokens (four
                     // columns at a time 192 us, the loads' latency 32 times a tile).  dG goes to the staging buffer as it
@@ -599,6 +682,8 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     store_box(std::false_type(), &p.out[1], w2, n, row0);
                 }
             }
+            if constexpr (KIND == kEpiParts)
+                if (m < M) e.vocab.parts[(2 * static_cast<int64_t>(tn) + half) * M + m] = Part{top, sum};
             if constexpr (!kSplit) {
                 // its TMEM loads have completed (tcgen05.wait::ld): hand the buffer back without release ordering,
                 // which would also wait for the warp's stores
@@ -685,7 +770,7 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
         a.N[j] = j > 0 ? x.N : p.N;
         a.ldo[j] = j > 0 ? x.ldo : p.epi.ldo;
         a.dst[j] = j > 0 ? x.out : p.epi.out;
-        a.direct[j] = (a.ldo[j] & 7) != 0;
+        a.direct[j] = (a.ldo[j] & 7) != 0 || !a.dst[j];
         if (!a.direct[j] && !map_2d(&a.out[j], a.dst[j], a.N[j], a.M[j], a.ldo[j], 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
             return DTP_ERR_CUDA;
         a.tiles_m[j] = static_cast<int>((a.M[j] + rows - 1) / rows);
@@ -714,6 +799,10 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     a.status = status;
     a.epi = p.epi;
     auto kernel = gated ? gemm_tc_kernel<kPair, BN, kEpiGated, kSplit, 1> : gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit, 1>;
+    if constexpr (BN >= 128 && !kSplit) {
+        if (p.epi.kind == kEpiParts) kernel = gemm_tc_kernel<kPair, BN, kEpiParts, kSplit, 1>;
+        if (p.epi.kind == kEpiProb) kernel = gemm_tc_kernel<kPair, BN, kEpiProb, kSplit, 1>;
+    }
     if constexpr (BN >= 128)
         if (p.epi.kind == kEpiGatedGrad) kernel = gemm_tc_kernel<kPair, BN, kEpiGatedGrad, kSplit, 1>;
     if constexpr (kPair && BN >= 128)
@@ -770,7 +859,10 @@ static int cluster_room(int split, int sms) {
     return n;
 }
 
-// bf16 operands whose rows are on 16-byte boundaries; M, N >= 1, K >= 1.
+// Chunks of columns that the parts of a product of kEpiParts have, at most: two for each tile of 128.
+int64_t most_chunks(int N) { return 2 * ((static_cast<int64_t>(N) + 127) / 128); }
+
+// bf16 operands whose rows are on 16-byte boundaries; M, N >= 1, K >= 1.  `chunks`: those that kEpiParts wrote.
 //
 // The form is the one with the smallest estimate, in clocks, from what the forms measured on a GB300: a launch's start, pipeline
 // fill and last epilogue (9000 for 256 x 256 pairs, 7000 for 256 x 128 and for single 128 x 128 tiles, which up to 128 rows may
@@ -778,7 +870,7 @@ static int cluster_room(int split, int sms) {
 // takes (515, 400, 500, 280), but no less than an epilogue; and for splitting a tile the exchange (8000 with 256 columns, 5000
 // with 128).  Tiles left over after the full rounds of 256 x 256 pairs may be split in a launch of their own, which begins as
 // the first one's SMs fall free (saving 4000).
-int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
+int launch(const Product& p, int* status, int reset, cudaStream_t stream, int64_t* chunks) {
     int dev = 0, sms = 0;
     DTP_CUDA_TRY(cudaGetDevice(&dev));
     DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -796,8 +888,9 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
         const int64_t round = kb * clocks > fixed / 3 ? kb * clocks : fixed / 3;
         return (n + workers - 1) / workers * round + fixed;
     };
+    const bool softmax = p.epi.kind == kEpiParts || p.epi.kind == kEpiProb;
     auto split_ok = [&](int64_t n, int bn, int split) {
-        return kb >= 4 * split && (gated ? bn / 2 : bn) / split >= 32 && n <= cluster_room(split, sms);
+        return !softmax && kb >= 4 * split && (gated ? bn / 2 : bn) / split >= 32 && n <= cluster_room(split, sms);
     };
     auto split_clocks = [&](int bn, int split) {
         return (kb + split - 1) / split * (bn == 256 ? 515 : 400) + (bn == 256 ? 9000 + 8000 : 7000 + 5000);
@@ -809,7 +902,7 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
         if (estimate < best) best = estimate, best_bn = bn, best_split = split, tail = left;
     };
     take(whole(tiles(2 * BM, 128), pairs, 400, 7000), 128, 1, 0);
-    if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad) take(whole(tiles(2 * BM, 64), pairs, 280, 5500), 64, 1, 0);
+    if (p.B[0].ks == 1 && p.epi.kind != kEpiGatedGrad && !softmax) take(whole(tiles(2 * BM, 64), pairs, 280, 5500), 64, 1, 0);
     if (p.M <= BM && p.batch == 1) take(whole(tiles(BM, 128), sms, 500, 7000), 0, 1, 0);
     const int64_t left = n256 % pairs;
     for (int split : {2, 4}) {
@@ -818,6 +911,7 @@ int launch(const Product& p, int* status, int reset, cudaStream_t stream) {
         if (n256 > pairs && left > 0 && split_ok(left, 256, split))
             take(whole(n256 - left, pairs, 515, 9000) + split_clocks(256, split) - 4000, 256, split, left);
     }
+    if (chunks) *chunks = 2 * ((static_cast<int64_t>(p.N) + (best_bn == 256 ? 255 : 127)) / (best_bn == 256 ? 256 : 128));
     if (tail) {
         const int st = launch_form<true, 256, false>(p, status, reset, 1, 0, 0, n256 - tail, pairs, stream);
         if (st != DTP_OK) return st;

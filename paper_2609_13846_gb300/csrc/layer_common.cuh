@@ -185,7 +185,29 @@ __host__ __device__ inline int64_t pre_index(int64_t t, int64_t n, int64_t N) {
 enum EpiKind {
     kEpiLinear = 0,     // out = act(acc + bias) + residual; Z = acc + bias
     kEpiGated = 1,      // out = act(acc0) acc1; pre = (acc0, acc1)
-    kEpiGatedGrad = 2   // acc = dH: out = dG = dH U act'(G), out2 = dU = dH act(G)
+    kEpiGatedGrad = 2,  // acc = dH: out = dG = dH U act'(G), out2 = dU = dH act(G)
+    kEpiParts = 3,      // acc = logits: each row's largest one and sum of exponentials of a chunk of columns (bf16 only)
+    kEpiProb = 4        // acc = logits: out = dZ = dloss (exp(acc - lse) - onehot) (bf16 only)
+};
+
+// A row's largest logit of a chunk of columns, times log2 e, and the sum of 2^(z log2 e - top).
+struct Part { float top, sum; };
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// What the softmax's epilogues know of the rows.
+struct Vocab {
+    const int64_t* targets = nullptr;      // [M]
+    int64_t ignore = 0;
+    int V = 0, v0 = 0;                     // the vocabulary, and the piece's first token
+    Part* parts = nullptr;                 // [chunk][M]
+    float* hit = nullptr;                  // [M] the target's logit
+    const float *lse = nullptr, *dloss = nullptr;
+    __device__ __forceinline__ bool bad(int64_t y) const { return y != ignore && (y < 0 || y >= V); }
+    __device__ __forceinline__ bool live(int64_t y) const { return y != ignore && y >= 0 && y < V; }
 };
 
 struct Epilogue {
@@ -193,10 +215,12 @@ struct Epilogue {
     int act = DTP_ACT_NONE;
     const void* bias = nullptr;       // [N]
     const void* residual = nullptr;   // [M, ldo]
-    void* out = nullptr;              // [M, ldo]
+    void* out = nullptr;              // [M, ldo]; kEpiLinear: NULL where Z alone is wanted
     void* out2 = nullptr;
     int64_t ldo = 0;
     float* Z = nullptr;               // [M, N]
+    int add = 0;                      // kEpiLinear, bf16 operands: Z += instead, and no out
+    Vocab vocab;
     float* pre = nullptr;
     int64_t M = 0;
     int N = 0;
@@ -212,6 +236,7 @@ __device__ __forceinline__ void epilogue_element(const Epilogue& e, int64_t m, i
         float z = a0;
         if (e.bias) z += to_f32(reinterpret_cast<const E*>(e.bias)[n]);
         if (e.Z) e.Z[m * e.N + n] = z;
+        if (!out) return;
         float y = act_value<kFast>(e.act, z);
         if (e.residual) y += to_f32(reinterpret_cast<const E*>(e.residual)[at]);
         out[at] = from_f32<E>(y);

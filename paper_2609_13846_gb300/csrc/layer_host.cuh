@@ -14,7 +14,8 @@ namespace simt {
 int launch(const layer::Product& p, int dtype, int* status, cudaStream_t stream);
 }  // namespace simt
 namespace gtc {
-int launch(const layer::Product& p, int* status, int reset, cudaStream_t stream);
+int64_t most_chunks(int N);
+int launch(const layer::Product& p, int* status, int reset, cudaStream_t stream, int64_t* chunks = nullptr);
 }  // namespace gtc
 namespace few {
 bool takes(const layer::Product& p);

@@ -4,8 +4,10 @@
 //     dz_t = dloss_t (exp(z_t - lse_t) - onehot(y_t)),  dX = dZ W,  dW = dZ^T X
 //
 // in pieces of the vocabulary, so that no more than a piece of the logits exists at a time.  Forward, each row's maximum and
-// sum of exponentials of every chunk of columns meet in a last launch.  Backward, a piece of the logits is made again, turned into dZ,
-// and multiplied both ways; dX is added up over the pieces in fp32.
+// sum of exponentials of every chunk of columns meet in a last launch; bf16 products of more than 32 tokens take them from the
+// accumulators (kEpiParts), and their logits are never stored.  Backward, a piece of the logits is made again and turned into
+// dZ, in the product's epilogue (kEpiProb) or by a kernel of its own, and multiplied both ways; dX is added up over the
+// pieces in fp32.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -20,12 +22,10 @@ namespace layer {
 constexpr int kChunk = 8192;                         // columns of a partial sum
 constexpr size_t kPieceBytes = size_t(256) << 20;    // of a piece of the logits
 
-// A row's maximum and its sum of exp(z - maximum).
-struct Part { float top, sum; };
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
     const float top = fmaxf(a.top, b.top);
     // a part that holds nothing, or only -inf, counts for nothing
-    const float u = a.top == top ? a.sum : a.sum * expf(a.top - top), v = b.top == top ? b.sum : b.sum * expf(b.top - top);
+    const float u = a.top == top ? a.sum : a.sum * exp2_fast(a.top - top), v = b.top == top ? b.sum : b.sum * exp2_fast(b.top - top);
     return Part{top, u + v};
 }
 
@@ -44,7 +44,7 @@ parts_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets
         bool nan = false;
         for (int j = c * kChunk + threadIdx.x; j < c1; j += 256) {
             nan |= isnan(z[j]);
-            p = join(p, Part{z[j], 1.0f});
+            p = join(p, Part{z[j] * kLog2e, 1.0f});
         }
         if (nan) p.sum = NAN;
 #pragma unroll
@@ -57,7 +57,7 @@ parts_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets
             for (int w = 1; w < 8; ++w) p = join(p, red[w]);
             parts[c * T + t] = p;
             const int64_t y = targets[t] - v0;
-            if (c == 0 && y >= 0 && y < cols) hit[t] = z[y];
+            if (c == 0 && y >= 0 && y < cols) hit[t] = z[y];      // of one piece
         }
     }
 }
@@ -78,7 +78,7 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
     __syncthreads();
     if (warp != 0 || t >= T) return;
     for (int w = 1; w < 8; ++w) p = join(p, red[w][lane]);
-    const float l = p.top + logf(p.sum);
+    const float l = kLn2 * (p.top + log2f(p.sum));
     lse[t] = l;
     const int64_t y = targets[t];
     const bool bad = y != ignore && (y < 0 || y >= V);
@@ -100,94 +100,139 @@ live_rows_kernel(const E* X, int64_t T, int d, int64_t pitch, const int64_t* tar
     }
 }
 
+// dZ of Z [T, cols], columns v0 .. of the vocabulary; a block takes kChunk columns of a token.  dZ may be Z.
 template <typename E>
 __global__ void __launch_bounds__(256)
-dz_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets, int64_t ignore, int V, const float* dloss,
-          const float* lse, E* dZ, int64_t ld, int* status) {
+dz_kernel(const float* Z, int64_t T, int cols, Vocab e, E* dZ, int64_t ld, int* status) {
     grid_wait();
     grid_release();
-    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-        const int64_t y = targets[t];
-        const bool bad = y != ignore && (y < 0 || y >= V), live = y != ignore && !bad;
-        if (bad && threadIdx.x == 0) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
-        const float g = dloss[t], l = lse[t];
-        for (int j = threadIdx.x; j < cols; j += 256) {
-            const float p = expf(Z[t * cols + j] - l) - (y - v0 == j ? 1.0f : 0.0f);
+    const int chunks = (cols + kChunk - 1) / kChunk;
+    for (int64_t i = blockIdx.x; i < T * chunks; i += gridDim.x) {
+        const int64_t t = i / chunks;
+        const int c = static_cast<int>(i - t * chunks), c1 = (c + 1) * kChunk < cols ? (c + 1) * kChunk : cols;
+        const int64_t y = e.targets[t];
+        if (c == 0 && threadIdx.x == 0 && e.bad(y)) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
+        const bool live = e.live(y);
+        const float g = live ? e.dloss[t] : 0.0f, lse2 = e.lse[t] * kLog2e;
+#pragma unroll 4
+        for (int j = c * kChunk + threadIdx.x; j < c1; j += 256) {
+            const float p = exp2_fast(fmaf(Z[t * cols + j], kLog2e, -lse2)) - (y - e.v0 == j ? 1.0f : 0.0f);
             dZ[t * ld + j] = from_f32<E>(live ? p * g : 0.0f);
         }
     }
 }
 
-// sum += part, and the last time the sum in its type
-template <typename E>
-__global__ void __launch_bounds__(256) add_kernel(const float* part, int64_t n, int first, float* sum, E* out) {
+// dX from its sums
+__global__ void __launch_bounds__(256) round_kernel(const float* sum, int64_t n, __nv_bfloat16* out) {
     grid_wait();
     grid_release();
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
-        const float v = first ? part[i] : sum[i] + part[i];
-        if (out) out[i] = from_f32<E>(v);
-        else sum[i] = v;
+    const int64_t words = n / 4;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < words; i += gridDim.x * 256ll) {
+        const float4 v = reinterpret_cast<const float4*>(sum)[i];
+        const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+        reinterpret_cast<uint2*>(out)[i] = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
     }
+    const int64_t rest = 4 * words + threadIdx.x;
+    if (blockIdx.x == 0 && rest < n) out[rest] = __float2bfloat16_rn(sum[rest]);
 }
 
 static int64_t grid_of(int64_t blocks) { return blocks < 8192 ? blocks : 8192; }
 
+// Whether a product's epilogue takes the softmax.  Up to 32 tokens the products are the few-token kernels', which stream the
+// weights at the memory's rate; their logits are small beside those.
+static bool fused(int64_t T, int dtype) { return dtype == DTP_BF16 && T > 32; }
+
+// Tokens of a forward run: its parts, and the logits' pieces where there are any, stay within 256 MB.
+static int64_t forward_rows(int64_t T, int V, int dtype) {
+    int64_t n = 16384;
+    if (fused(T, dtype)) n = static_cast<int64_t>(kPieceBytes / sizeof(Part)) / gtc::most_chunks(V) / 256 * 256;
+    if (n < 256) n = 256;
+    return n < T ? n : T;
+}
 // Columns of a piece of T tokens' logits.
-static int piece_cols(int64_t T, int V) {
-    int64_t n = static_cast<int64_t>(kPieceBytes / sizeof(float)) / T / 128 * 128;
-    if (n < 128) n = 128;
+static int piece_cols(int64_t T, int V, size_t bytes) {
+    int64_t n = static_cast<int64_t>(bytes) / T / 256 * 256;
+    if (n < 256) n = 256;
     return static_cast<int>(n < V ? n : V);
 }
-static int64_t parts_of(int64_t T, int V) {
-    const int piece = piece_cols(T, V);
+static int forward_piece(int64_t rows, int V, int dtype) {
+    return fused(rows, dtype) ? V : piece_cols(rows, V, kPieceBytes / sizeof(float));
+}
+static int backward_piece(int64_t T, int V, int dtype) { return piece_cols(T, V, kPieceBytes / elem(dtype)); }
+static int64_t parts_of(int64_t rows, int V, int dtype) {
+    if (fused(rows, dtype)) return gtc::most_chunks(V);
+    const int piece = forward_piece(rows, V, dtype);
     const int64_t whole = V / piece, rest = V % piece;
     return whole * ((piece + kChunk - 1) / kChunk) + (rest + kChunk - 1) / kChunk;
 }
 
 // What a call takes from its workspace.
-struct LossSpace {
-    float* Z;
-    void* dz;            // also what the products make of Z in their type
+struct ForwardSpace {
+    float* Z;            // a piece of the logits, where they are stored
     Part* parts;
     float* hit;
-    void* x;
-    float *part, *sum;
 };
-static LossSpace carve(Carver& c, int64_t T, int d, int V, int dtype, int backward) {
-    LossSpace s{};
-    const int piece = piece_cols(T, V);
-    s.Z = static_cast<float*>(c.take(static_cast<size_t>(T) * piece * sizeof(float)));
-    s.dz = c.take(static_cast<size_t>(T) * padded(piece) * elem(dtype));
-    s.parts = static_cast<Part*>(c.take(static_cast<size_t>(T) * parts_of(T, V) * sizeof(Part)));
-    s.hit = static_cast<float*>(c.take(static_cast<size_t>(T) * sizeof(float)));
-    if (backward) {
-        s.x = c.take(static_cast<size_t>(T) * padded(d) * elem(dtype));
-        s.part = static_cast<float*>(c.take(static_cast<size_t>(T) * d * sizeof(float)));
-        s.sum = static_cast<float*>(c.take(static_cast<size_t>(T) * d * sizeof(float)));
-    }
+static ForwardSpace carve_forward(Carver& c, int64_t rows, int V, int dtype) {
+    ForwardSpace s{};
+    if (!fused(rows, dtype)) s.Z = static_cast<float*>(c.take(static_cast<size_t>(rows) * forward_piece(rows, V, dtype) * sizeof(float)));
+    s.parts = static_cast<Part*>(c.take(static_cast<size_t>(rows) * parts_of(rows, V, dtype) * sizeof(Part)));
+    s.hit = static_cast<float*>(c.take(static_cast<size_t>(rows) * sizeof(float)));
+    return s;
+}
+struct BackwardSpace {
+    float* Z;            // the same; in fp32 dZ takes its place
+    void* dz;
+    void* x;
+    float *sum, *runs;
+};
+static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtype) {
+    BackwardSpace s{};
+    const int piece = backward_piece(T, V, dtype);
+    if (!fused(T, dtype)) s.Z = static_cast<float*>(c.take(static_cast<size_t>(T) * piece * sizeof(float)));
+    s.dz = dtype == DTP_F32 ? s.Z : c.take(static_cast<size_t>(T) * padded(piece) * elem(dtype));
+    s.x = c.take(static_cast<size_t>(T) * padded(d) * elem(dtype));
+    s.sum = static_cast<float*>(c.take(dtype == DTP_BF16 && piece < V ? static_cast<size_t>(T) * d * sizeof(float) : 0));
+    s.runs = static_cast<float*>(c.take(runs_bytes(T, piece, d)));
     return s;
 }
 
 size_t loss_workspace_bytes(int64_t T, int d, int V, int dtype, int backward) {
     if (T == 0) return kWorkspaceHeader;
-    Carver c(nullptr);
-    carve(c, T, d, V, dtype, backward);
-    c.take(repitch_bytes(T, d, dtype));
-    c.take(repitch_bytes(V, d, dtype));
-    if (backward) c.take(runs_bytes(T, piece_cols(T, V), d));
-    return c.used;
+    Carver f(nullptr);
+    f.take(repitch_bytes(V, d, dtype));
+    Carver b = f;
+    f.take(repitch_bytes(T, d, dtype));
+    const int64_t rows = forward_rows(T, V, dtype);
+    carve_forward(f, rows, V, dtype);
+    // the last run may be one of few tokens
+    if (T % rows) {
+        Carver last = f;
+        last.used = f.used;
+        carve_forward(last, T % rows, V, dtype);
+        f.used = last.used;
+    }
+    if (!backward) return f.used;
+    carve_backward(b, T, d, V, dtype);
+    return f.used > b.used ? f.used : b.used;
 }
 
-// Z = X W_piece^T in fp32
-static int logits(Call& call, const Rows& x, const Rows& w, int64_t T, int d, int v0, int cols, const LossSpace& s) {
+// The product of T tokens with columns v0 .. of the vocabulary.
+static Product logits(const Rows& x, int64_t t0, const Rows& w, int64_t T, int d, int v0, int cols, int dtype) {
+    auto from = [&](const Rows& r, int64_t row) {
+        return by_row(static_cast<const uint8_t*>(r.p) + static_cast<size_t>(row) * r.ld * elem(dtype), r.ld);
+    };
     Product p;
-    p.A[0] = by_row(x.p, x.ld);
-    p.B[0] = by_row(static_cast<const uint8_t*>(w.p) + static_cast<size_t>(v0) * w.ld * elem(call.dtype), w.ld);
+    p.A[0] = from(x, t0);
+    p.B[0] = from(w, v0);
     p.M = T, p.N = cols, p.K = d;
-    p.epi.out = call.dtype == DTP_F32 ? static_cast<void*>(s.Z) : s.dz;
-    p.epi.ldo = call.dtype == DTP_F32 ? cols : padded(cols);
-    p.epi.Z = call.dtype == DTP_F32 ? nullptr : s.Z;
-    p.epi.M = T, p.epi.N = cols;
+    p.epi.M = T, p.epi.N = cols, p.epi.ldo = cols;
+    return p;
+}
+
+// Stored logits: Z [T, cols] in fp32.
+static int store_logits(Call& call, Product& p, float* Z) {
+    if (call.dtype == DTP_F32) p.epi.out = Z;
+    else p.epi.Z = Z;
     return call.run(p);
 }
 
@@ -195,24 +240,40 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
                  float* loss, float* lse, void* workspace, cudaStream_t stream) {
     Call call{dtype, workspace, stream};
     Carver c(workspace);
-    const LossSpace s = carve(c, T, d, V, dtype, 0);
-    const int piece = piece_cols(T, V);
     Rows x, w;
-    int st = aligned_rows(X, T, d, dtype, c, stream, &x);
-    if (st == DTP_OK) st = aligned_rows(W, V, d, dtype, c, stream, &w);
-    Part* at = s.parts;
-    for (int v0 = 0; st == DTP_OK && v0 < V; v0 += piece) {
-        const int cols = V - v0 < piece ? V - v0 : piece;
-        st = logits(call, x, w, T, d, v0, cols, s);
-        const int64_t chunks = (cols + kChunk - 1) / kChunk;
+    int st = aligned_rows(W, V, d, dtype, c, stream, &w);
+    if (st == DTP_OK) st = aligned_rows(X, T, d, dtype, c, stream, &x);
+    int* status = static_cast<int*>(workspace);
+    const int64_t most = forward_rows(T, V, dtype);
+    ForwardSpace s = carve_forward(c, most, V, dtype);
+    for (int64_t t0 = 0; st == DTP_OK && t0 < T; t0 += most) {
+        const int64_t rows = T - t0 < most ? T - t0 : most;
+        if (rows < most) s = carve_forward(c, rows, V, dtype);
+        Vocab e;
+        e.targets = targets + t0, e.ignore = ignore, e.V = V, e.parts = s.parts, e.hit = s.hit;
+        int64_t count = 0;
+        if (fused(rows, dtype)) {
+            Product p = logits(x, t0, w, rows, d, 0, V, dtype);
+            p.epi.kind = kEpiParts, p.epi.vocab = e;
+            st = gtc::launch(p, status, call.fresh, stream, &count);
+            call.fresh = false;
+        }
+        const int piece = forward_piece(rows, V, dtype);
+        for (int v0 = 0; st == DTP_OK && s.Z && v0 < V; v0 += piece) {
+            const int cols = V - v0 < piece ? V - v0 : piece;
+            Product p = logits(x, t0, w, rows, d, v0, cols, dtype);
+            st = store_logits(call, p, s.Z);
+            const int64_t chunks = (cols + kChunk - 1) / kChunk;
+            if (st == DTP_OK)
+                st = launch_after(parts_kernel, grid_of(rows * chunks), stream, static_cast<const float*>(s.Z), rows, cols, v0,
+                                  e.targets, s.parts + count * rows, s.hit);
+            count += chunks;
+        }
         if (st == DTP_OK)
-            st = launch_after(parts_kernel, grid_of(T * chunks), stream, static_cast<const float*>(s.Z), T, cols, v0, targets, at,
-                              s.hit);
-        at += chunks * T;
+            st = launch_after(loss_kernel, (rows + 31) / 32, stream, static_cast<const Part*>(s.parts), count,
+                              static_cast<const float*>(s.hit), e.targets, rows, V, ignore, loss + t0, lse + t0, status);
     }
-    if (st != DTP_OK) return st;
-    return launch_after(loss_kernel, (T + 31) / 32, stream, static_cast<const Part*>(s.parts), parts_of(T, V),
-                        static_cast<const float*>(s.hit), targets, T, V, ignore, loss, lse, static_cast<int*>(workspace));
+    return st;
 }
 
 template <typename E>
@@ -220,46 +281,50 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
                     int V, int64_t ignore, int dtype, void* dX, void* dW, void* workspace, cudaStream_t stream) {
     Call call{dtype, workspace, stream};
     Carver c(workspace);
-    const LossSpace s = carve(c, T, d, V, dtype, 1);
-    const int piece = piece_cols(T, V);
+    Rows w;
+    int st = aligned_rows(W, V, d, dtype, c, stream, &w);
+    const BackwardSpace s = carve_backward(c, T, d, V, dtype);
+    const int piece = backward_piece(T, V, dtype);
     int* status = static_cast<int*>(workspace);
-    const int64_t ld = padded(d);
-    int st = launch_after(live_rows_kernel<E>, grid_of(T), stream, static_cast<const E*>(X), T, d, ld, targets, ignore, V,
+    const Rows x{s.x, padded(d)};
+    Vocab e;
+    e.targets = targets, e.ignore = ignore, e.V = V, e.lse = lse, e.dloss = dloss;
+    if (st == DTP_OK)
+        st = launch_after(live_rows_kernel<E>, grid_of(T), stream, static_cast<const E*>(X), T, d, x.ld, targets, ignore, V,
                           static_cast<E*>(s.x), status);
     call.fresh = false;
-    const Rows x{s.x, ld};
-    Rows w;
-    if (st == DTP_OK) st = aligned_rows(W, V, d, dtype, c, stream, &w);
-    auto* runs = static_cast<float*>(c.take(runs_bytes(T, piece, d)));
-    const int64_t values = T * d, add_blocks = grid_of((values + 255) / 256);
     for (int v0 = 0; st == DTP_OK && v0 < V; v0 += piece) {
         const int cols = V - v0 < piece ? V - v0 : piece;
-        const int64_t ldz = padded(cols);
-        st = logits(call, x, w, T, d, v0, cols, s);
-        if (st == DTP_OK)
-            st = launch_after(dz_kernel<E>, grid_of(T), stream, static_cast<const float*>(s.Z), T, cols, v0, targets, ignore, V,
-                              dloss, lse, static_cast<E*>(s.dz), ldz, status);
+        const int64_t ldz = dtype == DTP_F32 ? cols : padded(cols);
+        e.v0 = v0;
+        Product p = logits(x, 0, w, T, d, v0, cols, dtype);
+        if (fused(T, dtype)) {
+            p.epi.kind = kEpiProb, p.epi.vocab = e, p.epi.out = s.dz, p.epi.ldo = ldz;
+            st = gtc::launch(p, status, 0, stream);
+        } else {
+            st = store_logits(call, p, s.Z);
+            if (st == DTP_OK)
+                st = launch_after(dz_kernel<E>, grid_of(T * ((cols + kChunk - 1) / kChunk)), stream, static_cast<const float*>(s.Z),
+                                  T, cols, e, static_cast<E*>(s.dz), ldz, status);
+        }
         if (st == DTP_OK && dX) {
-            const bool last = cols == V - v0;
-            Product p;
-            p.A[0] = by_row(s.dz, ldz);
-            p.B[0] = by_col(static_cast<const uint8_t*>(w.p) + static_cast<size_t>(v0) * w.ld * sizeof(E), w.ld);
-            p.M = T, p.N = d, p.K = cols;
-            p.epi.out = dX, p.epi.ldo = d, p.epi.M = T, p.epi.N = d;
-            const bool one = last && v0 == 0;
-            if (!one) {
-                if (dtype == DTP_F32) p.epi.out = s.part;
-                else p.epi.Z = s.part;
-            }
-            st = call.run(p);
-            if (st == DTP_OK && !one)
-                st = launch_after(add_kernel<E>, add_blocks, stream, static_cast<const float*>(s.part), values,
-                                  static_cast<int>(v0 == 0), s.sum, last ? static_cast<E*>(dX) : nullptr);
+            Product q;
+            q.A[0] = by_row(s.dz, ldz);
+            q.B[0] = by_col(static_cast<const uint8_t*>(w.p) + static_cast<size_t>(v0) * w.ld * sizeof(E), w.ld);
+            q.M = T, q.N = d, q.K = cols;
+            q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
+            if (dtype == DTP_F32) q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
+            else if (piece >= V) q.epi.out = dX;
+            else q.epi.Z = s.sum, q.epi.add = v0 > 0;
+            st = call.run(q);
         }
         if (st == DTP_OK && dW)
             st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, static_cast<E*>(dW) + static_cast<int64_t>(v0) * d, d},
-                                 T, runs);
+                                 T, s.runs);
     }
+    if (st == DTP_OK && dX && dtype == DTP_BF16 && piece < V)
+        st = launch_after(round_kernel, grid_of((T * d / 4 + 255) / 256 + 1), stream, static_cast<const float*>(s.sum), T * d,
+                          static_cast<__nv_bfloat16*>(dX));
     return st;
 }
 
