@@ -104,8 +104,9 @@ __global__ void factors_kernel(const Step s) {
     f.b1 = static_cast<float>(s.b1), f.not_b1 = static_cast<float>(1.0 - s.b1);
     f.b2 = static_cast<float>(s.b2), f.not_b2 = static_cast<float>(1.0 - s.b2);
     f.keep = static_cast<float>(1.0 - lr * s.decay);
-    f.size = static_cast<float>(lr / -expm1(static_cast<double>(t) * s.log_b1));
-    f.root = static_cast<float>(rsqrt(-expm1(static_cast<double>(t) * s.log_b2)));
+    // 1 - b^t as -(e^(t log b) - 1) in fp32: exact to its rounding for small t too, and fp64's exponential would double the launch
+    f.size = static_cast<float>(lr) / -expm1f(static_cast<float>(static_cast<double>(t) * s.log_b1));
+    f.root = 1.0f / sqrtf(-expm1f(static_cast<float>(static_cast<double>(t) * s.log_b2)));
     f.eps = static_cast<float>(s.eps);
     f.key = static_cast<uint32_t>(t) * 0x9E3779B9u;
     *s.factors = f;
@@ -132,112 +133,224 @@ __device__ __forceinline__ uint32_t mix(int64_t i, uint32_t key) {
     x = (x ^ (x >> 15)) * 0x846CA68Bu;
     return x ^ (x >> 16);
 }
-__device__ __forceinline__ float fraction(uint32_t x) { return static_cast<float>(x >> 9) * 1.1920929e-7f; }   // [0, 1)
+// [0, 2^32) to [0, 1) in 23 bits
+__device__ __forceinline__ float fraction(uint32_t x) { return __uint_as_float(0x3F800000u | (x >> 9)) - 1.0f; }
 
 // The code of a in [0, 448] rounded up with probability u's share: a over its step (of at least the subnormal numbers'
 // 2^-9) is in [8, 16) for normal numbers, and codes count steps across the binades.
 __device__ __forceinline__ uint32_t encode(float a, float u) {
     const uint32_t least = 121u << 23, bits = __float_as_uint(a) & 0x7F800000u;
     const uint32_t e = bits > least ? bits : least;
-    const uint32_t k = static_cast<uint32_t>(__fadd_rn(__fmul_rn(a, __uint_as_float((257u << 23) - e)), u));
+    const float steps = __fadd_rn(__fmul_rn(a, __uint_as_float((257u << 23) - e)), u);
+    const uint32_t k = __float_as_uint(__fadd_rd(steps, 8388608.0f)) & 0x1Fu;        // the whole steps: below 2^23 + 17
     const uint32_t code = ((e - least) >> 20) + k;
     return code < 0x7Eu ? code : 0x7Eu;
 }
-__device__ __forceinline__ float decode(uint32_t code) {
-    return __half2float(__half(__nv_cvt_fp8_to_halfraw(static_cast<__nv_fp8_storage_t>(code), __NV_E4M3)));
+__device__ __forceinline__ void decode2(uint32_t codes, float& a, float& b) {        // the lower two
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(codes), __NV_E4M3);
+    const float2 v = __half22float2(__half2(h));
+    a = v.x, b = v.y;
 }
 
-// Eight elements from element i (of the lane's in the aligned form), or every 32nd from i.
-template <typename E, bool kAligned>
-__device__ __forceinline__ void load8(const E* p, int64_t i, int left, float (&v)[8]) {
+// A lane's eight elements of a block: four consecutive ones of either half, so that a warp's words are consecutive in every
+// type (eight consecutive ones, two words of fp32 a lane: 16 bytes of every 32 at a time, 2030 us for 415M elements and 32 bits), or every
+// 32nd of them where a tensor starts on another boundary or ends within the block.
+template <bool kWide>
+__device__ __forceinline__ int place(int j) {
+    const int lane = threadIdx.x & 31;
+    return kWide ? 4 * lane + (j & 3) + 128 * (j >> 2) : 32 * j + lane;
+}
+// What is read and written once a step does not stay in L2 for long: streaming loads and stores.
+template <bool kWide>
+__device__ __forceinline__ void load8(const float* p, int left, float (&v)[8]) {
+    if constexpr (kWide) {
+        const float4 a = __ldcs(reinterpret_cast<const float4*>(p + place<true>(0)));
+        const float4 b = __ldcs(reinterpret_cast<const float4*>(p + place<true>(4)));
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int at = kAligned ? j : 32 * j;
-        v[j] = at < left ? layer::to_f32(p[i + at]) : 0.0f;
+        for (int j = 0; j < 8; ++j) v[j] = place<false>(j) < left ? p[place<false>(j)] : 0.0f;
+    }
+}
+template <bool kWide>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, int left, float (&v)[8]) {
+    if constexpr (kWide) {
+        const uint2 a = __ldcs(reinterpret_cast<const uint2*>(p + place<true>(0)));
+        const uint2 b = __ldcs(reinterpret_cast<const uint2*>(p + place<true>(4)));
+        const uint32_t w[4] = {a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = place<false>(j) < left ? layer::to_f32(p[place<false>(j)]) : 0.0f;
+    }
+}
+template <bool kWide>
+__device__ __forceinline__ void store8(float* p, int left, const float (&v)[8]) {
+    if constexpr (kWide) {
+        __stcs(reinterpret_cast<float4*>(p + place<true>(0)), make_float4(v[0], v[1], v[2], v[3]));
+        __stcs(reinterpret_cast<float4*>(p + place<true>(4)), make_float4(v[4], v[5], v[6], v[7]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (place<false>(j) < left) p[place<false>(j)] = v[j];
+    }
+}
+template <bool kWide>
+__device__ __forceinline__ void store8(__nv_bfloat16* p, int left, const float (&v)[8]) {
+    if constexpr (kWide) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+        __stcs(reinterpret_cast<uint2*>(p + place<true>(0)), make_uint2(w[0], w[1]));
+        __stcs(reinterpret_cast<uint2*>(p + place<true>(4)), make_uint2(w[2], w[3]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (place<false>(j) < left) p[place<false>(j)] = __float2bfloat16_rn(v[j]);
+    }
+}
+template <bool kWide>
+__device__ __forceinline__ void load_codes(const uint8_t* p, int left, float (&v)[8]) {
+    uint32_t w[4];
+    if constexpr (kWide) {
+        w[0] = __ldcs(reinterpret_cast<const uint32_t*>(p + place<true>(0))), w[1] = w[0] >> 16;
+        w[2] = __ldcs(reinterpret_cast<const uint32_t*>(p + place<true>(4))), w[3] = w[2] >> 16;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int a = place<false>(2 * j), b = place<false>(2 * j + 1);
+            w[j] = (a < left ? p[a] : 0u) | (b < left ? static_cast<uint32_t>(p[b]) << 8 : 0u);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) decode2(w[j], v[2 * j], v[2 * j + 1]);
+}
+template <bool kWide>
+__device__ __forceinline__ void store_codes(uint8_t* p, int left, const uint32_t (&v)[8]) {
+    if constexpr (kWide) {
+        __stcs(reinterpret_cast<uint32_t*>(p + place<true>(0)), v[0] | v[1] << 8 | v[2] << 16 | v[3] << 24);
+        __stcs(reinterpret_cast<uint32_t*>(p + place<true>(4)), v[4] | v[5] << 8 | v[6] << 16 | v[7] << 24);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (place<false>(j) < left) p[place<false>(j)] = static_cast<uint8_t>(v[j]);
     }
 }
 
-// One block of 256 elements by a warp.
-template <typename P, typename G, bool kEight, int CAP>
-__device__ __forceinline__ void update(const Table<CAP>& t, int i, int64_t b, const Factors& f) {
-    const int lane = threadIdx.x & 31;
-    const int64_t at = b * kBlock + lane;
-    const int64_t rest = t.numel[i] - at;
-    const int left = rest > kBlock ? kBlock : static_cast<int>(rest);       // elements from the lane's first
-    P* p = static_cast<P*>(t.p[i]);
+// A block's values as codes over its scale.  kFine: they are all finite; else those that are not are held as NaN.
+__device__ __forceinline__ uint32_t largest(const float (&x)[8]) {       // of the warp's sizes as bits: infinities and NaNs are above all
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+        top = b > top ? b : top;
+    }
+    return __reduce_max_sync(0xFFFFFFFFu, top);
+}
+template <bool kRoot, typename F>
+__device__ __forceinline__ void hold(const float (&x)[8], F u, float* scale, uint32_t (&code)[8]) {
+    uint32_t top = largest(x);
+    const bool fine = top < 0x7F800000u;
+    if (!fine) {
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = isfinite(x[j]) ? x[j] : 0.0f;
+        top = largest(y);
+    }
+    const float size = __uint_as_float(top);
+    const bool some = size >= kLeast;
+    const float up = some ? __fmul_rn(__frcp_rn(size), 448.0f) : 0.0f;
+    if ((threadIdx.x & 31) == 0) *scale = some ? __fmul_rn(size, 1.0f / 448.0f) : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        code[j] = encode(__fmul_rn(fabsf(x[j]), up), u(j));
+        if constexpr (kRoot) code[j] = code[j] == 0 && x[j] > 0.0f ? 1u : code[j];       // a moment is never lost: its parameter would leap
+        else code[j] |= x[j] < 0.0f ? 0x80u : 0u;
+    }
+    if (!fine) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!isfinite(x[j])) code[j] = 0x7Fu;
+    }
+}
+
+// One block of 256 elements by a warp, `left` of which the tensor has.
+template <typename P, typename G, bool kEight, bool kWide, int CAP>
+__device__ __forceinline__ void update(const Table<CAP>& t, int i, int64_t b, int left, const Factors& f) {
+    const int64_t at = b * kBlock;
+    P* p = static_cast<P*>(t.p[i]) + at;
     float x[8], g[8], m[8], v[8];
-    load8<P, false>(p, at, left, x);
-    load8<G, false>(static_cast<const G*>(t.g[i]), at, left, g);
+    load8<kWide>(p, left, x);
+    load8<kWide>(static_cast<const G*>(t.g[i]) + at, left, g);
     if constexpr (kEight) {
+        load_codes<kWide>(static_cast<const uint8_t*>(t.m[i]) + at, left, m);
+        load_codes<kWide>(static_cast<const uint8_t*>(t.v[i]) + at, left, v);
         const float ms = t.ms[i][b], vs = t.vs[i][b];
-        const uint8_t *mc = static_cast<const uint8_t*>(t.m[i]), *vc = static_cast<const uint8_t*>(t.v[i]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            m[j] = 32 * j < left ? __fmul_rn(decode(mc[at + 32 * j]), ms) : 0.0f;
-            const float r = 32 * j < left ? __fmul_rn(decode(vc[at + 32 * j]), vs) : 0.0f;
-            v[j] = __fmul_rn(r, r);
+            m[j] = __fmul_rn(m[j], ms);
+            v[j] = __fmul_rn(v[j], vs);
+            v[j] = __fmul_rn(v[j], v[j]);
         }
     } else {
-        load8<float, false>(static_cast<const float*>(t.m[i]), at, left, m);
-        load8<float, false>(static_cast<const float*>(t.v[i]), at, left, v);
+        load8<kWide>(static_cast<const float*>(t.m[i]) + at, left, m);
+        load8<kWide>(static_cast<const float*>(t.v[i]) + at, left, v);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = __fmul_rn(g[j], f.clip);
+    if (f.down != 1.0f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = __fmul_rn(__fmul_rn(g[j], f.down), f.down);
     }
     float root[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        g[j] = __fmul_rn(__fmul_rn(__fmul_rn(g[j], f.clip), f.down), f.down);
         m[j] = __fadd_rn(__fmul_rn(m[j], f.b1), __fmul_rn(g[j], f.not_b1));
         v[j] = __fadd_rn(__fmul_rn(v[j], f.b2), __fmul_rn(__fmul_rn(g[j], g[j]), f.not_b2));
-        root[j] = sqrtf(v[j]);
-        x[j] = x[j] * f.keep - f.size * (m[j] / (root[j] * f.root + f.eps));
+        root[j] = kEight ? __fsqrt_rn(v[j]) : sqrtf(v[j]);
+        x[j] = x[j] * f.keep - f.size * __fdividef(m[j], fmaf(root[j], f.root, f.eps));
     }
+    [[maybe_unused]] uint32_t h[8];
+    if constexpr (kEight || sizeof(P) == 2) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (32 * j >= left) continue;
-        if constexpr (sizeof(P) == 2) {
-            const uint32_t bits = __float_as_uint(x[j]);
-            const uint32_t up = (bits + ((mix(at + 32 * j, f.key) * 0x85EBCA77u) >> 16)) & 0xFFFF0000u;
-            p[at + 32 * j] = isfinite(x[j]) ? __float2bfloat16_rn(__uint_as_float(up)) : __float2bfloat16_rn(x[j]);
-        } else {
-            p[at + 32 * j] = x[j];
-            if (t.copy[i]) t.copy[i][at + 32 * j] = __float2bfloat16_rn(x[j]);
-        }
-        if constexpr (!kEight) {
-            static_cast<float*>(t.m[i])[at + 32 * j] = m[j];
-            static_cast<float*>(t.v[i])[at + 32 * j] = v[j];
+        for (int j = 0; j < 8; ++j) h[j] = mix(at + place<kWide>(j), f.key);
+    }
+    if constexpr (sizeof(P) == 2) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t up = (__float_as_uint(x[j]) + ((h[j] * 0x85EBCA77u) >> 16)) & 0xFFFF0000u;
+            x[j] = isfinite(x[j]) ? __uint_as_float(up) : x[j];
         }
     }
+    store8<kWide>(p, left, x);
+    if constexpr (sizeof(P) == 4)
+        if (t.copy[i]) store8<kWide>(t.copy[i] + at, left, x);
     if constexpr (kEight) {
-        float mt = 0.0f, vt = 0.0f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (32 * j >= left) continue;
-            if (isfinite(m[j])) mt = fmaxf(mt, fabsf(m[j]));
-            if (isfinite(root[j])) vt = fmaxf(vt, root[j]);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            mt = fmaxf(mt, __shfl_xor_sync(0xFFFFFFFFu, mt, o));
-            vt = fmaxf(vt, __shfl_xor_sync(0xFFFFFFFFu, vt, o));
-        }
-        const float mu = mt >= kLeast ? __fmul_rn(__frcp_rn(mt), 448.0f) : 0.0f;
-        const float vu = vt >= kLeast ? __fmul_rn(__frcp_rn(vt), 448.0f) : 0.0f;
-        if (lane == 0) {
-            t.ms[i][b] = mt >= kLeast ? __fmul_rn(mt, 1.0f / 448.0f) : 0.0f;
-            t.vs[i][b] = vt >= kLeast ? __fmul_rn(vt, 1.0f / 448.0f) : 0.0f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (32 * j >= left) continue;
-            const uint32_t h = mix(at + 32 * j, f.key);
-            uint32_t mc = 0x7Fu, vc = 0x7Fu;
-            if (isfinite(m[j])) mc = encode(__fmul_rn(fabsf(m[j]), mu), fraction(h)) | (m[j] < 0.0f ? 0x80u : 0u);
-            if (isfinite(root[j])) {
-                vc = encode(__fmul_rn(root[j], vu), fraction(h * 0x9E3779B1u));
-                if (vc == 0 && root[j] > 0.0f) vc = 1;      // a moment is never lost: its parameter would leap
-            }
-            static_cast<uint8_t*>(t.m[i])[at + 32 * j] = static_cast<uint8_t>(mc);
-            static_cast<uint8_t*>(t.v[i])[at + 32 * j] = static_cast<uint8_t>(vc);
-        }
+        uint32_t code[8];
+        hold<false>(m, [&](int j) { return fraction(h[j]); }, t.ms[i] + b, code);
+        store_codes<kWide>(static_cast<uint8_t*>(t.m[i]) + at, left, code);
+        hold<true>(root, [&](int j) { return fraction(h[j] * 0x9E3779B1u); }, t.vs[i] + b, code);
+        store_codes<kWide>(static_cast<uint8_t*>(t.v[i]) + at, left, code);
+    } else {
+        store8<kWide>(static_cast<float*>(t.m[i]) + at, left, m);
+        store8<kWide>(static_cast<float*>(t.v[i]) + at, left, v);
+    }
+}
+
+__device__ __forceinline__ void prefetch(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// The blocks of [a, e) of tensor i, whose values have types P and G.
+template <typename P, typename G, bool kEight, int CAP>
+__device__ __forceinline__ void update_run(const Table<CAP>& t, int i, int64_t a, int64_t e, const Factors& f) {
+    const int64_t b1 = (e + kBlock - 1) / kBlock;
+    for (int64_t b = a / kBlock + (threadIdx.x >> 5); b < b1; b += kWarps) {
+        const int64_t left = t.numel[i] - b * kBlock;
+        if (t.flags[i].aligned && left >= kBlock) update<P, G, kEight, true>(t, i, b, kBlock, f);
+        else update<P, G, kEight, false>(t, i, b, left < kBlock ? static_cast<int>(left) : kBlock, f);
     }
 }
 
@@ -245,22 +358,36 @@ template <int CAP, bool kEight>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) step_kernel(const __grid_constant__ Table<CAP> t) {
     const int c0 = static_cast<int>(static_cast<int64_t>(t.chunks) * blockIdx.x / gridDim.x);
     const int c1 = static_cast<int>(static_cast<int64_t>(t.chunks) * (blockIdx.x + 1) / gridDim.x);
+    // elements [a, e) of tensor i in this block's chunks
+    auto part = [&](int i, int64_t& a, int64_t& e) {
+        a = c0 > t.first[i] ? (c0 - t.first[i]) * t.chunk : 0;
+        e = c1 < t.first[i + 1] ? (c1 - t.first[i]) * t.chunk : t.numel[i];
+    };
+    const int i0 = tensor_of(t, c0);
+    {   // the first block's values on their way while the factors are made
+        int64_t a, e;
+        part(i0, a, e);
+        a += (threadIdx.x >> 5) * kBlock + place<true>(0);
+        if (a < t.numel[i0]) {
+            prefetch(static_cast<const uint8_t*>(t.p[i0]) + a * (t.flags[i0].p_f32 ? 4 : 2));
+            prefetch(static_cast<const uint8_t*>(t.g[i0]) + a * (t.flags[i0].g_f32 ? 4 : 2));
+            prefetch(static_cast<const uint8_t*>(t.m[i0]) + a * (kEight ? 1 : 4));
+            prefetch(static_cast<const uint8_t*>(t.v[i0]) + a * (kEight ? 1 : 4));
+        }
+    }
     grid_wait();
     grid_release();
     const Factors f = *t.factors;
     if (f.skip || c0 >= c1) return;
-    for (int i = tensor_of(t, c0); i < t.count && t.first[i] < c1; ++i) {
-        const int64_t a = c0 > t.first[i] ? (c0 - t.first[i]) * t.chunk : 0;
-        const int64_t e = c1 < t.first[i + 1] ? (c1 - t.first[i]) * t.chunk : t.numel[i];
-        const int64_t b1 = (e + kBlock - 1) / kBlock;
-        for (int64_t b = a / kBlock + (threadIdx.x >> 5); b < b1; b += kWarps) {
-            if (t.flags[i].p_f32) {
-                if (t.flags[i].g_f32) update<float, float, kEight>(t, i, b, f);
-                else update<float, __nv_bfloat16, kEight>(t, i, b, f);
-            } else {
-                if (t.flags[i].g_f32) update<__nv_bfloat16, float, kEight>(t, i, b, f);
-                else update<__nv_bfloat16, __nv_bfloat16, kEight>(t, i, b, f);
-            }
+    for (int i = i0; i < t.count && t.first[i] < c1; ++i) {
+        int64_t a, e;
+        part(i, a, e);
+        if (t.flags[i].p_f32) {
+            if (t.flags[i].g_f32) update_run<float, float, kEight>(t, i, a, e, f);
+            else update_run<float, __nv_bfloat16, kEight>(t, i, a, e, f);
+        } else {
+            if (t.flags[i].g_f32) update_run<__nv_bfloat16, float, kEight>(t, i, a, e, f);
+            else update_run<__nv_bfloat16, __nv_bfloat16, kEight>(t, i, a, e, f);
         }
     }
 }
@@ -328,6 +455,12 @@ static int launch_tables(void* const* params, const int* param_dtypes, const voi
         t.numel[k] = numel[i];
         t.first[k] = chunks;
         t.flags[k].p_f32 = param_dtypes[i] == DTP_F32, t.flags[k].g_f32 = grad_dtypes[i] == DTP_F32;
+        uintptr_t all = reinterpret_cast<uintptr_t>(params[i]) | reinterpret_cast<uintptr_t>(grads[i]) |
+                        reinterpret_cast<uintptr_t>(t.copy[k]);
+        // four codes are a word of 4 bytes
+        const uintptr_t held = reinterpret_cast<uintptr_t>(m[i]) | reinterpret_cast<uintptr_t>(v[i]);
+        all |= eight ? 4 * held : held;
+        t.flags[k].aligned = (all & 15) == 0;
         chunks += static_cast<int>((numel[i] + t.chunk - 1) / t.chunk);
     }
     return t.count ? flush() : static_cast<int>(DTP_OK);

@@ -31,11 +31,11 @@ namespace layer {
 
 // A launch whose start may overlap the end of the one before it.
 template <typename... P, typename... A>
-int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t stream, A... args) {
+int launch_blocks(void (*kernel)(P...), int64_t blocks, int threads, cudaStream_t stream, A... args) {
     if (blocks > 0x7FFFFFFF) return DTP_ERR_UNSUPPORTED;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-    cfg.blockDim = dim3(256);
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -44,6 +44,11 @@ int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t stream, A...
     cfg.numAttrs = 1;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return DTP_OK;
+}
+
+template <typename... P, typename... A>
+int launch_after(void (*kernel)(P...), int64_t blocks, cudaStream_t stream, A... args) {
+    return launch_blocks(kernel, blocks, 256, stream, args...);
 }
 
 // Pieces of a workspace, in the order in which they are asked for.

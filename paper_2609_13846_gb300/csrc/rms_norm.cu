@@ -3,10 +3,17 @@
 //     rms_t = sqrt(mean_i x_ti^2 + eps),  y = gamma n,  n = x / rms
 //     dx = (dn - n mean_i(dn n)) / rms + dresidual,  dn = gamma dy,   dgamma_i = sum_t dy_ti n_ti
 //
-// Bound by memory.  Sums in fp32 (a row's in 256 threads' parts); dgamma's in runs of at most kRun rows, which are added in fp64.
+// Bound by memory: each value is read and written once.  A row lies in the registers of a warp (to 512 columns) or of a
+// block of 128 to 512 threads (to 8192), eight consecutive columns to a thread at a time, so that its sum and what is made of it need one read.  Backward,
+// a thread keeps its columns' sums for dgamma over the rows that its group takes, at most kRun; the groups of a block add theirs
+// in shared memory, and the blocks' are added by a last launch.  Wider rows go through memory again (from L2).  Rows that
+// are not on 16-byte boundaries are read element by element in the same places, with the same results bit for bit.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <string.h>
+
+#include <type_traits>
 
 #include "dtp_common.cuh"
 #include "layer_common.cuh"
@@ -22,6 +29,11 @@ using layer::to_f32;
 
 constexpr int kThreads = 256;
 constexpr int kRun = 256;              // rows of a partial sum of dgamma
+constexpr int kWidest = 8192;          // columns of a row in registers
+constexpr int kSms = 152;              // for which the backward pass's blocks are counted
+
+// Threads of a block whose rows take TPR threads each.
+__host__ __device__ constexpr int block_threads(int tpr) { return tpr > 32 ? tpr : kThreads; }
 constexpr float kDown = 5.4210109e-20f;      // 2^-64: a row whose squares leave fp32's range is summed again at this scale
 
 __device__ __forceinline__ float block_sum(float v, float* red) {
@@ -37,6 +49,259 @@ __device__ __forceinline__ float block_sum(float v, float* red) {
     return s;
 }
 
+// Sums over the threads of a row: 32 of them, or the block.  kRows values at once; `red` is used in turns, so that one barrier is
+// enough: who writes it again has passed the barrier of the turn between.
+template <int TPR, int kRows>
+__device__ __forceinline__ void row_sums(float (&v)[kRows], float (&red)[2][kRows][TPR / 32], int turn) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[r] += __shfl_xor_sync(0xFFFFFFFFu, v[r], o);
+    if constexpr (TPR > 32) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+            if (lane == 0) red[turn & 1][r][warp] = v[r];
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            v[r] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < TPR / 32; w += 4) {
+                const float4 a = *reinterpret_cast<const float4*>(red[turn & 1][r] + w);
+                v[r] += (a.x + a.y) + (a.z + a.w);
+            }
+        }
+    }
+}
+
+// Eight columns as they lie in memory.
+template <typename E>
+struct Octet {
+    uint4 q[sizeof(E) == 2 ? 1 : 2];
+    template <bool kWide>
+    __device__ __forceinline__ void load(const E* p, int left) {
+        if constexpr (kWide) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(q) / 16); ++i)
+                q[i] = left > 0 ? reinterpret_cast<const uint4*>(p)[i] : make_uint4(0, 0, 0, 0);
+        } else {
+            E e[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = j < left ? p[j] : from_f32<E>(0.0f);
+            memcpy(q, e, sizeof(q));
+        }
+    }
+    template <bool kWide>
+    __device__ __forceinline__ void store(E* p, int left) const {
+        if constexpr (kWide) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(q) / 16); ++i)
+                if (left > 0) reinterpret_cast<uint4*>(p)[i] = q[i];
+        } else {
+            E e[8];
+            memcpy(e, q, sizeof(q));
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < left) p[j] = e[j];
+        }
+    }
+    __device__ __forceinline__ void get(float (&v)[8]) const {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(q);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = sizeof(E) == 4 ? __uint_as_float(w[j])
+                                  : __uint_as_float(j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        E e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = from_f32<E>(v[j]);
+        memcpy(q, e, sizeof(q));
+    }
+};
+
+// A thread's columns: octets of row_threads, OCT of them.  kWide: every row and gamma on 16-byte boundaries.
+template <typename E, int TPR, int OCT, int kRows, bool kWide>
+__global__ void __launch_bounds__(block_threads(TPR)) forward_rows_kernel(const E* X, const float* gamma, int64_t T, int d, float eps, E* Y,
+                                                                float* rms) {
+    __shared__ __align__(16) float red[2][kRows][TPR / 32];
+    grid_wait();
+    grid_release();
+    constexpr int kGroups = block_threads(TPR) / TPR;
+    const int me = threadIdx.x % TPR;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups * kRows;
+    const float width = static_cast<float>(d);
+    int turn = 0;
+    // groups of a block stay together: their rows are first .. first + kGroups * kRows - 1
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T; first += stride) {
+        const int64_t t0 = first + threadIdx.x / TPR * kRows;
+        Octet<E> x[kRows][OCT];
+        float s[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int k = 0; k < OCT; ++k) {
+                const int c = (me + TPR * k) * 8;
+                x[r][k].template load<kWide>(X + (t0 + r) * d + c, t0 + r < T ? d - c : 0);
+            }
+        auto squares = [&](float scale) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                s[r] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < OCT; ++k) {
+                    float v[8];
+                    x[r][k].get(v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= scale, s[r] = fmaf(v[j], v[j], s[r]);
+                }
+            }
+            row_sums<TPR, kRows>(s, red, turn++);
+        };
+        squares(1.0f);
+        float root[kRows];
+        bool again = false;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            root[r] = sqrtf(s[r] / width + eps);
+            again |= !(s[r] / width <= 3.0e38f);
+        }
+        if (TPR > 32 ? again : __any_sync(0xFFFFFFFFu, again)) {       // the same for all threads of a row
+            squares(kDown);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
+                if (!(root[r] <= 1.7e19f)) root[r] = sqrtf(s[r] / width) / kDown;
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (t0 + r >= T) continue;
+            if (me == 0 && rms) rms[t0 + r] = root[r];
+            const float inv = 1.0f / root[r];
+            const bool tiny = !(root[r] <= 8.0e37f);       // its reciprocal would be among fp32's subnormal numbers
+#pragma unroll
+            for (int k = 0; k < OCT; ++k) {
+                const int c = (me + TPR * k) * 8;
+                Octet<float> g;
+                g.template load<kWide>(gamma + c, d - c);
+                float v[8], w[8];
+                x[r][k].get(v);
+                g.get(w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = (tiny ? v[j] / root[r] : v[j] * inv) * w[j];
+                Octet<E> y;
+                y.set(v);
+                y.template store<kWide>(Y + (t0 + r) * d + c, d - c);
+            }
+        }
+    }
+}
+
+// dX, and the block's part of dgamma in partial[block] [d].
+template <typename E, int TPR, int OCT, int kRows, bool kWide>
+__global__ void __launch_bounds__(block_threads(TPR), 512 / block_threads(TPR))
+backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* rms, const E* dres, int64_t T, int d, E* dX,
+                     float* partial) {
+    constexpr int kGroups = block_threads(TPR) / TPR;
+    __shared__ __align__(16) float red[2][kRows][TPR / 32];
+    __shared__ float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? TPR * 8 + 4 : 1];
+    grid_wait();
+    grid_release();
+    const int me = threadIdx.x % TPR;
+    float g[OCT][8], acc[OCT][8];
+#pragma unroll
+    for (int k = 0; k < OCT; ++k) {
+        const int c = (me + TPR * k) * 8;
+        Octet<float> q;
+        q.template load<kWide>(gamma ? gamma + c : gamma, gamma ? d - c : 0);
+        q.get(g[k]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[k][j] = 0.0f;
+    }
+    const float width = static_cast<float>(d);
+    int turn = 0;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T;
+         first += static_cast<int64_t>(gridDim.x) * kGroups * kRows) {
+        const int64_t t0 = first + threadIdx.x / TPR * kRows;
+        Octet<E> x[kRows][OCT], y[kRows][OCT], z[kRows][OCT];
+        float root[kRows], s[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const bool in = t0 + r < T;
+            root[r] = in ? rms[t0 + r] : 1.0f;
+#pragma unroll
+            for (int k = 0; k < OCT; ++k) {
+                const int c = (me + TPR * k) * 8;
+                const int64_t at = (t0 + r) * d + c;
+                x[r][k].template load<kWide>(X + at, in ? d - c : 0);
+                y[r][k].template load<kWide>(dY + at, in ? d - c : 0);
+                z[r][k].template load<kWide>(dres + at, in && dres ? d - c : 0);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const float inv = 1.0f / root[r];
+            s[r] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < OCT; ++k) {
+                float n[8], v[8];
+                x[r][k].get(n);
+                y[r][k].get(v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    n[j] *= inv;
+                    acc[k][j] = fmaf(v[j], n[j], acc[k][j]);
+                    s[r] = fmaf(v[j] * g[k][j], n[j], s[r]);
+                }
+            }
+        }
+        if (!dX) continue;
+        row_sums<TPR, kRows>(s, red, turn++);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            if (t0 + r >= T) continue;
+            const float inv = 1.0f / root[r], mean = s[r] / width;
+#pragma unroll
+            for (int k = 0; k < OCT; ++k) {
+                const int c = (me + TPR * k) * 8;
+                float n[8], v[8], w[8];
+                x[r][k].get(n);
+                y[r][k].get(v);
+                z[r][k].get(w);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = fmaf(fmaf(-n[j] * inv, mean, v[j] * g[k][j]), inv, w[j]);
+                Octet<E> o;
+                o.set(v);
+                o.template store<kWide>(dX + (t0 + r) * d + c, d - c);
+            }
+        }
+    }
+    if (!partial) return;
+#pragma unroll
+    for (int k = 0; k < OCT; ++k) {
+        if constexpr (kGroups > 1) {               // the groups' sums in order, a chunk of columns at a time
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[threadIdx.x / TPR][me * 8 + j] = acc[k][j];
+            __syncthreads();
+            for (int i = threadIdx.x; i < TPR * 8; i += block_threads(TPR)) {
+                float v = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kGroups; ++q) v += sums[q][i];
+                const int c = TPR * 8 * k + i;
+                if (c < d) partial[static_cast<int64_t>(blockIdx.x) * d + c] = v;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = (me + TPR * k) * 8 + j;
+                if (c < d) partial[static_cast<int64_t>(blockIdx.x) * d + c] = acc[k][j];
+            }
+        }
+    }
+}
+
+// Rows wider than kWidest.
 template <typename E>
 __global__ void __launch_bounds__(kThreads)
 forward_kernel(const E* X, const float* gamma, int64_t T, int d, float eps, E* Y, float* rms) {
@@ -55,7 +320,7 @@ forward_kernel(const E* X, const float* gamma, int64_t T, int d, float eps, E* Y
         };
         const float s = squares(1.0f);
         const float r = s <= 3.0e38f ? sqrtf(s + eps) : sqrtf(squares(kDown)) / kDown;
-        if (threadIdx.x == 0) rms[t] = r;
+        if (threadIdx.x == 0 && rms) rms[t] = r;
         for (int i = threadIdx.x; i < d; i += kThreads) Y[t * d + i] = from_f32<E>(to_f32(x[i]) / r * gamma[i]);
     }
 }
@@ -96,53 +361,120 @@ columns_kernel(const E* dY, const E* X, const float* rms, int64_t T, int d, floa
     partial[run * d + i] = s;
 }
 
+// A sum of many fp32 terms with the rounding errors of the additions carried along.
+struct Total {
+    float sum = 0.0f, lost = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float t = sum + x, b = t - sum;
+        lost += (sum - (t - b)) + (x - b);
+        sum = t;
+    }
+    // the errors of infinite sums are no numbers
+    __device__ __forceinline__ float value() const { return isfinite(sum) ? sum + lost : sum; }
+};
+
+// dgamma from the partial sums: each of 8 warps adds every eighth in order, then the warps' sums in order, with their errors (in fp64, whose
+// additions are slow here: 40 us for 304 sums of 1537 columns).
 __global__ void __launch_bounds__(256) join_kernel(const float* partial, int64_t runs, int d, float* dgamma) {
-    __shared__ double red[8][32];
+    __shared__ Total red[8][32];
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
-    double s = 0.0;
+    Total s;
     if (i < d)
-        for (int64_t r = warp; r < runs; r += 8) s += partial[r * d + i];
+#pragma unroll 8
+        for (int64_t r = warp; r < runs; r += 8) s.add(partial[r * d + i]);
     red[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && i < d) {
-        double v = 0.0;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) v += red[w][lane];
-        dgamma[i] = static_cast<float>(v);
+        for (int w = 1; w < 8; ++w) s.add(red[w][lane].sum), s.lost += red[w][lane].lost;
+        dgamma[i] = s.value();
     }
 }
 
-static int64_t runs_of(int64_t T) { return (T + kRun - 1) / kRun; }
+// The form for rows of d columns: threads of a row, octets of a thread, rows of a group at a time (so that loads of 64 to 128 bytes a
+// thread are in flight without spilling the backward pass's registers).
+template <int TPR_, int OCT_, int ROWS_>
+struct Form {
+    static constexpr int TPR = TPR_, OCT = OCT_, ROWS = ROWS_, kBlock = block_threads(TPR), kPerBlock = kBlock / TPR * ROWS;
+};
+template <int kHalf, typename F>
+static int64_t with_form(int d, F fn) {
+    if (d <= 256) return fn(Form<32, 1, 2 / kHalf>());
+    if (d <= 512) return fn(Form<32, 2, 1>());
+    if (d <= 1024) return fn(Form<128, 1, 4 / kHalf>());
+    if (d <= 2048) return fn(Form<256, 1, 4 / kHalf>());
+    if (d <= 4096) return fn(Form<256, 2, 2 / kHalf>());
+    return fn(Form<512, 2, 2 / kHalf>());
+}
+template <typename E, typename F>
+static int64_t with_form_of(int d, F fn) { return with_form<sizeof(E) / 2>(d, fn); }      // fp32 takes half the rows
+
+// Blocks of the backward pass, each with a partial sum of dgamma: as many as run at once, but no more than kRun rows for a group.
+template <typename E>
+static int64_t backward_blocks(int64_t T, int d) {
+    if (d > kWidest) return (T + kRun - 1) / kRun;
+    return with_form_of<E>(d, [&](auto form) -> int64_t {
+        using F = decltype(form);
+        const int64_t tiles = (T + F::kPerBlock - 1) / F::kPerBlock;
+        const int64_t least = (tiles * F::ROWS + kRun - 1) / kRun, once = kSms * (512 / F::kBlock);
+        const int64_t n = least > once ? least : once;
+        return n < tiles ? n : tiles;
+    });
+}
 
 size_t backward_workspace_bytes(int64_t T, int d) {
     layer::Carver c(nullptr);
-    c.take(static_cast<size_t>(runs_of(T)) * d * sizeof(float));
+    const int64_t a = backward_blocks<float>(T, d), b = backward_blocks<__nv_bfloat16>(T, d);
+    c.take(static_cast<size_t>(a > b ? a : b) * d * sizeof(float));
     return c.used;
+}
+
+static bool wide(int d, const void* a, const void* b, const void* c, const void* e, const void* gamma) {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c) |
+                          reinterpret_cast<uintptr_t>(e) | reinterpret_cast<uintptr_t>(gamma);
+    return (all & 15) == 0 && d % 8 == 0;
 }
 
 template <typename E>
 static int forward(const void* X, const float* gamma, int64_t T, int d, float eps, void* Y, float* rms, cudaStream_t stream) {
-    return layer::launch_after(forward_kernel<E>, T < 8192 ? T : 8192, stream, static_cast<const E*>(X), gamma, T, d, eps,
-                               static_cast<E*>(Y), rms);
+    const E* x = static_cast<const E*>(X);
+    E* y = static_cast<E*>(Y);
+    if (d > kWidest)
+        return layer::launch_blocks(forward_kernel<E>, T < 8192 ? T : 8192, kThreads, stream, x, gamma, T, d, eps, y, rms);
+    return static_cast<int>(with_form_of<E>(d, [&](auto form) -> int64_t {
+        using F = decltype(form);
+        const int64_t tiles = (T + F::kPerBlock - 1) / F::kPerBlock, blocks = tiles < 16384 ? tiles : 16384;
+        auto kernel = wide(d, X, Y, nullptr, nullptr, gamma) ? forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, true>
+                                                             : forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, false>;
+        return layer::launch_blocks(kernel, blocks, F::kBlock, stream, x, gamma, T, d, eps, y, rms);
+    }));
 }
 
 template <typename E>
 static int backward(const void* dY, const void* X, const float* gamma, const float* rms, const void* dres, int64_t T, int d,
                     void* dX, float* dgamma, void* workspace, cudaStream_t stream) {
-    int st = DTP_OK;
-    if (dX && T > 0)
-        st = layer::launch_after(rows_kernel<E>, T < 8192 ? T : 8192, stream, static_cast<const E*>(dY), static_cast<const E*>(X),
-                                 gamma, rms, static_cast<const E*>(dres), T, d, static_cast<E*>(dX));
-    if (st != DTP_OK || !dgamma) return st;
+    const E *dy = static_cast<const E*>(dY), *x = static_cast<const E*>(X), *dr = static_cast<const E*>(dres);
+    E* dx = static_cast<E*>(dX);
     layer::Carver c(workspace);
-    auto* partial = static_cast<float*>(c.take(static_cast<size_t>(runs_of(T)) * d * sizeof(float)));
-    if (T > 0)
-        st = layer::launch_after(columns_kernel<E>, runs_of(T) * ((d + kThreads - 1) / kThreads), stream,
-                                 static_cast<const E*>(dY), static_cast<const E*>(X), rms, T, d, partial);
-    if (st != DTP_OK) return st;
-    return layer::launch_after(join_kernel, (d + 31) / 32, stream, static_cast<const float*>(partial), runs_of(T), d, dgamma);
+    const int64_t blocks = backward_blocks<E>(T, d);
+    auto* partial = static_cast<float*>(c.take(static_cast<size_t>(blocks) * d * sizeof(float)));
+    int st = DTP_OK;
+    if (T > 0 && d > kWidest) {
+        if (dX) st = layer::launch_blocks(rows_kernel<E>, T < 8192 ? T : 8192, kThreads, stream, dy, x, gamma, rms, dr, T, d, dx);
+        if (st == DTP_OK && dgamma)
+            st = layer::launch_blocks(columns_kernel<E>, blocks * ((d + kThreads - 1) / kThreads), kThreads, stream, dy, x, rms, T, d, partial);
+    } else if (T > 0 && (dX || dgamma)) {
+        st = static_cast<int>(with_form_of<E>(d, [&](auto form) -> int64_t {
+            using F = decltype(form);
+            auto kernel = wide(d, dY, X, dres, dX, gamma) ? backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, true>
+                                                          : backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, false>;
+            return layer::launch_blocks(kernel, blocks, F::kBlock, stream, dy, x, gamma, rms, dr, T, d, dx, dgamma ? partial : nullptr);
+        }));
+    }
+    if (st != DTP_OK || !dgamma) return st;
+    return layer::launch_blocks(join_kernel, (d + 31) / 32, kThreads, stream, static_cast<const float*>(partial), T > 0 ? blocks : 0, d, dgamma);
 }
 
 int launch_forward(const void* X, const float* gamma, int64_t T, int d, float eps, int dtype, void* Y, float* rms,
