@@ -2,7 +2,8 @@
 
 Each ``csrc/*.cu`` translation unit is compiled in parallel into
 ``_build/*.o`` and linked into ``paper_2609_13846_gb300/libdtp.so`` in the
-source tree.  Run as ``python -m paper_2609_13846_gb300.build``.
+source tree; ``csrc/tensor_lists.cpp``, the binding's reader of lists of tensors, becomes the
+CPython module ``_tensor_lists.so`` beside it.  Run as ``python -m paper_2609_13846_gb300.build``.
 """
 from __future__ import annotations
 
@@ -12,12 +13,15 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdtp.so")
+LISTS = os.path.join(PKG, "_tensor_lists.so")
+LISTS_SOURCE = os.path.join(CSRC, "tensor_lists.cpp")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -52,12 +56,42 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def _build_lists() -> None:
+    import torch
+    root = os.path.dirname(torch.__file__)
+    lib = os.path.join(root, "lib")
+    cuda = os.path.dirname(os.path.dirname(nvcc()))
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    tmp = LISTS + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{p}" for p in include), LISTS_SOURCE, "-o", tmp, f"-L{lib}", f"-Wl,-rpath,{lib}", "-ltorch_python", "-ltorch_cpu",
+           "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for {LISTS_SOURCE}:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, LISTS)
+
+
+def _stale(target: str, sources) -> bool:
+    return not os.path.exists(target) or os.path.getmtime(target) < max(os.path.getmtime(p) for p in sources)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libdtp.so if any source or header is newer than it; return its path."""
+    """Build libdtp.so and _tensor_lists.so where a source or header is newer; return the library's path."""
     srcs = _sources()
-    newest = max(os.path.getmtime(p) for p in srcs + _headers() + [__file__])
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= newest:
-        return LIB
+    lists = force or _stale(LISTS, [LISTS_SOURCE, __file__])
+    library = force or _stale(LIB, srcs + _headers() + [__file__])
+    with cf.ThreadPoolExecutor(max_workers=1) as beside:
+        done = beside.submit(_build_lists) if lists else None
+        if library:
+            _build_library(srcs, verbose)
+        if done:
+            done.result()
+    return LIB
+
+
+def _build_library(srcs, verbose: bool) -> None:
     os.makedirs(BUILD, exist_ok=True)
     with cf.ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
@@ -67,7 +101,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    return LIB
 
 
 if __name__ == "__main__":

@@ -9,8 +9,10 @@ from __future__ import annotations
 
 import array
 import ctypes
+import importlib.util
 import operator
 import os
+import sys
 
 import torch
 
@@ -1322,11 +1324,32 @@ def _scalar_on(name, t, dtype, index):
     return t.data_ptr()
 
 
-def _codes_of(name, dtypes):
-    try:
-        return array.array("i", [_LAYER_CODES[d] for d in dtypes])
-    except KeyError:
-        raise TypeError(f"{name} must be bfloat16 or float32") from None
+_tensor_lists = None
+
+
+def _read_list(*args):
+    """(addresses, sizes, type codes), as bytes, of a list of tensors: _tensor_lists.read, which checks them too."""
+    global _tensor_lists
+    if _tensor_lists is None:
+        if not os.path.exists(os.path.join(_PKG, "_tensor_lists.so")):
+            raise RuntimeError("_tensor_lists.so is missing: build it with `python -m paper_2609_13846_gb300.build`")
+        spec = importlib.util.spec_from_file_location("_tensor_lists", os.path.join(_PKG, "_tensor_lists.so"))
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _tensor_lists = module
+    return _tensor_lists.read(*args)
+
+
+_E4M3 = 2                       # a type code of _tensor_lists alone
+
+
+def _all_codes(codes: bytes, code: int) -> bool:
+    return codes == code.to_bytes(4, sys.byteorder) * (len(codes) // 4)
+
+
+def _all_floats(name: str, codes: bytes):
+    if not set(array.array("i", codes)) <= {DTP_BF16, DTP_F32}:
+        raise TypeError(f"{name} must be bfloat16 or float32")
 
 
 def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
@@ -1341,50 +1364,29 @@ def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 
     written), and a norm that is not finite leaves everything as it is.  copies: bf16 tensors like fp32 params, which
     receive the updated parameters (None for those without).
     """
-    params, grads = list(params), list(grads)
+    params = list(params)
     count = len(params)
     if count == 0:
         raise ValueError("params must hold at least one tensor")
     index = params[0].get_device()
-    p, numel, pd = _flat_tensors("params", params, index)
-    g, g_numel, gd = _flat_tensors("grads", grads, index)
-    if g_numel != numel:
-        raise ValueError("grads must have the sizes of params")
-    held_at = [a for a, n in zip(p, numel) if n]
-    if len(set(held_at)) != len(held_at):
-        raise ValueError("params must not hold a tensor twice")
-    pc, gc = _codes_of("params", pd), _codes_of("grads", gd)
+    p, numel, pc = _read_list("params", params, index, None, 1, True)
+    g, _, gc = _read_list("grads", list(grads), index, numel, 1, False)
+    _all_floats("params", pc)
+    _all_floats("grads", gc)
     bits = state["bits"]
     if bits not in (8, 32):
         raise ValueError(f"the state's bits must be 8 or 32, got {bits}")
-    held = torch.float32 if bits == 32 else torch.float8_e4m3fn
-    at = [p, g]
-    for k in ("m", "v"):
-        a, n, d = _flat_tensors(f"the state's {k}", state[k], index)
-        if n != numel or d.count(held) != count:
-            raise ValueError(f"the state's {k} must be {held} tensors of the sizes of params")
-        at.append(a)
-    blocks = array.array("q", [-(-n // ADAMW_BLOCK) for n in numel])
-    for k in ("m_scale", "v_scale"):
-        if bits == 32:
-            at.append(None)
-            continue
-        a, n, d = _flat_tensors(f"the state's {k}", state[k], index)
-        if n != blocks or d.count(torch.float32) != count:
-            raise ValueError(f"the state's {k} must be fp32 tensors with a value for each {ADAMW_BLOCK} elements")
-        at.append(a)
-    if copies is not None:
-        copies = list(copies)
-        some = [(i, c) for i, c in enumerate(copies) if c is not None]
-        a, n, d = _flat_tensors("copies", [c for _, c in some], index)
-        if len(copies) != count or d.count(torch.bfloat16) != len(some) or any(
-                n[j] != numel[i] or pc[i] != DTP_F32 for j, (i, _) in enumerate(some)):
-            raise ValueError("copies must be bfloat16 tensors like params, which are float32, or None")
-        full = array.array("Q", bytes(8 * count))
-        for j, (i, _) in enumerate(some):
-            full[i] = a[j]
-        copies = full
-    at.append(copies)
+    held, ms, vs = (DTP_F32 if bits == 32 else _E4M3), None, None
+    m, _, mc = _read_list("the state's m", list(state["m"]), index, numel, 1, True)
+    v, _, vc = _read_list("the state's v", list(state["v"]), index, numel, 1, True)
+    if not (_all_codes(mc, held) and _all_codes(vc, held)):
+        raise TypeError(f"the state's moments must be {'float32' if bits == 32 else 'float8_e4m3fn'} with {bits} bits")
+    if bits == 8:
+        ms, _, mc = _read_list("the state's m_scale", list(state["m_scale"]), index, numel, ADAMW_BLOCK, True)
+        vs, _, vc = _read_list("the state's v_scale", list(state["v_scale"]), index, numel, ADAMW_BLOCK, True)
+        if not (_all_codes(mc, DTP_F32) and _all_codes(vc, DTP_F32)):
+            raise TypeError("the state's scales must be float32")
+    c = None if copies is None else _copies(list(copies), index, numel, pc)
     step = _scalar_on("the state's step", state["step"], torch.int64, index)
     lr_at = _scalar_on("lr", lr, torch.float32, index) if isinstance(lr, torch.Tensor) else None
     norm_at = None if norm is None else _scalar_on("norm", norm, torch.float32, index)
@@ -1393,10 +1395,25 @@ def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 
         workspace = _keep(adamw_workspace(params), stream)
     else:
         _workspace_check(workspace, index)
-    # the arrays themselves stay in `at` until the call has read them
-    first = [None if a is None else a.buffer_info()[0] for a in at]
-    st = lib().dtp_adamw(first[0], pc.buffer_info()[0], first[1], gc.buffer_info()[0], *first[2:], numel.buffer_info()[0], count,
-                         ctypes.byref(opts), lr_at, norm_at, step, _ptr(workspace), workspace.numel(),
-                         _layer_stream(stream, index))
+    st = lib().dtp_adamw(p, pc, g, gc, m, v, ms, vs, c, numel, count, ctypes.byref(opts), lr_at, norm_at, step, _ptr(workspace),
+                         workspace.numel(), _layer_stream(stream, index))
     if st:
         _check("dtp_adamw", st)
+
+
+def _copies(copies, index: int, numel: bytes, param_codes: bytes) -> bytes:
+    """Addresses of adamw_step's copies, 0 for None."""
+    sizes, codes = array.array("q", numel), array.array("i", param_codes)
+    if len(copies) != len(sizes):
+        raise ValueError(f"copies must hold as many tensors as params, got {len(copies)}")
+    some = [i for i, t in enumerate(copies) if t is not None]
+    like = numel if len(some) == len(copies) else array.array("q", [sizes[i] for i in some]).tobytes()
+    at, _, types = _read_list("copies", [copies[i] for i in some], index, like, 1, True)
+    if not _all_codes(types, DTP_BF16) or any(codes[i] != DTP_F32 for i in some):
+        raise TypeError("copies must be bfloat16, of float32 params")
+    if len(some) == len(copies):
+        return at
+    full = array.array("Q", bytes(8 * len(copies)))
+    for i, a in zip(some, array.array("Q", at)):
+        full[i] = a
+    return full.tobytes()
