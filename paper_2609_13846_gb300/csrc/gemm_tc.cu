@@ -63,6 +63,7 @@ struct Form {
 // A launch's products: one (of one or two segments, or with a second B or output), or up to three of the same K and
 // operand orders whose tiles follow one another, so that the last round of one is filled by the next.
 constexpr int kBatch = 3;
+constexpr int kPairOf = 2;       // JOBS of a launch of two products of different K and operand orders
 struct Args {
     CUtensorMap a[kBatch], b[kBatch], out[kBatch], z;     // by product; by segment, or gate and up, in a single one
     int segments;
@@ -81,6 +82,12 @@ struct Args {
     uint32_t idesc;
     int direct_z;         // rows of Z are not on 16-byte boundaries
     int reset;            // this launch clears the status word
+    // kPairOf: product 0's tiles (of all parts) and the extra tiles of product 1 that the workers without a last one of
+    // product 0 take first; parts of k; rows of a part's sums
+    int n0, extra, parts;
+    int KB0, KB1;
+    int rows_z;
+    uint32_t idesc0;
     int* status;
     Epilogue epi;
 };
@@ -127,8 +134,8 @@ __device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
 constexpr int kGroupM = 8;
 template <int JOBS>
 __device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, int& tn) {
-    job = 0;
-    if constexpr (JOBS > 1) {
+    if constexpr (JOBS != kPairOf) job = 0;
+    if constexpr (JOBS > kPairOf) {
         job = (u >= p.last[0]) + (u >= p.last[1]);
         if (job) u -= p.last[job - 1];
     }
@@ -138,6 +145,23 @@ __device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, 
     const unsigned gm = p.tiles_m[job] - m0 < kGroupM ? p.tiles_m[job] - m0 : kGroupM;
     tn = static_cast<int>(rest / gm);
     tm = m0 + static_cast<int>(rest % gm);
+}
+
+// Two products of different K and operand orders in one launch: the long tiles first, in rounds, and the short
+// ones dealt so that the workers end together.  Worker w of `workers` takes its i-th tile; false: it has no more.
+struct PairUnit { int job, part, u; };
+__device__ __forceinline__ bool pair_unit(const Args& p, int w, int workers, int i, PairUnit& r) {
+    const int last = p.n0 % workers, mine = p.n0 / workers + (w < last);
+    if (i < mine) {
+        const int u = w + i * workers, tiles = p.tiles_m[0] * p.tiles_n[0];
+        r.job = 0, r.part = u / tiles, r.u = u % tiles;
+        return true;
+    }
+    const int k = i - mine, others = workers - last;           // those without a tile in the last round
+    r.job = 1, r.part = 0;
+    if (last && w >= last) r.u = k < p.extra ? k * others + (w - last) : p.extra * others + (k - p.extra) * workers + w;
+    else r.u = (last ? p.extra * others : 0) + k * workers + w;
+    return r.u < p.units - p.n0;
 }
 
 __device__ __forceinline__ void st_shared_cluster_f32x4(uint32_t cluster_addr, float a, float b, float c, float d) {
@@ -178,8 +202,31 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     const int first = p.unit0 + static_cast<int>(blockIdx.x) / ctas, workers = static_cast<int>(gridDim.x) / ctas;
     const int part = kSplit ? static_cast<int>(cluster_rank >> 1) : 0;
     const int all_blocks = p.segments * p.KB;
-    const int kb0 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
-    const int kb1 = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * (part + 1) / p.split) : all_blocks;
+    // the i-th tile of this worker
+    auto next = [&](int i, int& job, int& tm, int& tn, int& part_z) {
+        part_z = 0;
+        if constexpr (JOBS == kPairOf) {
+            PairUnit r;
+            if (!pair_unit(p, first, workers, i, r)) return false;
+            job = r.job, part_z = r.part;
+            decode<JOBS>(p, r.u, job, tm, tn);
+            return true;
+        } else {
+            const int u = first + i * workers;
+            if (u >= p.units) return false;
+            decode<JOBS>(p, u, job, tm, tn);
+            return true;
+        }
+    };
+    // its k blocks
+    auto blocks_of = [&](int job, int part_z, int& b0, int& b1) {
+        if constexpr (JOBS == kPairOf) {
+            b0 = job ? 0 : static_cast<int>(static_cast<int64_t>(p.KB0) * part_z / p.parts);
+            b1 = job ? p.KB1 : static_cast<int>(static_cast<int64_t>(p.KB0) * (part_z + 1) / p.parts);
+        }
+    };
+    const int kb0_all = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
+    const int kb1_all = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * (part + 1) / p.split) : all_blocks;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -228,9 +275,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         int stage = 0;
         uint32_t phase = 0;
         bool ok = true;
-        for (int u = first; ok && u < p.units; u += workers) {
-            int job, tm, tn;
-            decode<JOBS>(p, u, job, tm, tn);
+        int job, tm, tn, part_z;
+        for (int i = 0; ok && next(i, job, tm, tn, part_z); ++i) {
+            int kb0 = kb0_all, kb1 = kb1_all;
+            blocks_of(job, part_z, kb0, kb1);
+            const bool a_mn = JOBS == kPairOf ? job == 1 : p.a_mn != 0;
             const int m0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM;
             const int n0 = tn * kCols;
             for (int kb = kb0; kb < kb1; kb += kBoxes) {
@@ -243,13 +292,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     for (int x = 0; x < kBoxes; ++x) {
                         if (x >= boxes) break;
                         const uint32_t sa = tiles0 + stage * kStageBytes + x * F::kBoxBytes, sb = sa + kTileA;
-                        const int seg = kb + x >= p.KB, at = seg + job;
+                        const int seg = JOBS != kPairOf && kb + x >= p.KB, at = seg + job;
                         const int k0 = (kb + x - seg * p.KB) * BK;
                         auto load = [&](uint32_t dst, const CUtensorMap* map, int cx, int cy) {
                             if constexpr (kPair) tma_load_2d_pair(dst, map, fb, cx, cy);
                             else tma_load_2d(dst, map, fb, cx, cy);
                         };
-                        if (p.a_mn) {
+                        if (a_mn) {
                             load(sa, &p.a[at], m0, k0);
                             load(sa + kTileA / 2, &p.a[at], m0 + 64, k0);
                         } else {
@@ -283,14 +332,19 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         uint32_t phase = 0, unit_count = 0;
         bool ok = true;
         // one step of 16 k: 32 bytes along a row of k, 16 rows of 128 bytes where the rows are contiguous
-        const uint32_t step_a = p.a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
         const uint32_t step_b = p.b_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
-        const uint32_t low_a = desc_low(smem_u32(tiles), p.a_mn), low_b = desc_low(smem_u32(tiles) + kTileA, p.b_mn);
-        const uint32_t idesc = p.idesc;
+        const uint32_t low_b = desc_low(smem_u32(tiles) + kTileA, p.b_mn);
         auto wait = [&](uint32_t bar, uint32_t parity) {
             return kPair ? warp_wait_cluster(bar, parity, abort_flag) : warp_wait(bar, parity, abort_flag);
         };
-        for (int u = first; ok && u < p.units; u += workers, ++unit_count) {
+        int job, tm, tn, part_z;
+        for (; ok && next(static_cast<int>(unit_count), job, tm, tn, part_z); ++unit_count) {
+            int kb0 = kb0_all, kb1 = kb1_all;
+            blocks_of(job, part_z, kb0, kb1);
+            const bool a_mn = JOBS == kPairOf ? job == 1 : p.a_mn != 0;
+            const uint32_t step_a = a_mn ? (UK * 128) >> 4 : (UK * 2) >> 4;
+            const uint32_t low_a = desc_low(smem_u32(tiles), a_mn);
+            const uint32_t idesc = JOBS == kPairOf && job == 0 ? p.idesc0 : p.idesc;
             const uint32_t buf = unit_count & 1u;
             const uint32_t use = (unit_count >> 1) & 1u;
             if (!wait(smem_u32(&acc_empty[buf]), use ^ 1u)) { ok = false; break; }
@@ -369,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
         uint8_t* stg = staging + (warp - kEpiWarp0) * kStageOut;
         // of the tile's product
         int64_t M = p.M[0], ldo = p.ldo[0];
-        int N = p.N[0], job = 0;
+        int N = p.N[0], job = 0, part_z = 0, tm, tn;
         const bool wide = (p.ldo[0] & 7) == 0;
         // 64 bytes of every lane's row into the staging buffer, once the store issued from it has read it
         auto stage_box = [&](const uint32_t* w) {
@@ -416,9 +470,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             else store_box(std::false_type(), &p.out[i], w, n, row0);
         };
         uint32_t unit_count = static_cast<uint32_t>(set);
-        for (int u = first + set * workers; u < p.units; u += 2 * workers, unit_count += 2) {
-            int tm, tn;
-            decode<JOBS>(p, u, job, tm, tn);
+        for (; next(static_cast<int>(unit_count), job, tm, tn, part_z); unit_count += 2) {
             if constexpr (JOBS > 1) M = p.M[job], N = p.N[job], ldo = p.ldo[job];
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
@@ -454,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             int target = -1;
             float lse2 = INFINITY, grad = 0.0f;
             if constexpr (KIND == kEpiParts || KIND == kEpiProb) {
-                if (m < M) {
+                if (m < e.vocab.T) {
                     const int64_t y = e.vocab.targets[m];
                     if (e.vocab.live(y)) {
                         target = static_cast<int>(y) - e.vocab.v0;
@@ -512,29 +564,31 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             v[2 * i + 1] += hi;
                         }
                     }
-                    if (e.Z) {
+                    if (JOBS == kPairOf ? job == 0 : e.Z != nullptr) {
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             if (n + 16 * q < N) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
+                                const int y = JOBS == kPairOf ? part_z * p.rows_z + row0 : row0;
                                 if (p.direct_z) {
-                                    store_elements(e.Z, static_cast<int64_t>(N), w, n + 16 * q, row0, e.add != 0);
+                                    store_elements(e.Z + static_cast<int64_t>(y - row0) * N, static_cast<int64_t>(N), w, n + 16 * q,
+                                                   row0, e.add != 0);
                                 } else if (e.add) {
                                     stage_box(w);
                                     fence_async_smem();
                                     __syncwarp();
                                     if (lane == 0) {
-                                        tma_add_2d(&p.z, smem_u32(stg), n + 16 * q, row0);
+                                        tma_add_2d(&p.z, smem_u32(stg), n + 16 * q, y);
                                         bulk_commit();
                                     }
                                 } else {
-                                    store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
+                                    store_box(std::bool_constant<JOBS != kPairOf>(), &p.z, w, n + 16 * q, y);
                                 }
                             }
                         }
                     }
-                    if (!e.out) continue;
+                    if (JOBS == kPairOf ? job == 0 : !e.out) continue;
                     act_values<true>(e.act, v);
                     if (e.residual && wide) {
                         // from the rows' quarters to the lane's row, through the staging buffer
@@ -746,6 +800,8 @@ static bool map_operand(CUtensorMap* m, const Mat& a, int64_t rows, int64_t K, i
     return map_2d(m, a.p, rows, K, a.ks, 64, BK, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+static Mat by(const void* p, int64_t ld, bool rows) { return rows ? Mat{p, ld, 1} : Mat{p, 1, ld}; }
+
 // Tiles unit0 .. unit0 + count - 1 of the product (count < 0: all the others), on at most `most` workers; `split`: pairs per
 // tile; `early`: see Args.
 template <bool kPair, int BN, bool kSplit>
@@ -756,7 +812,7 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     const int rows = kPair ? 2 * BM : BM, cols = gated ? BN / 2 : BN;
     Args a;
     for (int s = 0; s < 2; ++s) {            // only the maps that the kernel reads: an encoding is host time
-        if (s < p.segments && !map_operand(&a.a[s], p.A[s], p.M, p.K, BM)) return DTP_ERR_CUDA;
+        if (s < p.segments && !map_operand(&a.a[s], p.A[s], p.rows_a > p.M ? p.rows_a : p.M, p.K, BM)) return DTP_ERR_CUDA;
         if ((s < p.segments || gated) && !map_operand(&a.b[s], p.B[s], p.N, p.K, BN / 2)) return DTP_ERR_CUDA;
     }
     int64_t all = 0;
@@ -828,6 +884,97 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     cfg.numAttrs = 2;
     DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
     return DTP_OK;
+}
+
+// A form's launch on `workers` pairs.
+template <int BN>
+static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaStream_t stream) {
+    using F = Form<true, BN>;
+    Args a;
+    a.segments = 1, a.KB = 0, a.a_mn = 0, a.b_mn = 1, a.unit0 = 0, a.split = 1, a.early = 0, a.reset = 0;
+    a.KB0 = (g.cols + BK - 1) / BK, a.KB1 = static_cast<int>((g.rows + BK - 1) / BK);
+    a.parts = g.parts;
+    a.status = status;
+    const int64_t M[2] = {g.rows, g.cols};
+    int64_t units[2] = {0, 0};
+    for (int j = 0; j < 2; ++j) {
+        a.M[j] = M[j], a.N[j] = g.d, a.ldo[j] = g.d, a.dst[j] = j ? g.dw : nullptr, a.direct[j] = 1, a.last[j] = 0;
+        a.tiles_m[j] = static_cast<int>((M[j] + 2 * BM - 1) / (2 * BM));
+        a.tiles_n[j] = (g.d + BN - 1) / BN;
+        units[j] = static_cast<int64_t>(a.tiles_m[j]) * a.tiles_n[j];
+    }
+    units[0] = g.sum ? units[0] * g.parts : 0;
+    if (!g.dw) units[1] = 0;
+    if (units[0] + units[1] > 0x3FFFFFFF) return DTP_ERR_UNSUPPORTED;
+    if (units[0] + units[1] == 0) return DTP_OK;
+    a.n0 = static_cast<int>(units[0]), a.units = static_cast<int>(units[0] + units[1]);
+    a.rows_z = a.tiles_m[0] * 2 * BM;
+    const int64_t long_blocks = a.KB0 / a.parts;
+    a.extra = static_cast<int>((long_blocks + a.KB1 / 2) / a.KB1);
+    if (!map_operand(&a.a[0], by(g.dz, g.ldz, true), g.rows, g.cols, BM) ||
+        !map_operand(&a.b[0], by(g.w, g.ldw, false), g.d, g.cols, BN / 2) ||
+        !map_operand(&a.a[1], by(g.dz, g.ldz, false), g.cols, g.rows, BM) ||
+        !map_operand(&a.b[1], by(g.x, g.ldx, false), g.d, g.rows, BN / 2))
+        return DTP_ERR_CUDA;
+    a.direct_z = (g.d & 3) != 0;
+    if (g.sum && !a.direct_z &&
+        !map_2d(&a.z, g.sum, g.d, static_cast<int64_t>(a.rows_z) * a.parts, g.d, 16, 32, CU_TENSOR_MAP_SWIZZLE_64B, true))
+        return DTP_ERR_CUDA;
+    if (g.dw && g.d % 8 == 0) {
+        a.direct[1] = 0;
+        if (!map_2d(&a.out[1], g.dw, g.d, g.cols, g.d, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B)) return DTP_ERR_CUDA;
+    }
+    // bits 15 and 16: A and B stored with their rows contiguous
+    a.idesc0 = idesc_bf16_f32(2 * BM, BN) | 1u << 16;
+    a.idesc = a.idesc0 | 1u << 15;
+    a.epi = Epilogue();
+    a.epi.Z = g.sum, a.epi.add = g.add;
+    auto kernel = gemm_tc_kernel<true, BN, kEpiLinear, false, kPairOf>;
+    DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(F::kSmemBytes)));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * (a.units < pairs ? a.units : pairs)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = F::kSmemBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    DTP_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, a));
+    return DTP_OK;
+}
+
+// Up to 128 columns of d the narrower tiles: half of a wider one would be padding.
+int launch_pair(const GradPair& g, int* status, cudaStream_t stream) {
+    int dev = 0, sms = 0;
+    DTP_CUDA_TRY(cudaGetDevice(&dev));
+    DTP_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    return g.d <= 128 ? launch_pair_form<128>(g, status, sms / 2, stream) : launch_pair_form<256>(g, status, sms / 2, stream);
+}
+
+// As dealt by pair_unit on 76 pairs; a tile takes its k blocks, and no less than its epilogue (about 6 of them).
+int64_t pair_clocks(int64_t rows, int cols, int d, int* parts) {
+    constexpr int64_t W = 76;
+    const int64_t bn = d <= 128 ? 128 : 256, cols_d = (d + bn - 1) / bn;
+    auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
+    auto cost = [](int64_t blocks) { return blocks > 5 ? blocks + 1 : 6; };
+    const int64_t tiles0 = up(rows, 256) * cols_d, n1 = up(cols, 256) * cols_d, kb0 = up(cols, 64), kb1 = up(rows, 64);
+    const int64_t c1 = cost(kb1);
+    int64_t best = 0;
+    for (int h = 1; h <= 8 && (h == 1 || kb0 / h >= 8); ++h) {
+        const int64_t n0 = tiles0 * h, c0 = cost(up(kb0, h)), last = n0 % W, others = W - last;
+        const int64_t extra = last ? (kb0 / h + kb1 / 2) / kb1 : 0;
+        const int64_t lead = n0 / W * c0 + (last ? (c0 > extra * c1 ? c0 : extra * c1) : 0);
+        const int64_t left = n1 - extra * others;
+        const int64_t t = lead + (left > 0 ? up(left, W) * c1 : 0);
+        if (h == 1 || t < best - best / 100) best = t, *parts = h;
+    }
+    return best;
 }
 
 // Clusters of `split` pairs that the current device holds at once (they stay within a part of the chip).

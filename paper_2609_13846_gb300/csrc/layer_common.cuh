@@ -202,6 +202,7 @@ __device__ __forceinline__ float exp2_fast(float x) {
 struct Vocab {
     const int64_t* targets = nullptr;      // [M]
     int64_t ignore = 0;
+    int64_t T = 0;                         // rows beyond it are padding
     int V = 0, v0 = 0;                     // the vocabulary, and the piece's first token
     Part* parts = nullptr;                 // [chunk][M]
     float* hit = nullptr;                  // [M] the target's logit
@@ -281,7 +282,23 @@ struct Product {
     int64_t M = 0;
     int N = 0;
     int64_t K = 0;
+    int64_t rows_a = 0;      // rows that A has, where more than M (bf16 only)
     Epilogue epi;
+};
+
+// The two products that a piece of the softmax's gradient takes part in, for one launch (bf16): dZ [rows, cols] at pitch ldz
+//     sum[part] (+)= dZ[:, part's columns] W[part's rows, :]  for `parts` ranges of the columns, [tiles of 256 rows, d] each
+//     dW = dZ^T X
+// rows is a multiple of 64 (the last ones zeros in X and in dZ).
+struct GradPair {
+    const void *dz, *x, *w;
+    int64_t ldz, ldx, ldw;
+    int64_t rows;
+    int cols, d;
+    int parts;
+    int add;                 // to the sums, which hold those of earlier pieces
+    float* sum;              // or NULL
+    void* dw;                // [cols, d], or NULL
 };
 
 }  // namespace layer

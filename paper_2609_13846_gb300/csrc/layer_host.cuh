@@ -16,6 +16,9 @@ int launch(const layer::Product& p, int dtype, int* status, cudaStream_t stream)
 namespace gtc {
 int64_t most_chunks(int N);
 int launch(const layer::Product& p, int* status, int reset, cudaStream_t stream, int64_t* chunks = nullptr);
+// The time that launch_pair takes, in k blocks of a 256 x 256 tile, and the best number of parts for it.
+int64_t pair_clocks(int64_t rows, int cols, int d, int* parts);
+int launch_pair(const layer::GradPair& g, int* status, cudaStream_t stream);
 }  // namespace gtc
 namespace few {
 bool takes(const layer::Product& p);

@@ -4,8 +4,8 @@
 //     dz_t = dloss_t (exp(z_t - lse_t) - onehot(y_t)),  dX = dZ W,  dW = dZ^T X
 //
 // in pieces of the vocabulary, so that no more than a piece of the logits exists at a time.  Forward, each row's maximum and
-// sum of exponentials of every chunk of columns meet in a last launch; bf16 products of more than 32 tokens take them from the
-// accumulators (kEpiParts), and their logits are never stored.  Backward, a piece of the logits is made again and turned into
+// sum of exponentials of every chunk of columns meet in a last launch; bf16 products take them from the accumulators
+// (kEpiParts), and their logits are never stored.  Backward, a piece of the logits is made again and turned into
 // dZ, in the product's epilogue (kEpiProb) or by a kernel of its own, and multiplied both ways; dX is added up over the
 // pieces in fp32.
 #include <cuda_bf16.h>
@@ -62,22 +62,34 @@ parts_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets
     }
 }
 
-// The parts of each token joined in their order: a warp takes every eighth part of 32 tokens.  A target that is no token's sets the status.
-__global__ void __launch_bounds__(256)
+// The parts of each token joined: each of 32 warps takes every 32nd part of 32 tokens, eight in flight, and the first one joins the
+// warps' in order (a vocabulary of 131072 has 1024 parts; 8 warps and one part at a time: 65 us).  A target that is no token's sets
+// the status.
+constexpr int kLossWarps = 32;
+__global__ void __launch_bounds__(32 * kLossWarps)
 loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* targets, int64_t T, int V, int64_t ignore,
             float* loss, float* lse, int* status) {
-    __shared__ Part red[8][32];
+    __shared__ Part red[kLossWarps][32];
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t t = blockIdx.x * 32ll + lane;
     Part p{-INFINITY, 0.0f};
-    if (t < T)
-        for (int64_t c = warp; c < count; c += 8) p = join(p, parts[c * T + t]);
+    if (t < T) {
+        int64_t c = warp;
+        for (; c + 7 * kLossWarps < count; c += 8 * kLossWarps) {
+            Part q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = parts[(c + j * kLossWarps) * T + t];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p = join(p, q[j]);
+        }
+        for (; c < count; c += kLossWarps) p = join(p, parts[c * T + t]);
+    }
     red[warp][lane] = p;
     __syncthreads();
     if (warp != 0 || t >= T) return;
-    for (int w = 1; w < 8; ++w) p = join(p, red[w][lane]);
+    for (int w = 1; w < kLossWarps; ++w) p = join(p, red[w][lane]);
     const float l = kLn2 * (p.top + log2f(p.sum));
     lse[t] = l;
     const int64_t y = targets[t];
@@ -86,17 +98,29 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
     if (bad) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
 }
 
-// X at an aligned pitch, with zeros in the rows of tokens without a target: whatever stands there must not reach dW.
+// X at an aligned pitch in `rows` rows, with zeros in those beyond T and, where targets are given, in those of tokens that do not count:
+// whatever stands there must not reach dW.
 template <typename E>
 __global__ void __launch_bounds__(256)
-live_rows_kernel(const E* X, int64_t T, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V, E* out, int* status) {
+live_rows_kernel(const E* X, int64_t T, int64_t rows, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V, E* out,
+                 int* status) {
     grid_wait();
     grid_release();
-    if (blockIdx.x == 0 && threadIdx.x == 0) *status = DTP_OK;
-    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-        const int64_t y = targets[t];
-        const bool live = y != ignore && y >= 0 && y < V;
-        for (int i = threadIdx.x; i < d; i += 256) out[t * pitch + i] = live ? X[t * d + i] : from_f32<E>(0.0f);
+    if (targets && blockIdx.x == 0 && threadIdx.x == 0) *status = DTP_OK;
+    constexpr int kPer = 16 / sizeof(E);
+    const bool wide = d % kPer == 0 && pitch % kPer == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0;
+    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
+        bool live = t < T;
+        if (live && targets) {
+            const int64_t y = targets[t];
+            live = y != ignore && y >= 0 && y < V;
+        }
+        if (wide) {
+            for (int i = threadIdx.x; i < d / kPer; i += 256)
+                reinterpret_cast<uint4*>(out + t * pitch)[i] = live ? reinterpret_cast<const uint4*>(X + t * d)[i] : make_uint4(0, 0, 0, 0);
+        } else {
+            for (int i = threadIdx.x; i < d; i += 256) out[t * pitch + i] = live ? X[t * d + i] : from_f32<E>(0.0f);
+        }
     }
 }
 
@@ -122,77 +146,113 @@ dz_kernel(const float* Z, int64_t T, int cols, Vocab e, E* dZ, int64_t ld, int* 
     }
 }
 
-// dX from its sums
-__global__ void __launch_bounds__(256) round_kernel(const float* sum, int64_t n, __nv_bfloat16* out) {
+// dX from its sums: `parts` of them, `stride` values apart
+__global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts, int64_t stride, int64_t n, __nv_bfloat16* out) {
     grid_wait();
     grid_release();
     const int64_t words = n / 4;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < words; i += gridDim.x * 256ll) {
-        const float4 v = reinterpret_cast<const float4*>(sum)[i];
+        float4 v = reinterpret_cast<const float4*>(sum)[i];
+        for (int p = 1; p < parts; ++p) {
+            const float4 w = reinterpret_cast<const float4*>(sum + p * stride)[i];
+            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+        }
         const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
         reinterpret_cast<uint2*>(out)[i] = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
     }
     const int64_t rest = 4 * words + threadIdx.x;
-    if (blockIdx.x == 0 && rest < n) out[rest] = __float2bfloat16_rn(sum[rest]);
+    if (blockIdx.x == 0 && rest < n) {
+        float v = sum[rest];
+        for (int p = 1; p < parts; ++p) v += sum[p * stride + rest];
+        out[rest] = __float2bfloat16_rn(v);
+    }
 }
 
 static int64_t grid_of(int64_t blocks) { return blocks < 8192 ? blocks : 8192; }
 
-// Whether a product's epilogue takes the softmax.  Up to 32 tokens the products are the few-token kernels', which stream the
-// weights at the memory's rate; their logits are small beside those.
-static bool fused(int64_t T, int dtype) { return dtype == DTP_BF16 && T > 32; }
+// bf16: a product's epilogue takes the softmax, and two launches a piece make the gradients.  Rows of tokens are padded to 64: a
+// tensor that ends within the first 64 rows of a tile is loaded at half the rate (131072 x 1024 for 63 tokens: 65 us, for 64: 43).
+constexpr int64_t kRowPad = 64;
+static int64_t padded_rows(int64_t T) { return (T + kRowPad - 1) / kRowPad * kRowPad; }
 
-// Tokens of a forward run: its parts, and the logits' pieces where there are any, stay within 256 MB.
+// Tokens of a forward run: its parts, and the logits' pieces where there are any, stay within kPieceBytes.
 static int64_t forward_rows(int64_t T, int V, int dtype) {
     int64_t n = 16384;
-    if (fused(T, dtype)) n = static_cast<int64_t>(kPieceBytes / sizeof(Part)) / gtc::most_chunks(V) / 256 * 256;
+    if (dtype == DTP_BF16) n = static_cast<int64_t>(kPieceBytes / sizeof(Part)) / gtc::most_chunks(V) / 256 * 256;
     if (n < 256) n = 256;
     return n < T ? n : T;
 }
-// Columns of a piece of T tokens' logits.
-static int piece_cols(int64_t T, int V, size_t bytes) {
-    int64_t n = static_cast<int64_t>(bytes) / T / 256 * 256;
+// Columns of a piece of T tokens' logits (fp32), forward or backward.
+static int stored_cols(int64_t T, int V) {
+    int64_t n = static_cast<int64_t>(kPieceBytes / sizeof(float)) / T / 256 * 256;
     if (n < 256) n = 256;
     return static_cast<int>(n < V ? n : V);
 }
-static int forward_piece(int64_t rows, int V, int dtype) {
-    return fused(rows, dtype) ? V : piece_cols(rows, V, kPieceBytes / sizeof(float));
-}
-static int backward_piece(int64_t T, int V, int dtype) { return piece_cols(T, V, kPieceBytes / elem(dtype)); }
 static int64_t parts_of(int64_t rows, int V, int dtype) {
-    if (fused(rows, dtype)) return gtc::most_chunks(V);
-    const int piece = forward_piece(rows, V, dtype);
+    if (dtype == DTP_BF16) return gtc::most_chunks(V);
+    const int piece = stored_cols(rows, V);
     const int64_t whole = V / piece, rest = V % piece;
     return whole * ((piece + kChunk - 1) / kChunk) + (rest + kChunk - 1) / kChunk;
 }
 
+// The pieces of the backward pass: columns of each but the last, and the parts in which dX is summed.  bf16: of the numbers of pieces that
+// keep dZ within kPieceBytes, up to twice the least, the one whose tiles leave the fewest rounds of pairs unfilled; sizes near
+// 8192 x 131072 x 1024 differ by 10% in that.
+struct Pieces { int cols, parts; };
+static Pieces backward_pieces(int64_t T, int d, int V, int dtype) {
+    if (dtype == DTP_F32) return Pieces{stored_cols(T, V), 1};
+    const int64_t rows = padded_rows(T);
+    int64_t most = static_cast<int64_t>(kPieceBytes / 2) / rows / 256 * 256;
+    if (most < 256) most = 256;
+    if (most >= V) most = (V + 255) / 256 * 256;
+    const int64_t least = (V + most - 1) / most;
+    Pieces best{};
+    int64_t best_clocks = 0, seen = 0;
+    for (int64_t n = least; n <= 2 * least + 1 && n < least + 64; ++n) {
+        const int64_t cols = ((V + n - 1) / n + 255) / 256 * 256;
+        if (cols == seen) continue;
+        seen = cols;
+        auto clocks = [&](int64_t c, int* parts) {
+            const int64_t tiles = (rows + 255) / 256 * ((c + 255) / 256), blocks = (d + 63) / 64;
+            return (tiles + 75) / 76 * (blocks > 5 ? blocks + 1 : 6) + gtc::pair_clocks(rows, static_cast<int>(c), d, parts) + 30;
+        };
+        int parts = 1, other = 1;
+        const int64_t whole = V / cols, rest = V % cols;
+        const int64_t total = (whole ? whole * clocks(cols, &parts) : 0) + (rest ? clocks(rest, whole ? &other : &parts) : 0);
+        if (best.cols == 0 || total < best_clocks - best_clocks / 100)
+            best = Pieces{static_cast<int>(cols < V ? cols : V), parts}, best_clocks = total;
+    }
+    return best;
+}
+
 // What a call takes from its workspace.
 struct ForwardSpace {
-    float* Z;            // a piece of the logits, where they are stored
+    float* Z;            // a piece of the logits (fp32)
     Part* parts;
     float* hit;
 };
 static ForwardSpace carve_forward(Carver& c, int64_t rows, int V, int dtype) {
     ForwardSpace s{};
-    if (!fused(rows, dtype)) s.Z = static_cast<float*>(c.take(static_cast<size_t>(rows) * forward_piece(rows, V, dtype) * sizeof(float)));
+    if (dtype == DTP_F32) s.Z = static_cast<float*>(c.take(static_cast<size_t>(rows) * stored_cols(rows, V) * sizeof(float)));
     s.parts = static_cast<Part*>(c.take(static_cast<size_t>(rows) * parts_of(rows, V, dtype) * sizeof(Part)));
     s.hit = static_cast<float*>(c.take(static_cast<size_t>(rows) * sizeof(float)));
     return s;
 }
+// whether the forward pass copies X: to an aligned pitch, or to whole groups of rows (beyond 4096 tokens the last tile's rate is nothing)
+static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && (d % 8 != 0 || (T % kRowPad != 0 && T < 4096)); }
 struct BackwardSpace {
-    float* Z;            // the same; in fp32 dZ takes its place
-    void* dz;
+    void* dz;            // in fp32 the logits before
     void* x;
     float *sum, *runs;
 };
-static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtype) {
+static int64_t sum_rows(int64_t T) { return (padded_rows(T) + 255) / 256 * 256; }
+static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtype, const Pieces& pieces) {
     BackwardSpace s{};
-    const int piece = backward_piece(T, V, dtype);
-    if (!fused(T, dtype)) s.Z = static_cast<float*>(c.take(static_cast<size_t>(T) * piece * sizeof(float)));
-    s.dz = dtype == DTP_F32 ? s.Z : c.take(static_cast<size_t>(T) * padded(piece) * elem(dtype));
-    s.x = c.take(static_cast<size_t>(T) * padded(d) * elem(dtype));
-    s.sum = static_cast<float*>(c.take(dtype == DTP_BF16 && piece < V ? static_cast<size_t>(T) * d * sizeof(float) : 0));
-    s.runs = static_cast<float*>(c.take(runs_bytes(T, piece, d)));
+    const int64_t rows = dtype == DTP_BF16 ? padded_rows(T) : T;
+    s.dz = c.take(static_cast<size_t>(rows) * (dtype == DTP_BF16 ? padded(pieces.cols) : pieces.cols) * elem(dtype));
+    s.x = c.take(static_cast<size_t>(rows) * padded(d) * elem(dtype));
+    if (dtype == DTP_BF16) s.sum = static_cast<float*>(c.take(static_cast<size_t>(sum_rows(T)) * pieces.parts * d * sizeof(float)));
+    s.runs = static_cast<float*>(c.take(runs_bytes(rows, pieces.cols, d)));
     return s;
 }
 
@@ -201,77 +261,73 @@ size_t loss_workspace_bytes(int64_t T, int d, int V, int dtype, int backward) {
     Carver f(nullptr);
     f.take(repitch_bytes(V, d, dtype));
     Carver b = f;
-    f.take(repitch_bytes(T, d, dtype));
+    if (copies_x(T, d, dtype)) f.take(static_cast<size_t>(padded_rows(T)) * padded(d) * elem(dtype));
     const int64_t rows = forward_rows(T, V, dtype);
     carve_forward(f, rows, V, dtype);
-    // the last run may be one of few tokens
-    if (T % rows) {
-        Carver last = f;
-        last.used = f.used;
-        carve_forward(last, T % rows, V, dtype);
-        f.used = last.used;
-    }
+    if (T % rows) carve_forward(f, T % rows, V, dtype);
     if (!backward) return f.used;
-    carve_backward(b, T, d, V, dtype);
+    carve_backward(b, T, d, V, dtype, backward_pieces(T, d, V, dtype));
     return f.used > b.used ? f.used : b.used;
 }
 
-// The product of T tokens with columns v0 .. of the vocabulary.
-static Product logits(const Rows& x, int64_t t0, const Rows& w, int64_t T, int d, int v0, int cols, int dtype) {
+// The product of T tokens with columns v0 .. of the vocabulary; x has `rows_x` rows.
+static Product logits(const Rows& x, int64_t rows_x, int64_t t0, const Rows& w, int64_t T, int d, int v0, int cols, int dtype) {
     auto from = [&](const Rows& r, int64_t row) {
         return by_row(static_cast<const uint8_t*>(r.p) + static_cast<size_t>(row) * r.ld * elem(dtype), r.ld);
     };
     Product p;
     p.A[0] = from(x, t0);
     p.B[0] = from(w, v0);
-    p.M = T, p.N = cols, p.K = d;
+    p.M = T, p.N = cols, p.K = d, p.rows_a = rows_x - t0;
     p.epi.M = T, p.epi.N = cols, p.epi.ldo = cols;
     return p;
-}
-
-// Stored logits: Z [T, cols] in fp32.
-static int store_logits(Call& call, Product& p, float* Z) {
-    if (call.dtype == DTP_F32) p.epi.out = Z;
-    else p.epi.Z = Z;
-    return call.run(p);
 }
 
 int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V, int64_t ignore, int dtype,
                  float* loss, float* lse, void* workspace, cudaStream_t stream) {
     Call call{dtype, workspace, stream};
     Carver c(workspace);
-    Rows x, w;
+    Rows x{X, d}, w;
+    int64_t rows_x = T;
     int st = aligned_rows(W, V, d, dtype, c, stream, &w);
-    if (st == DTP_OK) st = aligned_rows(X, T, d, dtype, c, stream, &x);
     int* status = static_cast<int*>(workspace);
+    if (st == DTP_OK && copies_x(T, d, dtype)) {
+        rows_x = padded_rows(T);
+        void* to = c.take(static_cast<size_t>(rows_x) * padded(d) * elem(dtype));
+        x = Rows{to, padded(d)};
+        st = launch_after(live_rows_kernel<__nv_bfloat16>, grid_of(rows_x), stream, static_cast<const __nv_bfloat16*>(X), T, rows_x, d,
+                          x.ld, static_cast<const int64_t*>(nullptr), int64_t(0), 0, static_cast<__nv_bfloat16*>(to), status);
+    }
     const int64_t most = forward_rows(T, V, dtype);
     ForwardSpace s = carve_forward(c, most, V, dtype);
     for (int64_t t0 = 0; st == DTP_OK && t0 < T; t0 += most) {
         const int64_t rows = T - t0 < most ? T - t0 : most;
         if (rows < most) s = carve_forward(c, rows, V, dtype);
         Vocab e;
-        e.targets = targets + t0, e.ignore = ignore, e.V = V, e.parts = s.parts, e.hit = s.hit;
+        e.targets = targets + t0, e.ignore = ignore, e.T = rows, e.V = V, e.parts = s.parts, e.hit = s.hit;
         int64_t count = 0;
-        if (fused(rows, dtype)) {
-            Product p = logits(x, t0, w, rows, d, 0, V, dtype);
+        if (dtype == DTP_BF16) {
+            Product p = logits(x, rows_x, t0, w, rows, d, 0, V, dtype);
             p.epi.kind = kEpiParts, p.epi.vocab = e;
             st = gtc::launch(p, status, call.fresh, stream, &count);
             call.fresh = false;
-        }
-        const int piece = forward_piece(rows, V, dtype);
-        for (int v0 = 0; st == DTP_OK && s.Z && v0 < V; v0 += piece) {
-            const int cols = V - v0 < piece ? V - v0 : piece;
-            Product p = logits(x, t0, w, rows, d, v0, cols, dtype);
-            st = store_logits(call, p, s.Z);
-            const int64_t chunks = (cols + kChunk - 1) / kChunk;
-            if (st == DTP_OK)
-                st = launch_after(parts_kernel, grid_of(rows * chunks), stream, static_cast<const float*>(s.Z), rows, cols, v0,
-                                  e.targets, s.parts + count * rows, s.hit);
-            count += chunks;
+        } else {
+            const int piece = stored_cols(rows, V);
+            for (int v0 = 0; st == DTP_OK && v0 < V; v0 += piece) {
+                const int cols = V - v0 < piece ? V - v0 : piece;
+                Product p = logits(x, rows_x, t0, w, rows, d, v0, cols, dtype);
+                p.epi.out = s.Z;
+                st = call.run(p);
+                const int64_t chunks = (cols + kChunk - 1) / kChunk;
+                if (st == DTP_OK)
+                    st = launch_after(parts_kernel, grid_of(rows * chunks), stream, static_cast<const float*>(s.Z), rows, cols, v0,
+                                      e.targets, s.parts + count * rows, s.hit);
+                count += chunks;
+            }
         }
         if (st == DTP_OK)
-            st = launch_after(loss_kernel, (rows + 31) / 32, stream, static_cast<const Part*>(s.parts), count,
-                              static_cast<const float*>(s.hit), e.targets, rows, V, ignore, loss + t0, lse + t0, status);
+            st = launch_blocks(loss_kernel, (rows + 31) / 32, 32 * kLossWarps, stream, static_cast<const Part*>(s.parts), count,
+                               static_cast<const float*>(s.hit), e.targets, rows, V, ignore, loss + t0, lse + t0, status);
     }
     return st;
 }
@@ -279,52 +335,59 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
 template <typename E>
 static int backward(const float* dloss, const void* X, const void* W, const int64_t* targets, const float* lse, int64_t T, int d,
                     int V, int64_t ignore, int dtype, void* dX, void* dW, void* workspace, cudaStream_t stream) {
+    constexpr bool kBf16 = sizeof(E) == 2;
     Call call{dtype, workspace, stream};
     Carver c(workspace);
     Rows w;
     int st = aligned_rows(W, V, d, dtype, c, stream, &w);
-    const BackwardSpace s = carve_backward(c, T, d, V, dtype);
-    const int piece = backward_piece(T, V, dtype);
+    const Pieces pieces = backward_pieces(T, d, V, dtype);
+    const BackwardSpace s = carve_backward(c, T, d, V, dtype, pieces);
     int* status = static_cast<int*>(workspace);
+    const int64_t rows = kBf16 ? padded_rows(T) : T;
     const Rows x{s.x, padded(d)};
     Vocab e;
-    e.targets = targets, e.ignore = ignore, e.V = V, e.lse = lse, e.dloss = dloss;
+    e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss;
     if (st == DTP_OK)
-        st = launch_after(live_rows_kernel<E>, grid_of(T), stream, static_cast<const E*>(X), T, d, x.ld, targets, ignore, V,
+        st = launch_after(live_rows_kernel<E>, grid_of(rows), stream, static_cast<const E*>(X), T, rows, d, x.ld, targets, ignore, V,
                           static_cast<E*>(s.x), status);
     call.fresh = false;
-    for (int v0 = 0; st == DTP_OK && v0 < V; v0 += piece) {
-        const int cols = V - v0 < piece ? V - v0 : piece;
-        const int64_t ldz = dtype == DTP_F32 ? cols : padded(cols);
+    for (int v0 = 0; st == DTP_OK && v0 < V; v0 += pieces.cols) {
+        const int cols = V - v0 < pieces.cols ? V - v0 : pieces.cols;
+        const int64_t ldz = kBf16 ? padded(cols) : cols;
+        const void* w_at = static_cast<const E*>(w.p) + static_cast<int64_t>(v0) * w.ld;
+        E* dw_at = dW ? static_cast<E*>(dW) + static_cast<int64_t>(v0) * d : nullptr;
         e.v0 = v0;
-        Product p = logits(x, 0, w, T, d, v0, cols, dtype);
-        if (fused(T, dtype)) {
-            p.epi.kind = kEpiProb, p.epi.vocab = e, p.epi.out = s.dz, p.epi.ldo = ldz;
+        Product p = logits(x, rows, 0, w, rows, d, v0, cols, dtype);
+        p.epi.out = s.dz, p.epi.ldo = ldz;
+        if constexpr (kBf16) {
+            p.epi.kind = kEpiProb, p.epi.vocab = e;
             st = gtc::launch(p, status, 0, stream);
+            const bool runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs
+            GradPair g{s.dz, s.x, w_at, ldz, x.ld, w.ld, rows, cols, d, pieces.parts, v0 > 0, dX ? s.sum : nullptr, runs ? nullptr : dw_at};
+            if (g.parts > (cols + 63) / 64) g.parts = (cols + 63) / 64;       // a short last piece leaves the others' sums as they are
+            if (st == DTP_OK) st = gtc::launch_pair(g, status, stream);
+            if (st == DTP_OK && runs)
+                st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, rows, s.runs);
         } else {
-            st = store_logits(call, p, s.Z);
+            st = call.run(p);
             if (st == DTP_OK)
-                st = launch_after(dz_kernel<E>, grid_of(T * ((cols + kChunk - 1) / kChunk)), stream, static_cast<const float*>(s.Z),
+                st = launch_after(dz_kernel<E>, grid_of(T * ((cols + kChunk - 1) / kChunk)), stream, static_cast<const float*>(s.dz),
                                   T, cols, e, static_cast<E*>(s.dz), ldz, status);
+            if (st == DTP_OK && dX) {
+                Product q;
+                q.A[0] = by_row(s.dz, ldz);
+                q.B[0] = by_col(w_at, w.ld);
+                q.M = T, q.N = d, q.K = cols;
+                q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
+                q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
+                st = call.run(q);
+            }
+            if (st == DTP_OK && dW) st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, T, s.runs);
         }
-        if (st == DTP_OK && dX) {
-            Product q;
-            q.A[0] = by_row(s.dz, ldz);
-            q.B[0] = by_col(static_cast<const uint8_t*>(w.p) + static_cast<size_t>(v0) * w.ld * sizeof(E), w.ld);
-            q.M = T, q.N = d, q.K = cols;
-            q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
-            if (dtype == DTP_F32) q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
-            else if (piece >= V) q.epi.out = dX;
-            else q.epi.Z = s.sum, q.epi.add = v0 > 0;
-            st = call.run(q);
-        }
-        if (st == DTP_OK && dW)
-            st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, static_cast<E*>(dW) + static_cast<int64_t>(v0) * d, d},
-                                 T, s.runs);
     }
-    if (st == DTP_OK && dX && dtype == DTP_BF16 && piece < V)
-        st = launch_after(round_kernel, grid_of((T * d / 4 + 255) / 256 + 1), stream, static_cast<const float*>(s.sum), T * d,
-                          static_cast<__nv_bfloat16*>(dX));
+    if (kBf16 && st == DTP_OK && dX)
+        st = launch_after(round_kernel, grid_of((T * d / 4 + 255) / 256 + 1), stream, static_cast<const float*>(s.sum), pieces.parts,
+                          sum_rows(T) * d, T * d, static_cast<__nv_bfloat16*>(dX));
     return st;
 }
 
