@@ -75,35 +75,52 @@ __device__ __forceinline__ void row_sums(float (&v)[kRows], float (&red)[2][kRow
     }
 }
 
-// Eight columns as they lie in memory.
-template <typename E>
+// How a thread's columns lie: octets of consecutive ones in words; the same element by element, where rows start on other
+// boundaries; or, in rows whose length is no multiple of eight and which have no aligned form to agree with, every TPR-th column, so that a
+// warp's elements are consecutive (4095 columns: 2.5 times the octets' rate).
+enum Map { kWords, kOctets, kStrided };
+
+// Column of element j of octet k.
+template <int TPR, Map kMap>
+__device__ __forceinline__ int column(int k, int j) {
+    const int me = threadIdx.x % TPR;
+    return kMap == kStrided ? (8 * k + j) * TPR + me : (TPR * k + me) * 8 + j;
+}
+
+// Eight columns of a row of d.
+template <typename E, int TPR, Map kMap>
 struct Octet {
     uint4 q[sizeof(E) == 2 ? 1 : 2];
-    template <bool kWide>
-    __device__ __forceinline__ void load(const E* p, int left) {
-        if constexpr (kWide) {
+    __device__ __forceinline__ void load(const E* row, int k, int d, bool in) {
+        if constexpr (kMap == kWords) {
+            const int c = column<TPR, kMap>(k, 0);
 #pragma unroll
             for (int i = 0; i < static_cast<int>(sizeof(q) / 16); ++i)
-                q[i] = left > 0 ? reinterpret_cast<const uint4*>(p)[i] : make_uint4(0, 0, 0, 0);
+                q[i] = in && c < d ? reinterpret_cast<const uint4*>(row + c)[i] : make_uint4(0, 0, 0, 0);
         } else {
             E e[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = j < left ? p[j] : from_f32<E>(0.0f);
+            for (int j = 0; j < 8; ++j) {
+                const int c = column<TPR, kMap>(k, j);
+                e[j] = in && c < d ? row[c] : from_f32<E>(0.0f);
+            }
             memcpy(q, e, sizeof(q));
         }
     }
-    template <bool kWide>
-    __device__ __forceinline__ void store(E* p, int left) const {
-        if constexpr (kWide) {
+    __device__ __forceinline__ void store(E* row, int k, int d) const {
+        if constexpr (kMap == kWords) {
+            const int c = column<TPR, kMap>(k, 0);
 #pragma unroll
             for (int i = 0; i < static_cast<int>(sizeof(q) / 16); ++i)
-                if (left > 0) reinterpret_cast<uint4*>(p)[i] = q[i];
+                if (c < d) reinterpret_cast<uint4*>(row + c)[i] = q[i];
         } else {
             E e[8];
             memcpy(e, q, sizeof(q));
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (j < left) p[j] = e[j];
+            for (int j = 0; j < 8; ++j) {
+                const int c = column<TPR, kMap>(k, j);
+                if (c < d) row[c] = e[j];
+            }
         }
     }
     __device__ __forceinline__ void get(float (&v)[8]) const {
@@ -121,8 +138,17 @@ struct Octet {
     }
 };
 
-// A thread's columns: octets of row_threads, OCT of them.  kWide: every row and gamma on 16-byte boundaries.
-template <typename E, int TPR, int OCT, int kRows, bool kWide>
+// Rows t .. t + rows - 1 on their way to L2, by one thread (rows on 16-byte boundaries).
+template <typename E>
+__device__ __forceinline__ void prefetch_rows(const E* p, int64_t t, int rows, int64_t T, int d) {
+    if (t >= T) return;
+    const int64_t n = T - t < rows ? T - t : rows;
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p + t * d), "r"(static_cast<uint32_t>(n * d * sizeof(E))) : "memory");
+}
+constexpr int kAhead = 1;              // turns of a block by which its rows are prefetched (16384 x 4096: 138 us both ways, 148 with 2, 152 without)
+
+// OCT octets to a thread.  kWords: every row and gamma on 16-byte boundaries.
+template <typename E, int TPR, int OCT, int kRows, Map kMap>
 __global__ void __launch_bounds__(block_threads(TPR)) forward_rows_kernel(const E* X, const float* gamma, int64_t T, int d, float eps, E* Y,
                                                                 float* rms) {
     __shared__ __align__(16) float red[2][kRows][TPR / 32];
@@ -136,15 +162,13 @@ __global__ void __launch_bounds__(block_threads(TPR)) forward_rows_kernel(const 
     // groups of a block stay together: their rows are first .. first + kGroups * kRows - 1
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T; first += stride) {
         const int64_t t0 = first + threadIdx.x / TPR * kRows;
-        Octet<E> x[kRows][OCT];
+        if (kMap == kWords && threadIdx.x == 0) prefetch_rows(X, first + kAhead * stride, kGroups * kRows, T, d);
+        Octet<E, TPR, kMap> x[kRows][OCT];
         float s[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r)
 #pragma unroll
-            for (int k = 0; k < OCT; ++k) {
-                const int c = (me + TPR * k) * 8;
-                x[r][k].template load<kWide>(X + (t0 + r) * d + c, t0 + r < T ? d - c : 0);
-            }
+            for (int k = 0; k < OCT; ++k) x[r][k].load(X + (t0 + r) * d, k, d, t0 + r < T);
         auto squares = [&](float scale) {
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
@@ -181,24 +205,23 @@ __global__ void __launch_bounds__(block_threads(TPR)) forward_rows_kernel(const 
             const bool tiny = !(root[r] <= 8.0e37f);       // its reciprocal would be among fp32's subnormal numbers
 #pragma unroll
             for (int k = 0; k < OCT; ++k) {
-                const int c = (me + TPR * k) * 8;
-                Octet<float> g;
-                g.template load<kWide>(gamma + c, d - c);
+                Octet<float, TPR, kMap> g;
+                g.load(gamma, k, d, true);
                 float v[8], w[8];
                 x[r][k].get(v);
                 g.get(w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = (tiny ? v[j] / root[r] : v[j] * inv) * w[j];
-                Octet<E> y;
+                Octet<E, TPR, kMap> y;
                 y.set(v);
-                y.template store<kWide>(Y + (t0 + r) * d + c, d - c);
+                y.store(Y + (t0 + r) * d, k, d);
             }
         }
     }
 }
 
 // dX, and the block's part of dgamma in partial[block] [d].
-template <typename E, int TPR, int OCT, int kRows, bool kWide>
+template <typename E, int TPR, int OCT, int kRows, Map kMap>
 __global__ void __launch_bounds__(block_threads(TPR), 512 / block_threads(TPR))
 backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* rms, const E* dres, int64_t T, int d, E* dX,
                      float* partial) {
@@ -211,19 +234,23 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
     float g[OCT][8], acc[OCT][8];
 #pragma unroll
     for (int k = 0; k < OCT; ++k) {
-        const int c = (me + TPR * k) * 8;
-        Octet<float> q;
-        q.template load<kWide>(gamma ? gamma + c : gamma, gamma ? d - c : 0);
+        Octet<float, TPR, kMap> q;
+        q.load(gamma, k, d, gamma != nullptr);
         q.get(g[k]);
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[k][j] = 0.0f;
     }
     const float width = static_cast<float>(d);
     int turn = 0;
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T;
-         first += static_cast<int64_t>(gridDim.x) * kGroups * kRows) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups * kRows;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T; first += stride) {
         const int64_t t0 = first + threadIdx.x / TPR * kRows;
-        Octet<E> x[kRows][OCT], y[kRows][OCT], z[kRows][OCT];
+        if (kMap == kWords && threadIdx.x == 0) {
+            prefetch_rows(X, first + kAhead * stride, kGroups * kRows, T, d);
+            prefetch_rows(dY, first + kAhead * stride, kGroups * kRows, T, d);
+            if (dres) prefetch_rows(dres, first + kAhead * stride, kGroups * kRows, T, d);
+        }
+        Octet<E, TPR, kMap> x[kRows][OCT], y[kRows][OCT], z[kRows][OCT];
         float root[kRows], s[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -231,11 +258,10 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
             root[r] = in ? rms[t0 + r] : 1.0f;
 #pragma unroll
             for (int k = 0; k < OCT; ++k) {
-                const int c = (me + TPR * k) * 8;
-                const int64_t at = (t0 + r) * d + c;
-                x[r][k].template load<kWide>(X + at, in ? d - c : 0);
-                y[r][k].template load<kWide>(dY + at, in ? d - c : 0);
-                z[r][k].template load<kWide>(dres + at, in && dres ? d - c : 0);
+                const int64_t at = (t0 + r) * d;
+                x[r][k].load(X + at, k, d, in);
+                y[r][k].load(dY + at, k, d, in);
+                z[r][k].load(dres + at, k, d, in && dres);
             }
         }
 #pragma unroll
@@ -263,16 +289,15 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
             const float inv = 1.0f / root[r], mean = s[r] / width;
 #pragma unroll
             for (int k = 0; k < OCT; ++k) {
-                const int c = (me + TPR * k) * 8;
                 float n[8], v[8], w[8];
                 x[r][k].get(n);
                 y[r][k].get(v);
                 z[r][k].get(w);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = fmaf(fmaf(-n[j] * inv, mean, v[j] * g[k][j]), inv, w[j]);
-                Octet<E> o;
+                Octet<E, TPR, kMap> o;
                 o.set(v);
-                o.template store<kWide>(dX + (t0 + r) * d + c, d - c);
+                o.store(dX + (t0 + r) * d, k, d);
             }
         }
     }
@@ -282,7 +307,7 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
         if constexpr (kGroups > 1) {               // the groups' sums in order, a chunk of columns at a time
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[threadIdx.x / TPR][me * 8 + j] = acc[k][j];
+            for (int j = 0; j < 8; ++j) sums[threadIdx.x / TPR][column<TPR, kMap>(0, j)] = acc[k][j];
             __syncthreads();
             for (int i = threadIdx.x; i < TPR * 8; i += block_threads(TPR)) {
                 float v = 0.0f;
@@ -294,7 +319,7 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int c = (me + TPR * k) * 8 + j;
+                const int c = column<TPR, kMap>(k, j);
                 if (c < d) partial[static_cast<int64_t>(blockIdx.x) * d + c] = acc[k][j];
             }
         }
@@ -373,22 +398,23 @@ struct Total {
     __device__ __forceinline__ float value() const { return isfinite(sum) ? sum + lost : sum; }
 };
 
-// dgamma from the partial sums: each of 8 warps adds every eighth in order, then the warps' sums in order, with their errors (in fp64, whose
+// dgamma from the partial sums: each of 32 warps adds every 32nd in order, then the warps' sums in order, with their errors (in fp64, whose
 // additions are slow here: 40 us for 304 sums of 1537 columns).
-__global__ void __launch_bounds__(256) join_kernel(const float* partial, int64_t runs, int d, float* dgamma) {
-    __shared__ Total red[8][32];
+constexpr int kJoinWarps = 32;
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const float* partial, int64_t runs, int d, float* dgamma) {
+    __shared__ Total red[kJoinWarps][32];
     grid_wait();
     grid_release();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
     Total s;
     if (i < d)
 #pragma unroll 8
-        for (int64_t r = warp; r < runs; r += 8) s.add(partial[r * d + i]);
+        for (int64_t r = warp; r < runs; r += kJoinWarps) s.add(partial[r * d + i]);
     red[warp][lane] = s;
     __syncthreads();
     if (warp == 0 && i < d) {
 #pragma unroll
-        for (int w = 1; w < 8; ++w) s.add(red[w][lane].sum), s.lost += red[w][lane].lost;
+        for (int w = 1; w < kJoinWarps; ++w) s.add(red[w][lane].sum), s.lost += red[w][lane].lost;
         dgamma[i] = s.value();
     }
 }
@@ -431,10 +457,10 @@ size_t backward_workspace_bytes(int64_t T, int d) {
     return c.used;
 }
 
-static bool wide(int d, const void* a, const void* b, const void* c, const void* e, const void* gamma) {
+static Map map_of(int d, const void* a, const void* b, const void* c, const void* e, const void* gamma) {
     const uintptr_t all = reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b) | reinterpret_cast<uintptr_t>(c) |
                           reinterpret_cast<uintptr_t>(e) | reinterpret_cast<uintptr_t>(gamma);
-    return (all & 15) == 0 && d % 8 == 0;
+    return d % 8 != 0 ? kStrided : (all & 15) == 0 ? kWords : kOctets;
 }
 
 template <typename E>
@@ -445,9 +471,11 @@ static int forward(const void* X, const float* gamma, int64_t T, int d, float ep
         return layer::launch_blocks(forward_kernel<E>, T < 8192 ? T : 8192, kThreads, stream, x, gamma, T, d, eps, y, rms);
     return static_cast<int>(with_form_of<E>(d, [&](auto form) -> int64_t {
         using F = decltype(form);
-        const int64_t tiles = (T + F::kPerBlock - 1) / F::kPerBlock, blocks = tiles < 16384 ? tiles : 16384;
-        auto kernel = wide(d, X, Y, nullptr, nullptr, gamma) ? forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, true>
-                                                             : forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, false>;
+        const int64_t tiles = (T + F::kPerBlock - 1) / F::kPerBlock, most = kSms * (768 / F::kBlock), blocks = tiles < most ? tiles : most;
+        const Map map = map_of(d, X, Y, nullptr, nullptr, gamma);
+        auto kernel = map == kWords    ? forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kWords>
+                      : map == kOctets ? forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kOctets>
+                                       : forward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kStrided>;
         return layer::launch_blocks(kernel, blocks, F::kBlock, stream, x, gamma, T, d, eps, y, rms);
     }));
 }
@@ -468,13 +496,15 @@ static int backward(const void* dY, const void* X, const float* gamma, const flo
     } else if (T > 0 && (dX || dgamma)) {
         st = static_cast<int>(with_form_of<E>(d, [&](auto form) -> int64_t {
             using F = decltype(form);
-            auto kernel = wide(d, dY, X, dres, dX, gamma) ? backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, true>
-                                                          : backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, false>;
+            const Map map = map_of(d, dY, X, dres, dX, gamma);
+            auto kernel = map == kWords    ? backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kWords>
+                          : map == kOctets ? backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kOctets>
+                                           : backward_rows_kernel<E, F::TPR, F::OCT, F::ROWS, kStrided>;
             return layer::launch_blocks(kernel, blocks, F::kBlock, stream, dy, x, gamma, rms, dr, T, d, dx, dgamma ? partial : nullptr);
         }));
     }
     if (st != DTP_OK || !dgamma) return st;
-    return layer::launch_blocks(join_kernel, (d + 31) / 32, kThreads, stream, static_cast<const float*>(partial), T > 0 ? blocks : 0, d, dgamma);
+    return layer::launch_blocks(join_kernel, (d + 31) / 32, 32 * kJoinWarps, stream, static_cast<const float*>(partial), T > 0 ? blocks : 0, d, dgamma);
 }
 
 int launch_forward(const void* X, const float* gamma, int64_t T, int d, float eps, int dtype, void* Y, float* rms,

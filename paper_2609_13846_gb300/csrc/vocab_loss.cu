@@ -238,8 +238,9 @@ static ForwardSpace carve_forward(Carver& c, int64_t rows, int V, int dtype) {
     s.hit = static_cast<float*>(c.take(static_cast<size_t>(rows) * sizeof(float)));
     return s;
 }
-// whether the forward pass copies X: to an aligned pitch, or to whole groups of rows (beyond 4096 tokens the last tile's rate is nothing)
-static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && (d % 8 != 0 || (T % kRowPad != 0 && T < 4096)); }
+// whether the forward pass copies X: to an aligned pitch, or to whole groups of rows (from 257 tokens on the
+// copy costs more than the last tile's rate)
+static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && (d % 8 != 0 || (T % kRowPad != 0 && T < 256)); }
 struct BackwardSpace {
     void* dz;            // in fp32 the logits before
     void* x;
