@@ -138,12 +138,13 @@ struct Octet {
     }
 };
 
-// Rows t .. t + rows - 1 on their way to L2, by one thread (rows on 16-byte boundaries).
+// Rows t .. t + rows - 1 on their way to L2, by one thread; in whole 16-byte words, the first and last of which they may share.
 template <typename E>
 __device__ __forceinline__ void prefetch_rows(const E* p, int64_t t, int rows, int64_t T, int d) {
     if (t >= T) return;
     const int64_t n = T - t < rows ? T - t : rows;
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p + t * d), "r"(static_cast<uint32_t>(n * d * sizeof(E))) : "memory");
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p + t * d), from = a & ~uintptr_t(15), to = (a + n * d * sizeof(E) + 15) & ~uintptr_t(15);
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"(static_cast<uint32_t>(to - from)) : "memory");
 }
 constexpr int kAhead = 1;              // turns of a block by which its rows are prefetched (16384 x 4096: 138 us both ways, 148 with 2, 152 without)
 
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) forward_rows_kernel(const 
     // groups of a block stay together: their rows are first .. first + kGroups * kRows - 1
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T; first += stride) {
         const int64_t t0 = first + threadIdx.x / TPR * kRows;
-        if (kMap == kWords && threadIdx.x == 0) prefetch_rows(X, first + kAhead * stride, kGroups * kRows, T, d);
+        if (threadIdx.x == 0) prefetch_rows(X, first + kAhead * stride, kGroups * kRows, T, d);
         Octet<E, TPR, kMap> x[kRows][OCT];
         float s[kRows];
 #pragma unroll
@@ -245,7 +246,7 @@ backward_rows_kernel(const E* dY, const E* X, const float* gamma, const float* r
     const int64_t stride = static_cast<int64_t>(gridDim.x) * kGroups * kRows;
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * kRows; first < T; first += stride) {
         const int64_t t0 = first + threadIdx.x / TPR * kRows;
-        if (kMap == kWords && threadIdx.x == 0) {
+        if (threadIdx.x == 0) {
             prefetch_rows(X, first + kAhead * stride, kGroups * kRows, T, d);
             prefetch_rows(dY, first + kAhead * stride, kGroups * kRows, T, d);
             if (dres) prefetch_rows(dres, first + kAhead * stride, kGroups * kRows, T, d);

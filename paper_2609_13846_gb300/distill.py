@@ -1,8 +1,11 @@
-"""Running and distilling a layer whose weights a layout has permuted (Sec. 4).
+"""Running, distilling and tuning a layer whose weights a layout has permuted (Sec. 4).
 
 The part of a layer that a layout permutes, o_proj with the residual and the gated feed-forward block behind its norm,
 run forward, differentiated and updated with the library's operators: :func:`dtp.linear`, :func:`dtp.gated_ffn`, their
-backward passes and :func:`dtp.clip_grad_norm`.  The norm between them and the optimiser's update are plain torch.
+backward passes and :func:`dtp.clip_grad_norm`.  In :func:`distill_step` the norm between them and the update are plain
+torch.  :func:`tune_step` puts the model's end behind the layer, its last norm and its vocabulary, and trains both on the
+tokens that follow: :func:`dtp.rms_norm`, :func:`dtp.linear_cross_entropy`, their backward passes and
+:func:`dtp.adamw_step`, all of it in one stream's order without a synchronisation, so that a step can be captured.
 
     python -m paper_2609_13846_gb300.distill        # a perturbed, permuted layer learns its dense teacher's output
 """
@@ -70,6 +73,65 @@ def distill_step(master: dict, teacher: torch.Tensor, attn: torch.Tensor, x: tor
     return loss, norm
 
 
+HEAD_NAMES = ("head", "gamma_out")
+
+
+def head_forward(w: dict, y: torch.Tensor, targets: torch.Tensor):
+    """(loss [T] fp32 of each token, 0 where the target is -100, and what :func:`head_backward` needs) of the model's end:
+    the norm of y [T, d] with the gain gamma_out [d] fp32, and the vocabulary's rows head [V, d]."""
+    h, rms = dtp.rms_norm(y, w["gamma_out"], eps=EPS)
+    loss, lse = dtp.linear_cross_entropy(h, w["head"], targets)
+    return loss, (y, h, rms, lse, targets)
+
+
+def head_backward(w: dict, dloss: torch.Tensor, kept) -> tuple[torch.Tensor, dict]:
+    """(dy, gradients of head and gamma_out) for dloss [T] fp32."""
+    y, h, rms, lse, targets = kept
+    dh, dhead = dtp.linear_cross_entropy_backward(dloss, h, w["head"], targets, lse)
+    dy, dgamma = dtp.rms_norm_backward(dh, y, w["gamma_out"], rms)
+    return dy, dict(head=dhead, gamma_out=dgamma)
+
+
+def tune_state(master: dict, dtype: torch.dtype = torch.bfloat16, bits: int = 32) -> dict:
+    """What :func:`tune_step` keeps between steps for fp32 master weights (o, gate, up, down, gamma, head, gamma_out): their
+    copies in ``dtype`` that the layer runs on, and the optimiser's states, in ``bits`` for the matrices and 32 for the gains."""
+    matrices = [k for k, v in master.items() if v.dim() == 2]
+    gains = [k for k, v in master.items() if v.dim() == 1]
+    return dict(matrices=matrices, gains=gains, copies={k: master[k].to(dtype) for k in matrices},
+                adamw=dtp.adamw_state([master[k] for k in matrices], bits=bits),
+                adamw_gains=dtp.adamw_state([master[k] for k in gains]))
+
+
+def tune_step(master: dict, state: dict, attn: torch.Tensor, x: torch.Tensor, targets: torch.Tensor, lr, max_norm: float,
+              betas=(0.9, 0.95), weight_decay: float = 0.1):
+    """One AdamW step of the layer and the model's end on the mean loss of the tokens with a target.
+
+    master: fp32 weights, updated in place as ``state`` (of :func:`tune_state`) is; lr a number or a 0-d fp32 tensor on the
+    device.  Gradients count clipped to the global norm max_norm; gains are not decayed.  Returns (loss, gradient norm), both 0-d
+    tensors; a step whose norm is not finite changes nothing.
+    """
+    w = dict(state["copies"], **{k: master[k] for k in state["gains"]})
+    y, _, kept = layer_forward(w, attn, x, save=True)
+    loss, end = head_forward(w, y, targets)
+    share = (targets != -100).float()
+    share = share / share.sum().clamp(min=1.0)
+    dy, grads = head_backward(w, share, end)
+    grads.update(layer_backward(w, dy, kept))
+    norm = dtp.clip_grad_norm([grads[k] for k in state["matrices"] + state["gains"]], float("inf"))
+    common = dict(lr=lr, betas=betas, norm=norm, max_norm=max_norm)
+    dtp.adamw_step([master[k] for k in state["matrices"]], [grads[k] for k in state["matrices"]], state["adamw"],
+                   weight_decay=weight_decay, copies=[state["copies"][k] for k in state["matrices"]], **common)
+    dtp.adamw_step([master[k] for k in state["gains"]], [grads[k] for k in state["gains"]], state["adamw_gains"],
+                   weight_decay=0.0, **common)
+    return (loss * share).sum(), norm
+
+
+def make_head(d: int, V: int, seed: int, device="cuda:0") -> dict:
+    """A seeded vocabulary and last gain, in fp32."""
+    g = torch.Generator(device=device).manual_seed(seed)
+    return dict(head=torch.randn((V, d), generator=g, device=device) / d ** 0.5, gamma_out=torch.ones(d, device=device))
+
+
 def make_layer(d: int, N: int, Hq: int, G: int, head_dim: int, T: int, seed: int, device="cuda:0"):
     """(dense bf16 weights, attn, x) of one seeded layer."""
     P = synth.make_attention_inputs(T, d, Hq, head_dim, seed, device=device)
@@ -98,6 +160,14 @@ def main():
         loss, norm = distill_step(master, teacher, group, x, lr=2e-2, max_norm=5.0)
         if i % 5 == 0 or i == 19:
             print(f"step {i}: loss {float(loss):.5f}, gradient norm {float(norm):.4f}")
+    # the same layer with the model's end behind it, on the tokens that follow
+    master.update(make_head(d, 32000, seed=4))
+    targets = torch.randint(0, 32000, (T,), generator=g, device="cuda:0")
+    state = tune_state(master, bits=8)
+    for i in range(20):
+        loss, norm = tune_step(master, state, group, x, targets, lr=1e-3, max_norm=1.0)
+        if i % 5 == 0 or i == 19:
+            print(f"tokens, step {i}: loss {float(loss):.5f}, gradient norm {float(norm):.4f}")
 
 
 if __name__ == "__main__":
