@@ -783,7 +783,8 @@ int dtp_linear_cross_entropy(const void* X, const void* W, const int64_t* target
  *     dz_t = dloss_t (exp(z_t - lse_t) - onehot(targets_t)),  dX = dZ W,  dW = dZ^T X
  *   dloss [T] fp32;  lse [T] as dtp_linear_cross_entropy wrote it
  *   dX    [T, d], dW [V, d]: each out or NULL
- * dZ is rounded once to dtype before the products.  Tokens that do not count
+ * dZ is rounded once to dtype before the products (bf16: in units of the largest
+ * size of dloss, which the products get back).  Tokens that do not count
  * (and targets out of range, reported as in the forward direction) have zero
  * rows in dX and add nothing to dW, whatever stands in their rows of X and in
  * dloss.  T == 0 writes zeros to dW.

@@ -469,6 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             if (p.direct[job]) store_elements(static_cast<__nv_bfloat16*>(out), ldo, w, n, row0, false);
             else store_box(std::false_type(), &p.out[i], w, n, row0);
         };
+        [[maybe_unused]] const float unit = JOBS == kPairOf ? *e.unit : 1.0f;
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (; next(static_cast<int>(unit_count), job, tm, tn, part_z); unit_count += 2) {
             if constexpr (JOBS > 1) M = p.M[job], N = p.N[job], ldo = p.ldo[job];
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     const int64_t y = e.vocab.targets[m];
                     if (e.vocab.live(y)) {
                         target = static_cast<int>(y) - e.vocab.v0;
-                        if constexpr (KIND == kEpiProb) lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m];
+                        if constexpr (KIND == kEpiProb) lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m] / *e.vocab.unit;
                     } else if (KIND == kEpiProb && tn == 0 && half == 0 && e.vocab.bad(y)) {
                         atomicCAS(p.status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
                     }
@@ -589,6 +590,10 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         }
                     }
                     if (JOBS == kPairOf ? job == 0 : !e.out) continue;
+                    if constexpr (JOBS == kPairOf) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] *= unit;
+                    }
                     act_values<true>(e.act, v);
                     if (e.residual && wide) {
                         // from the rows' quarters to the lane's row, through the staging buffer
@@ -928,7 +933,7 @@ static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaS
     a.idesc0 = idesc_bf16_f32(2 * BM, BN) | 1u << 16;
     a.idesc = a.idesc0 | 1u << 15;
     a.epi = Epilogue();
-    a.epi.Z = g.sum, a.epi.add = g.add;
+    a.epi.Z = g.sum, a.epi.add = g.add, a.epi.unit = g.unit;
     auto kernel = gemm_tc_kernel<true, BN, kEpiLinear, false, kPairOf>;
     DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(F::kSmemBytes)));
     cudaLaunchConfig_t cfg = {};

@@ -207,6 +207,7 @@ struct Vocab {
     Part* parts = nullptr;                 // [chunk][M]
     float* hit = nullptr;                  // [M] the target's logit
     const float *lse = nullptr, *dloss = nullptr;
+    const float* unit = nullptr;           // of dZ: it holds dloss / unit
     __device__ __forceinline__ bool bad(int64_t y) const { return y != ignore && (y < 0 || y >= V); }
     __device__ __forceinline__ bool live(int64_t y) const { return y != ignore && y >= 0 && y < V; }
 };
@@ -221,6 +222,7 @@ struct Epilogue {
     int64_t ldo = 0;
     float* Z = nullptr;               // [M, N]
     int add = 0;                      // kEpiLinear, bf16 operands: Z += instead, and no out
+    const float* unit = nullptr;      // GradPair's
     Vocab vocab;
     float* pre = nullptr;
     int64_t M = 0;
@@ -297,6 +299,7 @@ struct GradPair {
     int cols, d;
     int parts;
     int add;                 // to the sums, which hold those of earlier pieces
+    const float* unit;       // device: dZ's, which dW gets back (the sums do not)
     float* sum;              // or NULL
     void* dw;                // [cols, d], or NULL
 };

@@ -99,17 +99,39 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
 }
 
 // X at an aligned pitch in `rows` rows, with zeros in those beyond T and, where targets are given, in those of tokens that do not count:
-// whatever stands there must not reach dW.
+// whatever stands there must not reach dW.  The last block finds dZ's unit, the largest finite size of dloss among them, where it is wanted
+// (else 1): rounding dloss (p - onehot) to bf16 would round dloss of a mean, the same in all rows, and the error would not average out.
 template <typename E>
 __global__ void __launch_bounds__(256)
-live_rows_kernel(const E* X, int64_t T, int64_t rows, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V, E* out,
-                 int* status) {
+live_rows_kernel(const E* X, int64_t T, int64_t rows, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V,
+                 const float* dloss, E* out, float* unit, int* status) {
+    __shared__ float red[8];
     grid_wait();
     grid_release();
     if (targets && blockIdx.x == 0 && threadIdx.x == 0) *status = DTP_OK;
+    if (unit && blockIdx.x == gridDim.x - 1) {
+        float top = 0.0f;
+        if (dloss)
+#pragma unroll 8
+            for (int64_t t = threadIdx.x; t < T; t += 256) {
+                const int64_t y = targets[t];
+                const float g = fabsf(dloss[t]);
+                if (y != ignore && y >= 0 && y < V && isfinite(g)) top = fmaxf(top, g);
+            }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            for (int w = 1; w < 8; ++w) top = fmaxf(top, red[w]);
+            *unit = top >= 1.1754944e-38f ? top : 1.0f;
+        }
+        if (gridDim.x > 1) return;
+    }
+    const int64_t blocks = unit && gridDim.x > 1 ? gridDim.x - 1 : gridDim.x;
     constexpr int kPer = 16 / sizeof(E);
     const bool wide = d % kPer == 0 && pitch % kPer == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0;
-    for (int64_t t = blockIdx.x; t < rows; t += gridDim.x) {
+    for (int64_t t = blockIdx.x; t < rows; t += blocks) {
         bool live = t < T;
         if (live && targets) {
             const int64_t y = targets[t];
@@ -146,10 +168,11 @@ dz_kernel(const float* Z, int64_t T, int cols, Vocab e, E* dZ, int64_t ld, int* 
     }
 }
 
-// dX from its sums: `parts` of them, `stride` values apart
-__global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts, int64_t stride, int64_t n, __nv_bfloat16* out) {
+// dX from its sums, in dZ's unit: `parts` of them, `stride` values apart
+__global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts, int64_t stride, int64_t n, const float* unit, __nv_bfloat16* out) {
     grid_wait();
     grid_release();
+    const float u = *unit;
     const int64_t words = n / 4;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < words; i += gridDim.x * 256ll) {
         float4 v = reinterpret_cast<const float4*>(sum)[i];
@@ -157,14 +180,14 @@ __global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts,
             const float4 w = reinterpret_cast<const float4*>(sum + p * stride)[i];
             v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
         }
-        const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+        const __nv_bfloat162 a = __floats2bfloat162_rn(u * v.x, u * v.y), b = __floats2bfloat162_rn(u * v.z, u * v.w);
         reinterpret_cast<uint2*>(out)[i] = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
     }
     const int64_t rest = 4 * words + threadIdx.x;
     if (blockIdx.x == 0 && rest < n) {
         float v = sum[rest];
         for (int p = 1; p < parts; ++p) v += sum[p * stride + rest];
-        out[rest] = __float2bfloat16_rn(v);
+        out[rest] = __float2bfloat16_rn(u * v);
     }
 }
 
@@ -244,7 +267,7 @@ static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && 
 struct BackwardSpace {
     void* dz;            // in fp32 the logits before
     void* x;
-    float *sum, *runs;
+    float *sum, *runs, *unit;
 };
 static int64_t sum_rows(int64_t T) { return (padded_rows(T) + 255) / 256 * 256; }
 static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtype, const Pieces& pieces) {
@@ -254,6 +277,7 @@ static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtyp
     s.x = c.take(static_cast<size_t>(rows) * padded(d) * elem(dtype));
     if (dtype == DTP_BF16) s.sum = static_cast<float*>(c.take(static_cast<size_t>(sum_rows(T)) * pieces.parts * d * sizeof(float)));
     s.runs = static_cast<float*>(c.take(runs_bytes(rows, pieces.cols, d)));
+    s.unit = static_cast<float*>(c.take(sizeof(float)));
     return s;
 }
 
@@ -297,7 +321,8 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
         void* to = c.take(static_cast<size_t>(rows_x) * padded(d) * elem(dtype));
         x = Rows{to, padded(d)};
         st = launch_after(live_rows_kernel<__nv_bfloat16>, grid_of(rows_x), stream, static_cast<const __nv_bfloat16*>(X), T, rows_x, d,
-                          x.ld, static_cast<const int64_t*>(nullptr), int64_t(0), 0, static_cast<__nv_bfloat16*>(to), status);
+                          x.ld, static_cast<const int64_t*>(nullptr), int64_t(0), 0, static_cast<const float*>(nullptr),
+                          static_cast<__nv_bfloat16*>(to), static_cast<float*>(nullptr), status);
     }
     const int64_t most = forward_rows(T, V, dtype);
     ForwardSpace s = carve_forward(c, most, V, dtype);
@@ -347,10 +372,11 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
     const int64_t rows = kBf16 ? padded_rows(T) : T;
     const Rows x{s.x, padded(d)};
     Vocab e;
-    e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss;
+    e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss, e.unit = s.unit;
+    const bool in_runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs, which know no unit
     if (st == DTP_OK)
-        st = launch_after(live_rows_kernel<E>, grid_of(rows), stream, static_cast<const E*>(X), T, rows, d, x.ld, targets, ignore, V,
-                          static_cast<E*>(s.x), status);
+        st = launch_after(live_rows_kernel<E>, grid_of(rows) + 1, stream, static_cast<const E*>(X), T, rows, d, x.ld, targets, ignore, V,
+                          kBf16 && !in_runs ? dloss : nullptr, static_cast<E*>(s.x), s.unit, status);
     call.fresh = false;
     for (int v0 = 0; st == DTP_OK && v0 < V; v0 += pieces.cols) {
         const int cols = V - v0 < pieces.cols ? V - v0 : pieces.cols;
@@ -363,11 +389,11 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
         if constexpr (kBf16) {
             p.epi.kind = kEpiProb, p.epi.vocab = e;
             st = gtc::launch(p, status, 0, stream);
-            const bool runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs
-            GradPair g{s.dz, s.x, w_at, ldz, x.ld, w.ld, rows, cols, d, pieces.parts, v0 > 0, dX ? s.sum : nullptr, runs ? nullptr : dw_at};
+            GradPair g{s.dz, s.x, w_at, ldz, x.ld, w.ld, rows, cols, d, pieces.parts, v0 > 0, s.unit, dX ? s.sum : nullptr,
+                       in_runs ? nullptr : dw_at};
             if (g.parts > (cols + 63) / 64) g.parts = (cols + 63) / 64;       // a short last piece leaves the others' sums as they are
             if (st == DTP_OK) st = gtc::launch_pair(g, status, stream);
-            if (st == DTP_OK && runs)
+            if (st == DTP_OK && in_runs)
                 st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, rows, s.runs);
         } else {
             st = call.run(p);
@@ -388,7 +414,7 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
     }
     if (kBf16 && st == DTP_OK && dX)
         st = launch_after(round_kernel, grid_of((T * d / 4 + 255) / 256 + 1), stream, static_cast<const float*>(s.sum), pieces.parts,
-                          sum_rows(T) * d, T * d, static_cast<__nv_bfloat16*>(dX));
+                          sum_rows(T) * d, T * d, static_cast<const float*>(s.unit), static_cast<__nv_bfloat16*>(dX));
     return st;
 }
 
