@@ -164,11 +164,13 @@ __global__ void __launch_bounds__(Tile<TY>::kThreads, Tile<TY>::kBlocks) gemm_f3
     const int64_t m0 = tile / g.tiles_n * TM;
     const int n0 = static_cast<int>(tile % g.tiles_n) * kCols;
     const int64_t blocks = (p.K + TK - 1) / TK;           // per segment
-    const int64_t b0 = p.segments * blocks * part / g.split, b1 = p.segments * blocks * (part + 1) / g.split;
+    // the launch's part of k, and of that this block's
+    const int64_t lo = p.segments * blocks * blockIdx.y / gridDim.y, hi = p.segments * blocks * (blockIdx.y + 1) / gridDim.y;
+    const int64_t b0 = lo + (hi - lo) * part / g.split, b1 = lo + (hi - lo) * (part + 1) / g.split;
 
     const Copies<TM, S::kThreads> ca(p.A, p.segments, m0, p.M, g.wide_a, false);
     const Copies<TN, S::kThreads> cb(p.B, p.segments, n0, p.N, g.wide_b, kGated);
-    if (g.status && blockIdx.x == 0 && tid == 0) *g.status = DTP_OK;
+    if (g.status && blockIdx.x == 0 && blockIdx.y == 0 && tid == 0) *g.status = DTP_OK;
     auto fetch = [&](int64_t b) {
         if (b < b1) {
             float* st = stages + (b % STAGES) * S::kStage;
@@ -224,7 +226,7 @@ __global__ void __launch_bounds__(Tile<TY>::kThreads, Tile<TY>::kBlocks) gemm_f3
             const float e[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (n0 + c + i < p.N) epilogue_element<float, KIND>(p.epi, m, n0 + c + i, e[i], 0.0f);
+                if (n0 + c + i < p.N) epilogue_element<float, KIND>(p.epi, m + blockIdx.y * p.M, n0 + c + i, e[i], 0.0f);
         }
     };
     auto sums = [&](int i, int q) {
@@ -274,7 +276,8 @@ static int launch_tiles(const Product& p, int* status, int sms, cudaStream_t str
     const int64_t tiles = (p.M + S::TM - 1) / S::TM * g.tiles_n;
     // blocks per tile: as many as the chip holds of them, with at least 64 k for each
     const int64_t room = S::kBlocks * static_cast<int64_t>(sms) / tiles, most = p.K * p.segments / 64;
-    const int64_t split = !S::kSplits ? 1 : room < most ? room : most;
+    const int64_t most_of = most / p.parts;
+    const int64_t split = !S::kSplits ? 1 : room < most_of ? room : most_of;
     g.split = static_cast<int>(split < 1 ? 1 : split < kMaxSplit ? split : kMaxSplit);
     if (tiles * g.split > 0x7FFFFFFF) return DTP_ERR_UNSUPPORTED;
     auto wide = [](const Mat& m) { return m.ks != 1 && m.ks % 4 == 0 && aligned16(m.p); };
@@ -286,7 +289,7 @@ static int launch_tiles(const Product& p, int* status, int sms, cudaStream_t str
     DTP_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       static_cast<int>(S::kSmem)));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(tiles * g.split));
+    cfg.gridDim = dim3(static_cast<unsigned>(tiles * g.split), static_cast<unsigned>(p.parts));
     cfg.blockDim = dim3(S::kThreads);
     cfg.dynamicSmemBytes = S::kSmem;
     cfg.stream = stream;

@@ -891,7 +891,14 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     return DTP_OK;
 }
 
-// A form's launch on `workers` pairs.
+// A tile of a pair's launch takes its k blocks, and no less than its epilogue: 3 us for 256 x 256 sums to bf16, 10 blocks.
+static int64_t tile_blocks(int64_t blocks) { return blocks > 9 ? blocks + 1 : 10; }
+// Tiles of product 1 in the time of one of product 0's (of a part).
+static int64_t extra_tiles(int64_t part_blocks, int64_t blocks1) {
+    const int64_t c1 = tile_blocks(blocks1);
+    return (tile_blocks(part_blocks) + c1 / 2) / c1;
+}
+
 template <int BN>
 static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaStream_t stream) {
     using F = Form<true, BN>;
@@ -914,8 +921,7 @@ static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaS
     if (units[0] + units[1] == 0) return DTP_OK;
     a.n0 = static_cast<int>(units[0]), a.units = static_cast<int>(units[0] + units[1]);
     a.rows_z = a.tiles_m[0] * 2 * BM;
-    const int64_t long_blocks = a.KB0 / a.parts;
-    a.extra = static_cast<int>((long_blocks + a.KB1 / 2) / a.KB1);
+    a.extra = static_cast<int>(extra_tiles(a.KB0 / a.parts, a.KB1));
     if (!map_operand(&a.a[0], by(g.dz, g.ldz, true), g.rows, g.cols, BM) ||
         !map_operand(&a.b[0], by(g.w, g.ldw, false), g.d, g.cols, BN / 2) ||
         !map_operand(&a.a[1], by(g.dz, g.ldz, false), g.cols, g.rows, BM) ||
@@ -962,18 +968,19 @@ int launch_pair(const GradPair& g, int* status, cudaStream_t stream) {
     return g.d <= 128 ? launch_pair_form<128>(g, status, sms / 2, stream) : launch_pair_form<256>(g, status, sms / 2, stream);
 }
 
-// As dealt by pair_unit on 76 pairs; a tile takes its k blocks, and no less than its epilogue (about 6 of them).
+// As dealt by pair_unit on 76 pairs.
 int64_t pair_clocks(int64_t rows, int cols, int d, int* parts) {
     constexpr int64_t W = 76;
     const int64_t bn = d <= 128 ? 128 : 256, cols_d = (d + bn - 1) / bn;
     auto up = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-    auto cost = [](int64_t blocks) { return blocks > 5 ? blocks + 1 : 6; };
     const int64_t tiles0 = up(rows, 256) * cols_d, n1 = up(cols, 256) * cols_d, kb0 = up(cols, 64), kb1 = up(rows, 64);
-    const int64_t c1 = cost(kb1);
+    const int64_t c1 = tile_blocks(kb1);
     int64_t best = 0;
-    for (int h = 1; h <= 8 && (h == 1 || kb0 / h >= 8); ++h) {
-        const int64_t n0 = tiles0 * h, c0 = cost(up(kb0, h)), last = n0 % W, others = W - last;
-        const int64_t extra = last ? (kb0 / h + kb1 / 2) / kb1 : 0;
+    // the parts' sums: 8 of them, or 64 MB (few tokens have few tiles: 64 x 1024 has 4)
+    const int64_t room = (int64_t(64) << 20) / (up(rows, 256) * 256 * d * 4), most = room < 8 ? 8 : room < 64 ? room : 64;
+    for (int h = 1; h <= most && (h == 1 || kb0 / h >= 8); ++h) {
+        const int64_t n0 = tiles0 * h, c0 = tile_blocks(up(kb0, h)), last = n0 % W, others = W - last;
+        const int64_t extra = last ? extra_tiles(kb0 / h, kb1) : 0;
         const int64_t lead = n0 / W * c0 + (last ? (c0 > extra * c1 ? c0 : extra * c1) : 0);
         const int64_t left = n1 - extra * others;
         const int64_t t = lead + (left > 0 ? up(left, W) * c1 : 0);

@@ -285,6 +285,7 @@ struct Product {
     int N = 0;
     int64_t K = 0;
     int64_t rows_a = 0;      // rows that A has, where more than M (bf16 only)
+    int parts = 1;           // fp32, kEpiLinear without anything beside the sums: ranges of k whose sums go to [parts][M, ldo] each
     Epilogue epi;
 };
 

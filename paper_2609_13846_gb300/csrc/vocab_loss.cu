@@ -168,6 +168,18 @@ dz_kernel(const float* Z, int64_t T, int cols, Vocab e, E* dZ, int64_t ld, int* 
     }
 }
 
+// fp32: dX (+)= the sums of its parts
+__global__ void __launch_bounds__(256) add_parts_kernel(const float* sums, int parts, int64_t n, int add, float* out) {
+    grid_wait();
+    grid_release();
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) {
+        float v = add ? out[i] : 0.0f;
+#pragma unroll 8
+        for (int p = 0; p < parts; ++p) v += sums[p * n + i];
+        out[i] = v;
+    }
+}
+
 // dX from its sums, in dZ's unit: `parts` of them, `stride` values apart
 __global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts, int64_t stride, int64_t n, const float* unit, __nv_bfloat16* out) {
     grid_wait();
@@ -221,9 +233,16 @@ static int64_t parts_of(int64_t rows, int V, int dtype) {
 // The pieces of the backward pass: columns of each but the last, and the parts in which dX is summed.  bf16: of the numbers of pieces that
 // keep dZ within kPieceBytes, up to twice the least, the one whose tiles leave the fewest rounds of pairs unfilled; sizes near
 // 8192 x 131072 x 1024 differ by 10% in that.
+// fp32: few tokens have few tiles, and dX a sum over the whole piece: as many parts of it as blocks of 64 x 128 leave the chip's 608
+// places empty after the tiles are split in eight, with at least 512 columns for each (5 tokens, 65536 x 112: 600 us in one).
 struct Pieces { int cols, parts; };
 static Pieces backward_pieces(int64_t T, int d, int V, int dtype) {
-    if (dtype == DTP_F32) return Pieces{stored_cols(T, V), 1};
+    if (dtype == DTP_F32) {
+        const int cols = stored_cols(T, V);
+        const int64_t tiles = (T + 63) / 64 * ((d + 127) / 128), room = 608 / (8 * tiles), most = cols / 512;
+        const int64_t parts = room < most ? room : most;
+        return Pieces{cols, static_cast<int>(parts > 1 ? parts : 1)};
+    }
     const int64_t rows = padded_rows(T);
     int64_t most = static_cast<int64_t>(kPieceBytes / 2) / rows / 256 * 256;
     if (most < 256) most = 256;
@@ -275,7 +294,8 @@ static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtyp
     const int64_t rows = dtype == DTP_BF16 ? padded_rows(T) : T;
     s.dz = c.take(static_cast<size_t>(rows) * (dtype == DTP_BF16 ? padded(pieces.cols) : pieces.cols) * elem(dtype));
     s.x = c.take(static_cast<size_t>(rows) * padded(d) * elem(dtype));
-    if (dtype == DTP_BF16) s.sum = static_cast<float*>(c.take(static_cast<size_t>(sum_rows(T)) * pieces.parts * d * sizeof(float)));
+    const int64_t summed = dtype == DTP_BF16 ? sum_rows(T) : pieces.parts > 1 ? T : 0;
+    s.sum = static_cast<float*>(c.take(static_cast<size_t>(summed) * pieces.parts * d * sizeof(float)));
     s.runs = static_cast<float*>(c.take(runs_bytes(rows, pieces.cols, d)));
     s.unit = static_cast<float*>(c.take(sizeof(float)));
     return s;
@@ -306,6 +326,15 @@ static Product logits(const Rows& x, int64_t rows_x, int64_t t0, const Rows& w, 
     p.M = T, p.N = cols, p.K = d, p.rows_a = rows_x - t0;
     p.epi.M = T, p.epi.N = cols, p.epi.ldo = cols;
     return p;
+}
+
+// Stored logits (fp32).  Beyond 8 tokens the tiles are faster than the few-token kernel's passes of 8 where the vocabulary fills the
+// chip (21 tokens, 65536 x 64: 150 us in passes).
+static int store_logits(Call& call, const Product& p) {
+    if (p.M <= 8 || p.N < 8192) return call.run(p);
+    int* status = call.fresh ? static_cast<int*>(call.workspace) : nullptr;
+    call.fresh = false;
+    return simt::launch(p, call.dtype, status, call.stream);
 }
 
 int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V, int64_t ignore, int dtype,
@@ -343,7 +372,7 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
                 const int cols = V - v0 < piece ? V - v0 : piece;
                 Product p = logits(x, rows_x, t0, w, rows, d, v0, cols, dtype);
                 p.epi.out = s.Z;
-                st = call.run(p);
+                st = store_logits(call, p);
                 const int64_t chunks = (cols + kChunk - 1) / kChunk;
                 if (st == DTP_OK)
                     st = launch_after(parts_kernel, grid_of(rows * chunks), stream, static_cast<const float*>(s.Z), rows, cols, v0,
@@ -396,7 +425,7 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
             if (st == DTP_OK && in_runs)
                 st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, rows, s.runs);
         } else {
-            st = call.run(p);
+            st = store_logits(call, p);
             if (st == DTP_OK)
                 st = launch_after(dz_kernel<E>, grid_of(T * ((cols + kChunk - 1) / kChunk)), stream, static_cast<const float*>(s.dz),
                                   T, cols, e, static_cast<E*>(s.dz), ldz, status);
@@ -405,9 +434,14 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
                 q.A[0] = by_row(s.dz, ldz);
                 q.B[0] = by_col(w_at, w.ld);
                 q.M = T, q.N = d, q.K = cols;
-                q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
                 q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
-                st = call.run(q);
+                q.parts = pieces.parts;
+                if (q.parts == 1) q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
+                else q.epi.out = s.sum;
+                st = simt::launch(q, dtype, nullptr, stream);
+                if (st == DTP_OK && q.parts > 1)
+                    st = launch_after(add_parts_kernel, grid_of((T * d + 255) / 256), stream, static_cast<const float*>(s.sum), q.parts,
+                                      T * d, static_cast<int>(v0 > 0), static_cast<float*>(dX));
             }
             if (st == DTP_OK && dW) st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, T, s.runs);
         }
