@@ -977,7 +977,8 @@ int64_t pair_clocks(int64_t rows, int cols, int d, int* parts) {
     const int64_t c1 = tile_blocks(kb1);
     int64_t best = 0;
     // the parts' sums: 8 of them, or 64 MB (few tokens have few tiles: 64 x 1024 has 4)
-    const int64_t room = (int64_t(64) << 20) / (up(rows, 256) * 256 * d * 4), most = room < 8 ? 8 : room < 64 ? room : 64;
+    const int64_t room = (int64_t(64) << 20) / (up(rows, 256) * 256 * d * 4), fit = 0x7FFFFFFF / (up(rows, 256) * 256);
+    const int64_t wanted = room < 8 ? 8 : room < 64 ? room : 64, most = wanted < fit ? wanted : fit;       // a row's number is an int
     for (int h = 1; h <= most && (h == 1 || kb0 / h >= 8); ++h) {
         const int64_t n0 = tiles0 * h, c0 = tile_blocks(up(kb0, h)), last = n0 % W, others = W - last;
         const int64_t extra = last ? extra_tiles(kb0 / h, kb1) : 0;

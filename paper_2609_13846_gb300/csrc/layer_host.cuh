@@ -30,6 +30,15 @@ bool takes(const layer::Product& p, int dtype);
 int launch(const layer::Product& p, int dtype, int* status, int second, cudaStream_t stream);
 }  // namespace fews
 
+// fp32, up to 32 tokens (few_loss_f32.cu)
+namespace fewl {
+int ranges_of(int64_t V, int d);
+bool takes_logits(int64_t T, int d);
+int launch_logits(const float* X, const float* W, int64_t T, int64_t V, int d, float* Z, cudaStream_t stream);
+int launch_dx(const float* dZ, const float* W, int64_t T, int64_t V, int d, int ranges, float* parts, cudaStream_t stream);
+int launch_dw(const float* dZ, const float* X, int64_t T, int64_t V, int d, float* dW, cudaStream_t stream);
+}  // namespace fewl
+
 namespace layer {
 
 // A launch whose start may overlap the end of the one before it.

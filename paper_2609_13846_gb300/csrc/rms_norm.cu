@@ -491,9 +491,10 @@ static int backward(const void* dY, const void* X, const float* gamma, const flo
     auto* partial = static_cast<float*>(c.take(static_cast<size_t>(blocks) * d * sizeof(float)));
     int st = DTP_OK;
     if (T > 0 && d > kWidest) {
-        if (dX) st = layer::launch_blocks(rows_kernel<E>, T < 8192 ? T : 8192, kThreads, stream, dy, x, gamma, rms, dr, T, d, dx);
-        if (st == DTP_OK && dgamma)
+        if (dgamma)                        // first: dX may take the place of dY
             st = layer::launch_blocks(columns_kernel<E>, blocks * ((d + kThreads - 1) / kThreads), kThreads, stream, dy, x, rms, T, d, partial);
+        if (st == DTP_OK && dX)
+            st = layer::launch_blocks(rows_kernel<E>, T < 8192 ? T : 8192, kThreads, stream, dy, x, gamma, rms, dr, T, d, dx);
     } else if (T > 0 && (dX || dgamma)) {
         st = static_cast<int>(with_form_of<E>(d, [&](auto form) -> int64_t {
             using F = decltype(form);

@@ -217,6 +217,7 @@ static int64_t forward_rows(int64_t T, int V, int dtype) {
     if (n < 256) n = 256;
     return n < T ? n : T;
 }
+constexpr int64_t kFew = 32;          // tokens of the fp32 kernels for few of them
 // Columns of a piece of T tokens' logits (fp32), forward or backward.
 static int stored_cols(int64_t T, int V) {
     int64_t n = static_cast<int64_t>(kPieceBytes / sizeof(float)) / T / 256 * 256;
@@ -234,11 +235,13 @@ static int64_t parts_of(int64_t rows, int V, int dtype) {
 // keep dZ within kPieceBytes, up to twice the least, the one whose tiles leave the fewest rounds of pairs unfilled; sizes near
 // 8192 x 131072 x 1024 differ by 10% in that.
 // fp32: few tokens have few tiles, and dX a sum over the whole piece: as many parts of it as blocks of 64 x 128 leave the chip's 608
-// places empty after the tiles are split in eight, with at least 512 columns for each (5 tokens, 65536 x 112: 600 us in one).
+// places empty after the tiles are split in eight, with at least 512 columns for each (64 tokens, 32768 x 1024: 570 us in one), or those
+// of the few tokens' kernel.
 struct Pieces { int cols, parts; };
 static Pieces backward_pieces(int64_t T, int d, int V, int dtype) {
     if (dtype == DTP_F32) {
         const int cols = stored_cols(T, V);
+        if (T <= kFew) return Pieces{cols, fewl::ranges_of(cols, d)};
         const int64_t tiles = (T + 63) / 64 * ((d + 127) / 128), room = 608 / (8 * tiles), most = cols / 512;
         const int64_t parts = room < most ? room : most;
         return Pieces{cols, static_cast<int>(parts > 1 ? parts : 1)};
@@ -294,7 +297,7 @@ static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtyp
     const int64_t rows = dtype == DTP_BF16 ? padded_rows(T) : T;
     s.dz = c.take(static_cast<size_t>(rows) * (dtype == DTP_BF16 ? padded(pieces.cols) : pieces.cols) * elem(dtype));
     s.x = c.take(static_cast<size_t>(rows) * padded(d) * elem(dtype));
-    const int64_t summed = dtype == DTP_BF16 ? sum_rows(T) : pieces.parts > 1 ? T : 0;
+    const int64_t summed = dtype == DTP_BF16 ? sum_rows(T) : pieces.parts > 1 || T <= kFew ? T : 0;
     s.sum = static_cast<float*>(c.take(static_cast<size_t>(summed) * pieces.parts * d * sizeof(float)));
     s.runs = static_cast<float*>(c.take(runs_bytes(rows, pieces.cols, d)));
     s.unit = static_cast<float*>(c.take(sizeof(float)));
@@ -328,13 +331,18 @@ static Product logits(const Rows& x, int64_t rows_x, int64_t t0, const Rows& w, 
     return p;
 }
 
-// Stored logits (fp32).  Beyond 8 tokens the tiles are faster than the few-token kernel's passes of 8 where the vocabulary fills the
-// chip (21 tokens, 65536 x 64: 150 us in passes).
+// Stored logits (fp32): few tokens have kernels of their own.
 static int store_logits(Call& call, const Product& p) {
-    if (p.M <= 8 || p.N < 8192) return call.run(p);
+    if (p.M <= kFew && !fewl::takes_logits(p.M, static_cast<int>(p.K))) return call.run(p);
     int* status = call.fresh ? static_cast<int*>(call.workspace) : nullptr;
+    if (p.M > kFew) {
+        call.fresh = false;
+        return simt::launch(p, call.dtype, status, call.stream);
+    }
+    if (status) DTP_CUDA_TRY(cudaMemsetAsync(status, 0, sizeof(int), call.stream));
     call.fresh = false;
-    return simt::launch(p, call.dtype, status, call.stream);
+    return fewl::launch_logits(static_cast<const float*>(p.A[0].p), static_cast<const float*>(p.B[0].p), p.M, p.N, static_cast<int>(p.K),
+                               static_cast<float*>(p.epi.out), call.stream);
 }
 
 int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T, int d, int V, int64_t ignore, int dtype,
@@ -399,7 +407,7 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
     const BackwardSpace s = carve_backward(c, T, d, V, dtype, pieces);
     int* status = static_cast<int*>(workspace);
     const int64_t rows = kBf16 ? padded_rows(T) : T;
-    const Rows x{s.x, padded(d)};
+    const Rows x{s.x, kBf16 || T > kFew ? padded(d) : d};
     Vocab e;
     e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss, e.unit = s.unit;
     const bool in_runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs, which know no unit
@@ -436,14 +444,22 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
                 q.M = T, q.N = d, q.K = cols;
                 q.epi.ldo = d, q.epi.M = T, q.epi.N = d;
                 q.parts = pieces.parts;
-                if (q.parts == 1) q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
+                const bool few = T <= kFew;
+                if (few) {
+                    q.parts = fewl::ranges_of(cols, d);
+                    st = fewl::launch_dx(static_cast<const float*>(s.dz), static_cast<const float*>(w_at), T, cols, d, q.parts, s.sum, stream);
+                } else if (q.parts == 1) q.epi.out = dX, q.epi.residual = v0 > 0 ? dX : nullptr;
                 else q.epi.out = s.sum;
-                st = simt::launch(q, dtype, nullptr, stream);
-                if (st == DTP_OK && q.parts > 1)
+                if (!few) st = simt::launch(q, dtype, nullptr, stream);
+                if (st == DTP_OK && (few || q.parts > 1))
                     st = launch_after(add_parts_kernel, grid_of((T * d + 255) / 256), stream, static_cast<const float*>(s.sum), q.parts,
                                       T * d, static_cast<int>(v0 > 0), static_cast<float*>(dX));
             }
-            if (st == DTP_OK && dW) st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, T, s.runs);
+            if (st == DTP_OK && dW && T <= kFew)
+                st = fewl::launch_dw(static_cast<const float*>(s.dz), static_cast<const float*>(x.p), T, cols, d,
+                                     reinterpret_cast<float*>(dw_at), stream);
+            else if (st == DTP_OK && dW)
+                st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, T, s.runs);
         }
     }
     if (kBf16 && st == DTP_OK && dX)

@@ -153,3 +153,29 @@ def test_streams_and_graphs():
     want, wrms = dtp.rms_norm(x.flip(0).contiguous(), gamma)
     wdx, wdgamma = dtp.rms_norm_backward(b, a, gamma, wrms, dresidual=dres)
     assert torch.equal(y3, want) and torch.equal(dx3, wdx) and torch.equal(dgamma3, wdgamma)
+
+
+@pytest.mark.parametrize("d", [200, 1001, 4096, 9000])
+@pytest.mark.parametrize("over", ["dY", "dresidual"])
+def test_gradient_in_place_of_an_input(d, over):
+    """At the C ABI dX may be dY or the residual's gradient; either output may be left out."""
+    x, gamma, dy, dres = _inputs(70, d, torch.bfloat16)
+    _, rms = dtp.rms_norm(x, gamma)
+    want, wgamma = dtp.rms_norm_backward(dy, x, gamma, rms, dresidual=dres)
+    ws = dtp.rms_norm_workspace(70, d, torch.bfloat16, DEV)
+
+    def call(dy, dres, dx, dgamma):
+        st = dtp.lib().dtp_rms_norm_backward(dy.data_ptr(), x.data_ptr(), gamma.data_ptr(), rms.data_ptr(), dres.data_ptr(), 70, d,
+                                             dtp.DTP_BF16, None if dx is None else dx.data_ptr(),
+                                             None if dgamma is None else dgamma.data_ptr(), ws.data_ptr(), ws.numel(),
+                                             torch.cuda.current_stream().cuda_stream)
+        assert st == dtp.DTP_OK
+
+    a, b, dgamma = dy.clone(), dres.clone(), torch.zeros_like(gamma)
+    dx = a if over == "dY" else b
+    call(a, b, dx, dgamma)
+    assert torch.equal(dx, want) and torch.equal(dgamma, wgamma)
+    alone, galone = torch.zeros_like(x), torch.zeros_like(gamma)
+    call(dy, dres, alone, None)
+    call(dy, dres, None, galone)
+    assert torch.equal(alone, want) and torch.equal(galone, wgamma)

@@ -56,7 +56,10 @@ def _check(x, w, y, dloss, loss, lse, dx=None, dw=None, ignore=IGNORE):
     assert (dx[~live] == 0).all()
 
 
-SIZES = [(1, 1, 1), (1, 8, 2), (1, 64, 1000), (2, 72, 129), (3, 40, 8193), (7, 100, 257), (17, 256, 5003), (64, 136, 640),
+# fp32 has kernels of its own up to 32 tokens, with X whole in shared memory or in pieces
+FEW = [(1, 1000, 33), (8, 130, 4096), (9, 2, 70), (16, 1537, 520), (17, 12, 999), (25, 2048, 321), (31, 3, 64), (32, 768, 1000),
+       (32, 1600, 97), (33, 40, 515)]
+SIZES = FEW + [(1, 1, 1), (1, 8, 2), (1, 64, 1000), (2, 72, 129), (3, 40, 8193), (7, 100, 257), (17, 256, 5003), (64, 136, 640),
          (65, 136, 641), (100, 64, 128), (128, 512, 1024), (129, 65, 1023), (257, 520, 5003), (300, 1024, 2500), (515, 96, 40001),
          (1000, 64, 300), (2048, 128, 70)]
 
@@ -209,3 +212,64 @@ def test_repeats_streams_and_graphs(T, d, V):
         ws.fill_(255)
         graph.replay()
         assert all(torch.equal(a, b) for a, b in zip(first, out))
+
+
+@pytest.mark.parametrize("T,d,V,dtype", [(17000, 64, 131072, torch.bfloat16), (16500, 24, 300, torch.float32)])
+def test_several_runs_of_tokens(T, d, V, dtype):
+    """More tokens than the forward pass takes at once: the runs meet at their edges."""
+    x, w, y, dloss = _inputs(T, d, V, dtype)
+    loss, lse = dtp.linear_cross_entropy(x, w, y, check=True)
+    some = torch.cat([torch.arange(0, T, 97, device=DEV), torch.arange(16384 - 3, 16384 + 3, device=DEV), torch.tensor([T - 1], device=DEV)])
+    _check(x[some], w, y[some], dloss[some], loss[some], lse[some])
+
+
+def test_very_many_tokens():
+    """More than 2^18: dW is made in runs, whose sums are added in 64 bits."""
+    T, d, V = (1 << 18) + 100, 64, 300
+    x, w, y, dloss = _inputs(T, d, V, torch.bfloat16)
+    loss, lse = dtp.linear_cross_entropy(x, w, y, check=True)
+    dx, dw = dtp.linear_cross_entropy_backward(dloss, x, w, y, lse, check=True)
+    some = torch.arange(0, T, 1009, device=DEV)
+    X, W = x.double(), w.double()
+    live = (y != IGNORE).double()
+    g = (dloss.double() * live)[:, None]
+    dz = torch.softmax(X @ W.t(), 1)
+    dz.scatter_add_(1, torch.where(y == IGNORE, 0, y)[:, None], -torch.ones_like(g))
+    dz *= g
+    half = torch.finfo(torch.bfloat16).eps / 2
+    # dZ's rounding and a probability's error (2^-13), the runs' sums (2^18 terms in 2^14 steps of 21/16 2^-22), the output's rounding
+    off = (1.01 * half + 2.0 ** -13 + 2.0 ** 14 * 21 / 16 * 2.0 ** -22) * dz.abs()
+    ref = dz.t() @ X
+    assert ((dw.double() - ref).abs() <= half * ref.abs() + off.t() @ X.abs()).all()
+    ref = dz[some] @ W
+    assert ((dx[some].double() - ref).abs() <= half * ref.abs() + off[some] @ W.abs()).all()
+
+
+@pytest.mark.parametrize("T,dtype", [(5, torch.bfloat16), (100, torch.bfloat16), (5, torch.float32), (100, torch.float32)])
+def test_one_gradient_alone(T, dtype):
+    """At the C ABI either gradient may be left out."""
+    x, w, y, dloss = _inputs(T, 72, 900, dtype)
+    _, lse = dtp.linear_cross_entropy(x, w, y)
+    dx, dw = dtp.linear_cross_entropy_backward(dloss, x, w, y, lse)
+    ws = dtp.linear_cross_entropy_workspace(T, 72, 900, dtype, DEV, backward=True)
+    for one in (True, False):
+        a, b = torch.full_like(x, 7.0), torch.full_like(w, 7.0)
+        st = dtp.lib().dtp_linear_cross_entropy_backward(
+            dloss.data_ptr(), x.data_ptr(), w.data_ptr(), y.data_ptr(), lse.data_ptr(), T, 72, 900, IGNORE, dtp._torch_code(dtype),
+            a.data_ptr() if one else None, None if one else b.data_ptr(), ws.data_ptr(), ws.numel(),
+            torch.cuda.current_stream().cuda_stream)
+        assert st == dtp.DTP_OK
+        assert torch.equal(a, dx if one else torch.full_like(x, 7.0)) and torch.equal(b, torch.full_like(w, 7.0) if one else dw)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1.0, 1e30])
+def test_gradients_of_any_size(scale):
+    """dloss far from one, and of both signs: dZ is held in units of its largest size."""
+    x, w, y, dloss = _inputs(150, 64, 400, torch.bfloat16)
+    dloss = dloss * 150 * scale
+    dloss[::3] *= -1e-4
+    loss, lse = dtp.linear_cross_entropy(x, w, y)
+    dx, dw = dtp.linear_cross_entropy_backward(dloss, x, w, y, lse)
+    _check(x, w, y, dloss, loss, lse, dx, dw)
+    dx, dw = dtp.linear_cross_entropy_backward(torch.zeros_like(dloss), x, w, y, lse)
+    assert (dx == 0).all() and (dw == 0).all()
