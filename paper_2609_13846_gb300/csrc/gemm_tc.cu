@@ -82,12 +82,12 @@ struct Args {
     uint32_t idesc;
     int direct_z;         // rows of Z are not on 16-byte boundaries
     int reset;            // this launch clears the status word
-    // kPairOf: product 0's tiles (of all parts) and the extra tiles of product 1 that the workers without a last one of
-    // product 0 take first; parts of k; rows of a part's sums
-    int n0, extra, parts;
-    int KB0, KB1;
+    // kPairOf: product 0's tiles (of all parts) at most; parts of k; its k blocks; rows of a part's sums
+    int n0, parts;
+    int KB0;
     int rows_z;
     uint32_t idesc0;
+    const int* live;      // kEpiProb and kPairOf: the rows that there are
     int* status;
     Epilogue epi;
 };
@@ -133,7 +133,7 @@ __device__ __forceinline__ void unpack_bf16(uint32_t v, float& a, float& b) {
 // tiles in flight share their rows and columns in L2.
 constexpr int kGroupM = 8;
 template <int JOBS>
-__device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, int& tn) {
+__device__ __forceinline__ void decode(const Args& p, int live_tiles_m, int u, int& job, int& tm, int& tn) {
     if constexpr (JOBS != kPairOf) job = 0;
     if constexpr (JOBS > kPairOf) {
         job = (u >= p.last[0]) + (u >= p.last[1]);
@@ -142,26 +142,52 @@ __device__ __forceinline__ void decode(const Args& p, int u, int& job, int& tm, 
     const unsigned per = static_cast<unsigned>(kGroupM) * p.tiles_n[job];
     const unsigned g = static_cast<unsigned>(u) / per, rest = static_cast<unsigned>(u) - g * per;
     const int m0 = static_cast<int>(g) * kGroupM;
-    const unsigned gm = p.tiles_m[job] - m0 < kGroupM ? p.tiles_m[job] - m0 : kGroupM;
+    const int tiles_m = live_tiles_m && job == 0 ? live_tiles_m : p.tiles_m[job];
+    const unsigned gm = tiles_m - m0 < kGroupM ? tiles_m - m0 : kGroupM;
     tn = static_cast<int>(rest / gm);
     tm = m0 + static_cast<int>(rest % gm);
+}
+
+// A tile of a pair's launch takes its k blocks, and no less than its epilogue: 3 us for 256 x 256 sums to bf16, 10 blocks.
+__host__ __device__ constexpr int64_t tile_blocks(int64_t blocks) { return blocks > 9 ? blocks + 1 : 10; }
+// Tiles of product 1 in the time of one of product 0's (of a part).
+__host__ __device__ constexpr int64_t extra_tiles(int64_t part_blocks, int64_t blocks1) {
+    return (tile_blocks(part_blocks) + tile_blocks(blocks1) / 2) / tile_blocks(blocks1);
+}
+
+// What a launch's tiles are where the number of rows is known on the device alone (kLive): tokens that do not count have been left out.
+struct Sizes { int rows, tiles_m, KB1, n0, extra, units; };
+template <bool kPair, int JOBS>
+__device__ __forceinline__ Sizes sizes_of(const Args& p) {
+    Sizes z{};
+    constexpr int rows = kPair ? 2 * BM : BM;
+    z.rows = *p.live;
+    z.tiles_m = (z.rows + rows - 1) / rows;
+    z.units = z.tiles_m * p.tiles_n[0];
+    if constexpr (JOBS == kPairOf) {
+        z.KB1 = z.rows / BK;
+        z.n0 = p.n0 ? z.units * p.parts : 0;
+        z.extra = static_cast<int>(extra_tiles(p.KB0 / p.parts, z.KB1));
+        z.units = z.n0 + p.units - p.n0;
+    }
+    return z;
 }
 
 // Two products of different K and operand orders in one launch: the long tiles first, in rounds, and the short
 // ones dealt so that the workers end together.  Worker w of `workers` takes its i-th tile; false: it has no more.
 struct PairUnit { int job, part, u; };
-__device__ __forceinline__ bool pair_unit(const Args& p, int w, int workers, int i, PairUnit& r) {
-    const int last = p.n0 % workers, mine = p.n0 / workers + (w < last);
+__device__ __forceinline__ bool pair_unit(const Args& p, const Sizes& z, int w, int workers, int i, PairUnit& r) {
+    const int last = z.n0 % workers, mine = z.n0 / workers + (w < last);
     if (i < mine) {
-        const int u = w + i * workers, tiles = p.tiles_m[0] * p.tiles_n[0];
+        const int u = w + i * workers, tiles = z.tiles_m * p.tiles_n[0];
         r.job = 0, r.part = u / tiles, r.u = u % tiles;
         return true;
     }
     const int k = i - mine, others = workers - last;           // those without a tile in the last round
     r.job = 1, r.part = 0;
-    if (last && w >= last) r.u = k < p.extra ? k * others + (w - last) : p.extra * others + (k - p.extra) * workers + w;
-    else r.u = (last ? p.extra * others : 0) + k * workers + w;
-    return r.u < p.units - p.n0;
+    if (last && w >= last) r.u = k < z.extra ? k * others + (w - last) : z.extra * others + (k - z.extra) * workers + w;
+    else r.u = (last ? z.extra * others : 0) + k * workers + w;
+    return r.u < z.units - z.n0;
 }
 
 __device__ __forceinline__ void st_shared_cluster_f32x4(uint32_t cluster_addr, float a, float b, float c, float d) {
@@ -202,19 +228,21 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     const int first = p.unit0 + static_cast<int>(blockIdx.x) / ctas, workers = static_cast<int>(gridDim.x) / ctas;
     const int part = kSplit ? static_cast<int>(cluster_rank >> 1) : 0;
     const int all_blocks = p.segments * p.KB;
+    constexpr bool kLive = KIND == kEpiProb || JOBS == kPairOf;
+    Sizes live{};         // set behind the wait below
     // the i-th tile of this worker
     auto next = [&](int i, int& job, int& tm, int& tn, int& part_z) {
         part_z = 0;
         if constexpr (JOBS == kPairOf) {
             PairUnit r;
-            if (!pair_unit(p, first, workers, i, r)) return false;
+            if (!pair_unit(p, live, first, workers, i, r)) return false;
             job = r.job, part_z = r.part;
-            decode<JOBS>(p, r.u, job, tm, tn);
+            decode<JOBS>(p, live.tiles_m, r.u, job, tm, tn);
             return true;
         } else {
             const int u = first + i * workers;
-            if (u >= p.units) return false;
-            decode<JOBS>(p, u, job, tm, tn);
+            if (u >= (kLive ? live.units : p.units)) return false;
+            decode<JOBS>(p, kLive ? live.tiles_m : 0, u, job, tm, tn);
             return true;
         }
     };
@@ -222,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     auto blocks_of = [&](int job, int part_z, int& b0, int& b1) {
         if constexpr (JOBS == kPairOf) {
             b0 = job ? 0 : static_cast<int>(static_cast<int64_t>(p.KB0) * part_z / p.parts);
-            b1 = job ? p.KB1 : static_cast<int>(static_cast<int64_t>(p.KB0) * (part_z + 1) / p.parts);
+            b1 = job ? live.KB1 : static_cast<int>(static_cast<int64_t>(p.KB0) * (part_z + 1) / p.parts);
         }
     };
     const int kb0_all = kSplit ? static_cast<int>(static_cast<int64_t>(all_blocks) * part / p.split) : 0;
@@ -262,6 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
     // An early launch works on other tiles than the one before it, which had itself waited: it waits at its end.
     if (!(kSplit && p.early)) grid_wait();
     grid_release();
+    if constexpr (kLive) live = sizes_of<kPair, JOBS>(p);
     asm volatile("fence.proxy.async;" ::: "memory");     // what was stored plainly is loaded by TMA
     // Clears the status of earlier calls.  A wait of this launch gives up two seconds after it began, long after
     // block 0, which starts first, has passed here.
@@ -469,10 +498,13 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             if (p.direct[job]) store_elements(static_cast<__nv_bfloat16*>(out), ldo, w, n, row0, false);
             else store_box(std::false_type(), &p.out[i], w, n, row0);
         };
+        [[maybe_unused]] const int live_tokens = KIND == kEpiProb ? *e.vocab.count : 0;
         [[maybe_unused]] const float unit = JOBS == kPairOf ? *e.unit : 1.0f;
         uint32_t unit_count = static_cast<uint32_t>(set);
         for (; next(static_cast<int>(unit_count), job, tm, tn, part_z); unit_count += 2) {
             if constexpr (JOBS > 1) M = p.M[job], N = p.N[job], ldo = p.ldo[job];
+            if constexpr (kLive)
+                if (job == 0) M = live.rows;
             const int row0 = (kPair ? 2 * tm + static_cast<int>(rank) : tm) * BM + quad * 32;
             const int64_t m = static_cast<int64_t>(row0) + lane;
             const uint32_t buf = unit_count & 1u;
@@ -507,13 +539,11 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
             int target = -1;
             float lse2 = INFINITY, grad = 0.0f;
             if constexpr (KIND == kEpiParts || KIND == kEpiProb) {
-                if (m < e.vocab.T) {
+                if (m < (KIND == kEpiProb ? static_cast<int64_t>(live_tokens) : e.vocab.T)) {
                     const int64_t y = e.vocab.targets[m];
                     if (e.vocab.live(y)) {
                         target = static_cast<int>(y) - e.vocab.v0;
                         if constexpr (KIND == kEpiProb) lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m] / *e.vocab.unit;
-                    } else if (KIND == kEpiProb && tn == 0 && half == 0 && e.vocab.bad(y)) {
-                        atomicCAS(p.status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
                     }
                 }
             }
@@ -857,6 +887,7 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     // bits 15 and 16: A and B stored with their rows contiguous
     a.idesc = idesc_bf16_f32(kPair ? 2 * BM : BM, BN) | (a.a_mn ? 1u << 15 : 0u) | (a.b_mn ? 1u << 16 : 0u);
     a.reset = reset;
+    a.live = p.live;
     a.status = status;
     a.epi = p.epi;
     auto kernel = gated ? gemm_tc_kernel<kPair, BN, kEpiGated, kSplit, 1> : gemm_tc_kernel<kPair, BN, kEpiLinear, kSplit, 1>;
@@ -891,20 +922,12 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
     return DTP_OK;
 }
 
-// A tile of a pair's launch takes its k blocks, and no less than its epilogue: 3 us for 256 x 256 sums to bf16, 10 blocks.
-static int64_t tile_blocks(int64_t blocks) { return blocks > 9 ? blocks + 1 : 10; }
-// Tiles of product 1 in the time of one of product 0's (of a part).
-static int64_t extra_tiles(int64_t part_blocks, int64_t blocks1) {
-    const int64_t c1 = tile_blocks(blocks1);
-    return (tile_blocks(part_blocks) + c1 / 2) / c1;
-}
-
 template <int BN>
 static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaStream_t stream) {
     using F = Form<true, BN>;
     Args a;
     a.segments = 1, a.KB = 0, a.a_mn = 0, a.b_mn = 1, a.unit0 = 0, a.split = 1, a.early = 0, a.reset = 0;
-    a.KB0 = (g.cols + BK - 1) / BK, a.KB1 = static_cast<int>((g.rows + BK - 1) / BK);
+    a.KB0 = (g.cols + BK - 1) / BK;
     a.parts = g.parts;
     a.status = status;
     const int64_t M[2] = {g.rows, g.cols};
@@ -921,7 +944,7 @@ static int launch_pair_form(const GradPair& g, int* status, int64_t pairs, cudaS
     if (units[0] + units[1] == 0) return DTP_OK;
     a.n0 = static_cast<int>(units[0]), a.units = static_cast<int>(units[0] + units[1]);
     a.rows_z = a.tiles_m[0] * 2 * BM;
-    a.extra = static_cast<int>(extra_tiles(a.KB0 / a.parts, a.KB1));
+    a.live = g.live;
     if (!map_operand(&a.a[0], by(g.dz, g.ldz, true), g.rows, g.cols, BM) ||
         !map_operand(&a.b[0], by(g.w, g.ldw, false), g.d, g.cols, BN / 2) ||
         !map_operand(&a.a[1], by(g.dz, g.ldz, false), g.cols, g.rows, BM) ||

@@ -203,6 +203,7 @@ struct Vocab {
     const int64_t* targets = nullptr;      // [M]
     int64_t ignore = 0;
     int64_t T = 0;                         // rows beyond it are padding
+    const int* count = nullptr;            // device: so are those beyond this
     int V = 0, v0 = 0;                     // the vocabulary, and the piece's first token
     Part* parts = nullptr;                 // [chunk][M]
     float* hit = nullptr;                  // [M] the target's logit
@@ -285,6 +286,7 @@ struct Product {
     int N = 0;
     int64_t K = 0;
     int64_t rows_a = 0;      // rows that A has, where more than M (bf16 only)
+    const int* live = nullptr;       // kEpiProb: device, the rows that there are, a multiple of 64 and at most M
     int parts = 1;           // fp32, kEpiLinear without anything beside the sums: ranges of k whose sums go to [parts][M, ldo] each
     Epilogue epi;
 };
@@ -292,11 +294,12 @@ struct Product {
 // The two products that a piece of the softmax's gradient takes part in, for one launch (bf16): dZ [rows, cols] at pitch ldz
 //     sum[part] (+)= dZ[:, part's columns] W[part's rows, :]  for `parts` ranges of the columns, [tiles of 256 rows, d] each
 //     dW = dZ^T X
-// rows is a multiple of 64 (the last ones zeros in X and in dZ).
+// rows is a multiple of 64, and so is *live, at most that and at least 64, the rows that there are (the last ones zeros in X and in dZ).
 struct GradPair {
     const void *dz, *x, *w;
     int64_t ldz, ldx, ldw;
     int64_t rows;
+    const int* live;
     int cols, d;
     int parts;
     int add;                 // to the sums, which hold those of earlier pieces

@@ -98,52 +98,116 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
     if (bad) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
 }
 
-// X at an aligned pitch in `rows` rows, with zeros in those beyond T and, where targets are given, in those of tokens that do not count:
-// whatever stands there must not reach dW.  The last block finds dZ's unit, the largest finite size of dloss among them, where it is wanted
-// (else 1): rounding dloss (p - onehot) to bf16 would round dloss of a mean, the same in all rows, and the error would not average out.
-template <typename E>
-__global__ void __launch_bounds__(256)
-live_rows_kernel(const E* X, int64_t T, int64_t rows, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V,
-                 const float* dloss, E* out, float* unit, int* status) {
-    __shared__ float red[8];
+// Which tokens count, for the backward pass (bf16): place[t] is token t's row among them, or -1, and what its row needs is put there; live[0]
+// is the rows that the products take, padded to 64 and at least that many, live[1] the tokens.  Tokens that do not count then cost
+// nothing, and whatever stands in their rows reaches nothing.  Also dZ's unit, the largest finite size of dloss among them (at least
+// 2^-126; else 1): rounding dloss (p - onehot) to bf16 would round dloss of a mean, the same in all rows, and the error would not average
+// out.  One block, 4096 tokens at a time.  compact 0: all tokens keep their rows, and the unit is 1.
+struct Compact {
+    int* place;
+    int* live;
+    int64_t* targets;
+    float *lse, *dloss, *unit;
+};
+constexpr int kIndexThreads = 1024;
+__global__ void __launch_bounds__(kIndexThreads)
+index_kernel(const int64_t* targets, const float* lse, const float* dloss, int64_t T, int64_t ignore, int V, int compact, const Compact to,
+             int* status) {
+    __shared__ int sums[2][kIndexThreads / 32];
+    __shared__ float tops[kIndexThreads / 32];
     grid_wait();
     grid_release();
-    if (targets && blockIdx.x == 0 && threadIdx.x == 0) *status = DTP_OK;
-    if (unit && blockIdx.x == gridDim.x - 1) {
-        float top = 0.0f;
-        if (dloss)
-#pragma unroll 8
-            for (int64_t t = threadIdx.x; t < T; t += 256) {
-                const int64_t y = targets[t];
-                const float g = fabsf(dloss[t]);
-                if (y != ignore && y >= 0 && y < V && isfinite(g)) top = fmaxf(top, g);
-            }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int base = 0, turn = 0;
+    float top = 0.0f;
+    bool bad = false;
+    for (int64_t t0 = 0; t0 < T; t0 += 4 * kIndexThreads, ++turn) {
+        const int64_t t = t0 + 4 * threadIdx.x;
+        int64_t y[4];
+        int count = 0;
+        bool live[4];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = top;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            for (int w = 1; w < 8; ++w) top = fmaxf(top, red[w]);
-            *unit = top >= 1.1754944e-38f ? top : 1.0f;
+        for (int j = 0; j < 4; ++j) {
+            y[j] = t + j < T ? targets[t + j] : ignore;
+            const bool in = y[j] >= 0 && y[j] < V;
+            bad |= y[j] != ignore && !in;
+            live[j] = t + j < T && (!compact || (y[j] != ignore && in));
+            count += live[j];
         }
-        if (gridDim.x > 1) return;
+        int before = count;          // of the lanes up to this one
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+            if (lane >= o) before += v;
+        }
+        if (lane == 31) sums[turn & 1][warp] = before;
+        __syncthreads();
+        const int mine = sums[turn & 1][lane];
+        int warps = mine;            // of the warps up to `lane`
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, warps, o);
+            if (lane >= o) warps += v;
+        }
+        const int all = __shfl_sync(0xFFFFFFFFu, warps, 31), earlier = __shfl_sync(0xFFFFFFFFu, warps - mine, warp);
+        int at = base + earlier + before - count;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (t + j >= T) continue;
+            to.place[t + j] = live[j] ? at : -1;
+            if (!live[j]) continue;
+            const float g = dloss[t + j];
+            to.targets[at] = y[j], to.lse[at] = lse[t + j], to.dloss[at] = g;
+            if (isfinite(g)) top = fmaxf(top, fabsf(g));
+            ++at;
+        }
+        base += all;
     }
-    const int64_t blocks = unit && gridDim.x > 1 ? gridDim.x - 1 : gridDim.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (lane == 0) tops[warp] = top;
+    const bool any = __syncthreads_or(bad);
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kIndexThreads / 32; ++w) top = fmaxf(top, tops[w]);
+        *to.unit = compact && top >= 1.1754944e-38f ? top : 1.0f;
+        const int rows = (base + 63) / 64 * 64;
+        to.live[0] = rows > 64 ? rows : 64;
+        to.live[1] = base;
+        *status = any ? static_cast<int>(DTP_ERR_ARG) : static_cast<int>(DTP_OK);
+    }
+}
+
+// X's rows at an aligned pitch.  With `place` at their places, and zeros in the rows behind the last; rows that have a place but do not count
+// are zeros too.  Without, zeros in the rows from T to `rows`.
+template <typename E>
+__global__ void __launch_bounds__(256)
+place_rows_kernel(const E* X, int64_t T, int64_t rows, int d, int64_t pitch, const int64_t* targets, int64_t ignore, int V,
+                  const int* place, const int* live, E* out) {
+    grid_wait();
+    grid_release();
     constexpr int kPer = 16 / sizeof(E);
     const bool wide = d % kPer == 0 && pitch % kPer == 0 && (reinterpret_cast<uintptr_t>(X) & 15) == 0;
-    for (int64_t t = blockIdx.x; t < rows; t += blocks) {
-        bool live = t < T;
-        if (live && targets) {
-            const int64_t y = targets[t];
-            live = y != ignore && y >= 0 && y < V;
-        }
+    auto row = [&](const E* from, E* to) {            // from NULL: zeros
         if (wide) {
+#pragma unroll 4
             for (int i = threadIdx.x; i < d / kPer; i += 256)
-                reinterpret_cast<uint4*>(out + t * pitch)[i] = live ? reinterpret_cast<const uint4*>(X + t * d)[i] : make_uint4(0, 0, 0, 0);
+                reinterpret_cast<uint4*>(to)[i] = from ? reinterpret_cast<const uint4*>(from)[i] : make_uint4(0, 0, 0, 0);
         } else {
-            for (int i = threadIdx.x; i < d; i += 256) out[t * pitch + i] = live ? X[t * d + i] : from_f32<E>(0.0f);
+#pragma unroll 4
+            for (int i = threadIdx.x; i < d; i += 256) to[i] = from ? from[i] : from_f32<E>(0.0f);
         }
+    };
+    auto counts = [&](int64_t t) {
+        if (!targets) return true;
+        const int64_t y = targets[t];
+        return y != ignore && y >= 0 && y < V;
+    };
+    const int64_t held = live ? live[1] : T, all = live ? live[0] : rows;
+    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+        const int64_t at = place ? place[t] : t;
+        if (at >= 0) row(counts(t) ? X + t * d : nullptr, out + at * pitch);
     }
+    for (int64_t t = held + blockIdx.x; t < all; t += gridDim.x) row(nullptr, out + t * pitch);
 }
 
 // dZ of Z [T, cols], columns v0 .. of the vocabulary; a block takes kChunk columns of a token.  dZ may be Z.
@@ -180,26 +244,48 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* sums, int p
     }
 }
 
-// dX from its sums, in dZ's unit: `parts` of them, `stride` values apart
-__global__ void __launch_bounds__(256) round_kernel(const float* sum, int parts, int64_t stride, int64_t n, const float* unit, __nv_bfloat16* out) {
+// dX from its sums, in dZ's unit: `parts` of them, `stride` values apart, each token's at its place; zeros for those without one.  A warp
+// takes 512 columns of a token.
+__global__ void __launch_bounds__(256)
+round_kernel(const float* sum, int parts, int64_t stride, int64_t T, int d, const int* place, const float* unit, __nv_bfloat16* out) {
     grid_wait();
     grid_release();
     const float u = *unit;
-    const int64_t words = n / 4;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < words; i += gridDim.x * 256ll) {
-        float4 v = reinterpret_cast<const float4*>(sum)[i];
-        for (int p = 1; p < parts; ++p) {
-            const float4 w = reinterpret_cast<const float4*>(sum + p * stride)[i];
-            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+    const int pieces = (d + 511) / 512, lane = threadIdx.x & 31;
+    const bool wide = d % 4 == 0;          // the binding's and the C ABI's tensors start on 16 bytes
+    for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < T * pieces; i += gridDim.x * 8ll) {
+        const int64_t t = i / pieces;
+        const int c0 = static_cast<int>(i - t * pieces) * 512, at = place[t];
+        const float* from = sum + static_cast<int64_t>(at) * d;
+        __nv_bfloat16* to = out + t * d;
+        if (wide) {
+            float4 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p = 0; p < (at >= 0 ? parts : 0); ++p) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int c = c0 + 128 * q + 4 * lane;
+                    if (c >= d) continue;
+                    const float4 w = *reinterpret_cast<const float4*>(from + p * stride + c);
+                    v[q].x += w.x, v[q].y += w.y, v[q].z += w.z, v[q].w += w.w;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = c0 + 128 * q + 4 * lane;
+                if (c >= d) continue;
+                const __nv_bfloat162 a = __floats2bfloat162_rn(u * v[q].x, u * v[q].y), b = __floats2bfloat162_rn(u * v[q].z, u * v[q].w);
+                *reinterpret_cast<uint2*>(to + c) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+            }
+        } else {
+            const int c1 = c0 + 512 < d ? c0 + 512 : d;
+            for (int c = c0 + lane; c < c1; c += 32) {
+                float v = 0.0f;
+                for (int p = 0; p < (at >= 0 ? parts : 0); ++p) v += from[p * stride + c];
+                to[c] = __float2bfloat16_rn(u * v);
+            }
         }
-        const __nv_bfloat162 a = __floats2bfloat162_rn(u * v.x, u * v.y), b = __floats2bfloat162_rn(u * v.z, u * v.w);
-        reinterpret_cast<uint2*>(out)[i] = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-    }
-    const int64_t rest = 4 * words + threadIdx.x;
-    if (blockIdx.x == 0 && rest < n) {
-        float v = sum[rest];
-        for (int p = 1; p < parts; ++p) v += sum[p * stride + rest];
-        out[rest] = __float2bfloat16_rn(u * v);
     }
 }
 
@@ -289,7 +375,8 @@ static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && 
 struct BackwardSpace {
     void* dz;            // in fp32 the logits before
     void* x;
-    float *sum, *runs, *unit;
+    float *sum, *runs;
+    Compact compact;     // bf16
 };
 static int64_t sum_rows(int64_t T) { return (padded_rows(T) + 255) / 256 * 256; }
 static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtype, const Pieces& pieces) {
@@ -300,7 +387,15 @@ static BackwardSpace carve_backward(Carver& c, int64_t T, int d, int V, int dtyp
     const int64_t summed = dtype == DTP_BF16 ? sum_rows(T) : pieces.parts > 1 || T <= kFew ? T : 0;
     s.sum = static_cast<float*>(c.take(static_cast<size_t>(summed) * pieces.parts * d * sizeof(float)));
     s.runs = static_cast<float*>(c.take(runs_bytes(rows, pieces.cols, d)));
-    s.unit = static_cast<float*>(c.take(sizeof(float)));
+    if (dtype == DTP_BF16) {
+        const size_t n = static_cast<size_t>(T);
+        s.compact.place = static_cast<int*>(c.take(n * sizeof(int)));
+        s.compact.live = static_cast<int*>(c.take(2 * sizeof(int)));
+        s.compact.targets = static_cast<int64_t*>(c.take(n * sizeof(int64_t)));
+        s.compact.lse = static_cast<float*>(c.take(n * sizeof(float)));
+        s.compact.dloss = static_cast<float*>(c.take(n * sizeof(float)));
+        s.compact.unit = static_cast<float*>(c.take(sizeof(float)));
+    }
     return s;
 }
 
@@ -357,9 +452,9 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
         rows_x = padded_rows(T);
         void* to = c.take(static_cast<size_t>(rows_x) * padded(d) * elem(dtype));
         x = Rows{to, padded(d)};
-        st = launch_after(live_rows_kernel<__nv_bfloat16>, grid_of(rows_x), stream, static_cast<const __nv_bfloat16*>(X), T, rows_x, d,
-                          x.ld, static_cast<const int64_t*>(nullptr), int64_t(0), 0, static_cast<const float*>(nullptr),
-                          static_cast<__nv_bfloat16*>(to), static_cast<float*>(nullptr), status);
+        st = launch_after(place_rows_kernel<__nv_bfloat16>, grid_of(rows_x), stream, static_cast<const __nv_bfloat16*>(X), T, rows_x, d,
+                          x.ld, static_cast<const int64_t*>(nullptr), int64_t(0), 0, static_cast<const int*>(nullptr),
+                          static_cast<const int*>(nullptr), static_cast<__nv_bfloat16*>(to));
     }
     const int64_t most = forward_rows(T, V, dtype);
     ForwardSpace s = carve_forward(c, most, V, dtype);
@@ -409,11 +504,20 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
     const int64_t rows = kBf16 ? padded_rows(T) : T;
     const Rows x{s.x, kBf16 || T > kFew ? padded(d) : d};
     Vocab e;
-    e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss, e.unit = s.unit;
-    const bool in_runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs, which know no unit
+    e.targets = targets, e.ignore = ignore, e.T = T, e.V = V, e.lse = lse, e.dloss = dloss;
+    const bool in_runs = rows > kRun && dW;          // dW's sums over so many tokens are made in runs of a known length
+    const Compact& k = s.compact;
+    if constexpr (kBf16) {
+        if (st == DTP_OK)
+            st = launch_blocks(index_kernel, 1, kIndexThreads, stream, targets, lse, dloss, T, ignore, V, static_cast<int>(!in_runs), k, status);
+        e.targets = k.targets, e.lse = k.lse, e.dloss = k.dloss, e.unit = k.unit, e.count = k.live + 1;
+    } else if (st == DTP_OK) {
+        DTP_CUDA_TRY(cudaMemsetAsync(status, 0, sizeof(int), stream));
+    }
     if (st == DTP_OK)
-        st = launch_after(live_rows_kernel<E>, grid_of(rows) + 1, stream, static_cast<const E*>(X), T, rows, d, x.ld, targets, ignore, V,
-                          kBf16 && !in_runs ? dloss : nullptr, static_cast<E*>(s.x), s.unit, status);
+        st = launch_after(place_rows_kernel<E>, grid_of(rows), stream, static_cast<const E*>(X), T, rows, d, x.ld, targets, ignore, V,
+                          static_cast<const int*>(kBf16 ? k.place : nullptr), static_cast<const int*>(kBf16 ? k.live : nullptr),
+                          static_cast<E*>(s.x));
     call.fresh = false;
     for (int v0 = 0; st == DTP_OK && v0 < V; v0 += pieces.cols) {
         const int cols = V - v0 < pieces.cols ? V - v0 : pieces.cols;
@@ -424,9 +528,9 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
         Product p = logits(x, rows, 0, w, rows, d, v0, cols, dtype);
         p.epi.out = s.dz, p.epi.ldo = ldz;
         if constexpr (kBf16) {
-            p.epi.kind = kEpiProb, p.epi.vocab = e;
+            p.epi.kind = kEpiProb, p.epi.vocab = e, p.live = k.live;
             st = gtc::launch(p, status, 0, stream);
-            GradPair g{s.dz, s.x, w_at, ldz, x.ld, w.ld, rows, cols, d, pieces.parts, v0 > 0, s.unit, dX ? s.sum : nullptr,
+            GradPair g{s.dz, s.x, w_at, ldz, x.ld, w.ld, rows, k.live, cols, d, pieces.parts, v0 > 0, k.unit, dX ? s.sum : nullptr,
                        in_runs ? nullptr : dw_at};
             if (g.parts > (cols + 63) / 64) g.parts = (cols + 63) / 64;       // a short last piece leaves the others' sums as they are
             if (st == DTP_OK) st = gtc::launch_pair(g, status, stream);
@@ -463,8 +567,9 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
         }
     }
     if (kBf16 && st == DTP_OK && dX)
-        st = launch_after(round_kernel, grid_of((T * d / 4 + 255) / 256 + 1), stream, static_cast<const float*>(s.sum), pieces.parts,
-                          sum_rows(T) * d, T * d, static_cast<const float*>(s.unit), static_cast<__nv_bfloat16*>(dX));
+        st = launch_after(round_kernel, grid_of((T * ((d + 511) / 512) + 7) / 8), stream, static_cast<const float*>(s.sum), pieces.parts,
+                          sum_rows(T) * d, T, d, static_cast<const int*>(k.place), static_cast<const float*>(k.unit),
+                          static_cast<__nv_bfloat16*>(dX));
     return st;
 }
 
