@@ -15,6 +15,9 @@ times, with nothing else in between, so that an ncu capture with
     python -m paper_2609_13846_gb300.profile_case --what ffn_train --workload qwen3_0.6b_layer
     python -m paper_2609_13846_gb300.profile_case --what linear_train --workload qwen3_0.6b_layer --T 8192
     python -m paper_2609_13846_gb300.profile_case --what clip --workload qwen3_0.6b_model --layers 4
+    python -m paper_2609_13846_gb300.profile_case --what norm_train --workload llama3.1_8b_layer --T 16384
+    python -m paper_2609_13846_gb300.profile_case --what loss_train --workload qwen3_0.6b_layer --T 4096 --vocabulary 65536
+    python -m paper_2609_13846_gb300.profile_case --what adamw --workload danube3_500m_model --layers 3 --bits 8
 """
 from __future__ import annotations
 
@@ -28,7 +31,8 @@ from . import ablation, dtp, synth
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--what", choices=["affinity", "search", "producer", "gather", "apply", "add",
-                                           "ffn", "ffn_train", "linear_train", "clip"], default="affinity")
+                                           "ffn", "ffn_train", "linear_train", "clip",
+                                           "norm_train", "loss_train", "adamw"], default="affinity")
     ap.add_argument("--qrow", type=int, default=1, help="producer: query heads per output row")
     ap.add_argument("--workload", default="qwen3_0.6b_layer")
     ap.add_argument("--T", type=int, default=None, help="token count (default: the workload's)")
@@ -36,6 +40,8 @@ def main():
     ap.add_argument("--launches", type=int, default=2)
     ap.add_argument("--D", type=int, default=None)
     ap.add_argument("--layers", type=int, default=1)
+    ap.add_argument("--vocabulary", type=int, default=65536, help="loss_train: tokens of the vocabulary")
+    ap.add_argument("--bits", type=int, default=32, help="adamw: bits of the states")
     args = ap.parse_args()
     w = synth.WORKLOADS[args.workload]
     dev = torch.device("cuda:0")
@@ -89,6 +95,41 @@ def main():
             n = dtp.clip_grad_norm(g, 1.0, out=out)
         torch.cuda.synchronize()
         print(f"clip {len(g)} tensors, {sum(t.numel() for t in g)} elements: {args.launches} launches, norm {float(n):.6e}")
+    elif args.what == "norm_train":
+        T = args.T or w.T
+        x, dy, dres = (torch.randn((T, w.d), device=dev).to(torch.bfloat16) for _ in range(3))
+        gamma = torch.ones(w.d, device=dev)
+        ws = dtp.rms_norm_workspace(T, w.d, torch.bfloat16, dev)
+        torch.cuda.synchronize()
+        for _ in range(args.launches):
+            _, rms = dtp.rms_norm(x, gamma)
+            dx, _ = dtp.rms_norm_backward(dy, x, gamma, rms, dresidual=dres, workspace=ws)
+        torch.cuda.synchronize()
+        print(f"norm_train {args.workload} T={T}: {args.launches} launches, dX sum {float(dx.double().sum()):.6e}")
+    elif args.what == "loss_train":
+        T, V = args.T or w.T, args.vocabulary
+        x = torch.randn((T, w.d), device=dev).to(torch.bfloat16)
+        W = (torch.randn((V, w.d), device=dev) * (2.0 / w.d ** 0.5)).to(torch.bfloat16)
+        y = torch.randint(0, V, (T,), device=dev)
+        dloss = torch.full((T,), 1.0 / T, device=dev)
+        ws = dtp.linear_cross_entropy_workspace(T, w.d, V, torch.bfloat16, dev, backward=True)
+        torch.cuda.synchronize()
+        for _ in range(args.launches):
+            loss, lse = dtp.linear_cross_entropy(x, W, y, workspace=ws)
+            dtp.linear_cross_entropy_backward(dloss, x, W, y, lse, workspace=ws)
+        torch.cuda.synchronize()
+        print(f"loss_train {args.workload} T={T} V={V}: {args.launches} launches, mean loss {float(loss.mean()):.6f}")
+    elif args.what == "adamw":
+        W = synth.make_dense_weights(args.layers, w.d, w.G * w.q_per_group, w.G, w.head_dim, w.N, w.seed, device=dev)
+        g = [t for v in W.values() for t in v]
+        p, copies = [t.float() for t in g], [torch.empty_like(t) for t in g]
+        state, ws = dtp.adamw_state(p, bits=args.bits), dtp.adamw_workspace(p)
+        torch.cuda.synchronize()
+        for _ in range(args.launches):
+            dtp.adamw_step(p, g, state, lr=1e-4, copies=copies, workspace=ws)
+        torch.cuda.synchronize()
+        print(f"adamw {len(g)} tensors, {sum(t.numel() for t in g)} elements, {args.bits} bits: {args.launches} launches, "
+              f"step {int(state['step'])}")
     elif args.what == "producer":
         T = args.T or w.T
         P = synth.make_attention_inputs(T, w.d, w.G * w.q_per_group, w.head_dim, w.seed, device=dev)
