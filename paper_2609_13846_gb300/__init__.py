@@ -11,7 +11,9 @@ Sharding for Delayed Tensor Parallelism" (arXiv 2609.13846), Sec. 3:
 
 Beside them are the layers that a layout permutes, run forward and backward
 (Sec. 4): a linear layer with its epilogue, the gated feed-forward block, and
-gradient clipping; :mod:`paper_2609_13846_gb300.distill` runs them together.
+gradient clipping; and the rest of a training step: the RMS norm, softmax cross
+entropy over the vocabulary, and the AdamW update.
+:mod:`paper_2609_13846_gb300.distill` runs them together.
 
 All of it lives in the C-ABI library ``libdtp.so`` (declared in ``include/dtp.h``);
 :mod:`paper_2609_13846_gb300.dtp` is the thin ctypes binding.  Import of the

@@ -16,6 +16,10 @@
 // fraction of the step that it has gone, by a hash of the element's index and the step's number, and is right on
 // average.  Parameters in bf16, whose updates are as small, are rounded alike.  What the states will be is
 // computed without contracted operations, so that the same inputs give the same codes wherever they are computed in fp32.
+//
+// fp32 parameters, bf16 gradients and copies, 415M elements: 32 bits 1.78 to 1.83 ms (6.4 TB/s of 28 bytes each); 8 bits 1.26 ms
+// (5.3 TB/s of 16), bound by 89 instructions an element, issued in 70% of the cycles.  bf16 parameters in 301 tensors off their words,
+// 60M: 0.24 ms.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
