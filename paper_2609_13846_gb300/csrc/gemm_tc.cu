@@ -710,7 +710,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                         sum *= exp2_fast(top - most);
                         top = most;
                     }
-                    const float shift = top == -INFINITY ? 0.0f : top;      // of a row of -inf alone: its sum is 0
+                    const float shift = isinf(top) ? 0.0f : top;      // a row of -inf alone sums to 0, one with an infinity to it
                     float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                     for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast(fmaf(v[i], kLog2e, -shift));

@@ -277,3 +277,23 @@ def test_betas_of_zero_and_negative_rates(betas):
     zero = torch.zeros(300, device=DEV)
     want, _, _, size = _exact(before, grads[0], zero, zero, 1, **hyper)
     assert ((params[0].double() - want).abs() <= 16 * ROUND * (size + 1e-3)).all()
+
+
+def test_offsets_beyond_32_bits():
+    """A tensor of more than 2^32 elements, its ends set: they move as those of small tensors do, and nothing between."""
+    n, k = (1 << 32) + 300, 700
+    p, g = (torch.zeros(n, dtype=BF16, device=DEV) for _ in range(2))
+    state = dtp.adamw_state([p], bits=8)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    ends = [torch.randn(k, generator=gen, device=DEV).to(BF16) for _ in range(4)]
+    p[:k], p[-k:], g[:k], g[-k:] = ends
+    dtp.adamw_step([p], [g], state, **HYPER)
+    for before, grad, at in ((ends[0], ends[2], slice(0, k)), (ends[1], ends[3], slice(n - k, n))):
+        zero = torch.zeros(k, device=DEV)
+        want, em, _, size = _exact(before, grad, zero, zero, 1, **HYPER)
+        _check_params(p[at], want, size, before)
+        held = state["m"][0][at].float() * state["m_scale"][0].repeat_interleave(256)[: n][at] if at.start == 0 else None
+        if held is not None:
+            assert ((held.double() - em).abs() <= em.abs() / 8 + 2.0 ** -9 / 448 * em.abs().max()).all()
+    assert int(torch.count_nonzero(p[k:-k].view(torch.int16).view(-1))) == 0
+    assert float(state["m_scale"][0][-1]) > 0 and float(state["v_scale"][0][1000]) == 0

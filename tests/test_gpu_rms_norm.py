@@ -179,3 +179,22 @@ def test_gradient_in_place_of_an_input(d, over):
     call(dy, dres, alone, None)
     call(dy, dres, None, galone)
     assert torch.equal(alone, want) and torch.equal(galone, wgamma)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements: the last rows are those of a call on them alone, bit for bit."""
+    T, d = 270_000, 8192
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.empty((T, d), dtype=torch.bfloat16, device=DEV)
+    for t in range(0, T, 30_000):
+        x[t:t + 30_000] = torch.randn((30_000, d), generator=g, device=DEV)
+    assert x.numel() > 1 << 31
+    gamma = 1.0 + 0.1 * torch.randn(d, generator=g, device=DEV)
+    y, rms = dtp.rms_norm(x, gamma)
+    last, lrms = dtp.rms_norm(x[-5:].contiguous(), gamma)
+    assert torch.equal(y[-5:], last) and torch.equal(rms[-5:], lrms)
+    dx, dgamma = dtp.rms_norm_backward(y, x, gamma, rms)
+    ldx, _ = dtp.rms_norm_backward(last, x[-5:].contiguous(), gamma, lrms)
+    assert torch.equal(dx[-5:], ldx)
+    want = sum((y[t:t + 30_000].double() * x[t:t + 30_000].double() / rms[t:t + 30_000, None].double()).sum(0) for t in range(0, T, 30_000))
+    assert ((dgamma.double() - want).abs() <= 600 * ROUND * want.abs()).all()       # terms of one sign

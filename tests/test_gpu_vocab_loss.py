@@ -273,3 +273,56 @@ def test_gradients_of_any_size(scale):
     _check(x, w, y, dloss, loss, lse, dx, dw)
     dx, dw = dtp.linear_cross_entropy_backward(torch.zeros_like(dloss), x, w, y, lse)
     assert (dx == 0).all() and (dw == 0).all()
+
+
+@pytest.mark.parametrize("T,dtype", [(40, torch.bfloat16), (300, torch.bfloat16), (20, torch.float32), (70, torch.float32)])
+def test_infinite_logits(T, dtype):
+    """A logit of infinity: lse and the other tokens' loss are infinite, its own loss is no number; a vocabulary of -inf but for
+    one token has that token's logit as lse; a NaN stays in its row."""
+    x, w, y, _ = _inputs(T, 64, 500, dtype)
+    x = x.abs()
+    x[3, 5] = float("nan")
+    y[:] = 7
+    y[0] = 100
+    w[100] = w[100].abs() + 0.1
+    w[100, 0] = float("inf")
+    x[:, 0] = 1.0
+    loss, lse = dtp.linear_cross_entropy(x, w, y)
+    others = torch.ones(T, dtype=torch.bool, device=DEV)
+    others[3] = False
+    assert torch.isinf(lse[others]).all() and (lse[others] > 0).all() and torch.isnan(lse[3])
+    assert torch.isnan(loss[0]) and torch.isinf(loss[1]) and torch.isnan(loss[3])
+    w[:, 0] = float("-inf")
+    w[7, 0] = 0.0
+    loss, lse = dtp.linear_cross_entropy(x, w, y)
+    z = (x.double() * w[7].double()).sum(1)
+    far = others.clone()
+    far[0] = False
+    assert ((lse[far].double() - z[far]).abs() <= 1e-4).all() and (loss[far].abs() <= 1e-4).all() and torch.isinf(loss[0])
+
+
+def test_weights_beyond_32_bits():
+    """A vocabulary whose weights have more than 2^31 elements: its last tokens are read, and written, where they are."""
+    T, d, V = 70, 2304, 1 << 20
+    g = torch.Generator(device=DEV).manual_seed(3)
+    x = torch.randn((T, d), generator=g, device=DEV).to(torch.bfloat16)
+    w = torch.empty((V, d), dtype=torch.bfloat16, device=DEV)
+    for v in range(0, V, 1 << 17):
+        w[v:v + (1 << 17)] = torch.randn((1 << 17, d), generator=g, device=DEV) / 48.0
+    assert w.numel() > 1 << 31
+    y = torch.randint(V - 1000, V, (T,), generator=g, device=DEV)
+    z = torch.cat([x.double() @ w[v:v + (1 << 16)].double().t() for v in range(0, V, 1 << 16)], 1)
+    L = torch.logsumexp(z, 1)
+    loss, lse = dtp.linear_cross_entropy(x, w, y, check=True)
+    assert ((lse.double() - L).abs() <= 1e-4).all()
+    assert ((loss.double() - (L - z.gather(1, y[:, None])[:, 0])).abs() <= 2e-4).all()
+    dloss = torch.full((T,), 1.0 / T, device=DEV)
+    dx, dw = dtp.linear_cross_entropy_backward(dloss, x, w, y, lse, check=True)
+    dz = torch.exp(z - L[:, None])
+    dz.scatter_add_(1, y[:, None], -torch.ones_like(L)[:, None])
+    dz /= T
+    for rows in (slice(0, 1000), slice(V // 2 - 500, V // 2 + 500), slice(V - 1000, V)):
+        ref = dz[:, rows].t() @ x.double()
+        assert (dw[rows].double() - ref).norm() <= 4e-3 * ref.norm()
+    ref = sum(dz[:, v:v + (1 << 16)] @ w[v:v + (1 << 16)].double() for v in range(0, V, 1 << 16))
+    assert (dx.double() - ref).norm() <= 4e-3 * ref.norm()
