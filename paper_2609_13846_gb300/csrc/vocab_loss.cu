@@ -10,7 +10,7 @@
 // pieces in fp32.
 // The price of not keeping the logits is their product again: 8 T d V operations a training step and not 6.  8192 x 131072 of 1024, a
 // tenth of the tokens without a target: 5.0 to 5.2 ms, at the power cap; 4096 x 65536 of 4096 4.8 to 4.9.  One token through 131072 x
-// 1024: 51 us, of which 44 stream W.
+// 1024: 50 us, of which 44 stream W.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -294,8 +294,7 @@ round_kernel(const float* sum, int parts, int64_t stride, int64_t T, int d, cons
 
 static int64_t grid_of(int64_t blocks) { return blocks < 8192 ? blocks : 8192; }
 
-// bf16: a product's epilogue takes the softmax, and two launches a piece make the gradients.  Rows of tokens are padded to 64: a
-// tensor that ends within the first 64 rows of a tile is loaded at half the rate (131072 x 1024 for 63 tokens: 65 us, for 64: 43).
+// bf16: a product's epilogue takes the softmax, and two launches a piece make the gradients, of rows padded to 64, the products' k block.
 constexpr int64_t kRowPad = 64;
 static int64_t padded_rows(int64_t T) { return (T + kRowPad - 1) / kRowPad * kRowPad; }
 
@@ -372,9 +371,8 @@ static ForwardSpace carve_forward(Carver& c, int64_t rows, int V, int dtype) {
     s.hit = static_cast<float*>(c.take(static_cast<size_t>(rows) * sizeof(float)));
     return s;
 }
-// whether the forward pass copies X: to an aligned pitch, or to whole groups of rows (from 257 tokens on the
-// copy costs more than the last tile's rate)
-static bool copies_x(int64_t T, int d, int dtype) { return dtype == DTP_BF16 && (d % 8 != 0 || (T % kRowPad != 0 && T < 256)); }
+// whether the forward pass copies X to an aligned pitch
+static bool copies_x(int d, int dtype) { return repitch_bytes(1, d, dtype) > 0; }
 struct BackwardSpace {
     void* dz;            // in fp32 the logits before
     void* x;
@@ -407,7 +405,7 @@ size_t loss_workspace_bytes(int64_t T, int d, int V, int dtype, int backward) {
     Carver f(nullptr);
     f.take(repitch_bytes(V, d, dtype));
     Carver b = f;
-    if (copies_x(T, d, dtype)) f.take(static_cast<size_t>(padded_rows(T)) * padded(d) * elem(dtype));
+    if (copies_x(d, dtype)) f.take(static_cast<size_t>(padded_rows(T)) * padded(d) * elem(dtype));
     const int64_t rows = forward_rows(T, V, dtype);
     carve_forward(f, rows, V, dtype);
     if (T % rows) carve_forward(f, T % rows, V, dtype);
@@ -451,7 +449,7 @@ int loss_forward(const void* X, const void* W, const int64_t* targets, int64_t T
     int64_t rows_x = T;
     int st = aligned_rows(W, V, d, dtype, c, stream, &w);
     int* status = static_cast<int*>(workspace);
-    if (st == DTP_OK && copies_x(T, d, dtype)) {
+    if (st == DTP_OK && copies_x(d, dtype)) {
         rows_x = padded_rows(T);
         void* to = c.take(static_cast<size_t>(rows_x) * padded(d) * elem(dtype));
         x = Rows{to, padded(d)};
