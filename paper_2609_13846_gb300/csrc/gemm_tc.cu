@@ -605,25 +605,30 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                             if (n + 16 * q < N) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * q + i]);
-                                const int y = JOBS == kPairOf ? part_z * p.rows_z + row0 : row0;
-                                if (p.direct_z) {
-                                    store_elements(e.Z + static_cast<int64_t>(y - row0) * N, static_cast<int64_t>(N), w, n + 16 * q,
-                                                   row0, e.add != 0);
-                                } else if (e.add) {
-                                    stage_box(w);
-                                    fence_async_smem();
-                                    __syncwarp();
-                                    if (lane == 0) {
-                                        tma_add_2d(&p.z, smem_u32(stg), n + 16 * q, y);
-                                        bulk_commit();
+                                if constexpr (JOBS == kPairOf) {
+                                    const int y = part_z * p.rows_z + row0;
+                                    if (p.direct_z) {
+                                        store_elements(e.Z + static_cast<int64_t>(y - row0) * N, static_cast<int64_t>(N), w, n + 16 * q,
+                                                       row0, e.add != 0);
+                                    } else if (e.add) {
+                                        stage_box(w);
+                                        fence_async_smem();
+                                        __syncwarp();
+                                        if (lane == 0) {
+                                            tma_add_2d(&p.z, smem_u32(stg), n + 16 * q, y);
+                                            bulk_commit();
+                                        }
+                                    } else {
+                                        store_box(std::false_type(), &p.z, w, n + 16 * q, y);
                                     }
                                 } else {
-                                    store_box(std::bool_constant<JOBS != kPairOf>(), &p.z, w, n + 16 * q, y);
+                                    if (p.direct_z) store_elements(e.Z, static_cast<int64_t>(N), w, n + 16 * q, row0, false);
+                                    else store_box(std::true_type(), &p.z, w, n + 16 * q, row0);
                                 }
                             }
                         }
                     }
-                    if (JOBS == kPairOf ? job == 0 : !e.out) continue;
+                    if (JOBS == kPairOf && job == 0) continue;
                     if constexpr (JOBS == kPairOf) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] *= unit;
@@ -870,7 +875,7 @@ static int launch_form(const Product& p, int* status, int reset, int split, int 
         a.N[j] = j > 0 ? x.N : p.N;
         a.ldo[j] = j > 0 ? x.ldo : p.epi.ldo;
         a.dst[j] = j > 0 ? x.out : p.epi.out;
-        a.direct[j] = (a.ldo[j] & 7) != 0 || !a.dst[j];
+        a.direct[j] = (a.ldo[j] & 7) != 0 || p.epi.kind == kEpiParts;        // which has no output to map
         if (!a.direct[j] && !map_2d(&a.out[j], a.dst[j], a.N[j], a.M[j], a.ldo[j], 32, 32, CU_TENSOR_MAP_SWIZZLE_64B))
             return DTP_ERR_CUDA;
         a.tiles_m[j] = static_cast<int>((a.M[j] + rows - 1) / rows);

@@ -218,12 +218,12 @@ struct Epilogue {
     int act = DTP_ACT_NONE;
     const void* bias = nullptr;       // [N]
     const void* residual = nullptr;   // [M, ldo]
-    void* out = nullptr;              // [M, ldo]; kEpiLinear: NULL where Z alone is wanted
+    void* out = nullptr;              // [M, ldo]
     void* out2 = nullptr;
     int64_t ldo = 0;
     float* Z = nullptr;               // [M, N]
-    int add = 0;                      // kEpiLinear, bf16 operands: Z += instead, and no out
-    const float* unit = nullptr;      // GradPair's
+    int add = 0;                      // GradPair's: Z, the sums, +=
+    const float* unit = nullptr;
     Vocab vocab;
     float* pre = nullptr;
     int64_t M = 0;
@@ -240,7 +240,6 @@ __device__ __forceinline__ void epilogue_element(const Epilogue& e, int64_t m, i
         float z = a0;
         if (e.bias) z += to_f32(reinterpret_cast<const E*>(e.bias)[n]);
         if (e.Z) e.Z[m * e.N + n] = z;
-        if (!out) return;
         float y = act_value<kFast>(e.act, z);
         if (e.residual) y += to_f32(reinterpret_cast<const E*>(e.residual)[at]);
         out[at] = from_f32<E>(y);
