@@ -23,7 +23,10 @@ namespace dtp {
 namespace layer {
 
 constexpr int kChunk = 8192;                         // columns of a partial sum
-constexpr size_t kPieceBytes = size_t(256) << 20;    // of a piece of the logits
+constexpr size_t kPieceBytes = size_t(256) << 20;    // of a piece of the logits, or of a run's parts
+// of a piece of dZ in bf16 (8192 x 131072 x 1024, forward and backward: 4.84 ms; with 256 MB 4.88, with 64, which L2 would hold, 5.58: the
+// launches' ends and the rounds left unfilled cost more than the traffic)
+constexpr size_t kDzBytes = size_t(512) << 20;
 
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
     const float top = fmaxf(a.top, b.top);
@@ -320,7 +323,7 @@ static int64_t parts_of(int64_t rows, int V, int dtype) {
 }
 
 // The pieces of the backward pass: columns of each but the last, and the parts in which dX is summed.  bf16: of the numbers of pieces that
-// keep dZ within kPieceBytes, up to twice the least, the one whose tiles leave the fewest rounds of pairs unfilled; sizes near
+// keep dZ within kDzBytes, up to twice the least, the one whose tiles leave the fewest rounds of pairs unfilled; sizes near
 // 8192 x 131072 x 1024 differ by 10% in that.
 // fp32: few tokens have few tiles, and dX a sum over the whole piece: as many parts of it as blocks of 64 x 128 leave the chip's 608
 // places empty after the tiles are split in eight, with at least 512 columns for each (64 tokens, 32768 x 1024: 570 us in one), or those
@@ -335,7 +338,7 @@ static Pieces backward_pieces(int64_t T, int d, int V, int dtype) {
         return Pieces{cols, static_cast<int>(parts > 1 ? parts : 1)};
     }
     const int64_t rows = padded_rows(T);
-    int64_t most = static_cast<int64_t>(kPieceBytes / 2) / rows / 256 * 256;
+    int64_t most = static_cast<int64_t>(kDzBytes / 2) / rows / 256 * 256;
     if (most < 256) most = 256;
     if (most >= V) most = (V + 255) / 256 * 256;
     const int64_t least = (V + most - 1) / most;
