@@ -98,8 +98,8 @@ __global__ void factors_kernel(const Step s) {
     f.clip = 1.0f, f.down = 1.0f;
     if (!f.skip && static_cast<double>(n) > s.max_norm) {
         const float c = __frcp_rn(n) * static_cast<float>(s.max_norm);
-        if (n <= 1.0e37f && (c >= 1.0e-30f || s.max_norm == 0.0)) {
-            f.clip = c;
+        if (s.max_norm == 0.0 || (n <= 1.0e37f && c >= 1.0e-30f)) {      // beyond, 1 / n is a subnormal number
+            f.clip = s.max_norm == 0.0 ? 0.0f : c;
         } else {                       // a factor among fp32's subnormal numbers would lose bits: in two parts
             const double r = s.max_norm / static_cast<double>(n);
             const int half = (-ilogb(r) - 1) / 2;
@@ -136,7 +136,8 @@ __device__ __forceinline__ int tensor_of(const Table<CAP>& t, int c) {
     return lo;
 }
 
-// Three numbers in [0, 2^32) of an element and a step.
+// A number in [0, 2^32) of an element and a step, by which the first moment is rounded; the second and the parameter go by its products
+// with two odd numbers.
 __device__ __forceinline__ uint32_t mix(int64_t i, uint32_t key) {
     uint32_t x = static_cast<uint32_t>(i) + static_cast<uint32_t>(i >> 32) * 0x85EBCA6Bu + key;
     x = (x ^ (x >> 16)) * 0x7FEB352Du;

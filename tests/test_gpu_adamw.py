@@ -297,3 +297,22 @@ def test_offsets_beyond_32_bits():
             assert ((held.double() - em).abs() <= em.abs() / 8 + 2.0 ** -9 / 448 * em.abs().max()).all()
     assert int(torch.count_nonzero(p[k:-k].view(torch.int16).view(-1))) == 0
     assert float(state["m_scale"][0][-1]) > 0 and float(state["v_scale"][0][1000]) == 0
+
+
+@pytest.mark.parametrize("std", [1e-2, 1e36])
+@pytest.mark.parametrize("limit", [0.0, 1e-300, 1e30])
+def test_limits_at_the_ends(std, limit):
+    """A limit of zero, or far below fp32's range, leaves the decay alone; norms near fp32's largest are divided by exactly."""
+    params, grads = _tensors([3000], F32, F32, std=std)
+    norm = dtp.clip_grad_norm(grads, math.inf)
+    assert torch.isfinite(norm)
+    state = dtp.adamw_state(params)
+    before = params[0].clone()
+    dtp.adamw_step(params, grads, state, norm=norm, max_norm=limit, **HYPER)
+    zero = torch.zeros_like(before)
+    want, em, _, size = _exact(before, grads[0], zero, zero, 1, factor=min(1.0, limit / float(norm)), **HYPER)
+    if limit < 1.0:
+        assert (state["m"][0] == 0).all()
+        assert ((params[0].double() - want).abs() <= 16 * ROUND * size + 1e-30).all()
+    else:
+        assert ((state["m"][0].double() - em).abs() <= 8 * ROUND * em.abs()).all()
