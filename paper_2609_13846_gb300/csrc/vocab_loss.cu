@@ -9,7 +9,7 @@
 // dZ, in the product's epilogue (kEpiProb) or by a kernel of its own, and multiplied both ways; dX is added up over the
 // pieces in fp32.
 // The price of not keeping the logits is their product again: 8 T d V operations a training step and not 6.  8192 x 131072 of 1024, a
-// tenth of the tokens without a target: 5.0 to 5.2 ms, at the power cap; 4096 x 65536 of 4096 4.8 to 4.9.  One token through 131072 x
+// tenth of the tokens without a target: 4.9 to 5.2 ms, at the power cap; 4096 x 65536 of 4096 4.8 to 4.9.  One token through 131072 x
 // 1024: 50 us, of which 44 stream W.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
