@@ -124,3 +124,67 @@ def test_the_norms_rms_is_the_producers():
     want = torch.einsum("thk,dhk->htd", attn.double().view(130, 16, 32), W_o.double().view(256, 16, 32))
     want = want / (r.double().square().mean(-1) + distill.EPS).sqrt()[None, :, None]
     assert (C.double() - want).norm() <= 2.0 ** -8 * want.norm()
+
+
+def test_two_streams_at_once():
+    """Calls of two streams with workspaces of their own, in flight together, give what they give one after the other."""
+    def work(seed):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        x = torch.randn((600 + seed, 256), generator=g, device=DEV).to(torch.bfloat16)
+        w = (torch.randn((9000, 256), generator=g, device=DEV) * 0.1).to(torch.bfloat16)
+        y = torch.randint(0, 9000, (x.shape[0],), generator=g, device=DEV)
+        y[::5] = -100
+        p = [torch.randn(n, generator=g, device=DEV) for n in (100_000, 33)]
+        gr = [torch.randn(n, generator=g, device=DEV).to(torch.bfloat16) for n in (100_000, 33)]
+        gamma = torch.rand(256, generator=g, device=DEV) + 0.5
+        dl = torch.full((x.shape[0],), 1e-3, device=DEV)
+        state = dtp.adamw_state(p, bits=8)
+        return x, w, y, p, gr, gamma, dl, state
+
+    def run(x, w, y, p, gr, gamma, dl, state):
+        out = []
+        for _ in range(3):
+            h, rms = dtp.rms_norm(x, gamma)
+            loss, lse = dtp.linear_cross_entropy(h, w, y)
+            dh, dw = dtp.linear_cross_entropy_backward(dl, h, w, y, lse)
+            dx, dgamma = dtp.rms_norm_backward(dh, x, gamma, rms)
+            dtp.adamw_step(p, gr, state, lr=1e-3)
+            out = [h, loss, lse, dw, dx, dgamma]
+        return out + p + state["m_scale"] + state["v_scale"]
+
+    want = [run(*work(s)) for s in (1, 2)]
+    inputs, streams, got = [work(s) for s in (1, 2)], [torch.cuda.Stream() for _ in range(2)], []
+    torch.cuda.synchronize()
+    for a, s in zip(inputs, streams):
+        with torch.cuda.stream(s):
+            got.append(run(*a))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_compaction_of_more_than_a_run_of_tokens():
+    """dX alone of more than 2^18 tokens, half of them padding: each token's row at its own place."""
+    T, d, V = (1 << 18) + 4097, 64, 200
+    g = torch.Generator(device=DEV).manual_seed(11)
+    x = torch.randn((T, d), generator=g, device=DEV).to(torch.bfloat16)
+    w = (torch.randn((V, d), generator=g, device=DEV) * 0.2).to(torch.bfloat16)
+    y = torch.randint(0, V, (T,), generator=g, device=DEV)
+    y[torch.rand(T, generator=g, device=DEV) < 0.5] = -100
+    _, lse = dtp.linear_cross_entropy(x, w, y)
+    dl = torch.rand(T, generator=g, device=DEV)
+    dx = torch.empty_like(x)
+    ws = dtp.linear_cross_entropy_workspace(T, d, V, torch.bfloat16, DEV, backward=True)
+    st = dtp.lib().dtp_linear_cross_entropy_backward(dl.data_ptr(), x.data_ptr(), w.data_ptr(), y.data_ptr(), lse.data_ptr(), T, d, V, -100,
+                                                     dtp.DTP_BF16, dx.data_ptr(), None, ws.data_ptr(), ws.numel(),
+                                                     torch.cuda.current_stream().cuda_stream)
+    assert st == dtp.DTP_OK
+    live = y != -100
+    dz = torch.softmax(x.double() @ w.double().t(), 1)
+    dz.scatter_add_(1, torch.where(live, y, 0)[:, None], -torch.ones((T, 1), dtype=torch.float64, device=DEV))
+    dz *= (dl * live).double()[:, None]
+    half = torch.finfo(torch.bfloat16).eps / 2
+    ref = dz @ w.double()
+    # dX is rounded once, each element of dZ once (1.01: the second order); 2^-12 is far above what fp32 logits and sums of 200 add
+    assert ((dx.double() - ref).abs() <= half * ref.abs() + (1.01 * half + 2.0 ** -12) * dz.abs() @ w.double().abs()).all()
+    assert (dx[~live] == 0).all()
