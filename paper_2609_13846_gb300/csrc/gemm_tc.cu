@@ -539,15 +539,17 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 }
             };
             if constexpr (KIND == kEpiLinear) fetch(32 * half);
-            // the row's target as a column, its lse times log2 e and its gradient: a row that does not count gets zeros
+            // the row's target as a column, its lse times log2 e and its gradient, and the bits of dZ that it keeps: none where it does not count
             int target = -1;
             float lse2 = INFINITY, grad = 0.0f;
+            [[maybe_unused]] uint32_t kept = 0u;
             if constexpr (KIND == kEpiParts || KIND == kEpiProb) {
                 if (m < (KIND == kEpiProb ? static_cast<int64_t>(live_tokens) : e.vocab.T)) {
                     const int64_t y = e.vocab.targets[m];
                     if (e.vocab.live(y)) {
                         target = static_cast<int>(y) - e.vocab.v0;
-                        if constexpr (KIND == kEpiProb) lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m] / *e.vocab.unit;
+                        if constexpr (KIND == kEpiProb)
+                            lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m] / *e.vocab.unit, kept = ~0u;
                     }
                 }
             }
@@ -733,8 +735,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
 #pragma unroll
                         for (int i = 0; i < 32; ++i) v[i] -= at == i ? 1.0f : 0.0f;
                     }
+                    // zeros by selection: a row of zeros has no numbers as logits where W has infinities
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i] * grad, v[2 * i + 1] * grad);
+                    for (int i = 0; i < 16; ++i) w[i] = kept & pack_bf16(v[2 * i] * grad, v[2 * i + 1] * grad);
                     store32(job, p.dst[job], w, n, row0);
                 } else {
                     // 16 columns at a time with all their saved values in flight: 144 us for 1024 x 3072 on 16384 tokens (four
