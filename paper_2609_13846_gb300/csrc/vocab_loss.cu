@@ -250,10 +250,21 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* sums, int p
     }
 }
 
-// dX from its sums, in dZ's unit: `parts` of them, `stride` values apart, each token's at its place; zeros for those without one.  A warp
-// takes 512 columns of a token.
+// fp32: zeros for the tokens that do not count, whose sums are 0 times what stands in W.
+__global__ void __launch_bounds__(256) clear_rows_kernel(int64_t T, int d, const Vocab e, float* dX) {
+    grid_wait();
+    grid_release();
+    for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+        if (e.live(e.targets[t])) continue;
+        for (int i = threadIdx.x; i < d; i += 256) dX[t * d + i] = 0.0f;
+    }
+}
+
+// dX from its sums, in dZ's unit: `parts` of them, `stride` values apart, each token's at its place; zeros for those that do not count.  A
+// warp takes 512 columns of a token.
 __global__ void __launch_bounds__(256)
-round_kernel(const float* sum, int parts, int64_t stride, int64_t T, int d, const int* place, const float* unit, __nv_bfloat16* out) {
+round_kernel(const float* sum, int parts, int64_t stride, int64_t T, int d, const int64_t* targets, int64_t ignore, int V,
+             const int* place, const float* unit, __nv_bfloat16* out) {
     grid_wait();
     grid_release();
     const float u = *unit;
@@ -261,7 +272,8 @@ round_kernel(const float* sum, int parts, int64_t stride, int64_t T, int d, cons
     const bool wide = d % 4 == 0;          // the binding's and the C ABI's tensors start on 16 bytes
     for (int64_t i = blockIdx.x * 8ll + (threadIdx.x >> 5); i < T * pieces; i += gridDim.x * 8ll) {
         const int64_t t = i / pieces;
-        const int c0 = static_cast<int>(i - t * pieces) * 512, at = place[t];
+        const int64_t y = targets[t];
+        const int c0 = static_cast<int>(i - t * pieces) * 512, at = y != ignore && y >= 0 && y < V ? place[t] : -1;
         const float* from = sum + static_cast<int64_t>(at) * d;
         __nv_bfloat16* to = out + t * d;
         if (wide) {
@@ -572,8 +584,9 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
     }
     if (kBf16 && st == DTP_OK && dX)
         st = launch_after(round_kernel, grid_of((T * ((d + 511) / 512) + 7) / 8), stream, static_cast<const float*>(s.sum), pieces.parts,
-                          sum_rows(T) * d, T, d, static_cast<const int*>(k.place), static_cast<const float*>(k.unit),
-                          static_cast<__nv_bfloat16*>(dX));
+                          sum_rows(T) * d, T, d, targets, ignore, V, static_cast<const int*>(k.place),
+                          static_cast<const float*>(k.unit), static_cast<__nv_bfloat16*>(dX));
+    if (!kBf16 && st == DTP_OK && dX) st = launch_after(clear_rows_kernel, grid_of(T), stream, T, d, e, static_cast<float*>(dX));
     return st;
 }
 

@@ -61,3 +61,15 @@ def test_masked_tokens_get_no_gradient(T, dtype, padding):
     live = y != IGNORE
     # column 0 is 0 times an infinity in the formula too
     assert ((dx.double() - ref).abs() <= half * ref.abs() + off * dz.abs() @ W.abs() + 1e-38)[live][:, 1:].all()
+
+
+@pytest.mark.parametrize("T,dtype", [(t, BF16) for t in (2, 40, 300, (1 << 18) + 100)] + [(t, F32) for t in (2, 5, 32, 40, 300)])
+@pytest.mark.parametrize("value", [float("-inf"), float("inf"), float("nan")])
+def test_tokens_that_do_not_count_have_zero_rows(T, dtype, value):
+    """Whatever stands in the weights: the gradient of a token without a target is 0, and not 0 times what is there."""
+    x, w, y, dloss = _inputs(T, dtype, 0.5)
+    y[0], y[1] = IGNORE, 7
+    w[3, 5] = value
+    _, lse = dtp.linear_cross_entropy(x, w, y)
+    dx, _ = dtp.linear_cross_entropy_backward(dloss, x, w, y, lse)
+    assert (dx[y == IGNORE] == 0).all()
