@@ -36,7 +36,9 @@ constexpr int kSms = 152;              // for which the backward pass's blocks a
 
 // Threads of a block whose rows take TPR threads each.
 __host__ __device__ constexpr int block_threads(int tpr) { return tpr > 32 ? tpr : kThreads; }
-constexpr float kDown = 5.4210109e-20f;      // 2^-64: a row whose squares leave fp32's range is summed again at this scale
+// A row whose squares leave fp32's range is summed again at this scale.  Its mean square is at least 2^127.8, so that what
+// counts stays far above the least number (2^-149), and 2^20 squares of numbers below 2^128 sum to no more than 2^84.
+constexpr float kDown = 0x1p-96f;
 
 __device__ __forceinline__ float block_sum(float v, float* red) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
