@@ -539,9 +539,9 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                 }
             };
             if constexpr (KIND == kEpiLinear) fetch(32 * half);
-            // the row's target as a column, its lse times log2 e and its gradient, and the bits of dZ that it keeps: none where it does not count
+            // the row's target as a column, its lse and its gradient, and the bits of dZ that it keeps: none where it does not count
             int target = -1;
-            float lse2 = INFINITY, grad = 0.0f;
+            float lse = INFINITY, grad = 0.0f;
             [[maybe_unused]] uint32_t kept = 0u;
             if constexpr (KIND == kEpiParts || KIND == kEpiProb) {
                 if (m < (KIND == kEpiProb ? static_cast<int64_t>(live_tokens) : e.vocab.T)) {
@@ -549,7 +549,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     if (e.vocab.live(y)) {
                         target = static_cast<int>(y) - e.vocab.v0;
                         if constexpr (KIND == kEpiProb)
-                            lse2 = e.vocab.lse[m] * kLog2e, grad = e.vocab.dloss[m] / *e.vocab.unit, kept = ~0u;
+                            lse = e.vocab.lse[m], grad = e.vocab.dloss[m] / *e.vocab.unit, kept = ~0u;
                     }
                 }
             }
@@ -713,15 +713,14 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     float most = v[0];
 #pragma unroll
                     for (int i = 1; i < 32; ++i) most = fmaxf(most, v[i]);
-                    most *= kLog2e;
                     if (most > top) {
-                        sum *= exp2_fast(top - most);
+                        sum *= exp2_fast((top - most) * kLog2e);
                         top = most;
                     }
                     const float shift = isinf(top) ? 0.0f : top;      // a row of -inf alone sums to 0, one with an infinity to it
                     float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast(fmaf(v[i], kLog2e, -shift));
+                    for (int i = 0; i < 32; ++i) s4[i & 3] += exp2_fast((v[i] - shift) * kLog2e);
                     sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
                 } else if constexpr (KIND == kEpiProb) {
                     float v[32];
@@ -729,7 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) gemm_tc_kernel(const __grid_const
                     get16(0, c + 16, v + 16);
                     got();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast(fmaf(v[i], kLog2e, -lse2));
+                    for (int i = 0; i < 32; ++i) v[i] = exp2_fast((v[i] - lse) * kLog2e);
                     const int at = target - n;
                     if (__any_sync(0xFFFFFFFFu, at >= 0 && at < 32)) {
 #pragma unroll

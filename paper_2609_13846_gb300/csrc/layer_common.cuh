@@ -190,7 +190,8 @@ enum EpiKind {
     kEpiProb = 4        // acc = logits: out = dZ = dloss (exp(acc - lse) - onehot) (bf16 only)
 };
 
-// A row's largest logit of a chunk of columns, times log2 e, and the sum of 2^(z log2 e - top).
+// A row's largest logit of a chunk of columns, and the sum of e^(z - top).  Differences of logits are taken before they are scaled for
+// the base of 2: the largest one's is 0 then, and its term 1, whatever its size.
 struct Part { float top, sum; };
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 __device__ __forceinline__ float exp2_fast(float x) {

@@ -28,11 +28,23 @@ constexpr size_t kPieceBytes = size_t(256) << 20;    // of a piece of the logits
 // launches' ends and the rounds left unfilled cost more than the traffic)
 constexpr size_t kDzBytes = size_t(512) << 20;
 
+// Parts joined at their largest logit.  Where that is infinite the terms are taken from 0: parts that hold nothing, or -inf alone, have no
+// sum, and one with an infinity has an infinite one.  The exponentials do not wait for one another (one part at a time, 1003 tokens
+// of 782 parts: 177 us in all, 172 so).
+template <int N>
+__device__ __forceinline__ Part join(const Part& a, const Part (&b)[N]) {
+    float top = a.top;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, b[j].top);
+    const float from = isinf(top) ? 0.0f : top;
+    float sum = a.sum * exp2_fast((a.top - from) * kLog2e);
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum = fmaf(b[j].sum, exp2_fast((b[j].top - from) * kLog2e), sum);
+    return Part{top, sum};
+}
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
-    const float top = fmaxf(a.top, b.top);
-    // a part that holds nothing, or only -inf, counts for nothing
-    const float u = a.top == top ? a.sum : a.sum * exp2_fast(a.top - top), v = b.top == top ? b.sum : b.sum * exp2_fast(b.top - top);
-    return Part{top, u + v};
+    const Part one[1] = {b};
+    return join(a, one);
 }
 
 // Z [T, cols] in fp32, columns v0 .. of the vocabulary: parts[chunk][t], and the target's logit where it is among them.
@@ -50,7 +62,7 @@ parts_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets
         bool nan = false;
         for (int j = c * kChunk + threadIdx.x; j < c1; j += 256) {
             nan |= isnan(z[j]);
-            p = join(p, Part{z[j] * kLog2e, 1.0f});
+            p = join(p, Part{z[j], 1.0f});
         }
         if (nan) p.sum = NAN;
 #pragma unroll
@@ -82,25 +94,29 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
     const int64_t t = blockIdx.x * 32ll + lane;
     Part p{-INFINITY, 0.0f};
     if (t < T) {
-        int64_t c = warp;
-        for (; c + 7 * kLossWarps < count; c += 8 * kLossWarps) {
+        for (int64_t c = warp; c < count; c += 8 * kLossWarps) {
             Part q[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q[j] = parts[(c + j * kLossWarps) * T + t];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p = join(p, q[j]);
+            for (int j = 0; j < 8; ++j) q[j] = c + j * kLossWarps < count ? parts[(c + j * kLossWarps) * T + t] : Part{-INFINITY, 0.0f};
+            p = join(p, q);
         }
-        for (; c < count; c += kLossWarps) p = join(p, parts[c * T + t]);
     }
     red[warp][lane] = p;
     __syncthreads();
     if (warp != 0 || t >= T) return;
-    for (int w = 1; w < kLossWarps; ++w) p = join(p, red[w][lane]);
-    const float l = kLn2 * (p.top + log2f(p.sum));
-    lse[t] = l;
+    for (int w = 0; w < kLossWarps; w += 8) {
+        Part q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[j] = w + j > 0 ? red[w + j][lane] : Part{-INFINITY, 0.0f};        // p is the first
+        p = join(p, q);
+    }
+    const float rest = kLn2 * log2f(p.sum);
+    lse[t] = p.top + rest;
     const int64_t y = targets[t];
     const bool bad = y != ignore && (y < 0 || y >= V);
-    loss[t] = y == ignore ? 0.0f : bad ? NAN : l - hit[t];
+    // the largest logit first: it takes the target's out exactly where that leads, and the sum beside it is at least 1, so that no
+    // loss is negative
+    loss[t] = y == ignore ? 0.0f : bad ? NAN : (p.top - hit[t]) + rest;
     if (bad) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
 }
 
@@ -229,10 +245,10 @@ dz_kernel(const float* Z, int64_t T, int cols, Vocab e, E* dZ, int64_t ld, int* 
         const int64_t y = e.targets[t];
         if (c == 0 && threadIdx.x == 0 && e.bad(y)) atomicCAS(status, static_cast<int>(DTP_OK), static_cast<int>(DTP_ERR_ARG));
         const bool live = e.live(y);
-        const float g = live ? e.dloss[t] : 0.0f, lse2 = e.lse[t] * kLog2e;
+        const float g = live ? e.dloss[t] : 0.0f, lse = e.lse[t];
 #pragma unroll 4
         for (int j = c * kChunk + threadIdx.x; j < c1; j += 256) {
-            const float p = exp2_fast(fmaf(Z[t * cols + j], kLog2e, -lse2)) - (y - e.v0 == j ? 1.0f : 0.0f);
+            const float p = exp2_fast((Z[t * cols + j] - lse) * kLog2e) - (y - e.v0 == j ? 1.0f : 0.0f);
             dZ[t * ld + j] = from_f32<E>(live ? p * g : 0.0f);
         }
     }
