@@ -131,8 +131,9 @@ struct Call {
 // to the workspace, and the runs are added in 64 bits.
 constexpr int64_t kRun = 1 << 18;
 size_t runs_bytes(int64_t T, int64_t rows, int64_t cols);
-// out [rows, cols] = sum over T tokens of A's rows times B's columns, both stored token by token; `runs` of runs_bytes
-int weight_gradient(Call& call, const Also& w, int64_t T, float* runs);
+// out [rows, cols] = sum over T tokens of A's rows times B's columns, both stored token by token; `runs` of runs_bytes.  `unit` (device; of
+// several runs only): what the sums are taken times.
+int weight_gradient(Call& call, const Also& w, int64_t T, float* runs, const float* unit = nullptr);
 
 }  // namespace layer
 }  // namespace dtp

@@ -329,14 +329,15 @@ repitch_kernel(const uint16_t* src, int64_t rows, int cols, int64_t pitch, uint1
 // The runs' sums of a weight gradient (see kRun), added in their order.
 template <typename E>
 __global__ void __launch_bounds__(256)
-sum_runs_kernel(const float* runs, int64_t count, int64_t values, E* out) {
+sum_runs_kernel(const float* runs, int64_t count, int64_t values, const float* unit, E* out) {
     grid_wait();
     grid_release();
+    const double u = unit ? static_cast<double>(*unit) : 1.0;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < values; i += gridDim.x * 256ll) {
         double s = 0.0;
 #pragma unroll 4
         for (int64_t r = 0; r < count; ++r) s += static_cast<double>(runs[r * values + i]);
-        out[i] = from_f32<E>(static_cast<float>(s));
+        out[i] = from_f32<E>(static_cast<float>(s * u));
     }
 }
 
@@ -366,8 +367,7 @@ size_t runs_bytes(int64_t T, int64_t rows, int64_t cols) {
     return T > kRun ? static_cast<size_t>((T + kRun - 1) / kRun) * rows * cols * sizeof(float) : 0;
 }
 
-// out [rows, cols] = sum over T tokens of A's rows times B's columns, both stored token by token
-int weight_gradient(Call& call, const Also& w, int64_t T, float* runs) {
+int weight_gradient(Call& call, const Also& w, int64_t T, float* runs, const float* unit) {
     const int64_t values = w.M * w.N, count = T > kRun ? (T + kRun - 1) / kRun : 1;
     for (int64_t r = 0; r < count; ++r) {
         const int64_t t0 = r * kRun;
@@ -386,9 +386,9 @@ int weight_gradient(Call& call, const Also& w, int64_t T, float* runs) {
     if (count == 1) return DTP_OK;
     const int64_t blocks = (values + 255) / 256 < 8192 ? (values + 255) / 256 : 8192;
     return call.dtype == DTP_BF16 ? launch_after(sum_runs_kernel<__nv_bfloat16>, blocks, call.stream, static_cast<const float*>(runs),
-                                                 count, values, static_cast<__nv_bfloat16*>(w.out))
+                                                 count, values, unit, static_cast<__nv_bfloat16*>(w.out))
                                   : launch_after(sum_runs_kernel<float>, blocks, call.stream, static_cast<const float*>(runs), count,
-                                                 values, static_cast<float*>(w.out));
+                                                 values, unit, static_cast<float*>(w.out));
 }
 
 // ------------------------------------------------------------------------------- linear layer

@@ -124,7 +124,7 @@ loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* t
 // is the rows that the products take, padded to 64 and at least that many, live[1] the tokens.  Tokens that do not count then cost
 // nothing, and whatever stands in their rows reaches nothing.  Also dZ's unit, the largest finite size of dloss among them (at least
 // 2^-126; else 1): rounding dloss (p - onehot) to bf16 would round dloss of a mean, the same in all rows, and the error would not average
-// out.  One block, 4096 tokens at a time.  compact 0: all tokens keep their rows, and the unit is 1.
+// out.  One block, 4096 tokens at a time.  compact 0: all tokens keep their rows.
 struct Compact {
     int* place;
     int* live;
@@ -147,13 +147,14 @@ index_kernel(const int64_t* targets, const float* lse, const float* dloss, int64
         const int64_t t = t0 + 4 * threadIdx.x;
         int64_t y[4];
         int count = 0;
-        bool live[4];
+        bool live[4], counts[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             y[j] = t + j < T ? targets[t + j] : ignore;
             const bool in = y[j] >= 0 && y[j] < V;
             bad |= y[j] != ignore && !in;
-            live[j] = t + j < T && (!compact || (y[j] != ignore && in));
+            counts[j] = t + j < T && y[j] != ignore && in;
+            live[j] = t + j < T && (!compact || counts[j]);
             count += live[j];
         }
         int before = count;          // of the lanes up to this one
@@ -180,7 +181,7 @@ index_kernel(const int64_t* targets, const float* lse, const float* dloss, int64
             if (!live[j]) continue;
             const float g = dloss[t + j];
             to.targets[at] = y[j], to.lse[at] = lse[t + j], to.dloss[at] = g;
-            if (isfinite(g)) top = fmaxf(top, fabsf(g));
+            if (counts[j] && isfinite(g)) top = fmaxf(top, fabsf(g));
             ++at;
         }
         base += all;
@@ -191,7 +192,7 @@ index_kernel(const int64_t* targets, const float* lse, const float* dloss, int64
     const bool any = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
         for (int w = 1; w < kIndexThreads / 32; ++w) top = fmaxf(top, tops[w]);
-        *to.unit = compact && top >= 1.1754944e-38f ? top : 1.0f;
+        *to.unit = top >= 1.1754944e-38f ? top : 1.0f;
         const int rows = (base + 63) / 64 * 64;
         to.live[0] = rows > 64 ? rows : 64;
         to.live[1] = base;
@@ -567,7 +568,7 @@ static int backward(const float* dloss, const void* X, const void* W, const int6
             if (g.parts > (cols + 63) / 64) g.parts = (cols + 63) / 64;       // a short last piece leaves the others' sums as they are
             if (st == DTP_OK) st = gtc::launch_pair(g, status, stream);
             if (st == DTP_OK && in_runs)
-                st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, rows, s.runs);
+                st = weight_gradient(call, Also{by_col(s.dz, ldz), by_col(x.p, x.ld), cols, d, dw_at, d}, rows, s.runs, k.unit);
         } else {
             st = store_logits(call, p);
             if (st == DTP_OK)
