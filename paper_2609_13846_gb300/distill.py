@@ -94,7 +94,10 @@ def head_backward(w: dict, dloss: torch.Tensor, kept) -> tuple[torch.Tensor, dic
 
 def tune_state(master: dict, dtype: torch.dtype = torch.bfloat16, bits: int = 32) -> dict:
     """What :func:`tune_step` keeps between steps for fp32 master weights (o, gate, up, down, gamma, head, gamma_out): their
-    copies in ``dtype`` that the layer runs on, and the optimiser's states, in ``bits`` for the matrices and 32 for the gains."""
+    copies in ``dtype`` that the layer runs on (bf16, or with fp32 the weights themselves), and the optimiser's states, in
+    ``bits`` for the matrices and 32 for the gains."""
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"a layer runs in bfloat16 or float32, got {dtype}")
     matrices = [k for k, v in master.items() if v.dim() == 2]
     gains = [k for k, v in master.items() if v.dim() == 1]
     return dict(matrices=matrices, gains=gains, copies={k: master[k].to(dtype) for k in matrices},
@@ -119,8 +122,10 @@ def tune_step(master: dict, state: dict, attn: torch.Tensor, x: torch.Tensor, ta
     grads.update(layer_backward(w, dy, kept))
     norm = dtp.clip_grad_norm([grads[k] for k in state["matrices"] + state["gains"]], float("inf"))
     common = dict(lr=lr, betas=betas, norm=norm, max_norm=max_norm)
+    copies = [state["copies"][k] for k in state["matrices"]]
+    copies = [c if c.dtype == torch.bfloat16 else None for c in copies]
     dtp.adamw_step([master[k] for k in state["matrices"]], [grads[k] for k in state["matrices"]], state["adamw"],
-                   weight_decay=weight_decay, copies=[state["copies"][k] for k in state["matrices"]], **common)
+                   weight_decay=weight_decay, copies=copies, **common)
     dtp.adamw_step([master[k] for k in state["gains"]], [grads[k] for k in state["gains"]], state["adamw_gains"],
                    weight_decay=0.0, **common)
     return (loss * share).sum(), norm
