@@ -98,12 +98,18 @@ __global__ void factors_kernel(const Step s) {
     f.clip = 1.0f, f.down = 1.0f;
     if (!f.skip && static_cast<double>(n) > s.max_norm) {
         const float c = __frcp_rn(n) * static_cast<float>(s.max_norm);
-        if (s.max_norm == 0.0 || (n <= 1.0e37f && c >= 1.0e-30f)) {      // beyond, 1 / n is a subnormal number
+        // the reciprocal of a normal number up to 1e37, and a limit, that lose no bits; a limit of 0 is one
+        const bool normal = n >= 1.2e-38f && n <= 1.0e37f && s.max_norm >= 1.2e-38;
+        if (s.max_norm == 0.0 || (normal && c >= 1.0e-30f)) {
             f.clip = s.max_norm == 0.0 ? 0.0f : c;
         } else {                       // a factor among fp32's subnormal numbers would lose bits: in two parts
             const double r = s.max_norm / static_cast<double>(n);
-            const int half = (-ilogb(r) - 1) / 2;
-            f.clip = static_cast<float>(ldexp(r, 2 * half)), f.down = ldexpf(1.0f, -half);
+            if (r < 1.0e-90) {         // no gradient times it is above half of fp32's least number
+                f.clip = 0.0f;
+            } else {
+                const int half = (-ilogb(r) - 1) / 2;
+                f.clip = static_cast<float>(ldexp(r, 2 * half)), f.down = ldexpf(1.0f, -half);
+            }
         }
     }
     const int64_t t = *s.step + 1;
