@@ -185,6 +185,12 @@ def _keep(t: torch.Tensor, stream) -> torch.Tensor:
     return t
 
 
+def _written(*tensors: torch.Tensor | None):
+    """Tell autograd that a call has written these tensors of its caller's: a graph that saved one of them then refuses to
+    differentiate with its new values.  (Replays of a captured call do not pass here.)"""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _device_mask(m, L: int, dev, stream) -> torch.Tensor | None:
     if m is None:
         return None
@@ -942,6 +948,7 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, r
         _layer_check("bias", bias, (N,), dtype, index)
     if residual is not None:
         _layer_check("residual", residual, (T, N), dtype, index)
+    given = Y
     if Y is None:
         Y = _keep(torch.empty((T, N), dtype=dtype, device=X.device), stream)
     else:
@@ -955,6 +962,8 @@ def linear(X: torch.Tensor, W: torch.Tensor, bias: torch.Tensor | None = None, r
                           _ptr(Z), workspace.data_ptr(), workspace.numel(), _layer_stream(stream, index))
     if st:
         _check("dtp_linear", st)
+    if given is not None:
+        _written(given)
     return (Y, Z) if save else Y
 
 
@@ -1025,6 +1034,7 @@ def gated_ffn(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down:
     code, act = _code_of(dtype), _act_code(activation)
     if residual is not None:
         _layer_check("residual", residual, (T, d), dtype, index)
+    given = Y
     if Y is None:
         Y = _keep(torch.empty((T, d), dtype=dtype, device=X.device), stream)
     else:
@@ -1043,6 +1053,8 @@ def gated_ffn(X: torch.Tensor, W_gate: torch.Tensor, W_up: torch.Tensor, W_down:
                              _layer_stream(stream, index))
     if st:
         _check("dtp_gated_ffn", st)
+    if given is not None:
+        _written(given)
     return (Y, (H, pre)) if save else Y
 
 
@@ -1120,6 +1132,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
         dst, out_numel, out_dtypes = _flat_tensors("out", out, index)
         if out_numel != numel or out_dtypes != dtypes:
             raise ValueError("out must have the sizes and dtypes of grads")
+    written = list(out) if out is not None else [] if max_norm == float("inf") else grads
     if norm is None:
         norm = _keep(torch.empty((), dtype=torch.float32, device=grads[0].device), stream)
     elif norm.dtype is not torch.float32 or norm.numel() != 1 or norm.get_device() != index:
@@ -1132,6 +1145,7 @@ def clip_grad_norm(grads, max_norm: float, out=None, norm: torch.Tensor | None =
                                   numel.buffer_info()[0], codes.buffer_info()[0], count, float(max_norm), _ptr(norm),
                                   _ptr(workspace), workspace.numel(), _layer_stream(stream, index))
     _check("dtp_clip_grad_norm", st)
+    _written(norm, *written)
     return norm
 
 
@@ -1157,6 +1171,7 @@ def rms_norm(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, Y: torch.T
     """
     T, d, dtype, index = _norm_shapes(X, gamma)
     code = _code_of(dtype)
+    given = Y
     if Y is None:
         Y = _keep(torch.empty((T, d), dtype=dtype, device=X.device), stream)
     else:
@@ -1166,6 +1181,8 @@ def rms_norm(X: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-6, Y: torch.T
                             _layer_stream(stream, index))
     if st:
         _check("dtp_rms_norm", st)
+    if given is not None:
+        _written(given)
     return Y, rms
 
 
@@ -1377,16 +1394,23 @@ def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 
     if bits not in (8, 32):
         raise ValueError(f"the state's bits must be 8 or 32, got {bits}")
     held, ms, vs = (DTP_F32 if bits == 32 else _E4M3), None, None
-    m, _, mc = _read_list("the state's m", list(state["m"]), index, numel, 1, True)
-    v, _, vc = _read_list("the state's v", list(state["v"]), index, numel, 1, True)
+    held_m, held_v = list(state["m"]), list(state["v"])
+    written = [params, held_m, held_v, [state["step"]]]
+    m, _, mc = _read_list("the state's m", held_m, index, numel, 1, True)
+    v, _, vc = _read_list("the state's v", held_v, index, numel, 1, True)
     if not (_all_codes(mc, held) and _all_codes(vc, held)):
         raise TypeError(f"the state's moments must be {'float32' if bits == 32 else 'float8_e4m3fn'} with {bits} bits")
     if bits == 8:
-        ms, _, mc = _read_list("the state's m_scale", list(state["m_scale"]), index, numel, ADAMW_BLOCK, True)
-        vs, _, vc = _read_list("the state's v_scale", list(state["v_scale"]), index, numel, ADAMW_BLOCK, True)
+        scales = list(state["m_scale"]), list(state["v_scale"])
+        written += scales
+        ms, _, mc = _read_list("the state's m_scale", scales[0], index, numel, ADAMW_BLOCK, True)
+        vs, _, vc = _read_list("the state's v_scale", scales[1], index, numel, ADAMW_BLOCK, True)
         if not (_all_codes(mc, DTP_F32) and _all_codes(vc, DTP_F32)):
             raise TypeError("the state's scales must be float32")
-    c = None if copies is None else _copies(list(copies), index, numel, pc)
+    if copies is not None:
+        copies = list(copies)
+        written.append(copies)
+    c = None if copies is None else _copies(copies, index, numel, pc)
     step = _scalar_on("the state's step", state["step"], torch.int64, index)
     lr_at = _scalar_on("lr", lr, torch.float32, index) if isinstance(lr, torch.Tensor) else None
     norm_at = None if norm is None else _scalar_on("norm", norm, torch.float32, index)
@@ -1399,6 +1423,7 @@ def adamw_step(params, grads, state: dict, lr, betas=(0.9, 0.999), eps: float = 
                          workspace.numel(), _layer_stream(stream, index))
     if st:
         _check("dtp_adamw", st)
+    _tensor_lists.written(*written)
 
 
 def _copies(copies, index: int, numel: bytes, param_codes: bytes) -> bytes:
