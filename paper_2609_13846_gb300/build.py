@@ -10,6 +10,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import glob
 import os
+import platform
 import shutil
 import subprocess
 import sys
@@ -22,6 +23,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdtp.so")
 LISTS = os.path.join(PKG, "_tensor_lists.so")
 LISTS_SOURCE = os.path.join(CSRC, "tensor_lists.cpp")
+LISTS_FOR = os.path.join(BUILD, "tensor_lists.for")     # the versions that the module was compiled against
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
               "-I", os.path.join(ROOT, "include"), "-I", CSRC]
@@ -56,6 +58,21 @@ def _compile(src: str, verbose: bool) -> str:
     return obj
 
 
+def versions() -> str:
+    """What the module of tensor lists depends on: torch's C++ classes, CPython's, and the machine."""
+    import torch
+    return f"torch {torch.__version__}, {sys.implementation.cache_tag}, {platform.machine()}"
+
+
+def lists_versions() -> str | None:
+    """The versions that the module was compiled against, None where that is not known."""
+    try:
+        with open(LISTS_FOR) as f:
+            return f.read()
+    except OSError:
+        return None
+
+
 def _build_lists() -> None:
     import torch
     root = os.path.dirname(torch.__file__)
@@ -70,7 +87,13 @@ def _build_lists() -> None:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for {LISTS_SOURCE}:\n{r.stdout}\n{r.stderr}")
+    os.makedirs(BUILD, exist_ok=True)
+    if os.path.exists(LISTS_FOR):
+        os.remove(LISTS_FOR)               # a module whose versions are not known is not loaded
     os.replace(tmp, LISTS)
+    with open(LISTS_FOR + ".tmp", "w") as f:
+        f.write(versions())
+    os.replace(LISTS_FOR + ".tmp", LISTS_FOR)
 
 
 def _stale(target: str, sources) -> bool:
@@ -78,9 +101,10 @@ def _stale(target: str, sources) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Build libdtp.so and _tensor_lists.so where a source or header is newer; return the library's path."""
+    """Build libdtp.so and _tensor_lists.so where a source or header is newer, the latter also where torch or Python is another than
+    it was compiled against; return the library's path."""
     srcs = _sources()
-    lists = force or _stale(LISTS, [LISTS_SOURCE, __file__])
+    lists = force or _stale(LISTS, [LISTS_SOURCE, __file__]) or lists_versions() != versions()
     library = force or _stale(LIB, srcs + _headers() + [__file__])
     with cf.ThreadPoolExecutor(max_workers=1) as beside:
         done = beside.submit(_build_lists) if lists else None

@@ -1350,6 +1350,10 @@ def _read_list(*args):
     if _tensor_lists is None:
         if not os.path.exists(os.path.join(_PKG, "_tensor_lists.so")):
             raise RuntimeError("_tensor_lists.so is missing: build it with `python -m paper_2609_13846_gb300.build`")
+        from . import build
+        if build.lists_versions() != build.versions():       # it would misread tensors laid out otherwise
+            raise RuntimeError(f"_tensor_lists.so was compiled against {build.lists_versions()}, and this is {build.versions()}: "
+                               "build it again with `python -m paper_2609_13846_gb300.build`")
         spec = importlib.util.spec_from_file_location("_tensor_lists", os.path.join(_PKG, "_tensor_lists.so"))
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
