@@ -10,7 +10,7 @@
 // pieces in fp32.
 // The price of not keeping the logits is their product again: 8 T d V operations a training step and not 6.  8192 x 131072 of 1024, a
 // tenth of the tokens without a target: 4.9 to 5.2 ms, at the power cap; 4096 x 65536 of 4096 4.8 to 4.9.  One token through 131072 x
-// 1024: 50 us, of which 44 stream W.
+// 1024: 51 us, of which 44 stream W.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -81,8 +81,8 @@ parts_kernel(const float* Z, int64_t T, int cols, int v0, const int64_t* targets
 }
 
 // The parts of each token joined: each of 32 warps takes every 32nd part of 32 tokens, eight in flight, and the first one joins the
-// warps' in order (a vocabulary of 131072 has 1024 parts; 8 warps and one part at a time: 65 us).  A target that is no token's sets
-// the status.
+// warps' in order (a vocabulary of 131072 has 1024 parts from 256-wide tiles, 2048 from the 128-wide ones that a few tokens get; with 8 warps
+// and one part at a time one token took 65 us).  A target that is no token's sets the status.
 constexpr int kLossWarps = 32;
 __global__ void __launch_bounds__(32 * kLossWarps)
 loss_kernel(const Part* parts, int64_t count, const float* hit, const int64_t* targets, int64_t T, int V, int64_t ignore,
