@@ -36,8 +36,8 @@ constexpr int kSms = 152;              // for which the backward pass's blocks a
 
 // Threads of a block whose rows take TPR threads each.
 __host__ __device__ constexpr int block_threads(int tpr) { return tpr > 32 ? tpr : kThreads; }
-// A row whose squares leave fp32's range is summed again at this scale.  Its mean square is at least 2^127.8, so that what
-// counts stays far above the least number (2^-149), and 2^20 squares of numbers below 2^128 sum to no more than 2^84.
+// A row whose mean square and eps leave fp32's range is summed again at this scale.  Their sum is at least 2^127.8, so that what counts
+// stays far above the least number (2^-149), and 2^20 squares of numbers below 2^128 sum to no more than 2^84.
 constexpr float kDown = 0x1p-96f;
 
 __device__ __forceinline__ float block_sum(float v, float* red) {
@@ -197,13 +197,13 @@ __global__ void __launch_bounds__(block_threads(TPR), forward_blocks(TPR)) forwa
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             root[r] = sqrtf(s[r] / width + eps);
-            again |= !(s[r] / width <= 3.0e38f);
+            again |= !(s[r] / width + eps <= 3.0e38f);
         }
         if (TPR > 32 ? again : __any_sync(0xFFFFFFFFu, again)) {       // the same for all threads of a row
             squares(kDown);
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
-                if (!(root[r] <= 1.7e19f)) root[r] = sqrtf(s[r] / width) / kDown;
+                if (!(root[r] <= 1.7e19f)) root[r] = sqrtf(s[r] / width + eps * kDown * kDown) / kDown;
         }
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
@@ -349,10 +349,10 @@ forward_kernel(const E* X, const float* gamma, int64_t T, int d, float eps, E* Y
                 const float v = to_f32(x[i]) * scale;
                 s = fmaf(v, v, s);
             }
-            return block_sum(s, red) / static_cast<float>(d);
+            return block_sum(s, red) / static_cast<float>(d) + eps * scale * scale;
         };
         const float s = squares(1.0f);
-        const float r = s <= 3.0e38f ? sqrtf(s + eps) : sqrtf(squares(kDown)) / kDown;
+        const float r = s <= 3.0e38f ? sqrtf(s) : sqrtf(squares(kDown)) / kDown;
         if (threadIdx.x == 0 && rms) rms[t] = r;
         for (int i = threadIdx.x; i < d; i += kThreads) Y[t * d + i] = from_f32<E>(to_f32(x[i]) / r * gamma[i]);
     }

@@ -43,3 +43,20 @@ def test_rows_beyond_the_range_of_their_squares(d, dtype):
     # 1 / rms may be a subnormal number: off by 2^-150 of at least 2^-128.1, in three places
     assert ((dx.double() - want).abs() <= half * want.abs() + (4 * e + 3 * 2.0 ** -21) * size + 1e-38).all()
     assert ((dgamma.double() - (D * n).sum(0)).abs() <= (23 + d / 32) * ROUND * (D * n).abs().sum(0) + 2.0 ** -21 * (D * n).abs().sum(0)).all()
+
+
+@pytest.mark.parametrize("d", [24, 1001, 4096, 8200])
+@pytest.mark.parametrize("eps", [1e30, 2e38, 3.4e38])
+def test_an_eps_of_any_size_counts(d, eps):
+    """Mean squares, eps and their sums on both sides of fp32's largest number."""
+    g = torch.Generator(device=DEV).manual_seed(d)
+    x = torch.rand((9, d), generator=g, device=DEV) + 0.5
+    x *= torch.tensor([0.0, 1e10, 1e15, 0.9e19, 1.2e19, 1.7e19, 1e20, 1e30, 1e37], device=DEV)[:, None]
+    gamma = torch.ones(d, device=DEV)
+    y, rms = dtp.rms_norm(x, gamma, eps=eps)
+    eps = float(torch.tensor(eps))
+    R = (x.double().square().mean(-1) + eps).sqrt()
+    n = x.double() / R[:, None]
+    e = (d / 32 + 24) * ROUND
+    assert ((rms.double() - R).abs() <= e * R).all()
+    assert ((y.double() - n).abs() <= (ROUND + e) * 1.01 * n.abs() + 1e-38).all()
